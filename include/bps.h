@@ -25,6 +25,7 @@
 #ifndef BPS_H
 #define BPS_H
 
+#include <stddef.h>
 #include <stdint.h>
 
 #ifdef __cplusplus
@@ -233,8 +234,122 @@ bps_status bps_read_diagnostics(bps_renderer *r, uint64_t *out, uint32_t capacit
  *       allocated for scenes so far, 9 = retired scene blocks waiting for reuse. */
 bps_status bps_query(bps_renderer *r, bps_scene scene, int32_t what, uint64_t *value);
 
+/* ---------------------------------------------------------------------------------------------------
+ * Operators of the policy that consumes the frames (paper Sec. 3.3 and 3.4): the embedding of tokens
+ * (a policy's previous actions, or a vocabulary), the scores of the tokens it takes, and the
+ * optimiser's step.  They work on DEVICE memory of the calling thread's current device, only enqueue on
+ * `stream` (a hipStream_t of that device, NULL = default stream) and return; all buffers must stay alive until the
+ * stream reaches the end of the call.  Nothing is allocated (bps_adamw_create aside) and nothing is copied from
+ * the host, so that calls can be captured into a graph.  Their failures' texts are those of bps_last_error(NULL)
+ * on the calling thread.  A call that fails has enqueued nothing, unless its status is BPS_ERR_HIP.
+ * Element types are BPS_F32, BPS_BF16 and BPS_F16; sums are held in float32 whatever the type.  A row may start at any
+ * element: rows of odd widths need no padding.  Tokens are int32 or int64 (token_bits 32 or 64).  No results depend on
+ * the order in which work-groups run: the same call gives the same bits. */
+enum { BPS_F32 = 0, BPS_BF16 = 1, BPS_F16 = 2 };
+
+/* Log probabilities of given tokens (PPO's ratio, a sequence's likelihood), with the entropy and the best alternatives.
+ *   logits    [rows][entries], rows row_stride elements apart (any sign; 0 = the same row for all)
+ *   tokens    [rows]  which entry was taken, -1 = none
+ *   mask      uint8 [rows][entries], rows mask_stride bytes apart (0 = one for all rows), or NULL; 0 = the entry is forbidden
+ *   scale     > 0, multiplies the logits (1 / temperature)
+ * An entry takes part when its mask allows it and its logit is not -inf; what the logit of a forbidden entry is does not
+ * matter.  With y = scale * logit over the entries that take part:
+ *   lse       float32 [rows]  ln sum e^y, -inf where nothing takes part
+ *   logp      float32 [rows]  y[token] - lse; 0 for token -1, -inf for a token that takes no part, NaN for one that is no entry
+ *   entropy   float32 [rows]  -sum p ln p, 0 where nothing takes part
+ *   norm      float32 [rows][2] the largest logit that takes part and ln sum e^(y - scale * it), for the gradient: the two
+ *             apart keep what their sum, lse, loses where the logits are large
+ *   top_ids   int32 [rows][top_k]   the top_k entries of the largest logits, ties to the lower index, -1 where there are fewer
+ *   top_logp  float32 [rows][top_k] their log probabilities, -inf where there are fewer;   both may be NULL where top_k is 0
+ * A row in which an entry that takes part is NaN or +inf has lse, entropy and log probabilities NaN (NaN counts as the
+ * largest logit).  0 <= top_k <= 64, entries < 2^30.
+ *   workspace  device memory of bps_log_probs_workspace bytes, 16-byte aligned; it may be NULL where that is 0 */
+size_t bps_log_probs_workspace(int32_t dtype, uint64_t rows, uint32_t entries, uint32_t top_k);
+bps_status bps_log_probs(const void *logits, int32_t dtype, uint64_t rows, uint32_t entries, int64_t row_stride, const void *tokens, int32_t token_bits,
+                         const uint8_t *mask, int64_t mask_stride, float scale, uint32_t top_k, float *logp, float *entropy, float *lse, float *norm,
+                         int32_t *top_ids, float *top_logp, void *workspace, size_t workspace_bytes, void *stream);
+
+/* The gradient: what bps_log_probs gave for the same arguments in, with grad_logp and grad_entropy (float32 [rows] each, or
+ * NULL = zero), and d logits out, in the logits' type:
+ *   out[j] = scale (grad_logp ([j = token] - p_j) - grad_entropy p_j (ln p_j + entropy)),  0 where entry j takes no part.
+ * grad_logp counts as 0 for token -1 and where logp is -inf.  `out` has rows out_stride elements apart; it may be
+ * the logits themselves where the strides are the same and rows do not overlap. */
+bps_status bps_log_probs_backward(const void *logits, int32_t dtype, uint64_t rows, uint32_t entries, int64_t row_stride, const void *tokens,
+                                  int32_t token_bits, const uint8_t *mask, int64_t mask_stride, float scale, const float *logp, const float *entropy,
+                                  const float *norm, const float *grad_logp, const float *grad_entropy, void *out, int64_t out_stride, void *stream);
+
+/* Embedding: out[n] = scale * weight[tokens[n]] (zeros for token -1, NaN for one that is no row), rounded once to the type.
+ *   weight [rows][width], out [count][width]; rows weight_stride and out_stride elements apart. */
+bps_status bps_embedding(const void *tokens, int32_t token_bits, uint64_t count, const void *weight, int32_t dtype, uint32_t rows, uint32_t width,
+                         int64_t weight_stride, float scale, void *out, int64_t out_stride, void *stream);
+
+/* Its gradient: grad_weight[v] = scale * sum of grad_out[n] over the n with tokens[n] = v; every row is written, zeros where
+ * a row has no token.  With accumulate the sums are added to what grad_weight holds, and other rows are not touched.
+ *   grad_out [count][width] of grad_dtype; grad_weight [rows][width] of weight_dtype.  Tokens that are no row are left out.
+ * Tokens are sorted by row first; each row's sum is taken in the tokens' order, in float32, over pieces of that order
+ * whose bounds depend on `count` alone, and rounded once.  count < 2^31.
+ *   workspace  device memory of bps_embedding_backward_workspace bytes, 16-byte aligned */
+size_t bps_embedding_backward_workspace(uint64_t count, uint32_t rows, uint32_t width);
+bps_status bps_embedding_backward(const void *tokens, int32_t token_bits, uint64_t count, const void *grad_out, int32_t grad_dtype, uint32_t rows,
+                                  uint32_t width, int64_t grad_stride, float scale, void *grad_weight, int32_t weight_dtype, int64_t weight_stride,
+                                  int32_t accumulate, void *workspace, size_t workspace_bytes, void *stream);
+
+/* AdamW over many tensors at once.  With g' = grad * grad_scale * clip, t the number of this step (1 for the first):
+ *   m = beta1 m + (1 - beta1) g';   v = beta2 v + ((1 - beta2) g') g'
+ *   w = w (1 - lr weight_decay) - (lr / (1 - beta1^t)) m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * in float32, each operation rounded by itself; clip = max_norm / norm where norm, the 2-norm of all gradients times
+ * grad_scale, is over max_norm > 0, else 1.  With max_norm > 0 a step whose norm is not finite changes nothing.
+ *
+ * The states of all tensors lie in one array each, a tensor's at `start` elements, a multiple of 256, in total elements, a multiple
+ * of 256 too; what lies between tensors belongs to nobody.  state_bits 32: exp_avg (m) and exp_avg_sq (v) are float32.  state_bits 8:
+ * one byte each, and one byte for each 256 consecutive ones in exp_avg_exponent and exp_avg_sq_exponent.  With E that byte,
+ * a code of exponent field f > 0 and mantissa field k stands for (1 + k/8) 2^(E - 127 - top + f), of field 0 for
+ * (k/8) 2^(E - 127 - top + 1);  m: bit 7 sign, bits 6..3 f, bits 2..0 k, top = 15;  v: bits 7..3 f, bits 2..0 k, top = 31.
+ * E is the least that holds the block's largest magnitude, at least 20 for m and 36 for v; 255 stands for a block with a magnitude
+ * that is infinite, NaN, or over 1.875 * 2^127, whose values all read as NaN.  Values are rounded up or down to a neighbouring
+ * code with probabilities that keep the mean, so that averages over many steps, which change by less than half the distance of two
+ * codes at a time, still move: n = floor(|x| / quantum + u), u 16 bits of a hash of (seed, step, element).
+ * The step itself uses m and v before they are rounded.
+ *
+ * float32 parameters are updated in place; BF16 and F16 ones need a float32 `master` (may not be NULL), which is
+ * updated, and get its value rounded.  Tensors are contiguous. */
+typedef struct bps_adamw bps_adamw;
+
+typedef struct {
+    void *param;             /* `count` elements of param_dtype */
+    float *master;           /* `count` float32, NULL for BPS_F32 parameters */
+    uint64_t count;          /* >= 1 */
+    uint64_t start;          /* of its states, a multiple of 256; tensors in ascending order without overlap */
+    float weight_decay;
+    float lr_scale;          /* lr of this tensor is lr * lr_scale */
+} bps_adamw_tensor;
+
+typedef struct {
+    int32_t param_dtype;
+    int32_t state_bits;      /* 32 or 8 */
+    uint32_t tensors;        /* >= 1 */
+    uint32_t seed;           /* of the rounding of 8-bit states */
+    uint64_t total;          /* elements of a state array */
+    const bps_adamw_tensor *tensor;
+    void *exp_avg, *exp_avg_sq;                          /* device, 16-byte aligned; the caller's, with their initial values (zeros) */
+    uint8_t *exp_avg_exponent, *exp_avg_sq_exponent;     /* device; NULL with 32 bits */
+} bps_adamw_config;
+
+/* Makes a plan of the tensors on the current device: a table of them in device memory (the one allocation, and the one
+ * wait for the device).  Parameters, masters and states stay the caller's, who keeps them where they are until
+ * bps_adamw_destroy.  Calls on one handle must not overlap: on the host, and on the device (one stream, or ordered streams). */
+bps_status bps_adamw_create(const bps_adamw_config *cfg, bps_adamw **out);
+void bps_adamw_destroy(bps_adamw *h);    /* waits for the device; NULL is ignored */
+/* One step.  grads: HOST array of `tensors` device pointers, each to `count` elements of grad_dtype (param_dtype or BPS_F32),
+ * NULL = no gradient: that tensor and its states are left as they are.  The addresses are consumed during the call.
+ * grad_norm: device float32 [1] or NULL, receives the norm where max_norm > 0. */
+bps_status bps_adamw_step(bps_adamw *h, const void *const *grads, int32_t grad_dtype, uint64_t step, double lr, double beta1, double beta2, double eps,
+                          double grad_scale, double max_norm, float *grad_norm, void *stream);
+/* 8-bit states as the float32 values they stand for, `total` elements each. */
+bps_status bps_adamw_read_states(bps_adamw *h, float *exp_avg, float *exp_avg_sq, void *stream);
+
 /* Text of the last error on this renderer (owned by the renderer; never NULL).
- * With r == NULL returns the text of the last failed bps_create on this thread. */
+ * With r == NULL returns the text of the last failed bps_create, or call of a policy's operator, on this thread. */
 const char *bps_last_error(const bps_renderer *r);
 
 #ifdef __cplusplus

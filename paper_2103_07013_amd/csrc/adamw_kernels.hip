@@ -1,0 +1,269 @@
+// AdamW over many tensors at once; states in 32 or in 8 bits.  The rule is in include/bps.h: every operation is rounded by itself
+// (the library is built without contraction), so that what 8-bit states are rounded to can be reproduced bit for bit.
+//
+// A work-group takes a chunk of kAdamChunk elements of one tensor; a table made with the handle says which.
+#include "policy_device.h"
+#include "policy_kernels.h"
+
+namespace bps {
+
+namespace {
+
+constexpr uint32_t kPerLane = 4, kStep = kAdamGroup * kPerLane;
+static_assert(kStateBlock == 64 * kPerLane, "a wavefront's elements share an exponent");
+static_assert(kAdamChunk % kStep == 0, "a chunk is whole steps");
+
+__device__ __forceinline__ float power(uint32_t biased) { return __uint_as_float(biased << 23); }
+
+// what an 8-bit code of exponent field and 3 mantissa bits stands for; e: the block's exponent byte
+template <int TOP>
+__device__ __forceinline__ float decoded(uint32_t code, uint32_t e) {
+    const uint32_t field = code >> 3 > 1u ? code >> 3 : 1u;
+    return e == 255u ? __builtin_nanf("") : (float)(code - 8u * (field - 1u)) * power(e - TOP + field - 3u);
+}
+
+// the block's exponent byte for the largest magnitude's bits: the least that holds it
+template <uint32_t LEAST>
+__device__ __forceinline__ uint32_t exponent_for(uint32_t largest) {
+    const uint32_t e = (largest + 0x0FFFFFu) >> 23;
+    return e < LEAST ? LEAST : e > 255u ? 255u : e;
+}
+
+template <int TOP>
+__device__ __forceinline__ uint32_t encoded(float magnitude, uint32_t e, float dither) {
+    if (e == 255u) return 0u;
+    const int f = (int)(__float_as_uint(magnitude) >> 23) - (int)e + TOP;
+    const uint32_t field = f > 1 ? (uint32_t)f : 1u;
+    return 8u * (field - 1u) + (uint32_t)(magnitude * power(254u - (e - TOP + field - 3u)) + dither);
+}
+
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
+#pragma unroll
+    for (int d = 32; d; d >>= 1) {
+        const uint32_t y = __shfl_xor(x, d, 64);
+        x = y > x ? y : x;
+    }
+    return x;
+}
+
+template <class G>
+__global__ __launch_bounds__(kAdamGroup) void k_adamw_norm(AdamPlan plan, AdamGrads grads, uint32_t first_tensor, uint32_t first_chunk, uint32_t all_chunks, AdamScalars s,
+                                                           float* norm_out) {
+    __shared__ float sums[kAdamGroup / 64];
+    __shared__ double total[kAdamGroup / 64];
+    __shared__ uint32_t is_last;
+    const AdamChunk chunk = plan.chunks[first_chunk + blockIdx.x];
+    const AdamTensor t = plan.tensors[chunk.tensor];
+    const typename G::raw* g = static_cast<const typename G::raw*>(grads.at[chunk.tensor - first_tensor]);
+    const uint32_t tid = threadIdx.x;
+    float sum = 0.0f;
+    if (g) {
+        const uint64_t from = (uint64_t)chunk.index * kAdamChunk, left = t.count - from;
+        const uint32_t n = left < kAdamChunk ? (uint32_t)left : kAdamChunk;
+        for (uint32_t i = tid; i < n; i += kAdamGroup) {
+            const float x = to_float(g[from + i]) * s.grad_scale;
+            sum = fmaf(x, x, sum);
+        }
+    }
+    sum = wave_sum(sum);
+    if ((tid & 63u) == 0) sums[tid >> 6] = sum;
+    __syncthreads();
+    if (tid == 0) {
+        plan.partial[first_chunk + blockIdx.x] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+        __threadfence();
+        is_last = atomicAdd(plan.arrived, 1u) + 1u == all_chunks;
+    }
+    __syncthreads();
+    if (!is_last) return;
+    // the last work-group adds up all sums, in an order that does not depend on which one it is
+    __threadfence();
+    double all = 0.0;
+    for (uint32_t i = tid; i < all_chunks; i += kAdamGroup) all += (double)__hip_atomic_load(&plan.partial[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+    for (int d = 32; d; d >>= 1) all += __shfl_xor(all, d, 64);
+    if ((tid & 63u) == 0) total[tid >> 6] = all;
+    __syncthreads();
+    if (tid == 0) {
+        const float norm = (float)sqrt((total[0] + total[1]) + (total[2] + total[3]));
+        plan.norm[0] = norm;
+        plan.norm[1] = norm > s.max_norm ? s.max_norm / norm : 1.0f;
+        if (norm_out) *norm_out = norm;
+        *plan.arrived = 0;
+    }
+}
+
+template <class P, class G, int BITS, bool CLIP>
+__global__ __launch_bounds__(kAdamGroup) void k_adamw(AdamPlan plan, AdamGrads grads, uint32_t first_tensor, uint32_t first_chunk, AdamScalars s) {
+    constexpr bool kMaster = sizeof(typename P::raw) == 2;
+    const AdamChunk chunk = plan.chunks[first_chunk + blockIdx.x];
+    const typename G::raw* g = static_cast<const typename G::raw*>(grads.at[chunk.tensor - first_tensor]);
+    if (!g) return;
+    const AdamTensor t = plan.tensors[chunk.tensor];
+    float clip = 1.0f;
+    if (CLIP) {
+        if (!(fabsf(plan.norm[0]) < __builtin_inff())) return;
+        clip = plan.norm[1];
+    }
+    const float keep = (float)(1.0 - s.lr * t.lr_scale * t.weight_decay), step_size = (float)(s.step_size * t.lr_scale);
+    const uint64_t from = (uint64_t)chunk.index * kAdamChunk, left = t.count - from;
+    const uint32_t n = left < kAdamChunk ? (uint32_t)left : kAdamChunk;
+    for (uint32_t i = threadIdx.x * kPerLane; i / kStateBlock * kStateBlock < n; i += kStep) {
+        const uint64_t at = from + i, state = t.start + at;
+        const uint32_t live = i >= n ? 0u : n - i < kPerLane ? n - i : kPerLane;
+        float x[kPerLane], w[kPerLane], m[kPerLane], v[kPerLane];
+        typename P::raw* param = static_cast<typename P::raw*>(t.param) + at;
+        float* weight = kMaster ? t.master + at : reinterpret_cast<float*>(t.param) + at;
+        if (live == kPerLane) {
+            load<G, kPerLane>(g + at, x);
+            load<F32, kPerLane>(weight, w);
+        } else {
+#pragma unroll
+            for (uint32_t k = 0; k < kPerLane; ++k) {
+                x[k] = k < live ? to_float(g[at + k]) : 0.0f;
+                w[k] = k < live ? weight[k] : 0.0f;
+            }
+        }
+        uint32_t code_m = 0, code_v = 0;
+        if (BITS == 32) {
+            // a state block belongs to one tensor, so that all four are this lane's
+            load<F32, kPerLane>(static_cast<float*>(plan.exp_avg) + state, m);
+            load<F32, kPerLane>(static_cast<float*>(plan.exp_avg_sq) + state, v);
+        } else {
+            code_m = *reinterpret_cast<const uint32_t*>(static_cast<uint8_t*>(plan.exp_avg) + state);
+            code_v = *reinterpret_cast<const uint32_t*>(static_cast<uint8_t*>(plan.exp_avg_sq) + state);
+            const uint32_t em = plan.exp_avg_exponent[state / kStateBlock], ev = plan.exp_avg_sq_exponent[state / kStateBlock];
+#pragma unroll
+            for (uint32_t k = 0; k < kPerLane; ++k) {
+                const uint32_t cm = code_m >> (8 * k) & 255u, cv = code_v >> (8 * k) & 255u;
+                m[k] = decoded<15>(cm & 127u, em);
+                m[k] = cm & 128u ? -m[k] : m[k];
+                v[k] = decoded<31>(cv, ev);
+                if (k >= live) m[k] = v[k] = 0.0f;      // behind the tensor's end: no part of the block's largest
+            }
+        }
+#pragma unroll
+        for (uint32_t k = 0; k < kPerLane; ++k) {
+            x[k] = x[k] * s.grad_scale;
+            if (CLIP) x[k] = x[k] * clip;
+            m[k] = m[k] * s.beta1 + x[k] * s.one_minus_beta1;
+            v[k] = v[k] * s.beta2 + x[k] * s.one_minus_beta2 * x[k];
+            w[k] = w[k] * keep - m[k] / (sqrtf(v[k]) * s.root_c2 + s.eps) * step_size;
+        }
+        if (live == kPerLane) {
+            store<F32, kPerLane>(weight, w);
+            if (kMaster) store<P, kPerLane>(param, w);
+        } else {
+#pragma unroll
+            for (uint32_t k = 0; k < kPerLane; ++k)
+                if (k < live) {
+                    weight[k] = w[k];
+                    if (kMaster) param[k] = rounded<P>(w[k]);
+                }
+        }
+        if (BITS == 32) {
+            if (live) {
+                store<F32, kPerLane>(static_cast<float*>(plan.exp_avg) + state, m);
+                store<F32, kPerLane>(static_cast<float*>(plan.exp_avg_sq) + state, v);
+            }
+        } else {
+            uint32_t largest_m = 0, largest_v = 0;
+#pragma unroll
+            for (uint32_t k = 0; k < kPerLane; ++k) {
+                const uint32_t bm = __float_as_uint(m[k]) & 0x7FFFFFFFu, bv = __float_as_uint(v[k]) & 0x7FFFFFFFu;
+                largest_m = bm > largest_m ? bm : largest_m;
+                largest_v = bv > largest_v ? bv : largest_v;
+            }
+            const uint32_t em = exponent_for<20>(wave_max(largest_m)), ev = exponent_for<36>(wave_max(largest_v));
+            code_m = code_v = 0;
+#pragma unroll
+            for (uint32_t k = 0; k < kPerLane; ++k) {
+                const uint32_t h = mixed(((uint32_t)(state + k) * kGolden) ^ s.key);
+                const uint32_t cm = encoded<15>(fabsf(m[k]), em, (float)(h & 0xFFFFu) * 0x1p-16f) | (m[k] < 0.0f ? 128u : 0u);
+                const uint32_t cv = encoded<31>(v[k], ev, (float)(h >> 16) * 0x1p-16f);
+                code_m |= cm << (8 * k);
+                code_v |= cv << (8 * k);
+            }
+            *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(plan.exp_avg) + state) = code_m;
+            *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(plan.exp_avg_sq) + state) = code_v;
+            if ((threadIdx.x & 63u) == 0) {
+                plan.exp_avg_exponent[state / kStateBlock] = (uint8_t)em;
+                plan.exp_avg_sq_exponent[state / kStateBlock] = (uint8_t)ev;
+            }
+        }
+    }
+}
+
+__global__ __launch_bounds__(256) void k_adamw_read(AdamPlan plan, uint64_t blocks, float* exp_avg, float* exp_avg_sq) {
+    for (uint64_t b = (uint64_t)blockIdx.x * 4 + (threadIdx.x >> 6); b < blocks; b += (uint64_t)gridDim.x * 4) {
+        const uint64_t at = b * kStateBlock + (threadIdx.x & 63u) * kPerLane;
+        const uint32_t code_m = *reinterpret_cast<const uint32_t*>(static_cast<uint8_t*>(plan.exp_avg) + at);
+        const uint32_t code_v = *reinterpret_cast<const uint32_t*>(static_cast<uint8_t*>(plan.exp_avg_sq) + at);
+        const uint32_t em = plan.exp_avg_exponent[b], ev = plan.exp_avg_sq_exponent[b];
+        float m[kPerLane], v[kPerLane];
+#pragma unroll
+        for (uint32_t k = 0; k < kPerLane; ++k) {
+            const uint32_t cm = code_m >> (8 * k) & 255u;
+            m[k] = decoded<15>(cm & 127u, em);
+            m[k] = cm & 128u ? -m[k] : m[k];
+            v[k] = decoded<31>(code_v >> (8 * k) & 255u, ev);
+        }
+        store<F32, kPerLane>(exp_avg + at, m);
+        store<F32, kPerLane>(exp_avg_sq + at, v);
+    }
+}
+
+template <class G>
+void norm(const AdamPlan& p, const AdamGrads& g, uint32_t first_tensor, uint32_t first_chunk, uint32_t chunks, uint32_t all, const AdamScalars& s, float* out, hipStream_t stream) {
+    hipLaunchKernelGGL((k_adamw_norm<G>), dim3(chunks), dim3(kAdamGroup), 0, stream, p, g, first_tensor, first_chunk, all, s, out);
+}
+
+template <class P, class G, int BITS>
+void step(const AdamPlan& p, const AdamGrads& g, uint32_t first_tensor, uint32_t first_chunk, uint32_t chunks, bool clipped, const AdamScalars& s, hipStream_t stream) {
+    if (clipped)
+        hipLaunchKernelGGL((k_adamw<P, G, BITS, true>), dim3(chunks), dim3(kAdamGroup), 0, stream, p, g, first_tensor, first_chunk, s);
+    else
+        hipLaunchKernelGGL((k_adamw<P, G, BITS, false>), dim3(chunks), dim3(kAdamGroup), 0, stream, p, g, first_tensor, first_chunk, s);
+}
+template <class P, class G>
+void step(int32_t bits, const AdamPlan& p, const AdamGrads& g, uint32_t first_tensor, uint32_t first_chunk, uint32_t chunks, bool clipped, const AdamScalars& s, hipStream_t stream) {
+    if (bits == 32)
+        step<P, G, 32>(p, g, first_tensor, first_chunk, chunks, clipped, s, stream);
+    else
+        step<P, G, 8>(p, g, first_tensor, first_chunk, chunks, clipped, s, stream);
+}
+
+}  // namespace
+
+hipError_t launch_adamw_norm(int32_t grad_dtype, const AdamPlan& p, const AdamGrads& g, uint32_t first_tensor, uint32_t first_chunk, uint32_t chunks,
+                             uint32_t all_chunks, const AdamScalars& s, float* norm_out, hipStream_t stream) {
+    if (grad_dtype == BPS_F32)
+        norm<F32>(p, g, first_tensor, first_chunk, chunks, all_chunks, s, norm_out, stream);
+    else if (grad_dtype == BPS_BF16)
+        norm<Bf16>(p, g, first_tensor, first_chunk, chunks, all_chunks, s, norm_out, stream);
+    else
+        norm<F16>(p, g, first_tensor, first_chunk, chunks, all_chunks, s, norm_out, stream);
+    return hipGetLastError();
+}
+
+hipError_t launch_adamw_step(int32_t param_dtype, int32_t grad_dtype, int32_t state_bits, const AdamPlan& p, const AdamGrads& g, uint32_t first_tensor,
+                             uint32_t first_chunk, uint32_t chunks, bool clipped, const AdamScalars& s, hipStream_t stream) {
+    if (param_dtype == BPS_F32)
+        step<F32, F32>(state_bits, p, g, first_tensor, first_chunk, chunks, clipped, s, stream);
+    else if (param_dtype == BPS_BF16 && grad_dtype == BPS_BF16)
+        step<Bf16, Bf16>(state_bits, p, g, first_tensor, first_chunk, chunks, clipped, s, stream);
+    else if (param_dtype == BPS_BF16)
+        step<Bf16, F32>(state_bits, p, g, first_tensor, first_chunk, chunks, clipped, s, stream);
+    else if (grad_dtype == BPS_F16)
+        step<F16, F16>(state_bits, p, g, first_tensor, first_chunk, chunks, clipped, s, stream);
+    else
+        step<F16, F32>(state_bits, p, g, first_tensor, first_chunk, chunks, clipped, s, stream);
+    return hipGetLastError();
+}
+
+hipError_t launch_adamw_read(const AdamPlan& p, uint64_t blocks, float* exp_avg, float* exp_avg_sq, hipStream_t stream) {
+    const uint64_t g = (blocks + 3) / 4;
+    hipLaunchKernelGGL(k_adamw_read, dim3((uint32_t)(g < 16384 ? g : 16384)), dim3(256), 0, stream, p, blocks, exp_avg, exp_avg_sq);
+    return hipGetLastError();
+}
+
+}  // namespace bps

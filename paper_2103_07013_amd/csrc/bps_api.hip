@@ -17,6 +17,7 @@
 
 #include "../../include/bps.h"
 #include "clusters.h"
+#include "policy_kernels.h"
 #include "raster_kernels.h"
 
 namespace {
@@ -175,6 +176,19 @@ bps_status fail(bps_renderer* r, bps_status code, const char* fmt, ...) {
     }
     return code;
 }
+
+}  // namespace
+
+bps_status bps::fail_here(bps_status code, const char* fmt, ...) {
+    char buf[512];
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(buf, sizeof(buf), fmt, ap);
+    va_end(ap);
+    return fail(nullptr, code, "%s", buf);
+}
+
+namespace {
 
 #define BPS_HIP(r, call)                                                                      \
     do {                                                                                      \

@@ -1,0 +1,226 @@
+"""Embedding lookup and its gradient by sorted tokens, against the definition in 64 bits.
+
+Lookup: one product, rounded once to float32 and once to the type; torch's operations do the same, so the bits are the same.
+Gradient: a sum of n terms in float32 is off by at most n 2^-24 times the sum of their magnitudes, its product with the scale
+by 2^-24 of itself, and the result's type adds half its distance."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+E = 2.0 ** -24
+HALF = {"float32": 0.0, "bfloat16": 2.0 ** -8, "float16": 2.0 ** -11}
+
+
+def _torch():
+    import torch
+    return torch
+
+
+def _tokens(N, V, how, seed=0):
+    torch = _torch()
+    g = torch.Generator().manual_seed(seed + N * 31 + V)
+    if how == "even":
+        t = torch.randint(0, V, (N,), generator=g)
+    elif how == "skewed":
+        t = (float(V) ** torch.rand(N, generator=g, dtype=torch.float64)).long().clamp(1, V) - 1
+    elif how == "one":
+        t = torch.full((N,), V // 2)
+    elif how == "runs":
+        t = (torch.arange(N) // 70) % V
+    else:
+        t = torch.full((N,), -1)
+        if N > 3:
+            t[N // 2] = V - 1
+    t[torch.rand(N, generator=g) < 0.05] = -1
+    return t.cuda()
+
+
+def _reference(tokens, grad, V, scale):
+    torch = _torch()
+    t, g = tokens.cpu().long().reshape(-1), grad.cpu().double().reshape(tokens.numel(), grad.shape[-1])
+    keep = (t >= 0) & (t < V)
+    out, size, count = (torch.zeros((V, g.shape[1] if k < 2 else 1), dtype=torch.float64) for k in range(3))
+    out.index_add_(0, t[keep], g[keep])
+    size.index_add_(0, t[keep], g[keep].abs())
+    count.index_add_(0, t[keep], torch.ones((int(keep.sum()), 1), dtype=torch.float64))
+    return out * scale, (count + 2) * E * size * abs(scale)
+
+
+def _near(got, ref, slack):
+    torch = _torch()
+    kind = str(got.dtype).replace("torch.", "")
+    off = (got.cpu().double() - ref).abs()
+    allowed = slack + HALF[kind] * (ref.abs() + slack) + 2.0 ** -25 * (kind == "float16")
+    assert (off <= allowed).all(), float((off - allowed).max())
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16", "float16"])
+@pytest.mark.parametrize("N,V,D", [(0, 3, 5), (1, 1, 1), (1, 9, 32), (1024, 5, 32), (70, 1000, 7), (33, 17, 769), (5, 50257, 64), (2000, 300, 129), (9, 4, 4097)])
+def test_lookup(N, V, D, dtype):
+    import paper_2103_07013_amd as bps
+    torch = _torch()
+    w = torch.randn((V, D), generator=torch.Generator().manual_seed(1)).to(getattr(torch, dtype)).cuda()
+    for kind in (torch.int32, torch.int64):
+        t = _tokens(N, V, "even").to(kind)
+        for scale in (1.0, 5.7):
+            out = bps.embedding(t, w, scale=scale)
+            ref = torch.where((t < 0)[:, None], 0.0, w[t.long().clamp(min=0)].float() * scale).to(w.dtype)
+            assert torch.equal(out, ref)
+
+
+@pytest.mark.parametrize("dtype,to", [("float32", "float32"), ("bfloat16", "float32"), ("bfloat16", "bfloat16"), ("float16", "float32"), ("float16", "float16"), ("float32", "bfloat16")])
+@pytest.mark.parametrize("how", ["even", "skewed", "one", "runs", "none"])
+@pytest.mark.parametrize("N,V,D", [(0, 3, 5), (1, 1, 1), (2, 300, 3), (63, 5, 32), (64, 5, 8), (65, 5, 16), (500, 7, 33), (2048, 511, 12), (2049, 512, 12), (5000, 513, 40), (4100, 70000, 9),
+                                   (1500, 40, 769)])
+def test_gradient(N, V, D, how, dtype, to):
+    import paper_2103_07013_amd as bps
+    torch = _torch()
+    t = _tokens(N, V, how)
+    g = torch.randn((N, D), generator=torch.Generator().manual_seed(N + D)).to(getattr(torch, dtype)).cuda()
+    ref, slack = _reference(t, g, V, 1.7)
+    _near(bps.embedding_backward(t, g, V, scale=1.7, dtype=getattr(torch, to)), ref, slack)
+
+
+@pytest.mark.parametrize("N,V,D", [(30000, 5, 32), (40000, 131072, 24), (300000, 200, 4), (9000, 3, 1200), (200000, 1, 1)])
+@pytest.mark.parametrize("how", ["even", "skewed", "one"])
+def test_gradient_of_long_batches(N, V, D, how):
+    import paper_2103_07013_amd as bps
+    torch = _torch()
+    t = _tokens(N, V, how)
+    g = torch.randn((N, D), generator=torch.Generator().manual_seed(N + D)).cuda()
+    ref, slack = _reference(t, g, V, 1.0)
+    _near(bps.embedding_backward(t.to(torch.int32), g, V), ref, slack)
+
+
+@pytest.mark.parametrize("N,V,D", [(300, 50, 33), (5000, 7, 64), (1, 1000, 8), (0, 10, 4)])
+@pytest.mark.parametrize("to", ["float32", "bfloat16"])
+def test_accumulation_leaves_other_rows_alone(N, V, D, to):
+    import paper_2103_07013_amd as bps
+    torch = _torch()
+    t = _tokens(N, V, "skewed")
+    g = torch.randn((N, D), device="cuda")
+    held = torch.randn((V, D), device="cuda").to(getattr(torch, to))
+    out = held.clone()
+    assert bps.embedding_backward(t, g, V, scale=0.5, out=out, accumulate=True) is out
+    ref, slack = _reference(t, g, V, 0.5)
+    used = torch.zeros(V, dtype=torch.bool)
+    used[t.cpu()[t.cpu() >= 0]] = True
+    assert torch.equal(out.cpu()[~used], held.cpu()[~used])
+    both = ref + held.cpu().double()
+    _near(out, both, slack + E * both.abs())
+
+
+def test_against_differences():
+    """The lookup is linear: the difference quotient of sum(out * c) is exact up to the rounding of the sums."""
+    import paper_2103_07013_amd as bps
+    torch = _torch()
+    V, D = 6, 5
+    t = _tokens(200, V, "even")
+    w = torch.randn((V, D), device="cuda").double().float()
+    c = torch.randn((200, D), device="cuda")
+    grad = bps.embedding_backward(t, c, V, scale=2.0)
+    for v, d in ((0, 0), (3, 2), (5, 4)):
+        up, down = w.clone(), w.clone()
+        up[v, d] += 0.5
+        down[v, d] -= 0.5
+        f = [(bps.embedding(t, x, scale=2.0).double() * c.double()).sum() for x in (up, down)]
+        step = float(up[v, d]) - float(down[v, d])
+        assert abs(float(f[0] - f[1]) / step - float(grad[v, d])) <= 400 * 4 * 202 * E
+
+
+def test_rows_that_lie_apart_and_begin_anywhere():
+    import paper_2103_07013_amd as bps
+    torch = _torch()
+    N, V, D = 700, 41, 19
+    t = _tokens(N, V, "even")
+    for kind in (torch.float32, torch.bfloat16, torch.float16):
+        w, g = torch.randn((V, D + 6), device="cuda").to(kind), torch.randn((N, D + 3), device="cuda").to(kind)
+        out = torch.full((N, D + 4), 7.0, device="cuda").to(kind)
+        assert torch.equal(bps.embedding(t, w[:, 1:D + 1], out=out[:, 3:D + 3]), bps.embedding(t, w[:, 1:D + 1].contiguous()))
+        assert (out[:, :3] == 7).all() and (out[:, D + 3:] == 7).all()
+        dw = torch.full((V, D + 2), 7.0, device="cuda")
+        bps.embedding_backward(t, g[:, 2:D + 2], V, out=dw[:, 1:D + 1])
+        assert torch.equal(dw[:, 1:D + 1], bps.embedding_backward(t, g[:, 2:D + 2].contiguous(), V))
+        assert (dw[:, 0] == 7).all() and (dw[:, D + 1] == 7).all()
+
+
+def test_tokens_that_are_no_row():
+    """NaN in the lookup, left out of the gradient; nothing outside the table is read or written."""
+    import paper_2103_07013_amd as bps
+    torch = _torch()
+    w = torch.randn((4, 24), device="cuda")
+    for kind in (torch.int32, torch.int64):
+        t = torch.tensor([-1, 4, -2, 2 ** 31 - 1, -2 ** 31, 3], dtype=kind, device="cuda")
+        out = bps.embedding(t, w)
+        assert (out[0] == 0).all() and torch.isnan(out[1:5]).all() and torch.equal(out[5], w[3])
+        grad = bps.embedding_backward(t, torch.ones((6, 24), device="cuda"), 4)
+        assert (grad[:3] == 0).all() and (grad[3] == 1).all()
+
+
+def test_nan_reaches_only_the_rows_of_its_tokens():
+    import paper_2103_07013_amd as bps
+    torch = _torch()
+    t = _tokens(400, 9, "even")
+    g = torch.randn((400, 10), device="cuda")
+    n = int((t == 4).nonzero()[0])
+    g[n, 3] = float("nan")
+    g[(t < 0).nonzero()[0, 0]] = float("inf")
+    grad = bps.embedding_backward(t, g, 9)
+    assert torch.isnan(grad[4, 3]) and int((~torch.isfinite(grad)).sum()) == 1
+
+
+def test_autograd_and_leading_dimensions():
+    import paper_2103_07013_amd as bps
+    torch = _torch()
+    for kind in (torch.float32, torch.bfloat16):
+        w = torch.randn((30, 12), device="cuda").to(kind).requires_grad_()
+        t = _tokens(24, 30, "even").view(2, 3, 4)
+        out = bps.embedding(t, w, scale=3.0)
+        assert out.shape == (2, 3, 4, 12)
+        c = torch.randn(out.shape, device="cuda").to(kind)
+        (out * c).sum().backward()
+        assert torch.equal(w.grad, bps.embedding_backward(t, c, 30, scale=3.0, dtype=kind))
+
+
+@pytest.mark.parametrize("N,V,D", [(20000, 5, 32), (70000, 5000, 16), (3000, 900, 100)])
+def test_the_same_bits_every_time_on_any_stream_and_in_a_graph(N, V, D):
+    import paper_2103_07013_amd as bps
+    torch = _torch()
+    sets = [(_tokens(N, V, how, seed), torch.randn((N, D), device="cuda")) for seed, how in enumerate(("even", "skewed", "one", "runs"))]
+    ref = [bps.embedding_backward(t, g, V) for t, g in sets]
+    torch.cuda.synchronize()
+    assert all(torch.equal(r, bps.embedding_backward(t, g, V)) for r, (t, g) in zip(ref, sets))
+    side = torch.cuda.Stream()
+    got = bps.embedding_backward(*sets[1], V, stream=side)
+    side.synchronize()
+    assert torch.equal(got, ref[1])
+    t, g = sets[0][0].clone(), sets[0][1].clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = bps.embedding_backward(t, g, V)
+    for k in (0, 1, 2, 3, 2):
+        t.copy_(sets[k][0])
+        g.copy_(sets[k][1])
+        graph.replay()
+        if k % 2:
+            assert torch.equal(bps.embedding_backward(*sets[3], V), ref[3])
+        torch.cuda.synchronize()
+        assert torch.equal(held, ref[k]), f"replay of set {k}"
+
+
+def test_tables_and_batches_behind_the_reach_of_32_bits():
+    import paper_2103_07013_amd as bps
+    torch = _torch()
+    V, D = 1_100_000, 2000              # 2.2e9 elements
+    w = torch.zeros((V, D), dtype=torch.bfloat16, device="cuda")
+    few = torch.tensor([0, 5, 1_073_741, 1_073_742, V - 1], device="cuda")
+    w[few] = torch.randn((5, D), device="cuda").bfloat16()
+    assert torch.equal(bps.embedding(few, w), w[few])
+    many = few.repeat(220_000)          # as many elements in the batch
+    out = bps.embedding(many, w)
+    assert torch.equal(out[-5:], w[few]) and torch.equal(out[549_995:550_005], w[few].repeat(2, 1))
+    grad = bps.embedding_backward(many[-1000:].contiguous(), out[-1000:], V, dtype=torch.bfloat16)
+    assert torch.equal(grad[few], (w[few].float() * 200).bfloat16())
+    assert int((grad != 0).any(1).sum()) == 5
+    del w, grad
+    grad = bps.embedding_backward(torch.arange(5, device="cuda").repeat(220_000), out, 5)
+    assert torch.allclose(grad, out[:5].float() * 220_000, rtol=220_000 * E)
