@@ -145,7 +145,7 @@ bps_status bps_adamw_create(const bps_adamw_config* cfg, bps_adamw** out) {
         end = t.start + (t.count + bps::kStateBlock - 1) / bps::kStateBlock * bps::kStateBlock;
         chunks += (t.count + bps::kAdamChunk - 1) / bps::kAdamChunk;
     }
-    if (chunks >= 1ull << 31) return fail_here(BPS_ERR_UNSUPPORTED, "%s: too many elements", what);
+    if (chunks >= 1ull << 23) return fail_here(BPS_ERR_UNSUPPORTED, "%s: too many elements", what);
     int ndev = 0, device = 0;
     if (hipGetDeviceCount(&ndev) != hipSuccess || ndev <= 0 || hipGetDevice(&device) != hipSuccess)
         return fail_here(BPS_ERR_HIP, "%s: no HIP device available (this library has no CPU path)", what);

@@ -60,10 +60,44 @@ __device__ __forceinline__ int64_t token_at(const void* tokens, int tokens64, ui
     return tokens64 ? static_cast<const int64_t*>(tokens)[i] : (int64_t) static_cast<const int32_t*>(tokens)[i];
 }
 
-__device__ __forceinline__ float wave_sum(float x) {
-#pragma unroll
-    for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d, 64);
+// The value of lane (lane ^ X): a permutation within 16 lanes where there is one, through the LDS crossbar otherwise.
+template <int X>
+__device__ __forceinline__ uint32_t from_lane_xor(uint32_t v) {
+    static_assert(X > 0 && X < 64, "within the wavefront");
+    if constexpr (X == 1) return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xF, 0xF, true);          // quad_perm 1 0 3 2
+    else if constexpr (X == 2) return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x4E, 0xF, 0xF, true);     // quad_perm 2 3 0 1
+    else if constexpr (X == 3) return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x1B, 0xF, 0xF, true);     // quad_perm 3 2 1 0
+    else if constexpr (X == 7) return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x141, 0xF, 0xF, true);    // mirrored within 8
+    else if constexpr (X == 8) return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x128, 0xF, 0xF, true);    // rotated by 8 within 16
+    else if constexpr (X == 15) return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x140, 0xF, 0xF, true);   // mirrored within 16
+    else if constexpr (X == 4) return from_lane_xor<7>(from_lane_xor<3>(v));
+    else if constexpr (X < 32) return (uint32_t)__builtin_amdgcn_ds_swizzle((int)v, (X << 10) | 0x1F);
+    else return (uint32_t)__shfl_xor((int)v, X, 64);
+}
+template <int X>
+__device__ __forceinline__ float from_lane_xor(float v) { return __uint_as_float(from_lane_xor<X>(__float_as_uint(v))); }
+template <int X>
+__device__ __forceinline__ uint64_t from_lane_xor(uint64_t v) {
+    return (uint64_t)from_lane_xor<X>((uint32_t)(v >> 32)) << 32 | from_lane_xor<X>((uint32_t)v);
+}
+
+__device__ __forceinline__ uint32_t lanes_before(uint64_t lanes) {
+    return __builtin_amdgcn_mbcnt_hi((uint32_t)(lanes >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)lanes, 0u));
+}
+
+// f(x, value of x in the other lane) over all G lanes of a group
+template <int G, class X, class F>
+__device__ __forceinline__ X group_reduce(X x, F f) {
+    if constexpr (G > 1) x = f(x, from_lane_xor<1>(x));
+    if constexpr (G > 2) x = f(x, from_lane_xor<2>(x));
+    if constexpr (G > 4) x = f(x, from_lane_xor<4>(x));
+    if constexpr (G > 8) x = f(x, from_lane_xor<8>(x));
+    if constexpr (G > 16) x = f(x, from_lane_xor<16>(x));
+    if constexpr (G > 32) x = f(x, from_lane_xor<32>(x));
     return x;
+}
+__device__ __forceinline__ float wave_sum(float x) {
+    return group_reduce<64>(x, [](float a, float b) { return a + b; });
 }
 
 }  // namespace bps

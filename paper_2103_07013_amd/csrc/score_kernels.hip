@@ -76,133 +76,491 @@ __device__ __forceinline__ uint64_t order_of(float x, uint32_t at) {
     return (uint64_t)up << 32 | (uint32_t)~at;
 }
 
-template <class T, bool MASK>
-__global__ __launch_bounds__(256) void k_score(ScoreArgs a) {
-    constexpr int N = T::kPer16;
-    __shared__ Part parts[4];
-    __shared__ uint64_t best[4];
-    const uint32_t tid = threadIdx.x, wave = tid >> 6, lane = tid & 63u;
+template <int X>
+__device__ __forceinline__ Part from_lane_xor(const Part& p) {
+    return {bps::from_lane_xor<X>(p.m), bps::from_lane_xor<X>(p.z), bps::from_lane_xor<X>(p.s)};
+}
+template <int G>
+__device__ __forceinline__ Part group_part(Part p, float c) {
+    if constexpr (G > 1) p = joined(p, from_lane_xor<1>(p), c);
+    if constexpr (G > 2) p = joined(p, from_lane_xor<2>(p), c);
+    if constexpr (G > 4) p = joined(p, from_lane_xor<4>(p), c);
+    if constexpr (G > 8) p = joined(p, from_lane_xor<8>(p), c);
+    if constexpr (G > 16) p = joined(p, from_lane_xor<16>(p), c);
+    if constexpr (G > 32) p = joined(p, from_lane_xor<32>(p), c);
+    return p;
+}
+
+// What a row's sums say, written by one lane.
+template <class T>
+__device__ __forceinline__ void write_row(const ScoreArgs& a, uint64_t r, const Part& p, float ln_z, const typename T::raw* row, const uint8_t* mask) {
+    const bool empty = p.z == 0.0f;
+    a.norm[2 * r] = p.m;
+    a.norm[2 * r + 1] = ln_z;
+    a.lse[r] = empty ? -kInf : fmaf(a.scale, p.m, ln_z);
+    a.entropy[r] = empty ? 0.0f : ln_z - kLn2 * (p.s / p.z);
+    const int64_t t = token_at(a.tokens, a.tokens64, r);
+    float lp = 0.0f;
+    if (t < -1 || t >= (int64_t)a.entries) {
+        lp = __builtin_nanf("");
+    } else if (t >= 0) {
+        const float x = !mask || mask[t] ? to_float(row[t]) : -kInf;
+        lp = empty ? -kInf : fmaf(x - p.m, a.scale, -ln_z);
+    }
+    a.logp[r] = lp;
+}
+template <class T>
+__device__ __forceinline__ void write_alternative(const ScoreArgs& a, uint64_t to, uint64_t order, const Part& p, float ln_z, const typename T::raw* row) {
+    const uint32_t at = ~(uint32_t)order;
+    a.top_ids[to] = order ? (int32_t)at : -1;
+    a.top_logp[to] = order ? fmaf(to_float(row[at]) - p.m, a.scale, -ln_z) : -kInf;
+}
+
+// ---- rows of up to G * N entries: G lanes for a row, N entries of it in each; alternatives one after the other
+
+template <class T, bool MASK, bool TOP, int G, int N>
+__global__ __launch_bounds__(256) void k_score_short(ScoreArgs a) {
+    const uint32_t lane = threadIdx.x & (G - 1);
+    const uint64_t r = (uint64_t)blockIdx.x * (256 / G) + threadIdx.x / G;
+    if (r >= a.rows) return;
     const float c = a.scale * kLog2e;
-    for (uint64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
-        const typename T::raw* row = static_cast<const typename T::raw*>(a.logits) + (int64_t)r * a.row_stride;
-        const uint8_t* mask = MASK ? a.mask + (int64_t)r * a.mask_stride : nullptr;
-        Part p = nothing();
-        for (uint32_t at = tid * N; at < a.entries; at += 256 * N) {
-            float x[N];
-            row_entries<T, N, MASK>(row, mask, at, a.entries, x);
-            add(p, x, c);
-        }
-        for (int d = 32; d; d >>= 1) p = joined(p, {__shfl_xor(p.m, d, 64), __shfl_xor(p.z, d, 64), __shfl_xor(p.s, d, 64)}, c);
-        __syncthreads();
-        if (lane == 0) parts[wave] = p;
-        __syncthreads();
-        p = joined(joined(parts[0], parts[1], c), joined(parts[2], parts[3], c), c);
-        const float ln_z = logf(p.z);
-        if (tid == 0) {
-            const bool empty = p.z == 0.0f;
-            a.norm[2 * r] = p.m;
-            a.norm[2 * r + 1] = ln_z;
-            a.lse[r] = empty ? -kInf : fmaf(a.scale, p.m, ln_z);
-            a.entropy[r] = empty ? 0.0f : ln_z - kLn2 * (p.s / p.z);
-            const int64_t t = token_at(a.tokens, a.tokens64, r);
-            float lp = 0.0f;
-            if (t < -1 || t >= (int64_t)a.entries) {
-                lp = __builtin_nanf("");
-            } else if (t >= 0) {
-                const float x = !MASK || mask[t] ? to_float(row[t]) : -kInf;
-                lp = empty ? -kInf : fmaf(x - p.m, a.scale, -ln_z);
-            }
-            a.logp[r] = lp;
-        }
+    const typename T::raw* row = static_cast<const typename T::raw*>(a.logits) + (int64_t)r * a.row_stride;
+    const uint8_t* mask = MASK ? a.mask + (int64_t)r * a.mask_stride : nullptr;
+    float x[N];
+    row_entries<T, N, MASK>(row, mask, lane * N, a.entries, x);
+    Part p = nothing();
+    add(p, x, c);
+    p = group_part<G>(p, c);
+    const float ln_z = logf(p.z);
+    if (lane == 0) write_row<T>(a, r, p, ln_z, row, mask);
+    if constexpr (TOP) {
         uint64_t below = ~0ull;
         for (uint32_t k = 0; k < a.top_k; ++k) {
             uint64_t b = 0;
-            for (uint32_t at = tid; at < a.entries; at += 256) {
-                const float x = !MASK || mask[at] ? to_float(row[at]) : -kInf;
-                const uint64_t o = order_of(x, at);
-                if (x != -kInf && o < below && o > b) b = o;
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const uint64_t o = order_of(x[e], lane * N + e);
+                if (x[e] != -kInf && o < below && o > b) b = o;
             }
-            for (int d = 32; d; d >>= 1) {
-                const uint64_t o = __shfl_xor((unsigned long long)b, d, 64);
-                b = o > b ? o : b;
-            }
-            __syncthreads();
-            if (lane == 0) best[wave] = b;
-            __syncthreads();
-            for (int w = 0; w < 4; ++w) b = best[w] > b ? best[w] : b;
-            if (tid == 0) {
-                const uint64_t to = r * a.top_k + k;
-                const uint32_t at = ~(uint32_t)b;
-                a.top_ids[to] = b ? (int32_t)at : -1;
-                a.top_logp[to] = b ? fmaf(to_float(row[at]) - p.m, a.scale, -ln_z) : -kInf;
-            }
+            b = group_reduce<G>(b, [](uint64_t u, uint64_t v) { return u > v ? u : v; });
+            if (lane == 0) write_alternative<T>(a, r * a.top_k + k, b, p, ln_z, row);
             below = b;
         }
     }
 }
 
-template <class T, bool MASK>
-__global__ __launch_bounds__(256) void k_score_grad(ScoreGradArgs a) {
-    constexpr int N = T::kPer16;
-    for (uint64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
-        const typename T::raw* row = static_cast<const typename T::raw*>(a.logits) + (int64_t)r * a.row_stride;
-        const uint8_t* mask = MASK ? a.mask + (int64_t)r * a.mask_stride : nullptr;
-        typename T::raw* out = static_cast<typename T::raw*>(a.out) + (int64_t)r * a.out_stride;
-        const float m = a.norm[2 * r], ln_z = a.norm[2 * r + 1], entropy = a.entropy[r], logp = a.logp[r];
-        const int64_t t = token_at(a.tokens, a.tokens64, r);
-        const float gh = a.grad_entropy ? a.grad_entropy[r] : 0.0f;
-        const float gl = !a.grad_logp || t == -1 || logp == -kInf ? 0.0f : t < -1 || t >= (int64_t)a.entries ? __builtin_nanf("") : a.grad_logp[r];
-        const float base = fmaf(gh, entropy, gl);
-        for (uint32_t at = threadIdx.x * N; at < a.entries; at += 256 * N) {
-            float x[N], g[N];
-            row_entries<T, N, MASK>(row, mask, at, a.entries, x);
+// ---- longer rows: a wavefront, or a work-group, streams a row or a piece of one
+
+// The best 64 of what a wavefront has seen, one in each lane in descending order; 0 = none.
+// A bitonic network: halves that are sorted are joined by a comparison with the mirrored lane, then with lanes at falling distances.
+template <int X>
+__device__ __forceinline__ uint64_t exchanged(uint64_t v, bool keep_larger) {
+    const uint64_t o = bps::from_lane_xor<X>(v);
+    return (o > v) == keep_larger ? o : v;
+}
+template <int X>
+__device__ __forceinline__ uint64_t settled(uint64_t v, uint32_t lane) {      // comparisons at the distances X, X / 2 .. 1
+    v = exchanged<X>(v, (lane & X) == 0);
+    if constexpr (X > 1) v = settled<X / 2>(v, lane);
+    return v;
+}
+__device__ __forceinline__ uint64_t sorted(uint64_t v, uint32_t lane) {
+    v = exchanged<1>(v, (lane & 1) == 0);
+    v = settled<1>(exchanged<3>(v, (lane & 2) == 0), lane);
+    v = settled<2>(exchanged<7>(v, (lane & 4) == 0), lane);
+    v = settled<4>(exchanged<15>(v, (lane & 8) == 0), lane);
+    v = settled<8>(exchanged<31>(v, (lane & 16) == 0), lane);
+    return settled<16>(exchanged<63>(v, (lane & 32) == 0), lane);
+}
+// the best 64 of two lists that are sorted
+__device__ __forceinline__ uint64_t merged(uint64_t a, uint64_t b, uint32_t lane) {
+    const uint64_t o = bps::from_lane_xor<63>(b);
+    return settled<32>(o > a ? o : a, lane);
+}
+
+// The float that an order stands for (see order_of); an order of 0 stands for -inf.
+__device__ __forceinline__ float value_of(uint64_t order) {
+    const uint32_t up = (uint32_t)(order >> 32);
+    return up == 0u ? -kInf : __uint_as_float((up & 0x80000000u) ? up & 0x7FFFFFFFu : ~up);
+}
+
+constexpr uint32_t kWaiting = 128;     // candidates that wait for a sort, per wavefront
+
+struct Best {
+    uint64_t list;            // sorted, one per lane
+    uint64_t* waiting;        // LDS, kWaiting of this wavefront
+    uint32_t count;           // of them, below 64 between calls
+    float least;              // entries below it are no candidates
+
+    __device__ __forceinline__ void take_in(uint32_t lane, uint32_t k, uint32_t n) {
+        // the wavefront's own stores, in order before its loads
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        const uint64_t v = lane < n ? waiting[lane] : 0;
+        list = merged(list, sorted(v, lane), lane);
+        const uint64_t last = __shfl((unsigned long long)list, (int)k - 1, 64);
+        least = value_of(last);
+    }
+    __device__ __forceinline__ void offer(float x, uint32_t at, uint32_t lane, uint32_t k) {
+        const bool is = !(x < least) && x != -kInf;
+        const uint64_t who = __ballot(is);
+        if (!who) return;
+        if (is) waiting[count + lanes_before(who)] = order_of(x, at);
+        count += (uint32_t)__popcll(who);
+        if (count >= 64) {
+            take_in(lane, k, 64);
+            count -= 64;
+            const uint64_t v = waiting[64 + lane];
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            if (lane < count) waiting[lane] = v;
+        }
+    }
+    __device__ __forceinline__ void finish(uint32_t lane, uint32_t k) {
+        if (count) take_in(lane, k, count);
+        count = 0;
+    }
+};
+
+// Entries [from, to) of a row, by `threads` threads.
+template <class T, bool MASK, bool TOP>
+__device__ __forceinline__ Part stream(const typename T::raw* row, const uint8_t* mask, uint32_t from, uint32_t to, uint32_t tid, uint32_t threads, float c, Best& best,
+                                       uint32_t k) {
+    constexpr int N = T::kPer16, U = 4;
+    const uint32_t lane = tid & 63u;
+    Part p = nothing();
+    bool first = true;
+    for (uint32_t base = from; base < to; base += threads * N * U) {
+        float x[U][N];
 #pragma unroll
-            for (int k = 0; k < N; ++k) {
-                const float lp = fmaf(x[k] - m, a.scale, -ln_z);
-                const float p = __builtin_amdgcn_exp2f(lp * kLog2e);
-                g[k] = -p * fmaf(gh, lp, base);
-                if (at + k == (uint64_t)t) g[k] += gl;
-                g[k] = x[k] == -kInf ? 0.0f : g[k] * a.scale;
+        for (int u = 0; u < U; ++u) row_entries<T, N, MASK>(row, mask, base + (u * threads + tid) * N, to, x[u]);
+        float flat[U * N];
+#pragma unroll
+        for (int e = 0; e < U * N; ++e) flat[e] = x[e / N][e % N];
+        add(p, flat, c);
+        if constexpr (TOP) {
+            float top = -kInf;
+#pragma unroll
+            for (int e = 0; e < U * N; ++e) top = fmaxf(top, flat[e]);
+            if (first) {
+                // the k-th best of the lanes' own best is no better than the k-th of all
+                const uint64_t own = sorted(top != -kInf ? order_of(top, 0u) : 0ull, lane);
+                best.least = value_of(__shfl((unsigned long long)own, (int)k - 1, 64));
+                first = false;
             }
-            if (at + N <= a.entries) {
-                store<T, N>(out + at, g);
-            } else {
+            if (__ballot((top >= best.least && top != -kInf) || p.z != p.z)) {
 #pragma unroll
-                for (int k = 0; k < N; ++k)
-                    if (at + k < a.entries) out[at + k] = rounded<T>(g[k]);
+                for (int e = 0; e < U * N; ++e) best.offer(flat[e], base + ((e / N) * threads + tid) * N + e % N, lane, k);
             }
         }
     }
+    return p;
 }
 
-uint32_t groups(uint64_t n) { return (uint32_t)(n < 65536 ? n : 65536); }
+// WAVES wavefronts for a row, four or more to a work-group.
+template <class T, bool MASK, bool TOP, int WAVES>
+__global__ __launch_bounds__(WAVES > 4 ? WAVES * 64 : 256) void k_score(ScoreArgs a) {
+    constexpr uint32_t kGroup = WAVES > 4 ? WAVES * 64 : 256, kWaves = kGroup / 64;
+    __shared__ uint64_t waiting[TOP ? kWaves * kWaiting : 1];
+    __shared__ Part parts[kWaves];
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
+    const uint64_t r = (uint64_t)blockIdx.x * (kWaves / WAVES) + wave / WAVES;
+    const float c = a.scale * kLog2e;
+    if (r >= a.rows) return;        // whole wavefronts, and where they share a row whole work-groups
+    const typename T::raw* row = static_cast<const typename T::raw*>(a.logits) + (int64_t)r * a.row_stride;
+    const uint8_t* mask = MASK ? a.mask + (int64_t)r * a.mask_stride : nullptr;
+    Best best = {0, waiting + (TOP ? wave * kWaiting : 0), 0, -kInf};
+    Part p = stream<T, MASK, TOP>(row, mask, 0, a.entries, threadIdx.x % (64 * WAVES), 64 * WAVES, c, best, a.top_k);
+    p = group_part<64>(p, c);
+    if constexpr (TOP) best.finish(lane, a.top_k);
+    if constexpr (WAVES > 1) {
+        if (lane == 0) parts[wave] = p;
+        if (TOP) best.waiting[lane] = best.list;
+        __syncthreads();
+        if (wave) return;
+        p = parts[0];
+        for (uint32_t w = 1; w < WAVES; ++w) {
+            p = joined(p, parts[w], c);
+            if (TOP) best.list = merged(best.list, waiting[w * kWaiting + lane], lane);
+        }
+    }
+    const float ln_z = logf(p.z);
+    if (lane == 0) write_row<T>(a, r, p, ln_z, row, mask);
+    if (TOP && lane < a.top_k) write_alternative<T>(a, r * a.top_k + lane, best.list, p, ln_z, row);
+}
 
+// ---- few long rows: a work-group for each piece of a row, and one for each row that joins them
+
+struct Pieces {
+    uint32_t count, length;      // of a row; length in entries
+};
+struct __align__(16) PieceSums {
+    Part p;
+    float pad;
+};
+
+template <class T, bool MASK, bool TOP>
+__global__ __launch_bounds__(256) void k_score_piece(ScoreArgs a, Pieces pieces, PieceSums* sums, uint64_t* lists) {
+    __shared__ uint64_t waiting[TOP ? 4 * kWaiting : 1];
+    __shared__ Part parts[4];
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
+    const uint64_t r = blockIdx.x / pieces.count;
+    const uint32_t piece = blockIdx.x % pieces.count, from = piece * pieces.length;
+    const uint32_t to = a.entries - from < pieces.length ? a.entries : from + pieces.length;
+    const float c = a.scale * kLog2e;
+    const typename T::raw* row = static_cast<const typename T::raw*>(a.logits) + (int64_t)r * a.row_stride;
+    const uint8_t* mask = MASK ? a.mask + (int64_t)r * a.mask_stride : nullptr;
+    Best best = {0, waiting + (TOP ? wave * kWaiting : 0), 0, -kInf};
+    Part p = stream<T, MASK, TOP>(row, mask, from, to, threadIdx.x, 256, c, best, a.top_k);
+    p = group_part<64>(p, c);
+    if constexpr (TOP) best.finish(lane, a.top_k);
+    if (lane == 0) parts[wave] = p;
+    if (TOP) best.waiting[lane] = best.list;
+    __syncthreads();
+    if (wave) return;
+    p = joined(joined(parts[0], parts[1], c), joined(parts[2], parts[3], c), c);
+    if (lane == 0) sums[blockIdx.x] = {p, 0.0f};
+    if constexpr (TOP) {
+        for (uint32_t w = 1; w < 4; ++w) best.list = merged(best.list, waiting[w * kWaiting + lane], lane);
+        if (lane < a.top_k) lists[(uint64_t)blockIdx.x * a.top_k + lane] = best.list;
+    }
+}
+
+constexpr uint32_t kMaxPieces = 64;
+
+template <class T, bool TOP>
+__global__ __launch_bounds__(TOP ? 1024 : 64) void k_score_join(ScoreArgs a, Pieces pieces, const PieceSums* sums, const uint64_t* lists) {
+    constexpr uint32_t kWaves = TOP ? 16 : 1;
+    __shared__ uint64_t held[kWaves * 64];
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
+    const uint64_t r = blockIdx.x;
+    const float c = a.scale * kLog2e;
+    const typename T::raw* row = static_cast<const typename T::raw*>(a.logits) + (int64_t)r * a.row_stride;
+    const uint8_t* mask = a.mask ? a.mask + (int64_t)r * a.mask_stride : nullptr;
+    uint64_t list = 0;
+    if constexpr (TOP) {
+        const uint32_t n = pieces.count * a.top_k;
+        for (uint32_t at = wave * 64; at < n; at += kWaves * 64) {
+            const uint64_t v = at + lane < n ? lists[r * n + at + lane] : 0;
+            list = merged(list, sorted(v, lane), lane);
+        }
+        held[threadIdx.x] = list;
+        // half of the lists are joined to the other half, until one is left
+        for (uint32_t half = kWaves / 2; half; half /= 2) {
+            __syncthreads();
+            if (wave < half) {
+                list = merged(list, held[(wave + half) * 64 + lane], lane);
+                held[threadIdx.x] = list;
+            }
+        }
+        if (wave) return;
+    }
+    Part p = lane < pieces.count ? sums[r * pieces.count + lane].p : nothing();
+    p = group_part<64>(p, c);
+    const float ln_z = logf(p.z);
+    if (lane == 0) write_row<T>(a, r, p, ln_z, row, mask);
+    if (TOP && lane < a.top_k) write_alternative<T>(a, r * a.top_k + lane, list, p, ln_z, row);
+}
+
+// ---- gradient
+
+struct RowGrad {
+    float m, ln_z, gl, gh, base;
+    int64_t t;
+};
+__device__ __forceinline__ RowGrad row_grad(const ScoreGradArgs& a, uint64_t r) {
+    RowGrad g;
+    g.m = a.norm[2 * r];
+    g.ln_z = a.norm[2 * r + 1];
+    g.t = token_at(a.tokens, a.tokens64, r);
+    g.gh = a.grad_entropy ? a.grad_entropy[r] : 0.0f;
+    g.gl = !a.grad_logp || g.t == -1 || a.logp[r] == -kInf ? 0.0f : g.t < -1 || g.t >= (int64_t)a.entries ? __builtin_nanf("") : a.grad_logp[r];
+    g.base = fmaf(g.gh, a.entropy[r], g.gl);
+    return g;
+}
+template <int N>
+__device__ __forceinline__ void gradient(const RowGrad& g, float scale, uint32_t at, const float (&x)[N], float (&d)[N]) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const float lp = fmaf(x[k] - g.m, scale, -g.ln_z);
+        const float p = __builtin_amdgcn_exp2f(lp * kLog2e);
+        d[k] = -p * fmaf(g.gh, lp, g.base);
+        if (at + k == (uint64_t)g.t) d[k] += g.gl;
+        d[k] = x[k] == -kInf ? 0.0f : d[k] * scale;
+    }
+}
+template <class T, int N>
+__device__ __forceinline__ void store_entries(typename T::raw* out, uint32_t at, uint32_t end, const float (&d)[N]) {
+    if (at + N <= end) {
+        store<T, N>(out + at, d);
+    } else {
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+            if (at + k < end) out[at + k] = rounded<T>(d[k]);
+    }
+}
+
+template <class T, bool MASK, int G, int N>
+__global__ __launch_bounds__(256) void k_score_grad_short(ScoreGradArgs a) {
+    const uint32_t lane = threadIdx.x & (G - 1);
+    const uint64_t r = (uint64_t)blockIdx.x * (256 / G) + threadIdx.x / G;
+    if (r >= a.rows) return;
+    const RowGrad g = row_grad(a, r);
+    float x[N], d[N];
+    row_entries<T, N, MASK>(static_cast<const typename T::raw*>(a.logits) + (int64_t)r * a.row_stride, MASK ? a.mask + (int64_t)r * a.mask_stride : nullptr, lane * N, a.entries, x);
+    gradient(g, a.scale, lane * N, x, d);
+    store_entries<T, N>(static_cast<typename T::raw*>(a.out) + (int64_t)r * a.out_stride, lane * N, a.entries, d);
+}
+
+// Work-groups take pieces of rows, the last row first: what of the logits the forward pass read last may still be in a cache.
+template <class T, bool MASK, int GROUP>
+__global__ __launch_bounds__(GROUP) void k_score_grad(ScoreGradArgs a, uint32_t pieces) {
+    constexpr int N = T::kPer16, U = 4;
+    const uint64_t r = a.rows - 1 - blockIdx.x / pieces;
+    const uint32_t from = blockIdx.x % pieces * (GROUP * N * U);
+    const RowGrad g = row_grad(a, r);
+    const typename T::raw* row = static_cast<const typename T::raw*>(a.logits) + (int64_t)r * a.row_stride;
+    const uint8_t* mask = MASK ? a.mask + (int64_t)r * a.mask_stride : nullptr;
+    typename T::raw* out = static_cast<typename T::raw*>(a.out) + (int64_t)r * a.out_stride;
+    float x[U][N], d[N];
+#pragma unroll
+    for (int u = 0; u < U; ++u) row_entries<T, N, MASK>(row, mask, from + (u * GROUP + threadIdx.x) * N, a.entries, x[u]);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const uint32_t at = from + (u * GROUP + threadIdx.x) * N;
+        gradient(g, a.scale, at, x[u], d);
+        store_entries<T, N>(out, at, a.entries, d);
+    }
+}
+
+// ---- which kernel
+
+// Rows of up to this many entries are shared by few lanes (see below), longer ones by a wavefront at least.
+constexpr uint32_t kShort = 128;
+// Rows of up to kWaveRow entries have one wavefront.
+constexpr uint32_t kWaveRow = 2048;
+constexpr uint32_t kComputeUnits = 256;
+
+// How many pieces a row is cut into: where there is not a work-group of whole rows for each compute unit, but never below 4096 entries.
+Pieces pieces_of(uint64_t rows, uint32_t entries) {
+    if (entries <= 2 * 4096 || rows >= kComputeUnits) return {1, entries};
+    uint64_t n = (2 * kComputeUnits + rows - 1) / rows;
+    const uint32_t most = (entries + 4095) / 4096;
+    if (n > most) n = most;
+    if (n > kMaxPieces) n = kMaxPieces;
+    uint32_t length = (uint32_t)((entries + n - 1) / n);
+    length = (length + 63) / 64 * 64;
+    return {(entries + length - 1) / length, length};
+}
+
+#define BPS_ROWS(kernel, per_group, threads, ...) \
+    hipLaunchKernelGGL((kernel<T, MASK, __VA_ARGS__>), dim3((uint32_t)((a.rows + (per_group) - 1) / (per_group))), dim3(threads), 0, stream, a)
+
+template <class T, bool MASK, bool TOP>
+hipError_t score(const ScoreArgs& a, hipStream_t stream) {
+    const Pieces pieces = pieces_of(a.rows, a.entries);
+    if (a.entries <= kShort && a.top_k <= 8) {
+        if (a.entries <= 8)
+            BPS_ROWS(k_score_short, 64, 256, TOP, 4, 2);
+        else if (a.entries <= 32)
+            BPS_ROWS(k_score_short, 32, 256, TOP, 8, 4);
+        else
+            BPS_ROWS(k_score_short, 16, 256, TOP, 16, 8);
+    } else if (pieces.count > 1) {
+        PieceSums* sums = static_cast<PieceSums*>(a.workspace);
+        uint64_t* lists = reinterpret_cast<uint64_t*>(sums + a.rows * pieces.count);
+        hipLaunchKernelGGL((k_score_piece<T, MASK, TOP>), dim3((uint32_t)(a.rows * pieces.count)), dim3(256), 0, stream, a, pieces, sums, lists);
+        hipLaunchKernelGGL((k_score_join<T, TOP>), dim3((uint32_t)a.rows), dim3(TOP ? 1024 : 64), 0, stream, a, pieces, sums, lists);
+    } else if (a.entries <= kWaveRow) {
+        BPS_ROWS(k_score, 4, 256, TOP, 1);
+    } else {
+        BPS_ROWS(k_score, 1, 256, TOP, 4);
+    }
+    return hipGetLastError();
+}
 template <class T>
 hipError_t score(const ScoreArgs& a, hipStream_t stream) {
-    if (a.mask)
-        hipLaunchKernelGGL((k_score<T, true>), dim3(groups(a.rows)), dim3(256), 0, stream, a);
-    else
-        hipLaunchKernelGGL((k_score<T, false>), dim3(groups(a.rows)), dim3(256), 0, stream, a);
+    if (a.mask) return a.top_k ? score<T, true, true>(a, stream) : score<T, true, false>(a, stream);
+    return a.top_k ? score<T, false, true>(a, stream) : score<T, false, false>(a, stream);
+}
+
+template <class T, bool MASK>
+hipError_t score_grad_masked(const ScoreGradArgs& a, hipStream_t stream) {
+    if (a.entries <= 8) {
+        BPS_ROWS(k_score_grad_short, 64, 256, 4, 2);
+    } else if (a.entries <= 32) {
+        BPS_ROWS(k_score_grad_short, 32, 256, 8, 4);
+    } else if (a.entries <= kShort) {
+        BPS_ROWS(k_score_grad_short, 16, 256, 16, 8);
+    } else {
+        const uint32_t wave = 64 * T::kPer16 * 4, group = 4 * wave;
+        const uint32_t pieces = a.entries <= wave ? 1 : (a.entries + group - 1) / group;
+        if (a.entries <= wave)
+            hipLaunchKernelGGL((k_score_grad<T, MASK, 64>), dim3((uint32_t)a.rows), dim3(64), 0, stream, a, pieces);
+        else
+            hipLaunchKernelGGL((k_score_grad<T, MASK, 256>), dim3((uint32_t)(a.rows * pieces)), dim3(256), 0, stream, a, pieces);
+    }
     return hipGetLastError();
 }
+#undef BPS_ROWS
 template <class T>
 hipError_t score_grad(const ScoreGradArgs& a, hipStream_t stream) {
-    if (a.mask)
-        hipLaunchKernelGGL((k_score_grad<T, true>), dim3(groups(a.rows)), dim3(256), 0, stream, a);
-    else
-        hipLaunchKernelGGL((k_score_grad<T, false>), dim3(groups(a.rows)), dim3(256), 0, stream, a);
-    return hipGetLastError();
+    return a.mask ? score_grad_masked<T, true>(a, stream) : score_grad_masked<T, false>(a, stream);
 }
 
 }  // namespace
 
-size_t score_workspace(int32_t, uint64_t, uint32_t, uint32_t) { return 0; }
+namespace {
+
+// Work-groups of one launch; a grid has to have less than 2^32 threads.
+constexpr uint64_t kMaxGroups = 1u << 21;
+
+template <class A>
+A rows_of(const A& a, int32_t dtype, uint64_t first, uint64_t rows) {
+    A s = a;
+    s.rows = rows;
+    s.logits = static_cast<const char*>(a.logits) + (int64_t)first * a.row_stride * (dtype == BPS_F32 ? 4 : 2);
+    s.tokens = static_cast<const char*>(a.tokens) + first * (a.tokens64 ? 8 : 4);
+    if (a.mask) s.mask = a.mask + (int64_t)first * a.mask_stride;
+    s.logp = a.logp + first;
+    s.entropy = a.entropy + first;
+    s.norm = a.norm + 2 * first;
+    return s;
+}
+
+}  // namespace
+
+size_t score_workspace(int32_t, uint64_t rows, uint32_t entries, uint32_t top_k) {
+    const Pieces pieces = pieces_of(rows, entries);
+    return pieces.count > 1 ? rows * pieces.count * (sizeof(PieceSums) + top_k * sizeof(uint64_t)) : 0;
+}
 
 hipError_t launch_score(int32_t dtype, const ScoreArgs& a, hipStream_t stream) {
-    return dtype == BPS_F32 ? score<F32>(a, stream) : dtype == BPS_BF16 ? score<Bf16>(a, stream) : score<F16>(a, stream);
+    // rows that are cut into pieces are few, others have at most one work-group each
+    for (uint64_t first = 0; first < a.rows; first += kMaxGroups) {
+        ScoreArgs s = rows_of(a, dtype, first, a.rows - first < kMaxGroups ? a.rows - first : kMaxGroups);
+        s.lse = a.lse + first;
+        if (a.top_k) {
+            s.top_ids = a.top_ids + first * a.top_k;
+            s.top_logp = a.top_logp + first * a.top_k;
+        }
+        const hipError_t e = dtype == BPS_F32 ? score<F32>(s, stream) : dtype == BPS_BF16 ? score<Bf16>(s, stream) : score<F16>(s, stream);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
+
 hipError_t launch_score_grad(int32_t dtype, const ScoreGradArgs& a, hipStream_t stream) {
-    return dtype == BPS_F32 ? score_grad<F32>(a, stream) : dtype == BPS_BF16 ? score_grad<Bf16>(a, stream) : score_grad<F16>(a, stream);
+    const uint64_t each = kMaxGroups / (1 + a.entries / 4096);
+    for (uint64_t left = a.rows; left;) {      // the last rows first, as within a launch
+        const uint64_t n = left < each ? left : each;
+        left -= n;
+        ScoreGradArgs s = rows_of(a, dtype, left, n);
+        if (a.grad_logp) s.grad_logp = a.grad_logp + left;
+        if (a.grad_entropy) s.grad_entropy = a.grad_entropy + left;
+        s.out = static_cast<char*>(a.out) + (int64_t)left * a.out_stride * (dtype == BPS_F32 ? 4 : 2);
+        const hipError_t e = dtype == BPS_F32 ? score_grad<F32>(s, stream) : dtype == BPS_BF16 ? score_grad<Bf16>(s, stream) : score_grad<F16>(s, stream);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace bps
