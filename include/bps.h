@@ -257,7 +257,7 @@ enum { BPS_F32 = 0, BPS_BF16 = 1, BPS_F16 = 2 };
  *   lse       float32 [rows]  ln sum e^y, -inf where nothing takes part
  *   logp      float32 [rows]  y[token] - lse; 0 for token -1, -inf for a token that takes no part, NaN for one that is no entry
  *   entropy   float32 [rows]  -sum p ln p, 0 where nothing takes part
- *   norm      float32 [rows][2] the largest logit that takes part and ln sum e^(y - scale * it), for the gradient: the two
+ *   norm      float32 [2][rows] the largest logits that take part, then ln sum e^(y - scale * it), for the gradient: the two
  *             apart keep what their sum, lse, loses where the logits are large
  *   top_ids   int32 [rows][top_k]   the top_k entries of the largest logits, ties to the lower index, -1 where there are fewer
  *   top_logp  float32 [rows][top_k] their log probabilities, -inf where there are fewer;   both may be NULL where top_k is 0

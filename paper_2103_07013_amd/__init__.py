@@ -16,9 +16,13 @@ __all__ = ["BpsError", "Renderer", "bps_create", "bps_destroy", "bps_last_error"
            "log_probs", "log_probs_backward", "LogProbs", "embedding", "embedding_backward", "AdamW"]
 
 
+_POLICY = ("log_probs", "log_probs_backward", "LogProbs", "embedding", "embedding_backward", "AdamW")
+
+
 def __getattr__(name):
     # the policy's operators need torch from the start, the renderer only where it is given torch's tensors
-    if name in ("log_probs", "log_probs_backward", "LogProbs", "embedding", "embedding_backward", "AdamW"):
+    if name in _POLICY:
         from . import policy
-        return getattr(policy, name)
+        globals().update((n, getattr(policy, n)) for n in _POLICY)
+        return globals()[name]
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

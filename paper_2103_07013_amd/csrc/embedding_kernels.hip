@@ -3,7 +3,8 @@
 // Gradient: (row, token) pairs are sorted by row, stably, by digits of a few bits from the lowest up; the sorted order
 // is cut into pieces of equal length, and one group of lanes walks a piece, adding up gradient rows in float32 in
 // that order.  A row that lies within one piece is written at once.  One that is cut by a piece's bounds leaves a
-// partial sum per piece, which are added in order by a second kernel.  Rows without a token are found by search.
+// partial sum per piece, which are added in order by a second kernel.  The sort marks the rows that have a token; the others
+// are written as zeros next to the sums.
 #include "policy_device.h"
 #include "policy_kernels.h"
 
@@ -12,6 +13,11 @@ namespace bps {
 namespace {
 
 constexpr uint32_t kSortGroup = 256, kSortTile = 2048, kMaxDigit = 9;
+// Up to this many tokens are sorted by one work-group, in one launch: the passes of a work-group take longer the more there are,
+// those of many pay two launches each.
+constexpr uint32_t kSortOne = 4096, kSortOneGroup = 1024;
+// Up to this many tiles each work-group adds up the counts of those before its own by itself; for more a launch in between does.
+constexpr uint32_t kSumTiles = 32;
 
 uint32_t bits_of(uint32_t v) {
     uint32_t b = 0;
@@ -46,30 +52,70 @@ __device__ __forceinline__ uint64_t peers_of(uint32_t digit, uint32_t bits, bool
     return same;
 }
 
-// counts[digit][tile]
-__global__ __launch_bounds__(kSortGroup) void k_sort_count(const void* tokens, int tokens64, const uint32_t* keys, uint32_t count, uint32_t rows,
-                                                           uint32_t shift, uint32_t bits, uint32_t tiles, uint32_t* counts) {
+struct SortArgs {
+    const void* tokens;       // of the first pass, where keys is null
+    const uint32_t *keys, *places;
+    uint32_t *out_keys, *out_places;
+    uint32_t* counts;         // [tile][digit], and the digits' totals behind the last tile
+    uint8_t* marks;           // [rows, in whole words], 1 where a row has a token
+    int32_t tokens64;
+    uint32_t count, rows, shift, bits, tiles, last;
+};
+__device__ __forceinline__ uint32_t sort_key(const SortArgs& a, uint32_t i) { return a.keys ? a.keys[i] : key_at(a.tokens, a.tokens64, i, a.rows); }
+
+__global__ __launch_bounds__(kSortGroup) void k_sort_count(SortArgs a) {
     __shared__ uint32_t hist[1u << kMaxDigit];
-    const uint32_t bins = 1u << bits;
+    const uint32_t bins = 1u << a.bits;
     for (uint32_t b = threadIdx.x; b < bins; b += kSortGroup) hist[b] = 0;
     __syncthreads();
     const uint32_t first = blockIdx.x * kSortTile;
-    for (uint32_t k = threadIdx.x; k < kSortTile; k += kSortGroup) {
-        const uint32_t i = first + k;
-        if (i < count) atomicAdd(&hist[((keys ? keys[i] : key_at(tokens, tokens64, i, rows)) >> shift) & (bins - 1)], 1u);
+    uint32_t key[kSortTile / kSortGroup];
+#pragma unroll
+    for (uint32_t k = 0; k < kSortTile / kSortGroup; ++k) {
+        const uint32_t i = first + k * kSortGroup + threadIdx.x;
+        key[k] = i < a.count ? sort_key(a, i) : 0u;
     }
+#pragma unroll
+    for (uint32_t k = 0; k < kSortTile / kSortGroup; ++k)
+        if (first + k * kSortGroup + threadIdx.x < a.count) atomicAdd(&hist[(key[k] >> a.shift) & (bins - 1)], 1u);
+    // marks are cleared by the first pass and set by the last
+    if (!a.keys && a.marks)
+        for (uint32_t r = blockIdx.x * kSortGroup + threadIdx.x; r < (a.rows + 3) / 4; r += gridDim.x * kSortGroup) reinterpret_cast<uint32_t*>(a.marks)[r] = 0;
     __syncthreads();
-    for (uint32_t b = threadIdx.x; b < bins; b += kSortGroup) counts[(size_t)b * tiles + blockIdx.x] = hist[b];
+    for (uint32_t b = threadIdx.x; b < bins; b += kSortGroup) a.counts[(size_t)blockIdx.x * bins + b] = hist[b];
 }
 
-// exclusive sums in place, by one work-group
-__global__ __launch_bounds__(1024) void k_sort_scan(uint32_t* counts, uint32_t n) {
-    __shared__ uint32_t sums[16];
-    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6;
-    const uint32_t each = (n + 1023u) / 1024u, from = tid * each < n ? tid * each : n, to = from + each < n ? from + each : n;
+// Many tiles: a thread for each digit turns its counts into the number of equal digits in tiles before, 64 digits to a wavefront.
+__global__ __launch_bounds__(64) void k_sort_sum(SortArgs a) {
+    const uint32_t bins = 1u << a.bits, b = blockIdx.x * 64 + threadIdx.x;
+    if (b >= bins) return;
     uint32_t sum = 0;
-    for (uint32_t i = from; i < to; ++i) sum += counts[i];
+    for (uint32_t t = 0; t < a.tiles; t += 8) {
+        uint32_t n[8];
+#pragma unroll
+        for (uint32_t k = 0; k < 8; ++k) n[k] = t + k < a.tiles ? a.counts[(size_t)(t + k) * bins + b] : 0u;
+#pragma unroll
+        for (uint32_t k = 0; k < 8; ++k) {
+            if (t + k < a.tiles) a.counts[(size_t)(t + k) * bins + b] = sum;
+            sum += n[k];
+        }
+    }
+    a.counts[(size_t)a.tiles * bins + b] = sum;
+}
+
+// Exclusive sums over `bins` numbers in LDS, by a work-group of GROUP threads; `sums`: GROUP / 64 numbers.
+template <uint32_t GROUP>
+__device__ __forceinline__ void exclusive_sums(uint32_t* v, uint32_t bins, uint32_t* sums) {
+    constexpr uint32_t kEach = ((1u << kMaxDigit) + GROUP - 1) / GROUP;
+    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6;
+    uint32_t n[kEach], sum = 0;
+#pragma unroll
+    for (uint32_t k = 0; k < kEach; ++k) {
+        n[k] = tid * kEach + k < bins ? v[tid * kEach + k] : 0u;
+        sum += n[k];
+    }
     uint32_t before = sum;
+#pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
         const uint32_t x = __shfl_up(before, d, 64);
         if (lane >= (uint32_t)d) before += x;
@@ -78,194 +124,406 @@ __global__ __launch_bounds__(1024) void k_sort_scan(uint32_t* counts, uint32_t n
     __syncthreads();
     before -= sum;
     for (uint32_t w = 0; w < wave; ++w) before += sums[w];
-    for (uint32_t i = from; i < to; ++i) {
-        const uint32_t x = counts[i];
-        counts[i] = before;
-        before += x;
+#pragma unroll
+    for (uint32_t k = 0; k < kEach; ++k) {
+        if (tid * kEach + k < bins) v[tid * kEach + k] = before;
+        before += n[k];
     }
+    __syncthreads();
 }
 
-// A wavefront takes kSortTile / 4 consecutive pairs, 64 at a time; among the lanes of equal digits the rank is the number of
-// lanes before, so that pairs of equal digits keep their order.
-__global__ __launch_bounds__(kSortGroup) void k_sort_place(const void* tokens, int tokens64, const uint32_t* keys, const uint32_t* places, uint32_t count,
-                                                           uint32_t rows, uint32_t shift, uint32_t bits, uint32_t tiles, const uint32_t* starts,
-                                                           uint32_t* out_keys, uint32_t* out_places) {
+// Where the pairs of ROUNDS * 64 consecutive places that a wavefront holds go, 64 at a time: among the lanes of equal digits the rank
+// is the number of lanes before, so that pairs of equal digits keep their order.  at[wave][digit]: first how many the
+// wavefront has, then, after `spread` has turned counts into places, the next free one.
+template <uint32_t ROUNDS>
+struct Ranks {
+    uint64_t same[ROUNDS];
+
+    __device__ __forceinline__ void count(const uint32_t (&digit)[ROUNDS], const bool (&held)[ROUNDS], uint32_t bits, uint32_t lane, uint32_t* at) {
+#pragma unroll
+        for (uint32_t j = 0; j < ROUNDS; ++j) {
+            same[j] = peers_of(digit[j], bits, held[j]);
+            if (held[j] && lanes_before(same[j]) == 0) atomicAdd(&at[digit[j]], (uint32_t)__popcll(same[j]));
+        }
+    }
+    __device__ __forceinline__ void places(const uint32_t (&digit)[ROUNDS], const bool (&held)[ROUNDS], uint32_t* at, uint32_t (&to)[ROUNDS]) {
+#pragma unroll
+        for (uint32_t j = 0; j < ROUNDS; ++j) {
+            const uint32_t before = lanes_before(same[j]);
+            to[j] = held[j] ? at[digit[j]] + before : 0u;
+            // the wavefront's LDS accesses are carried out in order; they only have to stay in it
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            if (held[j] && before == 0) at[digit[j]] = to[j] + (uint32_t)__popcll(same[j]);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        }
+    }
+};
+
+__global__ __launch_bounds__(kSortGroup) void k_sort_place(SortArgs a) {
     constexpr uint32_t kWaves = kSortGroup / 64, kEach = kSortTile / kWaves, kRounds = kEach / 64;
     __shared__ uint32_t at[kWaves][1u << kMaxDigit];
-    const uint32_t bins = 1u << bits, lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
-    for (uint32_t b = threadIdx.x; b < kWaves * bins; b += kSortGroup) at[b / bins][b % bins] = 0;
-    __syncthreads();
+    __shared__ uint32_t start[1u << kMaxDigit];
+    __shared__ uint32_t sums[kWaves];
+    const uint32_t bins = 1u << a.bits, lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
     const uint32_t first = blockIdx.x * kSortTile + wave * kEach;
-    uint32_t key[kRounds];
-    uint64_t same[kRounds];
+    uint32_t key[kRounds], place[kRounds], digit[kRounds], to[kRounds];
+    bool held[kRounds];
 #pragma unroll
     for (uint32_t j = 0; j < kRounds; ++j) {
         const uint32_t i = first + 64 * j + lane;
-        key[j] = i < count ? (keys ? keys[i] : key_at(tokens, tokens64, i, rows)) : 0u;
+        held[j] = i < a.count;
+        key[j] = held[j] ? sort_key(a, i) : 0u;
+        place[j] = held[j] && a.places ? a.places[i] : i;
+        digit[j] = (key[j] >> a.shift) & (bins - 1);
     }
+    // how many pairs of equal digits are in tiles before this one, and how many pairs have lower digits
+    constexpr uint32_t kBins = (1u << kMaxDigit) / kSortGroup;
+    uint32_t before[kBins] = {};
 #pragma unroll
-    for (uint32_t j = 0; j < kRounds; ++j) {
-        const bool held = first + 64 * j + lane < count;
-        const uint32_t digit = (key[j] >> shift) & (bins - 1);
-        same[j] = peers_of(digit, bits, held);
-        if (held && (same[j] & ((1ull << lane) - 1)) == 0) atomicAdd(&at[wave][digit], (uint32_t)__popcll(same[j]));
+    for (uint32_t k = 0; k < kBins; ++k) {
+        const uint32_t b = threadIdx.x + k * kSortGroup;
+        if (b >= bins) continue;
+        uint32_t total;
+        if (a.tiles > kSumTiles) {
+            before[k] = a.counts[(size_t)blockIdx.x * bins + b];
+            total = a.counts[(size_t)a.tiles * bins + b];
+        } else {
+            total = 0;
+            for (uint32_t t = 0; t < a.tiles; ++t) {
+                const uint32_t n = a.counts[(size_t)t * bins + b];
+                if (t < blockIdx.x) before[k] += n;
+                total += n;
+            }
+        }
+        start[b] = total;
+        for (uint32_t w = 0; w < kWaves; ++w) at[w][b] = 0;
     }
     __syncthreads();
-    for (uint32_t b = threadIdx.x; b < bins; b += kSortGroup) {
-        uint32_t to = starts[(size_t)b * tiles + blockIdx.x];
+    Ranks<kRounds> ranks;
+    ranks.count(digit, held, a.bits, lane, at[wave]);
+    exclusive_sums<kSortGroup>(start, bins, sums);
+#pragma unroll
+    for (uint32_t k = 0; k < kBins; ++k) {
+        const uint32_t b = threadIdx.x + k * kSortGroup;
+        if (b >= bins) continue;
+        uint32_t next = start[b] + before[k];
         for (uint32_t w = 0; w < kWaves; ++w) {
             const uint32_t n = at[w][b];
-            at[w][b] = to;
-            to += n;
+            at[w][b] = next;
+            next += n;
         }
     }
     __syncthreads();
+    ranks.places(digit, held, at[wave], to);
 #pragma unroll
     for (uint32_t j = 0; j < kRounds; ++j) {
-        const uint32_t i = first + 64 * j + lane, digit = (key[j] >> shift) & (bins - 1);
-        const bool held = i < count;
-        const uint32_t before = (uint32_t)__popcll(same[j] & ((1ull << lane) - 1));
-        uint32_t to = 0;
-        if (held) to = at[wave][digit] + before;
-        __builtin_amdgcn_wave_barrier();
-        if (held && before == 0) at[wave][digit] += (uint32_t)__popcll(same[j]);
-        __builtin_amdgcn_wave_barrier();
-        if (held) {
-            out_keys[to] = key[j];
-            out_places[to] = places ? places[i] : i;
-        }
+        if (!held[j]) continue;
+        a.out_keys[to[j]] = key[j];
+        a.out_places[to[j]] = place[j];
+        if (a.last && a.marks && key[j] < a.rows) a.marks[key[j]] = 1;
     }
 }
 
-template <class T>
+// All passes by one work-group, the pairs in LDS between them.  bits: of the whole key, digit: of one pass.
+__global__ __launch_bounds__(kSortOneGroup) void k_sort_one(SortArgs a, uint32_t passes) {
+    constexpr uint32_t kWaves = kSortOneGroup / 64, kEach = kSortOne / kWaves, kRounds = kEach / 64;
+    __shared__ uint32_t at[kWaves][1u << kMaxDigit];
+    __shared__ uint32_t start[1u << kMaxDigit];
+    __shared__ uint32_t sums[kWaves];
+    __shared__ uint64_t pairs[kSortOne];
+    const uint32_t bins = 1u << a.bits, lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
+    const uint32_t first = wave * kEach;
+    uint32_t key[kRounds], place[kRounds], digit[kRounds], to[kRounds];
+    bool held[kRounds];
+#pragma unroll
+    for (uint32_t j = 0; j < kRounds; ++j) {
+        const uint32_t i = first + 64 * j + lane;
+        held[j] = i < a.count;
+        key[j] = held[j] ? sort_key(a, i) : 0u;
+        place[j] = i;
+    }
+    if (a.marks)
+        for (uint32_t r = threadIdx.x; r < (a.rows + 3) / 4; r += kSortOneGroup) reinterpret_cast<uint32_t*>(a.marks)[r] = 0;
+    for (uint32_t p = 0; p < passes; ++p) {
+        for (uint32_t b = threadIdx.x; b < kWaves * bins; b += kSortOneGroup) at[b >> a.bits][b & (bins - 1)] = 0;
+#pragma unroll
+        for (uint32_t j = 0; j < kRounds; ++j) digit[j] = (key[j] >> (p * a.bits)) & (bins - 1);
+        __syncthreads();
+        Ranks<kRounds> ranks;
+        ranks.count(digit, held, a.bits, lane, at[wave]);
+        __syncthreads();
+        for (uint32_t b = threadIdx.x; b < bins; b += kSortOneGroup) {
+            uint32_t sum = 0;
+            for (uint32_t w = 0; w < kWaves; ++w) {
+                const uint32_t n = at[w][b];
+                at[w][b] = sum;
+                sum += n;
+            }
+            start[b] = sum;
+        }
+        __syncthreads();
+        exclusive_sums<kSortOneGroup>(start, bins, sums);
+        for (uint32_t b = threadIdx.x; b < kWaves * bins; b += kSortOneGroup) at[b >> a.bits][b & (bins - 1)] += start[b & (bins - 1)];
+        __syncthreads();
+        ranks.places(digit, held, at[wave], to);
+#pragma unroll
+        for (uint32_t j = 0; j < kRounds; ++j)
+            if (held[j]) pairs[to[j]] = (uint64_t)key[j] << 32 | place[j];
+        __syncthreads();
+#pragma unroll
+        for (uint32_t j = 0; j < kRounds; ++j)
+            if (held[j]) {
+                const uint64_t v = pairs[first + 64 * j + lane];
+                key[j] = (uint32_t)(v >> 32);
+                place[j] = (uint32_t)v;
+            }
+    }
+#pragma unroll
+    for (uint32_t j = 0; j < kRounds; ++j) {
+        const uint32_t i = first + 64 * j + lane;
+        if (!held[j]) continue;
+        a.out_keys[i] = key[j];
+        a.out_places[i] = place[j];
+        // the clearing above lies behind the barriers of at least one pass
+        if (a.marks && key[j] < a.rows) a.marks[key[j]] = 1;
+    }
+}
+
+// GROUP lanes for a row (or for GROUP * N columns of it), one after the other where there are more columns.
+template <class T, int GROUP>
 __global__ __launch_bounds__(256) void k_embed(EmbedArgs a) {
-    constexpr int N = T::kPer16;
-    const uint32_t per_row = (a.width + N - 1) / N;
-    const uint64_t all = a.count * per_row;
-    for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (uint64_t)gridDim.x * 256) {
-        const uint64_t n = i / per_row;
-        const uint32_t at = (uint32_t)(i - n * per_row) * N;
-        const int64_t t = token_at(a.tokens, a.tokens64, n);
-        const bool row = t >= 0 && t < (int64_t)a.rows;
-        const float other = t == -1 ? 0.0f : __builtin_nanf("");
-        const typename T::raw* from = static_cast<const typename T::raw*>(a.weight) + (row ? t : 0) * a.weight_stride + at;
-        typename T::raw* to = static_cast<typename T::raw*>(a.out) + (int64_t)n * a.out_stride + at;
+    constexpr int N = T::kPer16, kRows = 256 / GROUP;
+    const uint64_t n = (uint64_t)blockIdx.x * kRows + threadIdx.x / GROUP;
+    if (n >= a.count) return;
+    const int64_t t = token_at(a.tokens, a.tokens64, n);
+    const bool row = t >= 0 && t < (int64_t)a.rows;
+    const float other = t == -1 ? 0.0f : __builtin_nanf("");
+    const typename T::raw* from = static_cast<const typename T::raw*>(a.weight) + (row ? t : 0) * a.weight_stride;
+    typename T::raw* to = static_cast<typename T::raw*>(a.out) + (int64_t)n * a.out_stride;
+    for (uint32_t at = threadIdx.x % GROUP * N; at < a.width; at += GROUP * N) {
         if (at + N <= a.width) {
             float x[N];
-            load<T, N>(from, x);
+            load<T, N>(from + at, x);
 #pragma unroll
             for (int k = 0; k < N; ++k) x[k] = row ? x[k] * a.scale : other;
-            store<T, N>(to, x);
+            store<T, N>(to + at, x);
         } else {
-            for (uint32_t k = 0; at + k < a.width; ++k) to[k] = rounded<T>(row ? to_float(from[k]) * a.scale : other);
+            for (uint32_t k = at; k < a.width; ++k) to[k] = rounded<T>(row ? to_float(from[k]) * a.scale : other);
         }
     }
 }
 
 // ---- gradient
 
-constexpr uint32_t kPiece = 64;
+// Tokens of a piece: 64, more where there would be more than kMaxPieces pieces.
+constexpr uint32_t kPiece = 64, kMaxPieces = 4096;
+uint32_t piece_length(uint32_t count) {
+    uint32_t n = kPiece;
+    while ((count + (uint64_t)n - 1) / n > kMaxPieces) n *= 2;
+    return n;
+}
 
 struct SumArgs {
     const uint32_t *keys, *places;
+    const uint8_t* marks;     // null with accumulate
     const void* grad;
     void* out;
     float* partial;           // [piece][2][width]: of the row that began before the piece, of the row that goes on behind it
     int64_t grad_stride, out_stride;
-    uint32_t count, rows, width, pieces;
+    uint32_t count, rows, width, pieces, length;
+    uint32_t sum_groups, blocks;      // work-groups that add up, the others write zeros; groups of columns of a row
     float scale;
     int32_t accumulate;
 };
 
 template <class O, int N>
-__device__ __forceinline__ void write_row(const SumArgs& a, uint32_t row, uint32_t at, float (&sum)[N]) {
+__device__ __forceinline__ void write_sum(const SumArgs& a, uint32_t row, uint32_t at, const float (&sum)[N]) {
     typename O::raw* to = static_cast<typename O::raw*>(a.out) + (int64_t)row * a.out_stride + at;
-    const uint32_t n = a.width - at < (uint32_t)N ? a.width - at : (uint32_t)N;
+    if (at + N <= a.width) {
+        float y[N];
+        if (a.accumulate) {
+            load<O, N>(to, y);
 #pragma unroll
-    for (int k = 0; k < N; ++k)
-        if ((uint32_t)k < n) to[k] = rounded<O>(a.accumulate ? fmaf(sum[k], a.scale, to_float(to[k])) : sum[k] * a.scale);
+            for (int k = 0; k < N; ++k) y[k] = fmaf(sum[k], a.scale, y[k]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < N; ++k) y[k] = sum[k] * a.scale;
+        }
+        store<O, N>(to, y);
+    } else {
+        for (uint32_t k = 0; at + k < a.width; ++k) to[k] = rounded<O>(a.accumulate ? fmaf(sum[k], a.scale, to_float(to[k])) : sum[k] * a.scale);
+    }
 }
 
-// One thread for N columns of a piece.
-template <class T, class O>
+// Zeros in rows that are not marked, GROUP lanes to a row.
+template <class O, int GROUP>
+__device__ __forceinline__ void write_zeros(const SumArgs& a, uint32_t group, uint32_t groups) {
+    constexpr int N = O::kPer16, kRows = 256 / GROUP;
+    float zero[N] = {};
+    for (uint64_t row = (uint64_t)group * kRows + threadIdx.x / GROUP; row < a.rows; row += (uint64_t)groups * kRows) {
+        if (a.marks && a.marks[row]) continue;
+        typename O::raw* to = static_cast<typename O::raw*>(a.out) + (int64_t)row * a.out_stride;
+        for (uint32_t at = threadIdx.x % GROUP * N; at < a.width; at += GROUP * N) {
+            if (at + N <= a.width) {
+                store<O, N>(to + at, zero);
+            } else {
+                for (uint32_t k = at; k < a.width; ++k) to[k] = rounded<O>(0.0f);
+            }
+        }
+    }
+}
+template <class O>
+__global__ __launch_bounds__(256) void k_embed_zero(SumArgs a) { write_zeros<O, 64>(a, blockIdx.x, gridDim.x); }
+
+// GROUP lanes for N columns each of a piece; 256 / GROUP pieces (or column blocks of one) to a work-group.  Keys and places are
+// fetched 64 at a time, rows kAhead at a time, so that that many are on their way at once.
+template <class T, class O, int GROUP>
 __global__ __launch_bounds__(256) void k_embed_sum(SumArgs a) {
-    constexpr int N = T::kPer16;
-    const uint32_t per_row = (a.width + N - 1) / N;
-    const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
-    const uint32_t piece = (uint32_t)(i / per_row);
-    if (piece >= a.pieces) return;
-    const uint32_t at = (uint32_t)(i - (uint64_t)piece * per_row) * N;
-    const uint32_t from = piece * kPiece, to = from + kPiece < a.count ? from + kPiece : a.count;
-    bool began_before = piece > 0 && a.keys[from - 1] == a.keys[from];
+    constexpr int N = T::kPer16, kSlots = 256 / GROUP, kAhead = 8;
+    __shared__ uint32_t keys[kSlots][kPiece + 1], places[kSlots][kPiece];
+    if (blockIdx.x >= a.sum_groups) {
+        write_zeros<O, GROUP>(a, blockIdx.x - a.sum_groups, gridDim.x - a.sum_groups);
+        return;
+    }
+    const uint32_t lane = threadIdx.x % GROUP, slot = threadIdx.x / GROUP;
+    const uint64_t work = (uint64_t)blockIdx.x * kSlots + slot;
+    const uint32_t piece = (uint32_t)(work / a.blocks), at = ((uint32_t)(work % a.blocks) * GROUP + lane) * N;
+    const uint32_t from = piece * a.length;
+    const uint32_t end = piece >= a.pieces ? from : a.count - from < a.length ? a.count : from + a.length;
+    bool began_before = piece < a.pieces && from > 0 && a.keys[from - 1] == a.keys[from];
     float sum[N];
 #pragma unroll
     for (int k = 0; k < N; ++k) sum[k] = 0.0f;
-    for (uint32_t j = from; j < to; ++j) {
-        const uint32_t key = a.keys[j];
-        if (key >= a.rows) break;
-        const typename T::raw* g = static_cast<const typename T::raw*>(a.grad) + (int64_t)a.places[j] * a.grad_stride + at;
-        if (at + N <= a.width) {
-            float x[N];
-            load<T, N>(g, x);
-#pragma unroll
-            for (int k = 0; k < N; ++k) sum[k] += x[k];
-        } else {
-#pragma unroll
-            for (int k = 0; k < N; ++k)
-                if (at + k < a.width) sum[k] += to_float(g[k]);
+    for (uint32_t batch = 0; batch < a.length; batch += kPiece) {
+        const uint32_t base = from + batch, n = base >= end ? 0u : end - base < kPiece ? end - base : kPiece;
+        __syncthreads();
+        for (uint32_t k = lane; k < n; k += GROUP) {
+            keys[slot][k] = a.keys[base + k];
+            places[slot][k] = a.places[base + k];
         }
-        const bool last = j + 1 == to, ends = j + 1 == a.count || a.keys[j + 1] != key;
-        if (!last && !ends) continue;
-        if (ends && !began_before) {
-            write_row<O, N>(a, key, at, sum);
-        } else {
-            float* p = a.partial + ((size_t)piece * 2 + (began_before ? 0 : 1)) * a.width + at;
+        if (lane == 0 && n) keys[slot][n] = base + n < a.count ? a.keys[base + n] : 0xFFFFFFFFu;
+        __syncthreads();
+        if (at >= a.width) continue;
+        for (uint32_t j = 0; j < n; j += kAhead) {
+            float x[kAhead][N];
 #pragma unroll
-            for (int k = 0; k < N; ++k)
-                if (at + k < a.width) p[k] = sum[k];
+            for (int u = 0; u < kAhead; ++u) {
+                const typename T::raw* g = static_cast<const typename T::raw*>(a.grad) + (j + u < n ? (int64_t)places[slot][j + u] * a.grad_stride : 0) + at;
+                if (at + N <= a.width) {
+                    load<T, N>(g, x[u]);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < N; ++k) x[u][k] = at + k < a.width ? to_float(g[k]) : 0.0f;
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                if (j + u >= n) continue;
+                const uint32_t key = keys[slot][j + u];
+                if (key >= a.rows) continue;
+#pragma unroll
+                for (int k = 0; k < N; ++k) sum[k] += x[u][k];
+                const bool ends = keys[slot][j + u + 1] != key;
+                if (!ends && base + j + u + 1 != end) continue;
+                if (ends && !began_before) {
+                    write_sum<O, N>(a, key, at, sum);
+                } else {
+                    float* p = a.partial + ((size_t)piece * 2 + (began_before ? 0 : 1)) * a.width + at;
+                    if (at + N <= a.width) {
+                        store<F32, N>(p, sum);
+                    } else {
+                        for (uint32_t k = 0; at + k < a.width; ++k) p[k] = sum[k];
+                    }
+                }
+                began_before = false;
+#pragma unroll
+                for (int k = 0; k < N; ++k) sum[k] = 0.0f;
+            }
         }
-        began_before = false;
-#pragma unroll
-        for (int k = 0; k < N; ++k) sum[k] = 0.0f;
     }
 }
 
-// The rows that are cut: a thread for each column of the piece that such a row begins in.
+// The rows that are cut.  Each work-group looks for the pieces in which such a row begins, and takes its share of them, by columns;
+// its wavefronts add up a part of the row's partial sums each, in order, and then those parts.
 template <class O>
-__global__ __launch_bounds__(256) void k_embed_join(SumArgs a) {
-    const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x;
-    const uint32_t piece = (uint32_t)(i / a.width), at = (uint32_t)(i - (uint64_t)piece * a.width);
-    if (piece + 1 >= a.pieces) return;
-    const uint32_t from = piece * kPiece, next = from + kPiece, key = a.keys[next - 1];
-    if (key >= a.rows || a.keys[next] != key) return;
-    if (a.keys[from] == key && piece > 0 && a.keys[from - 1] == key) return;      // it began before this piece
-    float sum[1] = {a.partial[((size_t)piece * 2 + 1) * a.width + at]};
-    for (uint32_t p = piece + 1; p < a.pieces && a.keys[p * kPiece] == key; ++p) sum[0] += a.partial[(size_t)p * 2 * a.width + at];
-    typename O::raw* to = static_cast<typename O::raw*>(a.out) + (int64_t)key * a.out_stride + at;
-    *to = rounded<O>(a.accumulate ? fmaf(sum[0], a.scale, to_float(*to)) : sum[0] * a.scale);
-}
-
-// Zeros in rows without a token: a wavefront looks for each row among the sorted keys.
-template <class O>
-__global__ __launch_bounds__(256) void k_embed_zero(SumArgs a) {
-    const uint32_t lane = threadIdx.x & 63u;
-    for (uint32_t row = blockIdx.x * 4u + (threadIdx.x >> 6); row < a.rows; row += gridDim.x * 4u) {
-        uint32_t lo = 0, hi = a.count;      // the first key >= row is in [lo, hi]
+__global__ __launch_bounds__(1024) void k_embed_join(SumArgs a) {
+    constexpr uint32_t kWaves = 16, kColumns = 64;
+    __shared__ uint32_t begins[kMaxPieces];
+    __shared__ uint32_t counts[kWaves], found;
+    __shared__ float part[kWaves][kColumns];
+    const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6;
+    if (tid == 0) found = 0;
+    for (uint32_t first = 0; first + 1 < a.pieces; first += 1024) {
+        const uint32_t piece = first + tid;
+        bool is = false;
+        if (piece + 1 < a.pieces) {
+            const uint32_t from = piece * a.length, next = from + a.length, key = a.keys[next - 1];
+            is = key < a.rows && a.keys[next] == key && !(a.keys[from] == key && from > 0 && a.keys[from - 1] == key);
+        }
+        const uint64_t who = __ballot(is);
+        __syncthreads();
+        if (lane == 0) counts[wave] = (uint32_t)__popcll(who);
+        __syncthreads();
+        uint32_t to = found + lanes_before(who);
+        for (uint32_t w = 0; w < wave; ++w) to += counts[w];
+        if (is) begins[to] = piece;
+        __syncthreads();
+        if (tid == 0)
+            for (uint32_t w = 0; w < kWaves; ++w) found += counts[w];
+    }
+    __syncthreads();
+    const uint32_t blocks = (a.width + kColumns - 1) / kColumns;
+    const uint64_t all = (uint64_t)found * blocks;
+    for (uint64_t work = blockIdx.x; work < all; work += gridDim.x) {
+        const uint32_t piece = begins[work / blocks], at = (uint32_t)(work % blocks) * kColumns + lane;
+        const uint32_t key = a.keys[(piece + 1) * a.length - 1];
+        uint32_t lo = piece + 2, hi = a.pieces;      // the first piece behind piece + 1 that begins with another key
         while (lo < hi) {
             const uint32_t mid = lo + (hi - lo) / 2;
-            if (a.keys[mid] < row) lo = mid + 1; else hi = mid;
+            if (a.keys[mid * a.length] == key) lo = mid + 1; else hi = mid;
         }
-        if (lo < a.count && a.keys[lo] == row) continue;
-        typename O::raw* to = static_cast<typename O::raw*>(a.out) + (int64_t)row * a.out_stride;
-        for (uint32_t at = lane; at < a.width; at += 64) to[at] = rounded<O>(0.0f);
+        // partial sums piece (second kind), piece + 1 .. lo - 1 (first kind), in kWaves shares
+        const uint32_t n = lo - piece, each = (n + kWaves - 1) / kWaves, begin = wave * each, stop = begin + each < n ? begin + each : n;
+        float sum = 0.0f;
+        if (at < a.width) {
+            for (uint32_t k = begin; k < stop; k += 4) {
+                float x[4];
+#pragma unroll
+                for (uint32_t u = 0; u < 4; ++u) x[u] = k + u < stop ? a.partial[((size_t)(piece + k + u) * 2 + (k + u == 0)) * a.width + at] : 0.0f;
+#pragma unroll
+                for (uint32_t u = 0; u < 4; ++u) sum += x[u];
+            }
+        }
+        __syncthreads();
+        part[wave][lane] = sum;
+        __syncthreads();
+        if (wave == 0 && at < a.width) {
+            float all_of[1] = {part[0][lane]};
+#pragma unroll
+            for (uint32_t w = 1; w < kWaves; ++w) all_of[0] += part[w][lane];
+            write_sum<O, 1>(a, key, at, all_of);
+        }
     }
 }
 
-uint32_t groups_of(uint64_t threads) { return (uint32_t)((threads + 255) / 256); }
 size_t whole(size_t n) { return (n + 255) / 256 * 256; }
+
+template <class T, class O, int GROUP>
+void sum(SumArgs s, hipStream_t stream) {
+    constexpr uint32_t kSlots = 256 / GROUP;
+    s.blocks = (s.width + GROUP * T::kPer16 - 1) / (GROUP * T::kPer16);
+    s.sum_groups = (uint32_t)(((uint64_t)s.pieces * s.blocks + kSlots - 1) / kSlots);
+    const uint32_t zero = s.accumulate ? 0u : (s.rows + kSlots - 1) / kSlots;
+    hipLaunchKernelGGL((k_embed_sum<T, O, GROUP>), dim3(s.sum_groups + (zero < 4096 ? zero : 4096)), dim3(256), 0, stream, s);
+}
 
 template <class T, class O>
 hipError_t embed_grad(const EmbedGradArgs& a, hipStream_t stream) {
+    SumArgs s = {nullptr, nullptr, nullptr, a.grad, a.out, nullptr, a.grad_stride, a.out_stride, a.count, a.rows, a.width, 0, 0, 0, 0, a.scale, a.accumulate};
+    if (!a.count) {
+        if (!a.accumulate) hipLaunchKernelGGL((k_embed_zero<O>), dim3((a.rows + 3) / 4 < 16384 ? (a.rows + 3) / 4 : 16384), dim3(256), 0, stream, s);
+        return hipGetLastError();
+    }
     const SortPlan plan = sort_plan(a.count, a.rows);
     char* w = static_cast<char*>(a.workspace);
     uint32_t* buffer[4];
@@ -274,30 +532,39 @@ hipError_t embed_grad(const EmbedGradArgs& a, hipStream_t stream) {
         w += whole((size_t)a.count * 4);
     }
     uint32_t* counts = reinterpret_cast<uint32_t*>(w);
-    w += whole(((size_t)plan.tiles << plan.digit) * 4);
-    const uint32_t* keys = nullptr;
-    const uint32_t* places = nullptr;
-    for (uint32_t p = 0; p < plan.passes && a.count; ++p) {
-        const uint32_t shift = p * plan.digit;
-        uint32_t *to_keys = buffer[2 * (p & 1)], *to_places = buffer[2 * (p & 1) + 1];
-        hipLaunchKernelGGL(k_sort_count, dim3(plan.tiles), dim3(kSortGroup), 0, stream, a.tokens, a.tokens64, keys, a.count, a.rows, shift, plan.digit, plan.tiles, counts);
-        hipLaunchKernelGGL(k_sort_scan, dim3(1), dim3(1024), 0, stream, counts, plan.tiles << plan.digit);
-        hipLaunchKernelGGL(k_sort_place, dim3(plan.tiles), dim3(kSortGroup), 0, stream, a.tokens, a.tokens64, keys, places, a.count, a.rows, shift, plan.digit, plan.tiles,
-                           counts, to_keys, to_places);
-        keys = to_keys;
-        places = to_places;
+    w += whole(((size_t)(plan.tiles + 1) << plan.digit) * 4);
+    uint8_t* marks = reinterpret_cast<uint8_t*>(w);
+    w += whole(a.rows);
+    s.partial = reinterpret_cast<float*>(w);
+    SortArgs sort = {a.tokens, nullptr, nullptr, buffer[0], buffer[1], counts, a.accumulate ? nullptr : marks, a.tokens64, a.count, a.rows, 0, plan.digit, plan.tiles, 1};
+    if (a.count <= kSortOne) {
+        hipLaunchKernelGGL(k_sort_one, dim3(1), dim3(kSortOneGroup), 0, stream, sort, plan.passes);
+    } else {
+        for (uint32_t p = 0; p < plan.passes; ++p) {
+            sort.shift = p * plan.digit;
+            sort.last = p + 1 == plan.passes;
+            sort.out_keys = buffer[2 * (p & 1)];
+            sort.out_places = buffer[2 * (p & 1) + 1];
+            hipLaunchKernelGGL(k_sort_count, dim3(plan.tiles), dim3(kSortGroup), 0, stream, sort);
+            if (plan.tiles > kSumTiles) hipLaunchKernelGGL(k_sort_sum, dim3(((1u << plan.digit) + 63) / 64), dim3(64), 0, stream, sort);
+            hipLaunchKernelGGL(k_sort_place, dim3(plan.tiles), dim3(kSortGroup), 0, stream, sort);
+            sort.keys = sort.out_keys;
+            sort.places = sort.out_places;
+        }
     }
-    SumArgs s = {keys, places, a.grad, a.out, reinterpret_cast<float*>(w), a.grad_stride, a.out_stride, a.count, a.rows, a.width,
-                 (a.count + kPiece - 1) / kPiece, a.scale, a.accumulate};
-    if (!a.accumulate) {
-        const uint32_t g = (a.rows + 3) / 4;
-        hipLaunchKernelGGL((k_embed_zero<O>), dim3(g < 8192 ? g : 8192), dim3(256), 0, stream, s);
-    }
-    if (a.count) {
-        const uint32_t per_row = (a.width + T::kPer16 - 1) / T::kPer16;
-        hipLaunchKernelGGL((k_embed_sum<T, O>), dim3(groups_of((uint64_t)s.pieces * per_row)), dim3(256), 0, stream, s);
-        if (s.pieces > 1) hipLaunchKernelGGL((k_embed_join<O>), dim3(groups_of((uint64_t)(s.pieces - 1) * a.width)), dim3(256), 0, stream, s);
-    }
+    s.keys = sort.out_keys;
+    s.places = sort.out_places;
+    s.marks = sort.marks;
+    s.length = piece_length(a.count);
+    s.pieces = (uint32_t)((a.count + (uint64_t)s.length - 1) / s.length);
+    const uint32_t lanes = (a.width + T::kPer16 - 1) / T::kPer16;
+    if (lanes <= 4)
+        sum<T, O, 4>(s, stream);
+    else if (lanes <= 16)
+        sum<T, O, 16>(s, stream);
+    else
+        sum<T, O, 64>(s, stream);
+    if (s.pieces > 1) hipLaunchKernelGGL((k_embed_join<O>), dim3(256), dim3(1024), 0, stream, s);
     return hipGetLastError();
 }
 
@@ -306,10 +573,29 @@ hipError_t embed_grad_to(int32_t out_dtype, const EmbedGradArgs& a, hipStream_t 
     return out_dtype == BPS_F32 ? embed_grad<T, F32>(a, stream) : out_dtype == BPS_BF16 ? embed_grad<T, Bf16>(a, stream) : embed_grad<T, F16>(a, stream);
 }
 
+// Launches of at most this many rows: a grid has to have less than 2^32 threads.
+constexpr uint64_t kMaxRows = 1u << 22;
+
+template <class T, int GROUP>
+void embed_rows(const EmbedArgs& a, hipStream_t stream) {
+    constexpr uint32_t kRows = 256 / GROUP;
+    hipLaunchKernelGGL((k_embed<T, GROUP>), dim3((uint32_t)((a.count + kRows - 1) / kRows)), dim3(256), 0, stream, a);
+}
 template <class T>
 hipError_t embed(const EmbedArgs& a, hipStream_t stream) {
-    const uint64_t g = (a.count * ((a.width + T::kPer16 - 1) / T::kPer16) + 255) / 256;
-    hipLaunchKernelGGL((k_embed<T>), dim3((uint32_t)(g < (1u << 20) ? g : (1u << 20))), dim3(256), 0, stream, a);
+    const uint32_t lanes = (a.width + T::kPer16 - 1) / T::kPer16;
+    for (uint64_t first = 0; first < a.count; first += kMaxRows) {
+        EmbedArgs s = a;
+        s.count = a.count - first < kMaxRows ? a.count - first : kMaxRows;
+        s.tokens = static_cast<const char*>(a.tokens) + first * (a.tokens64 ? 8 : 4);
+        s.out = static_cast<typename T::raw*>(a.out) + (int64_t)first * a.out_stride;
+        if (lanes <= 4)
+            embed_rows<T, 4>(s, stream);
+        else if (lanes <= 16)
+            embed_rows<T, 16>(s, stream);
+        else
+            embed_rows<T, 64>(s, stream);
+    }
     return hipGetLastError();
 }
 
@@ -318,7 +604,8 @@ hipError_t embed(const EmbedArgs& a, hipStream_t stream) {
 size_t embed_grad_workspace(uint32_t count, uint32_t rows, uint32_t width) {
     if (!count) return 0;
     const SortPlan plan = sort_plan(count, rows);
-    return 4 * whole((size_t)count * 4) + whole(((size_t)plan.tiles << plan.digit) * 4) + (size_t)((count + kPiece - 1) / kPiece) * 2 * width * 4;
+    const uint32_t length = piece_length(count);
+    return 4 * whole((size_t)count * 4) + whole(((size_t)(plan.tiles + 1) << plan.digit) * 4) + whole(rows) + (count + (size_t)length - 1) / length * 2 * width * 4;
 }
 
 hipError_t launch_embed(int32_t dtype, const EmbedArgs& a, hipStream_t stream) {

@@ -63,7 +63,7 @@ bps_status bps_log_probs(const void* logits, int32_t dtype, uint64_t rows, uint3
     const size_t need = bps::score_workspace(dtype, rows, entries, top_k);
     if (need && (!workspace || workspace_bytes < need || !aligned(workspace, 16)))
         return fail_here(BPS_ERR_INVALID_ARG, "%s: needs %zu bytes of workspace, 16-byte aligned (got %zu)", what, need, workspace ? workspace_bytes : 0);
-    const bps::ScoreArgs a = {logits, tokens, mask, row_stride, mask_stride, rows, entries, scale, top_k, token_bits == 64, logp, entropy, lse, norm, top_ids, top_logp, workspace};
+    const bps::ScoreArgs a = {logits, tokens, mask, row_stride, mask_stride, rows, entries, scale, top_k, token_bits == 64, logp, entropy, lse, norm, norm + rows, top_ids, top_logp, workspace};
     return launched(what, bps::launch_score(dtype, a, static_cast<hipStream_t>(stream)));
 }
 
@@ -77,7 +77,7 @@ bps_status bps_log_probs_backward(const void* logits, int32_t dtype, uint64_t ro
     if (!aligned(out, size_of(dtype))) return fail_here(BPS_ERR_INVALID_ARG, "%s: misaligned out", what);
     if (rows > 1 && (out_stride < 0 ? -out_stride : out_stride) < (int64_t)entries) return fail_here(BPS_ERR_INVALID_ARG, "%s: rows of out overlap", what);
     const bps::ScoreGradArgs a = {logits, tokens, mask, row_stride, mask_stride, out_stride, rows, entries, scale, token_bits == 64,
-                                  logp, entropy, norm, grad_logp, grad_entropy, out};
+                                  logp, entropy, norm, norm + rows, grad_logp, grad_entropy, out};
     return launched(what, bps::launch_score_grad(dtype, a, static_cast<hipStream_t>(stream)));
 }
 

@@ -22,7 +22,7 @@ struct ScoreArgs {
     float scale;
     uint32_t top_k;
     int32_t tokens64;
-    float *logp, *entropy, *lse, *norm;
+    float *logp, *entropy, *lse, *largest, *ln_z;
     int32_t* top_ids;
     float* top_logp;
     void* workspace;
@@ -39,7 +39,7 @@ struct ScoreGradArgs {
     uint32_t entries;
     float scale;
     int32_t tokens64;
-    const float *logp, *entropy, *norm, *grad_logp, *grad_entropy;   // grad_* may be null (zero)
+    const float *logp, *entropy, *largest, *ln_z, *grad_logp, *grad_entropy;   // grad_* may be null (zero)
     void* out;
 };
 hipError_t launch_score_grad(int32_t dtype, const ScoreGradArgs& a, hipStream_t stream);

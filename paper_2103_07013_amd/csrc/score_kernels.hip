@@ -95,8 +95,8 @@ __device__ __forceinline__ Part group_part(Part p, float c) {
 template <class T>
 __device__ __forceinline__ void write_row(const ScoreArgs& a, uint64_t r, const Part& p, float ln_z, const typename T::raw* row, const uint8_t* mask) {
     const bool empty = p.z == 0.0f;
-    a.norm[2 * r] = p.m;
-    a.norm[2 * r + 1] = ln_z;
+    a.largest[r] = p.m;
+    a.ln_z[r] = ln_z;
     a.lse[r] = empty ? -kInf : fmaf(a.scale, p.m, ln_z);
     a.entropy[r] = empty ? 0.0f : ln_z - kLn2 * (p.s / p.z);
     const int64_t t = token_at(a.tokens, a.tokens64, r);
@@ -368,8 +368,8 @@ struct RowGrad {
 };
 __device__ __forceinline__ RowGrad row_grad(const ScoreGradArgs& a, uint64_t r) {
     RowGrad g;
-    g.m = a.norm[2 * r];
-    g.ln_z = a.norm[2 * r + 1];
+    g.m = a.largest[r];
+    g.ln_z = a.ln_z[r];
     g.t = token_at(a.tokens, a.tokens64, r);
     g.gh = a.grad_entropy ? a.grad_entropy[r] : 0.0f;
     g.gl = !a.grad_logp || g.t == -1 || a.logp[r] == -kInf ? 0.0f : g.t < -1 || g.t >= (int64_t)a.entries ? __builtin_nanf("") : a.grad_logp[r];
@@ -522,7 +522,8 @@ A rows_of(const A& a, int32_t dtype, uint64_t first, uint64_t rows) {
     if (a.mask) s.mask = a.mask + (int64_t)first * a.mask_stride;
     s.logp = a.logp + first;
     s.entropy = a.entropy + first;
-    s.norm = a.norm + 2 * first;
+    s.largest = a.largest + first;
+    s.ln_z = a.ln_z + first;
     return s;
 }
 

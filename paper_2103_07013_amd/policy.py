@@ -10,7 +10,6 @@ from __future__ import annotations
 
 import collections
 import ctypes
-import functools
 
 import torch
 
@@ -20,7 +19,8 @@ _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _TOKEN_BITS = {torch.int32: 32, torch.int64: 64}
 STATE_BLOCK = 256
 
-LogProbs = collections.namedtuple("LogProbs", "logp entropy lse top_ids top_logp norm")
+#: what log_probs returns; `held` is what log_probs_backward needs of it: float32 [5, ...]
+LogProbs = collections.namedtuple("LogProbs", "logp entropy lse top_ids top_logp held")
 
 
 class _Tensor(ctypes.Structure):
@@ -65,28 +65,20 @@ def _checked(status):
         raise BpsError(status, bps_last_error())
 
 
-def _on(device, call, *arguments):
-    """call(*arguments, stream) with the tensors' device current and torch's stream of it."""
-    index = device.index
-    stream = torch._C._cuda_getCurrentRawStream(index)
-    if index == torch._C._cuda_getDevice():
-        return call(*arguments, stream)
+_current_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+
+
+def _on(index, call, *arguments):
+    """call(*arguments, stream) with device `index` current and torch's stream of it."""
+    if index == _current_device():
+        return call(*arguments, _current_stream(index))
     with torch.cuda.device(index):
-        return call(*arguments, stream)
+        return call(*arguments, _current_stream(index))
 
 
-def _streamed(f):
-    """f with a keyword `stream` that is current during the call."""
-    @functools.wraps(f)
-    def call(*args, stream=None, **kwargs):
-        if stream is None:
-            return f(*args, **kwargs)
-        if isinstance(stream, int):
-            device = next(a.device for a in (*args, *kwargs.values()) if hasattr(a, "device"))
-            stream = torch.cuda.ExternalStream(stream, device=device)
-        with torch.cuda.stream(stream):
-            return f(*args, **kwargs)
-    return call
+def _stream(stream, device):
+    """A context in which `stream` is current."""
+    return torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device) if isinstance(stream, int) else stream)
 
 
 def _rows(t, name, width=None):
@@ -126,8 +118,6 @@ def _mask(mask, shape, rows, width, device):
     if mask.shape == (width,):
         step = 0
     elif mask.shape == (*shape, width):
-        if not mask.is_contiguous():
-            raise ValueError("mask: need a contiguous tensor")
         step = width
     else:
         raise ValueError(f"mask: need shape {(width,)} or {(*shape, width)}, got {tuple(mask.shape)}")
@@ -145,71 +135,81 @@ def _vector(t, shape, device, name):
 
 
 def _log_probs(logits, tokens, mask, scale, top_k):
-    lib = _library()
+    lib = _lib or _library()
     shape, rows, width, step = _rows(logits, "logits")
     device = logits.device
     bits = _tokens(tokens, shape, device)
-    mask_at, mask_step = _mask(mask, shape, rows, width, device)
-    if not 0 <= top_k <= 64:
-        raise ValueError("top_k must be 0 .. 64")
-    logp, entropy, lse = torch.empty((3, *shape), dtype=torch.float32, device=device).unbind(0)
-    norm = torch.empty((*shape, 2), dtype=torch.float32, device=device)
-    top_ids = top_logp = None
+    mask_at, mask_step = _mask(mask, shape, rows, width, device) if mask is not None else (None, 0)
+    held = torch.empty((5, *shape), dtype=torch.float32, device=device)
+    at, size = held.data_ptr(), 4 * rows
+    dtype = _TYPES[logits.dtype]
+    top_ids = top_logp = ids_at = top_at = space = None
     if top_k:
+        if not 0 < top_k <= 64:
+            raise ValueError("top_k must be 0 .. 64")
         top_ids = torch.empty((*shape, top_k), dtype=torch.int32, device=device)
         top_logp = torch.empty((*shape, top_k), dtype=torch.float32, device=device)
-    dtype = _TYPES[logits.dtype]
-    size = lib.bps_log_probs_workspace(dtype, rows, width, top_k)
-    space = torch.empty(size, dtype=torch.uint8, device=device) if size else None
-    _checked(_on(device, lib.bps_log_probs, logits.data_ptr(), dtype, rows, width, step, tokens.data_ptr(), bits, mask_at, mask_step, scale, top_k,
-                 logp.data_ptr(), entropy.data_ptr(), lse.data_ptr(), norm.data_ptr(), top_ids.data_ptr() if top_k else None, top_logp.data_ptr() if top_k else None,
-                 space.data_ptr() if size else None, size))
-    return LogProbs(logp, entropy, lse, top_ids, top_logp, norm)
+        ids_at, top_at = top_ids.data_ptr(), top_logp.data_ptr()
+    space_size = lib.bps_log_probs_workspace(dtype, rows, width, top_k)
+    if space_size:
+        space = torch.empty(space_size, dtype=torch.uint8, device=device)
+    status = _on(device.index, lib.bps_log_probs, logits.data_ptr(), dtype, rows, width, step, tokens.data_ptr(), bits, mask_at, mask_step, scale, top_k, at, at + size, at + 2 * size,
+                 at + 3 * size, ids_at, top_at, None if space is None else space.data_ptr(), space_size)
+    if status:
+        _checked(status)
+    logp, entropy, lse, _, _ = held.unbind(0)
+    return LogProbs(logp, entropy, lse, top_ids, top_logp, held)
 
 
 class _LogProbs(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, tokens, mask, scale, top_k):
         r = _log_probs(logits, tokens, mask, scale, top_k)
-        ctx.save_for_backward(logits, tokens, mask, r.logp, r.entropy, r.norm)
+        ctx.save_for_backward(logits, tokens, mask, r.held)
         ctx.scale = scale
+        # logp and entropy are the caller's, who may write to them; the gradient has what is held
+        logp, entropy = r.logp.clone(), r.entropy.clone()
         ctx.mark_non_differentiable(*(t for t in r[2:] if t is not None))
         ctx.set_materialize_grads(False)
-        return tuple(r)
+        return logp, entropy, *r[2:]
 
     @staticmethod
     def backward(ctx, grad_logp, grad_entropy, *_):
-        logits, tokens, mask, logp, entropy, norm = ctx.saved_tensors
+        logits, tokens, mask, held = ctx.saved_tensors
         plain = [None if g is None else g.to(torch.float32).contiguous() for g in (grad_logp, grad_entropy)]
-        grad = log_probs_backward(logits, tokens, LogProbs(logp, entropy, None, None, None, norm), *plain, mask=mask, scale=ctx.scale)
-        return grad, None, None, None, None
+        return log_probs_backward(logits, tokens, held, *plain, mask=mask, scale=ctx.scale), None, None, None, None
 
 
-@_streamed
-def log_probs(logits, tokens, mask=None, scale=1.0, top_k=0):
+def log_probs(logits, tokens, mask=None, scale=1.0, top_k=0, stream=None):
     """Log probabilities of `tokens` under softmax(scale * logits), with the entropy and the `top_k` best alternatives.
 
     logits  float32, bfloat16 or float16 [..., entries]; tokens int32 or int64 [...], -1 = none; mask bool [..., entries] or
-    [entries], False = the entry is forbidden.  -> LogProbs(logp, entropy, lse, top_ids, top_logp, norm), float32 [...] (top_ids int32,
-    [..., top_k]; both None without top_k; norm [..., 2], which the gradient needs).  logp and entropy carry a gradient to the logits; the rest is for reading.
+    [entries], False = the entry is forbidden.  -> LogProbs(logp, entropy, lse, top_ids, top_logp, held), float32 [...] (top_ids int32,
+    [..., top_k]; both None without top_k; held [5, ...], which the gradient needs).  logp and entropy carry a gradient to the logits; the rest is for reading.
     """
-    if torch.is_grad_enabled() and logits.requires_grad:
+    if stream is not None:
+        with _stream(stream, logits.device):
+            return log_probs(logits, tokens, mask, scale, top_k)
+    if logits.requires_grad and torch.is_grad_enabled():
         return LogProbs(*_LogProbs.apply(logits, tokens, mask, scale, top_k))
     return _log_probs(logits, tokens, mask, scale, top_k)
 
 
-@_streamed
-def log_probs_backward(logits, tokens, result, grad_logp=None, grad_entropy=None, mask=None, scale=1.0, out=None):
+def log_probs_backward(logits, tokens, result, grad_logp=None, grad_entropy=None, mask=None, scale=1.0, out=None, stream=None):
     """The gradient of log_probs' logp and entropy with respect to the logits, in their type.
 
-    result: what log_probs returned for the same arguments; grad_*: float32 [...] or None (zero); out: where it is written, may
-    be the logits.
+    result: what log_probs returned for the same arguments (or its `held`); grad_*: float32 [...] or None (zero); out: where it is
+    written, may be the logits.
     """
-    lib = _library()
+    if stream is not None:
+        with _stream(stream, logits.device):
+            return log_probs_backward(logits, tokens, result, grad_logp, grad_entropy, mask, scale, out)
+    lib = _lib or _library()
     shape, rows, width, step = _rows(logits, "logits")
     device = logits.device
     bits = _tokens(tokens, shape, device)
-    mask_at, mask_step = _mask(mask, shape, rows, width, device)
+    mask_at, mask_step = _mask(mask, shape, rows, width, device) if mask is not None else (None, 0)
+    at, size = _vector(result.held if isinstance(result, LogProbs) else result, (5, *shape), device, "result"), 4 * rows
     if out is None:
         out = torch.empty(logits.shape, dtype=logits.dtype, device=device)
         out_step = width
@@ -217,14 +217,15 @@ def log_probs_backward(logits, tokens, result, grad_logp=None, grad_entropy=None
         if out.dtype != logits.dtype or out.device != device or out.shape != logits.shape:
             raise ValueError("out: need a tensor of the logits' shape, type and device")
         out_step = _rows(out, "out", width)[3]
-    _checked(_on(device, lib.bps_log_probs_backward, logits.data_ptr(), _TYPES[logits.dtype], rows, width, step, tokens.data_ptr(), bits, mask_at, mask_step,
-                 scale, _vector(result.logp, shape, device, "logp"), _vector(result.entropy, shape, device, "entropy"), _vector(result.norm, (*shape, 2), device, "norm"),
-                 _vector(grad_logp, shape, device, "grad_logp"), _vector(grad_entropy, shape, device, "grad_entropy"), out.data_ptr(), out_step))
+    status = _on(device.index, lib.bps_log_probs_backward, logits.data_ptr(), _TYPES[logits.dtype], rows, width, step, tokens.data_ptr(), bits, mask_at, mask_step, scale,
+                 at, at + size, at + 3 * size, _vector(grad_logp, shape, device, "grad_logp"), _vector(grad_entropy, shape, device, "grad_entropy"), out.data_ptr(), out_step)
+    if status:
+        _checked(status)
     return out
 
 
 def _embedding(tokens, weight, scale, out):
-    lib = _library()
+    lib = _lib or _library()
     if weight.dim() != 2:
         raise ValueError("weight: need a tensor [rows, width]")
     _, rows, width, step = _rows(weight, "weight")
@@ -237,7 +238,7 @@ def _embedding(tokens, weight, scale, out):
         if out.dtype != weight.dtype or out.device != device or out.shape != (*tokens.shape, width):
             raise ValueError(f"out: need a {weight.dtype} tensor of shape {(*tokens.shape, width)} on {device}")
         out_step = _rows(out, "out", width)[3] if out.numel() else width
-    _checked(_on(device, lib.bps_embedding, tokens.data_ptr(), bits, tokens.numel(), weight.data_ptr(), _TYPES[weight.dtype], rows, width, step, scale,
+    _checked(_on(device.index, lib.bps_embedding, tokens.data_ptr(), bits, tokens.numel(), weight.data_ptr(), _TYPES[weight.dtype], rows, width, step, scale,
                  out.data_ptr(), out_step))
     return out
 
@@ -254,22 +255,26 @@ class _Embedding(torch.autograd.Function):
         return None, embedding_backward(ctx.saved_tensors[0], grad_out.contiguous(), ctx.rows, ctx.scale, dtype=ctx.dtype), None
 
 
-@_streamed
-def embedding(tokens, weight, scale=1.0, out=None):
+def embedding(tokens, weight, scale=1.0, out=None, stream=None):
     """Rows of `weight` [rows, width] for int32 or int64 tokens [...], times scale; zeros for token -1. -> [..., width]
 
     Carries a gradient to the weight, unless `out` is given."""
+    if stream is not None:
+        with _stream(stream, weight.device):
+            return embedding(tokens, weight, scale, out)
     if out is None and torch.is_grad_enabled() and weight.requires_grad:
         return _Embedding.apply(tokens, weight, scale)
     return _embedding(tokens, weight, scale, out)
 
 
-@_streamed
-def embedding_backward(tokens, grad_out, rows, scale=1.0, dtype=torch.float32, out=None, accumulate=False):
+def embedding_backward(tokens, grad_out, rows, scale=1.0, dtype=torch.float32, out=None, accumulate=False, stream=None):
     """The gradient of embedding's weight, [rows, width] of `dtype`: sums over equal tokens in float32, the same bits every time.
 
     out: where it is written; with accumulate the sums are added to what `out` holds."""
-    lib = _library()
+    if stream is not None:
+        with _stream(stream, grad_out.device):
+            return embedding_backward(tokens, grad_out, rows, scale, dtype, out, accumulate)
+    lib = _lib or _library()
     if accumulate and out is None:
         raise ValueError("accumulate needs out")
     if grad_out.dim() == 0 or grad_out.shape[:-1] != tokens.shape:
@@ -291,7 +296,7 @@ def embedding_backward(tokens, grad_out, rows, scale=1.0, dtype=torch.float32, o
         raise ValueError("need float32, bfloat16 or float16 CUDA tensors")
     size = lib.bps_embedding_backward_workspace(count, rows, width)
     space = torch.empty(size, dtype=torch.uint8, device=device) if size else None
-    _checked(_on(device, lib.bps_embedding_backward, tokens.data_ptr(), bits, count, grad_out.data_ptr(), _TYPES[grad_out.dtype], rows, width, step, scale,
+    _checked(_on(device.index, lib.bps_embedding_backward, tokens.data_ptr(), bits, count, grad_out.data_ptr(), _TYPES[grad_out.dtype], rows, width, step, scale,
                  out.data_ptr(), _TYPES[out.dtype], out_step, int(accumulate), space.data_ptr() if size else None, size))
     return out
 
@@ -358,10 +363,12 @@ class AdamW:
         self._handle = handle
         self._grads = (ctypes.c_void_p * n)()
 
-    @_streamed
-    def step(self, grads=None, grad_scale=1.0):
+    def step(self, grads=None, grad_scale=1.0, stream=None):
         """One step with the parameters' gradients, or with `grads`: one contiguous tensor (or None) for each, of the
         parameters' type or all float32, times grad_scale (one over a loss scale).  grad_norm receives the norm."""
+        if stream is not None:
+            with _stream(stream, self.device):
+                return self.step(grads, grad_scale)
         if self._handle is None:
             raise ValueError("this optimiser is closed")
         if [p.data_ptr() for p in self.params] != self._places:
@@ -384,21 +391,23 @@ class AdamW:
         self._grads[:] = [None if g is None else g.data_ptr() for g in grads]
         self.steps += 1
         try:
-            _checked(_on(self.device, _library().bps_adamw_step, self._handle, self._grads, _TYPES[kind], self.steps, self.lr, *self.betas, self.eps, grad_scale,
+            _checked(_on(self.device.index, _library().bps_adamw_step, self._handle, self._grads, _TYPES[kind], self.steps, self.lr, *self.betas, self.eps, grad_scale,
                          self.max_grad_norm, self.grad_norm.data_ptr()))
         except BpsError:
             self.steps -= 1
             raise
 
-    @_streamed
-    def states(self):
+    def states(self, stream=None):
         """(exp_avg, exp_avg_sq) as float32: the arrays themselves with 32 bits, what their codes stand for with 8."""
+        if stream is not None:
+            with _stream(stream, self.device):
+                return self.states()
         if self.state_bits == 32:
             return self.exp_avg, self.exp_avg_sq
         if self._handle is None:
             raise ValueError("this optimiser is closed")
         m, v = torch.empty((2, self.total), dtype=torch.float32, device=self.device).unbind(0)
-        _checked(_on(self.device, _library().bps_adamw_read_states, self._handle, m.data_ptr(), v.data_ptr()))
+        _checked(_on(self.device.index, _library().bps_adamw_read_states, self._handle, m.data_ptr(), v.data_ptr()))
         return m, v
 
     def close(self):

@@ -355,7 +355,7 @@ def test_rows_behind_the_reach_of_32_bits():
     r = bps.log_probs(logits, tokens, top_k=2)
     s = bps.log_probs(logits[few].contiguous(), tokens[few], top_k=2)
     assert torch.equal(r.top_ids[few], s.top_ids)
-    for a, b in zip(r, s):
+    for a, b in zip(r[:5], s[:5]):           # held has five rows
         assert torch.allclose(a[few].double(), b.double(), rtol=1e-5, atol=1e-5)
     assert torch.allclose(r.entropy[2:8191], torch.full((1,), math.log(V), device="cuda"), rtol=1e-5)
     one = torch.ones(N, device="cuda")
