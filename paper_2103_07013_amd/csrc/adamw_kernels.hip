@@ -60,10 +60,25 @@ __global__ __launch_bounds__(kAdamGroup) void k_adamw_norm(AdamPlan plan, AdamGr
     if (g) {
         const uint64_t from = (uint64_t)chunk.index * kAdamChunk, left = t.count - from;
         const uint32_t n = left < kAdamChunk ? (uint32_t)left : kAdamChunk;
-        for (uint32_t i = tid; i < n; i += kAdamGroup) {
-            const float x = to_float(g[from + i]) * s.grad_scale;
-            sum = fmaf(x, x, sum);
+        constexpr uint32_t kLoads = kAdamChunk / kStep;
+        float x[kLoads][kPerLane];
+#pragma unroll
+        for (uint32_t u = 0; u < kLoads; ++u) {
+            const uint32_t i = u * kStep + tid * kPerLane;
+            if (i + kPerLane <= n) {
+                load<G, kPerLane>(g + from + i, x[u]);
+            } else {
+#pragma unroll
+                for (uint32_t k = 0; k < kPerLane; ++k) x[u][k] = i + k < n ? to_float(g[from + i + k]) : 0.0f;
+            }
         }
+#pragma unroll
+        for (uint32_t u = 0; u < kLoads; ++u)
+#pragma unroll
+            for (uint32_t k = 0; k < kPerLane; ++k) {
+                const float y = x[u][k] * s.grad_scale;
+                sum = fmaf(y, y, sum);
+            }
     }
     sum = wave_sum(sum);
     if ((tid & 63u) == 0) sums[tid >> 6] = sum;
@@ -78,7 +93,16 @@ __global__ __launch_bounds__(kAdamGroup) void k_adamw_norm(AdamPlan plan, AdamGr
     // the last work-group adds up all sums, in an order that does not depend on which one it is
     __threadfence();
     double all = 0.0;
-    for (uint32_t i = tid; i < all_chunks; i += kAdamGroup) all += (double)__hip_atomic_load(&plan.partial[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    for (uint32_t i = 0; i < all_chunks; i += 8 * kAdamGroup) {
+        float x[8];
+#pragma unroll
+        for (uint32_t u = 0; u < 8; ++u) {
+            const uint32_t j = i + u * kAdamGroup + tid;
+            x[u] = j < all_chunks ? __hip_atomic_load(&plan.partial[j], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0f;
+        }
+#pragma unroll
+        for (uint32_t u = 0; u < 8; ++u) all += (double)x[u];
+    }
 #pragma unroll
     for (int d = 32; d; d >>= 1) all += __shfl_xor(all, d, 64);
     if ((tid & 63u) == 0) total[tid >> 6] = all;

@@ -25,7 +25,7 @@ uint32_t bits_of(uint32_t v) {
     return b;
 }
 struct SortPlan {
-    uint32_t passes, digit, tiles;
+    uint32_t passes, digit, tiles, row;
 };
 // keys are 0..rows, where `rows` stands for no row
 SortPlan sort_plan(uint32_t count, uint32_t rows) {
@@ -34,6 +34,7 @@ SortPlan sort_plan(uint32_t count, uint32_t rows) {
     p.passes = (bits + kMaxDigit - 1) / kMaxDigit;
     p.digit = (bits + p.passes - 1) / p.passes;
     p.tiles = (count + kSortTile - 1) / kSortTile;
+    p.row = (p.tiles + 3) / 4 * 4;
     return p;
 }
 
@@ -56,10 +57,10 @@ struct SortArgs {
     const void* tokens;       // of the first pass, where keys is null
     const uint32_t *keys, *places;
     uint32_t *out_keys, *out_places;
-    uint32_t* counts;         // [tile][digit], and the digits' totals behind the last tile
+    uint32_t* counts;         // [digit][row of tiles], tiles in whole words of 16 bytes; then the digits' totals
     uint8_t* marks;           // [rows, in whole words], 1 where a row has a token
     int32_t tokens64;
-    uint32_t count, rows, shift, bits, tiles, last;
+    uint32_t count, rows, shift, bits, tiles, row, last;
 };
 __device__ __forceinline__ uint32_t sort_key(const SortArgs& a, uint32_t i) { return a.keys ? a.keys[i] : key_at(a.tokens, a.tokens64, i, a.rows); }
 
@@ -82,25 +83,27 @@ __global__ __launch_bounds__(kSortGroup) void k_sort_count(SortArgs a) {
     if (!a.keys && a.marks)
         for (uint32_t r = blockIdx.x * kSortGroup + threadIdx.x; r < (a.rows + 3) / 4; r += gridDim.x * kSortGroup) reinterpret_cast<uint32_t*>(a.marks)[r] = 0;
     __syncthreads();
-    for (uint32_t b = threadIdx.x; b < bins; b += kSortGroup) a.counts[(size_t)blockIdx.x * bins + b] = hist[b];
+    for (uint32_t b = threadIdx.x; b < bins; b += kSortGroup) a.counts[(size_t)b * a.row + blockIdx.x] = hist[b];
 }
 
-// Many tiles: a thread for each digit turns its counts into the number of equal digits in tiles before, 64 digits to a wavefront.
-__global__ __launch_bounds__(64) void k_sort_sum(SortArgs a) {
-    const uint32_t bins = 1u << a.bits, b = blockIdx.x * 64 + threadIdx.x;
+// Many tiles: a wavefront for each digit turns its counts into the number of equal digits in tiles before.
+__global__ __launch_bounds__(256) void k_sort_sum(SortArgs a) {
+    const uint32_t bins = 1u << a.bits, b = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63u;
     if (b >= bins) return;
+    uint32_t* counts = a.counts + (size_t)b * a.row;
     uint32_t sum = 0;
-    for (uint32_t t = 0; t < a.tiles; t += 8) {
-        uint32_t n[8];
+    for (uint32_t t = 0; t < a.tiles; t += 64) {
+        const uint32_t n = t + lane < a.tiles ? counts[t + lane] : 0u;
+        uint32_t with = n;
 #pragma unroll
-        for (uint32_t k = 0; k < 8; ++k) n[k] = t + k < a.tiles ? a.counts[(size_t)(t + k) * bins + b] : 0u;
-#pragma unroll
-        for (uint32_t k = 0; k < 8; ++k) {
-            if (t + k < a.tiles) a.counts[(size_t)(t + k) * bins + b] = sum;
-            sum += n[k];
+        for (int d = 1; d < 64; d <<= 1) {
+            const uint32_t x = __shfl_up(with, d, 64);
+            if (lane >= (uint32_t)d) with += x;
         }
+        if (t + lane < a.tiles) counts[t + lane] = sum + with - n;
+        sum += __shfl(with, 63, 64);
     }
-    a.counts[(size_t)a.tiles * bins + b] = sum;
+    if (lane == 0) a.counts[(size_t)bins * a.row + b] = sum;
 }
 
 // Exclusive sums over `bins` numbers in LDS, by a work-group of GROUP threads; `sums`: GROUP / 64 numbers.
@@ -185,14 +188,19 @@ __global__ __launch_bounds__(kSortGroup) void k_sort_place(SortArgs a) {
         if (b >= bins) continue;
         uint32_t total;
         if (a.tiles > kSumTiles) {
-            before[k] = a.counts[(size_t)blockIdx.x * bins + b];
-            total = a.counts[(size_t)a.tiles * bins + b];
+            before[k] = a.counts[(size_t)b * a.row + blockIdx.x];
+            total = a.counts[(size_t)bins * a.row + b];
         } else {
+            uint4 n[kSumTiles / 4];
+#pragma unroll
+            for (uint32_t t = 0; t < kSumTiles / 4; ++t)
+                n[t] = 4 * t < a.tiles ? *reinterpret_cast<const uint4*>(a.counts + (size_t)b * a.row + 4 * t) : make_uint4(0, 0, 0, 0);
             total = 0;
-            for (uint32_t t = 0; t < a.tiles; ++t) {
-                const uint32_t n = a.counts[(size_t)t * bins + b];
-                if (t < blockIdx.x) before[k] += n;
-                total += n;
+#pragma unroll
+            for (uint32_t t = 0; t < kSumTiles; ++t) {
+                const uint32_t m = t >= a.tiles ? 0u : t % 4 == 0 ? n[t / 4].x : t % 4 == 1 ? n[t / 4].y : t % 4 == 2 ? n[t / 4].z : n[t / 4].w;
+                if (t < blockIdx.x) before[k] += m;
+                total += m;
             }
         }
         start[b] = total;
@@ -323,11 +331,15 @@ uint32_t piece_length(uint32_t count) {
     return n;
 }
 
+// A piece's last row goes on in the next piece: it began in this one, or before it.
+enum : uint8_t { kGoesOn = 1, kThrough = 2 };
+
 struct SumArgs {
     const uint32_t *keys, *places;
     const uint8_t* marks;     // null with accumulate
     const void* grad;
     void* out;
+    uint8_t* cuts;            // [piece] what its last row is: kGoesOn, kThrough or 0
     float* partial;           // [piece][2][width]: of the row that began before the piece, of the row that goes on behind it
     int64_t grad_stride, out_stride;
     uint32_t count, rows, width, pieces, length;
@@ -391,6 +403,10 @@ __global__ __launch_bounds__(256) void k_embed_sum(SumArgs a) {
     const uint32_t from = piece * a.length;
     const uint32_t end = piece >= a.pieces ? from : a.count - from < a.length ? a.count : from + a.length;
     bool began_before = piece < a.pieces && from > 0 && a.keys[from - 1] == a.keys[from];
+    if (at == 0 && piece < a.pieces) {
+        const uint32_t last = a.keys[end - 1];
+        a.cuts[piece] = last >= a.rows || end == a.count || a.keys[end] != last ? 0 : began_before && a.keys[from] == last ? kThrough : kGoesOn;
+    }
     float sum[N];
 #pragma unroll
     for (int k = 0; k < N; ++k) sum[k] = 0.0f;
@@ -443,65 +459,105 @@ __global__ __launch_bounds__(256) void k_embed_sum(SumArgs a) {
     }
 }
 
-// The rows that are cut.  Each work-group looks for the pieces in which such a row begins, and takes its share of them, by columns;
-// its wavefronts add up a part of the row's partial sums each, in order, and then those parts.
+// The rows that are cut.  Each work-group lists the pieces in which such a row begins, and how many partial sums there are of it.  Of rows
+// with few a wavefront adds up 256 columns; of rows with many a work-group does, each wavefront a part of them in order, and then those
+// parts in order.
 template <class O>
 __global__ __launch_bounds__(1024) void k_embed_join(SumArgs a) {
-    constexpr uint32_t kWaves = 16, kColumns = 64;
-    __shared__ uint32_t begins[kMaxPieces];
-    __shared__ uint32_t counts[kWaves], found;
+    constexpr uint32_t kWaves = 16, kColumns = 256, kFew = 32;
+    __shared__ uint64_t through[kMaxPieces / 64 + 1];
+    __shared__ uint16_t begins[kMaxPieces];
+    __shared__ uint32_t counts[kMaxPieces / 64];
     __shared__ float part[kWaves][kColumns];
     const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6;
-    if (tid == 0) found = 0;
-    for (uint32_t first = 0; first + 1 < a.pieces; first += 1024) {
-        const uint32_t piece = first + tid;
-        bool is = false;
-        if (piece + 1 < a.pieces) {
-            const uint32_t from = piece * a.length, next = from + a.length, key = a.keys[next - 1];
-            is = key < a.rows && a.keys[next] == key && !(a.keys[from] == key && from > 0 && a.keys[from - 1] == key);
+    uint64_t mine[kMaxPieces / 1024];
+#pragma unroll
+    for (uint32_t k = 0; k < kMaxPieces / 1024; ++k) {
+        const uint32_t piece = k * 1024 + tid;
+        const uint32_t cut = piece < a.pieces ? a.cuts[piece] : 0u;
+        mine[k] = __ballot(cut == kGoesOn);
+        const uint64_t with = __ballot(cut == kThrough);
+        if (lane == 0) {
+            through[piece / 64] = with;
+            counts[piece / 64] = (uint32_t)__popcll(mine[k]);
         }
-        const uint64_t who = __ballot(is);
-        __syncthreads();
-        if (lane == 0) counts[wave] = (uint32_t)__popcll(who);
-        __syncthreads();
-        uint32_t to = found + lanes_before(who);
-        for (uint32_t w = 0; w < wave; ++w) to += counts[w];
-        if (is) begins[to] = piece;
-        __syncthreads();
-        if (tid == 0)
-            for (uint32_t w = 0; w < kWaves; ++w) found += counts[w];
     }
     __syncthreads();
+    uint32_t found = 0;
+    if (wave == 0) {
+        const uint32_t n = counts[lane];
+        uint32_t with = n;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const uint32_t x = __shfl_up(with, d, 64);
+            if (lane >= (uint32_t)d) with += x;
+        }
+        counts[lane] = with;
+    }
+    __syncthreads();
+    found = counts[kMaxPieces / 64 - 1];
+#pragma unroll
+    for (uint32_t k = 0; k < kMaxPieces / 1024; ++k) {
+        const uint32_t piece = k * 1024 + tid, word = piece / 64;
+        if (mine[k] >> lane & 1u) begins[(word ? counts[word - 1] : 0u) + lanes_before(mine[k])] = (uint16_t)piece;
+    }
+    __syncthreads();
+    // partial sums of the row that begins in a piece: of this one, of those that it goes through, and of the one that it ends in
+    auto partial_sums = [&](uint32_t piece) {
+        uint32_t at = piece + 1;
+        for (uint32_t word = at / 64; word < kMaxPieces / 64; ++word) {
+            const uint64_t ends = ~through[word] & (word == at / 64 ? ~0ull << (at % 64) : ~0ull);
+            if (ends) return word * 64 + (uint32_t)__builtin_ctzll(ends) + 1 - piece;
+        }
+        return (uint32_t)kMaxPieces - piece;
+    };
+    auto add = [&](uint32_t piece, uint32_t from, uint32_t to, uint32_t at, float (&sum)[4]) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) sum[c] = 0.0f;
+        for (uint32_t k = from; k < to; k += 4) {
+            float x[4][4];
+#pragma unroll
+            for (uint32_t u = 0; u < 4; ++u) {
+                const float* p = a.partial + ((size_t)(piece + (k + u < to ? k + u : from)) * 2 + ((k + u < to ? k + u : from) == 0)) * a.width + at;
+                if (at + 4 <= a.width) {
+                    load<F32, 4>(p, x[u]);
+                } else {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) x[u][c] = at + c < a.width ? p[c] : 0.0f;
+                }
+            }
+#pragma unroll
+            for (uint32_t u = 0; u < 4; ++u)
+                if (k + u < to) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) sum[c] += x[u][c];
+                }
+        }
+    };
     const uint32_t blocks = (a.width + kColumns - 1) / kColumns;
     const uint64_t all = (uint64_t)found * blocks;
+    for (uint64_t work = (uint64_t)wave * gridDim.x + blockIdx.x; work < all; work += (uint64_t)kWaves * gridDim.x) {
+        const uint32_t piece = begins[work / blocks], n = partial_sums(piece), at = (uint32_t)(work % blocks) * kColumns + lane * 4;
+        if (n > kFew || at >= a.width) continue;
+        float sum[4];
+        add(piece, 0, n, at, sum);
+        write_sum<O, 4>(a, a.keys[(piece + 1) * a.length - 1], at, sum);
+    }
     for (uint64_t work = blockIdx.x; work < all; work += gridDim.x) {
-        const uint32_t piece = begins[work / blocks], at = (uint32_t)(work % blocks) * kColumns + lane;
-        const uint32_t key = a.keys[(piece + 1) * a.length - 1];
-        uint32_t lo = piece + 2, hi = a.pieces;      // the first piece behind piece + 1 that begins with another key
-        while (lo < hi) {
-            const uint32_t mid = lo + (hi - lo) / 2;
-            if (a.keys[mid * a.length] == key) lo = mid + 1; else hi = mid;
-        }
-        // partial sums piece (second kind), piece + 1 .. lo - 1 (first kind), in kWaves shares
-        const uint32_t n = lo - piece, each = (n + kWaves - 1) / kWaves, begin = wave * each, stop = begin + each < n ? begin + each : n;
-        float sum = 0.0f;
-        if (at < a.width) {
-            for (uint32_t k = begin; k < stop; k += 4) {
-                float x[4];
-#pragma unroll
-                for (uint32_t u = 0; u < 4; ++u) x[u] = k + u < stop ? a.partial[((size_t)(piece + k + u) * 2 + (k + u == 0)) * a.width + at] : 0.0f;
-#pragma unroll
-                for (uint32_t u = 0; u < 4; ++u) sum += x[u];
-            }
-        }
+        const uint32_t piece = begins[work / blocks], n = partial_sums(piece), at = (uint32_t)(work % blocks) * kColumns + lane * 4;
+        if (n <= kFew) continue;
+        const uint32_t each = (n + kWaves - 1) / kWaves, begin = wave * each < n ? wave * each : n, stop = begin + each < n ? begin + each : n;
+        float sum[4] = {};
+        if (at < a.width) add(piece, begin, stop, at, sum);
         __syncthreads();
-        part[wave][lane] = sum;
+        store<F32, 4>(&part[wave][lane * 4], sum);
         __syncthreads();
         if (wave == 0 && at < a.width) {
-            float all_of[1] = {part[0][lane]};
+            for (uint32_t w = 1; w < kWaves; ++w) {
 #pragma unroll
-            for (uint32_t w = 1; w < kWaves; ++w) all_of[0] += part[w][lane];
-            write_sum<O, 1>(a, key, at, all_of);
+                for (int c = 0; c < 4; ++c) sum[c] += part[w][lane * 4 + c];
+            }
+            write_sum<O, 4>(a, a.keys[(piece + 1) * a.length - 1], at, sum);
         }
     }
 }
@@ -519,7 +575,7 @@ void sum(SumArgs s, hipStream_t stream) {
 
 template <class T, class O>
 hipError_t embed_grad(const EmbedGradArgs& a, hipStream_t stream) {
-    SumArgs s = {nullptr, nullptr, nullptr, a.grad, a.out, nullptr, a.grad_stride, a.out_stride, a.count, a.rows, a.width, 0, 0, 0, 0, a.scale, a.accumulate};
+    SumArgs s = {nullptr, nullptr, nullptr, a.grad, a.out, nullptr, nullptr, a.grad_stride, a.out_stride, a.count, a.rows, a.width, 0, 0, 0, 0, a.scale, a.accumulate};
     if (!a.count) {
         if (!a.accumulate) hipLaunchKernelGGL((k_embed_zero<O>), dim3((a.rows + 3) / 4 < 16384 ? (a.rows + 3) / 4 : 16384), dim3(256), 0, stream, s);
         return hipGetLastError();
@@ -532,11 +588,13 @@ hipError_t embed_grad(const EmbedGradArgs& a, hipStream_t stream) {
         w += whole((size_t)a.count * 4);
     }
     uint32_t* counts = reinterpret_cast<uint32_t*>(w);
-    w += whole(((size_t)(plan.tiles + 1) << plan.digit) * 4);
+    w += whole(((size_t)(plan.row + 1) << plan.digit) * 4);
     uint8_t* marks = reinterpret_cast<uint8_t*>(w);
     w += whole(a.rows);
+    s.cuts = reinterpret_cast<uint8_t*>(w);
+    w += kMaxPieces;
     s.partial = reinterpret_cast<float*>(w);
-    SortArgs sort = {a.tokens, nullptr, nullptr, buffer[0], buffer[1], counts, a.accumulate ? nullptr : marks, a.tokens64, a.count, a.rows, 0, plan.digit, plan.tiles, 1};
+    SortArgs sort = {a.tokens, nullptr, nullptr, buffer[0], buffer[1], counts, a.accumulate ? nullptr : marks, a.tokens64, a.count, a.rows, 0, plan.digit, plan.tiles, plan.row, 1};
     if (a.count <= kSortOne) {
         hipLaunchKernelGGL(k_sort_one, dim3(1), dim3(kSortOneGroup), 0, stream, sort, plan.passes);
     } else {
@@ -546,7 +604,7 @@ hipError_t embed_grad(const EmbedGradArgs& a, hipStream_t stream) {
             sort.out_keys = buffer[2 * (p & 1)];
             sort.out_places = buffer[2 * (p & 1) + 1];
             hipLaunchKernelGGL(k_sort_count, dim3(plan.tiles), dim3(kSortGroup), 0, stream, sort);
-            if (plan.tiles > kSumTiles) hipLaunchKernelGGL(k_sort_sum, dim3(((1u << plan.digit) + 63) / 64), dim3(64), 0, stream, sort);
+            if (plan.tiles > kSumTiles) hipLaunchKernelGGL(k_sort_sum, dim3(((1u << plan.digit) + 3) / 4), dim3(256), 0, stream, sort);
             hipLaunchKernelGGL(k_sort_place, dim3(plan.tiles), dim3(kSortGroup), 0, stream, sort);
             sort.keys = sort.out_keys;
             sort.places = sort.out_places;
@@ -564,7 +622,7 @@ hipError_t embed_grad(const EmbedGradArgs& a, hipStream_t stream) {
         sum<T, O, 16>(s, stream);
     else
         sum<T, O, 64>(s, stream);
-    if (s.pieces > 1) hipLaunchKernelGGL((k_embed_join<O>), dim3(256), dim3(1024), 0, stream, s);
+    if (s.pieces > 1) hipLaunchKernelGGL((k_embed_join<O>), dim3(s.pieces < 256 ? s.pieces : 256), dim3(1024), 0, stream, s);
     return hipGetLastError();
 }
 
@@ -605,7 +663,7 @@ size_t embed_grad_workspace(uint32_t count, uint32_t rows, uint32_t width) {
     if (!count) return 0;
     const SortPlan plan = sort_plan(count, rows);
     const uint32_t length = piece_length(count);
-    return 4 * whole((size_t)count * 4) + whole(((size_t)(plan.tiles + 1) << plan.digit) * 4) + whole(rows) + (count + (size_t)length - 1) / length * 2 * width * 4;
+    return 4 * whole((size_t)count * 4) + whole(((size_t)(plan.row + 1) << plan.digit) * 4) + whole(rows) + kMaxPieces + (count + (size_t)length - 1) / length * 2 * width * 4;
 }
 
 hipError_t launch_embed(int32_t dtype, const EmbedArgs& a, hipStream_t stream) {

@@ -153,18 +153,19 @@ __global__ __launch_bounds__(256) void k_score_short(ScoreArgs a) {
 
 // The best 64 of what a wavefront has seen, one in each lane in descending order; 0 = none.
 // A bitonic network: halves that are sorted are joined by a comparison with the mirrored lane, then with lanes at falling distances.
-template <int X>
-__device__ __forceinline__ uint64_t exchanged(uint64_t v, bool keep_larger) {
-    const uint64_t o = bps::from_lane_xor<X>(v);
+template <int X, class V>
+__device__ __forceinline__ V exchanged(V v, bool keep_larger) {
+    const V o = bps::from_lane_xor<X>(v);
     return (o > v) == keep_larger ? o : v;
 }
-template <int X>
-__device__ __forceinline__ uint64_t settled(uint64_t v, uint32_t lane) {      // comparisons at the distances X, X / 2 .. 1
+template <int X, class V>
+__device__ __forceinline__ V settled(V v, uint32_t lane) {      // comparisons at the distances X, X / 2 .. 1
     v = exchanged<X>(v, (lane & X) == 0);
     if constexpr (X > 1) v = settled<X / 2>(v, lane);
     return v;
 }
-__device__ __forceinline__ uint64_t sorted(uint64_t v, uint32_t lane) {
+template <class V>
+__device__ __forceinline__ V sorted(V v, uint32_t lane) {
     v = exchanged<1>(v, (lane & 1) == 0);
     v = settled<1>(exchanged<3>(v, (lane & 2) == 0), lane);
     v = settled<2>(exchanged<7>(v, (lane & 4) == 0), lane);
@@ -177,11 +178,25 @@ __device__ __forceinline__ uint64_t merged(uint64_t a, uint64_t b, uint32_t lane
     const uint64_t o = bps::from_lane_xor<63>(b);
     return settled<32>(o > a ? o : a, lane);
 }
+// The best of WAVES lists, in the first wavefront: half of the lists are joined to the other half, until one is left.
+template <int WAVES>
+__device__ __forceinline__ uint64_t merged_waves(uint64_t list, uint64_t* held, uint32_t stride, uint32_t wave, uint32_t lane) {
+    held[wave * stride + lane] = list;
+#pragma unroll
+    for (uint32_t half = WAVES / 2; half; half /= 2) {
+        __syncthreads();
+        if (wave < half) {
+            list = merged(list, held[(wave + half) * stride + lane], lane);
+            held[wave * stride + lane] = list;
+        }
+    }
+    return list;
+}
 
-// The float that an order stands for (see order_of); an order of 0 stands for -inf.
-__device__ __forceinline__ float value_of(uint64_t order) {
-    const uint32_t up = (uint32_t)(order >> 32);
-    return up == 0u ? -kInf : __uint_as_float((up & 0x80000000u) ? up & 0x7FFFFFFFu : ~up);
+// The upper half of an order (see order_of), which the float alone decides, and the float that it stands for; 0 stands for -inf.
+__device__ __forceinline__ uint32_t rank_of(float x) { return (uint32_t)(order_of(x, 0u) >> 32); }
+__device__ __forceinline__ float value_of(uint32_t rank) {
+    return rank == 0u ? -kInf : __uint_as_float((rank & 0x80000000u) ? rank & 0x7FFFFFFFu : ~rank);
 }
 
 constexpr uint32_t kWaiting = 128;     // candidates that wait for a sort, per wavefront
@@ -190,18 +205,25 @@ struct Best {
     uint64_t list;            // sorted, one per lane
     uint64_t* waiting;        // LDS, kWaiting of this wavefront
     uint32_t count;           // of them, below 64 between calls
-    float least;              // entries below it are no candidates
+    float least;              // entries below it, or as large and not before least_at, are no candidates
+    uint32_t least_at;
 
+    __device__ __forceinline__ void raise(float to, uint32_t at) {
+        if (to > least || to != to || (to == least && at < least_at)) {
+            least = to;
+            least_at = at;
+        }
+    }
     __device__ __forceinline__ void take_in(uint32_t lane, uint32_t k, uint32_t n) {
         // the wavefront's own stores, in order before its loads
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         const uint64_t v = lane < n ? waiting[lane] : 0;
         list = merged(list, sorted(v, lane), lane);
         const uint64_t last = __shfl((unsigned long long)list, (int)k - 1, 64);
-        least = value_of(last);
+        if (last) raise(value_of((uint32_t)(last >> 32)), ~(uint32_t)last);
     }
     __device__ __forceinline__ void offer(float x, uint32_t at, uint32_t lane, uint32_t k) {
-        const bool is = !(x < least) && x != -kInf;
+        const bool is = x > least || (x == least && at < least_at) || x != x;
         const uint64_t who = __ballot(is);
         if (!who) return;
         if (is) waiting[count + lanes_before(who)] = order_of(x, at);
@@ -220,35 +242,55 @@ struct Best {
     }
 };
 
-// Entries [from, to) of a row, by `threads` threads.
-template <class T, bool MASK, bool TOP>
-__device__ __forceinline__ Part stream(const typename T::raw* row, const uint8_t* mask, uint32_t from, uint32_t to, uint32_t tid, uint32_t threads, float c, Best& best,
-                                       uint32_t k) {
-    constexpr int N = T::kPer16, U = 4;
-    const uint32_t lane = tid & 63u;
+// Entries [from, to) of a row, by WAVES wavefronts; bars: LDS, 2 * WAVES numbers.
+template <class T, bool MASK, bool TOP, int WAVES>
+__device__ __forceinline__ Part stream(const typename T::raw* row, const uint8_t* mask, uint32_t from, uint32_t to, uint32_t tid, float c, Best& best, uint32_t k,
+                                       uint32_t* bars) {
+    constexpr int N = T::kPer16, U = 4, kThreads = 64 * WAVES;
+    const uint32_t lane = tid & 63u, wave = tid >> 6;
     Part p = nothing();
     bool first = true;
-    for (uint32_t base = from; base < to; base += threads * N * U) {
-        float x[U][N];
+    for (uint32_t base = from; base < to; base += kThreads * N * U) {
+        float x[U * N];
 #pragma unroll
-        for (int u = 0; u < U; ++u) row_entries<T, N, MASK>(row, mask, base + (u * threads + tid) * N, to, x[u]);
-        float flat[U * N];
+        for (int u = 0; u < U; ++u) {
+            float y[N];
+            row_entries<T, N, MASK>(row, mask, base + (u * kThreads + tid) * N, to, y);
 #pragma unroll
-        for (int e = 0; e < U * N; ++e) flat[e] = x[e / N][e % N];
-        add(p, flat, c);
+            for (int e = 0; e < N; ++e) x[u * N + e] = y[e];
+        }
+        add(p, x, c);
         if constexpr (TOP) {
             float top = -kInf;
 #pragma unroll
-            for (int e = 0; e < U * N; ++e) top = fmaxf(top, flat[e]);
+            for (int e = 0; e < U * N; ++e) top = fmaxf(top, x[e]);
             if (first) {
-                // the k-th best of the lanes' own best is no better than the k-th of all
-                const uint64_t own = sorted(top != -kInf ? order_of(top, 0u) : 0ull, lane);
-                best.least = value_of(__shfl((unsigned long long)own, (int)k - 1, 64));
+                // Where at least k lanes' own best reach a bar, the k-th best of all does: the k-th of any wavefront's lanes, and what the
+                // k / WAVES best lanes of every wavefront reach.
+                const uint32_t own = sorted(top != -kInf ? rank_of(top) : 0u, lane);
+                uint32_t bar = __shfl(own, (int)k - 1, 64);
+                if constexpr (WAVES > 1) {
+                    const uint32_t all = __shfl(own, (int)((k + WAVES - 1) / WAVES) - 1, 64);
+                    if (lane == 0) {
+                        bars[wave] = bar;
+                        bars[WAVES + wave] = all;
+                    }
+                    __syncthreads();
+                    uint32_t least = 0xFFFFFFFFu;
+#pragma unroll
+                    for (int w = 0; w < WAVES; ++w) {
+                        bar = bars[w] > bar ? bars[w] : bar;
+                        least = bars[WAVES + w] < least ? bars[WAVES + w] : least;
+                    }
+                    bar = least > bar ? least : bar;
+                }
+                best.least = value_of(bar);
+                best.least_at = bar ? 0xFFFFFFFFu : 0u;
                 first = false;
             }
             if (__ballot((top >= best.least && top != -kInf) || p.z != p.z)) {
 #pragma unroll
-                for (int e = 0; e < U * N; ++e) best.offer(flat[e], base + ((e / N) * threads + tid) * N + e % N, lane, k);
+                for (int e = 0; e < U * N; ++e) best.offer(x[e], base + ((e / N) * kThreads + tid) * N + e % N, lane, k);
             }
         }
     }
@@ -260,6 +302,7 @@ template <class T, bool MASK, bool TOP, int WAVES>
 __global__ __launch_bounds__(WAVES > 4 ? WAVES * 64 : 256) void k_score(ScoreArgs a) {
     constexpr uint32_t kGroup = WAVES > 4 ? WAVES * 64 : 256, kWaves = kGroup / 64;
     __shared__ uint64_t waiting[TOP ? kWaves * kWaiting : 1];
+    __shared__ uint32_t bars[2 * kWaves];
     __shared__ Part parts[kWaves];
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
     const uint64_t r = (uint64_t)blockIdx.x * (kWaves / WAVES) + wave / WAVES;
@@ -267,20 +310,18 @@ __global__ __launch_bounds__(WAVES > 4 ? WAVES * 64 : 256) void k_score(ScoreArg
     if (r >= a.rows) return;        // whole wavefronts, and where they share a row whole work-groups
     const typename T::raw* row = static_cast<const typename T::raw*>(a.logits) + (int64_t)r * a.row_stride;
     const uint8_t* mask = MASK ? a.mask + (int64_t)r * a.mask_stride : nullptr;
-    Best best = {0, waiting + (TOP ? wave * kWaiting : 0), 0, -kInf};
-    Part p = stream<T, MASK, TOP>(row, mask, 0, a.entries, threadIdx.x % (64 * WAVES), 64 * WAVES, c, best, a.top_k);
+    Best best = {0, waiting + (TOP ? wave * kWaiting : 0), 0, -kInf, 0};
+    Part p = stream<T, MASK, TOP, WAVES>(row, mask, 0, a.entries, threadIdx.x % (64 * WAVES), c, best, a.top_k, bars);
     p = group_part<64>(p, c);
     if constexpr (TOP) best.finish(lane, a.top_k);
     if constexpr (WAVES > 1) {
         if (lane == 0) parts[wave] = p;
-        if (TOP) best.waiting[lane] = best.list;
-        __syncthreads();
+        if (TOP)
+            best.list = merged_waves<WAVES>(best.list, waiting, kWaiting, wave, lane);
+        else
+            __syncthreads();
         if (wave) return;
-        p = parts[0];
-        for (uint32_t w = 1; w < WAVES; ++w) {
-            p = joined(p, parts[w], c);
-            if (TOP) best.list = merged(best.list, waiting[w * kWaiting + lane], lane);
-        }
+        p = group_part<WAVES>(parts[lane % WAVES], c);
     }
     const float ln_z = logf(p.z);
     if (lane == 0) write_row<T>(a, r, p, ln_z, row, mask);
@@ -300,6 +341,7 @@ struct __align__(16) PieceSums {
 template <class T, bool MASK, bool TOP>
 __global__ __launch_bounds__(256) void k_score_piece(ScoreArgs a, Pieces pieces, PieceSums* sums, uint64_t* lists) {
     __shared__ uint64_t waiting[TOP ? 4 * kWaiting : 1];
+    __shared__ uint32_t bars[8];
     __shared__ Part parts[4];
     const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
     const uint64_t r = blockIdx.x / pieces.count;
@@ -308,20 +350,19 @@ __global__ __launch_bounds__(256) void k_score_piece(ScoreArgs a, Pieces pieces,
     const float c = a.scale * kLog2e;
     const typename T::raw* row = static_cast<const typename T::raw*>(a.logits) + (int64_t)r * a.row_stride;
     const uint8_t* mask = MASK ? a.mask + (int64_t)r * a.mask_stride : nullptr;
-    Best best = {0, waiting + (TOP ? wave * kWaiting : 0), 0, -kInf};
-    Part p = stream<T, MASK, TOP>(row, mask, from, to, threadIdx.x, 256, c, best, a.top_k);
+    Best best = {0, waiting + (TOP ? wave * kWaiting : 0), 0, -kInf, 0};
+    Part p = stream<T, MASK, TOP, 4>(row, mask, from, to, threadIdx.x, c, best, a.top_k, bars);
     p = group_part<64>(p, c);
     if constexpr (TOP) best.finish(lane, a.top_k);
     if (lane == 0) parts[wave] = p;
-    if (TOP) best.waiting[lane] = best.list;
-    __syncthreads();
+    if (TOP)
+        best.list = merged_waves<4>(best.list, waiting, kWaiting, wave, lane);
+    else
+        __syncthreads();
     if (wave) return;
-    p = joined(joined(parts[0], parts[1], c), joined(parts[2], parts[3], c), c);
+    p = group_part<4>(parts[lane % 4], c);
     if (lane == 0) sums[blockIdx.x] = {p, 0.0f};
-    if constexpr (TOP) {
-        for (uint32_t w = 1; w < 4; ++w) best.list = merged(best.list, waiting[w * kWaiting + lane], lane);
-        if (lane < a.top_k) lists[(uint64_t)blockIdx.x * a.top_k + lane] = best.list;
-    }
+    if (TOP && lane < a.top_k) lists[(uint64_t)blockIdx.x * a.top_k + lane] = best.list;
 }
 
 constexpr uint32_t kMaxPieces = 64;
@@ -342,15 +383,7 @@ __global__ __launch_bounds__(TOP ? 1024 : 64) void k_score_join(ScoreArgs a, Pie
             const uint64_t v = at + lane < n ? lists[r * n + at + lane] : 0;
             list = merged(list, sorted(v, lane), lane);
         }
-        held[threadIdx.x] = list;
-        // half of the lists are joined to the other half, until one is left
-        for (uint32_t half = kWaves / 2; half; half /= 2) {
-            __syncthreads();
-            if (wave < half) {
-                list = merged(list, held[(wave + half) * 64 + lane], lane);
-                held[threadIdx.x] = list;
-            }
-        }
+        list = merged_waves<kWaves>(list, held, 64, wave, lane);
         if (wave) return;
     }
     Part p = lane < pieces.count ? sums[r * pieces.count + lane].p : nothing();
@@ -471,8 +504,10 @@ hipError_t score(const ScoreArgs& a, hipStream_t stream) {
         hipLaunchKernelGGL((k_score_join<T, TOP>), dim3((uint32_t)a.rows), dim3(TOP ? 1024 : 64), 0, stream, a, pieces, sums, lists);
     } else if (a.entries <= kWaveRow) {
         BPS_ROWS(k_score, 4, 256, TOP, 1);
-    } else {
+    } else if (a.rows >= 2 * kComputeUnits) {
         BPS_ROWS(k_score, 1, 256, TOP, 4);
+    } else {
+        BPS_ROWS(k_score, 1, 1024, TOP, 16);
     }
     return hipGetLastError();
 }
