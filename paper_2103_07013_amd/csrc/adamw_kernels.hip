@@ -46,21 +46,20 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t x) {
     return x;
 }
 
+// Sums of squares: each work-group those of every gridDim.x-th chunk.
 template <class G>
-__global__ __launch_bounds__(kAdamGroup) void k_adamw_norm(AdamPlan plan, AdamGrads grads, uint32_t first_tensor, uint32_t first_chunk, uint32_t all_chunks, AdamScalars s,
-                                                           float* norm_out) {
+__global__ __launch_bounds__(kAdamGroup) void k_adamw_norm(AdamPlan plan, AdamGrads grads, uint32_t first_tensor, uint32_t first_chunk, uint32_t chunks, uint32_t first_sum,
+                                                           AdamScalars s) {
     __shared__ float sums[kAdamGroup / 64];
-    __shared__ double total[kAdamGroup / 64];
-    __shared__ uint32_t is_last;
-    const AdamChunk chunk = plan.chunks[first_chunk + blockIdx.x];
-    const AdamTensor t = plan.tensors[chunk.tensor];
-    const typename G::raw* g = static_cast<const typename G::raw*>(grads.at[chunk.tensor - first_tensor]);
+    constexpr uint32_t kLoads = kAdamChunk / kStep;
     const uint32_t tid = threadIdx.x;
     float sum = 0.0f;
-    if (g) {
-        const uint64_t from = (uint64_t)chunk.index * kAdamChunk, left = t.count - from;
+    for (uint32_t c = blockIdx.x; c < chunks; c += gridDim.x) {
+        const AdamChunk chunk = plan.chunks[first_chunk + c];
+        const typename G::raw* g = static_cast<const typename G::raw*>(grads.at[chunk.tensor - first_tensor]);
+        if (!g) continue;
+        const uint64_t from = (uint64_t)chunk.index * kAdamChunk, left = plan.tensors[chunk.tensor].count - from;
         const uint32_t n = left < kAdamChunk ? (uint32_t)left : kAdamChunk;
-        constexpr uint32_t kLoads = kAdamChunk / kStep;
         float x[kLoads][kPerLane];
 #pragma unroll
         for (uint32_t u = 0; u < kLoads; ++u) {
@@ -83,51 +82,43 @@ __global__ __launch_bounds__(kAdamGroup) void k_adamw_norm(AdamPlan plan, AdamGr
     sum = wave_sum(sum);
     if ((tid & 63u) == 0) sums[tid >> 6] = sum;
     __syncthreads();
-    if (tid == 0) {
-        plan.partial[first_chunk + blockIdx.x] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
-        __threadfence();
-        is_last = atomicAdd(plan.arrived, 1u) + 1u == all_chunks;
-    }
-    __syncthreads();
-    if (!is_last) return;
-    // the last work-group adds up all sums, in an order that does not depend on which one it is
-    __threadfence();
+    if (tid == 0) plan.partial[first_sum + blockIdx.x] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+}
+
+// The 2-norm from the sums of squares, by every work-group of the step for itself: in 64 bits, in an order that all share.
+__device__ __forceinline__ float norm_of(const float* partial, uint32_t n, double* total) {
+    const uint32_t tid = threadIdx.x;
     double all = 0.0;
-    for (uint32_t i = 0; i < all_chunks; i += 8 * kAdamGroup) {
-        float x[8];
+    for (uint32_t i = 0; i < n; i += 4 * kAdamGroup) {
+        float x[4];
 #pragma unroll
-        for (uint32_t u = 0; u < 8; ++u) {
-            const uint32_t j = i + u * kAdamGroup + tid;
-            x[u] = j < all_chunks ? __hip_atomic_load(&plan.partial[j], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0f;
-        }
+        for (uint32_t u = 0; u < 4; ++u) x[u] = i + u * kAdamGroup + tid < n ? partial[i + u * kAdamGroup + tid] : 0.0f;
 #pragma unroll
-        for (uint32_t u = 0; u < 8; ++u) all += (double)x[u];
+        for (uint32_t u = 0; u < 4; ++u) all += (double)x[u];
     }
 #pragma unroll
     for (int d = 32; d; d >>= 1) all += __shfl_xor(all, d, 64);
     if ((tid & 63u) == 0) total[tid >> 6] = all;
     __syncthreads();
-    if (tid == 0) {
-        const float norm = (float)sqrt((total[0] + total[1]) + (total[2] + total[3]));
-        plan.norm[0] = norm;
-        plan.norm[1] = norm > s.max_norm ? s.max_norm / norm : 1.0f;
-        if (norm_out) *norm_out = norm;
-        *plan.arrived = 0;
-    }
+    return (float)sqrt((total[0] + total[1]) + (total[2] + total[3]));
 }
 
 template <class P, class G, int BITS, bool CLIP>
-__global__ __launch_bounds__(kAdamGroup) void k_adamw(AdamPlan plan, AdamGrads grads, uint32_t first_tensor, uint32_t first_chunk, AdamScalars s) {
+__global__ __launch_bounds__(kAdamGroup) void k_adamw(AdamPlan plan, AdamGrads grads, uint32_t first_tensor, uint32_t first_chunk, AdamScalars s,
+                                                      float* norm_out) {
     constexpr bool kMaster = sizeof(typename P::raw) == 2;
+    float clip = 1.0f;
+    if (CLIP) {
+        __shared__ double total[kAdamGroup / 64];
+        const float norm = norm_of(plan.partial, s.partials, total);
+        if (norm_out && first_chunk + blockIdx.x == 0 && threadIdx.x == 0) *norm_out = norm;
+        if (!(norm < __builtin_inff())) return;
+        clip = norm > s.max_norm ? s.max_norm / norm : 1.0f;
+    }
     const AdamChunk chunk = plan.chunks[first_chunk + blockIdx.x];
     const typename G::raw* g = static_cast<const typename G::raw*>(grads.at[chunk.tensor - first_tensor]);
     if (!g) return;
     const AdamTensor t = plan.tensors[chunk.tensor];
-    float clip = 1.0f;
-    if (CLIP) {
-        if (!(fabsf(plan.norm[0]) < __builtin_inff())) return;
-        clip = plan.norm[1];
-    }
     const float keep = (float)(1.0 - s.lr * t.lr_scale * t.weight_decay), step_size = (float)(s.step_size * t.lr_scale);
     const uint64_t from = (uint64_t)chunk.index * kAdamChunk, left = t.count - from;
     const uint32_t n = left < kAdamChunk ? (uint32_t)left : kAdamChunk;
@@ -237,50 +228,54 @@ __global__ __launch_bounds__(256) void k_adamw_read(AdamPlan plan, uint64_t bloc
 }
 
 template <class G>
-void norm(const AdamPlan& p, const AdamGrads& g, uint32_t first_tensor, uint32_t first_chunk, uint32_t chunks, uint32_t all, const AdamScalars& s, float* out, hipStream_t stream) {
-    hipLaunchKernelGGL((k_adamw_norm<G>), dim3(chunks), dim3(kAdamGroup), 0, stream, p, g, first_tensor, first_chunk, all, s, out);
+void norm(const AdamPlan& p, const AdamGrads& g, uint32_t first_tensor, uint32_t first_chunk, uint32_t chunks, uint32_t first_sum, uint32_t groups, const AdamScalars& s,
+          hipStream_t stream) {
+    hipLaunchKernelGGL((k_adamw_norm<G>), dim3(groups), dim3(kAdamGroup), 0, stream, p, g, first_tensor, first_chunk, chunks, first_sum, s);
 }
 
 template <class P, class G, int BITS>
-void step(const AdamPlan& p, const AdamGrads& g, uint32_t first_tensor, uint32_t first_chunk, uint32_t chunks, bool clipped, const AdamScalars& s, hipStream_t stream) {
+void step(const AdamPlan& p, const AdamGrads& g, uint32_t first_tensor, uint32_t first_chunk, uint32_t chunks, bool clipped, const AdamScalars& s, float* norm_out,
+          hipStream_t stream) {
     if (clipped)
-        hipLaunchKernelGGL((k_adamw<P, G, BITS, true>), dim3(chunks), dim3(kAdamGroup), 0, stream, p, g, first_tensor, first_chunk, s);
+        hipLaunchKernelGGL((k_adamw<P, G, BITS, true>), dim3(chunks), dim3(kAdamGroup), 0, stream, p, g, first_tensor, first_chunk, s, norm_out);
     else
-        hipLaunchKernelGGL((k_adamw<P, G, BITS, false>), dim3(chunks), dim3(kAdamGroup), 0, stream, p, g, first_tensor, first_chunk, s);
+        hipLaunchKernelGGL((k_adamw<P, G, BITS, false>), dim3(chunks), dim3(kAdamGroup), 0, stream, p, g, first_tensor, first_chunk, s, norm_out);
 }
 template <class P, class G>
-void step(int32_t bits, const AdamPlan& p, const AdamGrads& g, uint32_t first_tensor, uint32_t first_chunk, uint32_t chunks, bool clipped, const AdamScalars& s, hipStream_t stream) {
+void step(int32_t bits, const AdamPlan& p, const AdamGrads& g, uint32_t first_tensor, uint32_t first_chunk, uint32_t chunks, bool clipped, const AdamScalars& s, float* norm_out,
+          hipStream_t stream) {
     if (bits == 32)
-        step<P, G, 32>(p, g, first_tensor, first_chunk, chunks, clipped, s, stream);
+        step<P, G, 32>(p, g, first_tensor, first_chunk, chunks, clipped, s, norm_out, stream);
     else
-        step<P, G, 8>(p, g, first_tensor, first_chunk, chunks, clipped, s, stream);
+        step<P, G, 8>(p, g, first_tensor, first_chunk, chunks, clipped, s, norm_out, stream);
 }
 
 }  // namespace
 
 hipError_t launch_adamw_norm(int32_t grad_dtype, const AdamPlan& p, const AdamGrads& g, uint32_t first_tensor, uint32_t first_chunk, uint32_t chunks,
-                             uint32_t all_chunks, const AdamScalars& s, float* norm_out, hipStream_t stream) {
+                             uint32_t first_sum, uint32_t groups, const AdamScalars& s, hipStream_t stream) {
     if (grad_dtype == BPS_F32)
-        norm<F32>(p, g, first_tensor, first_chunk, chunks, all_chunks, s, norm_out, stream);
+        norm<F32>(p, g, first_tensor, first_chunk, chunks, first_sum, groups, s, stream);
     else if (grad_dtype == BPS_BF16)
-        norm<Bf16>(p, g, first_tensor, first_chunk, chunks, all_chunks, s, norm_out, stream);
+        norm<Bf16>(p, g, first_tensor, first_chunk, chunks, first_sum, groups, s, stream);
     else
-        norm<F16>(p, g, first_tensor, first_chunk, chunks, all_chunks, s, norm_out, stream);
+        norm<F16>(p, g, first_tensor, first_chunk, chunks, first_sum, groups, s, stream);
     return hipGetLastError();
 }
 
 hipError_t launch_adamw_step(int32_t param_dtype, int32_t grad_dtype, int32_t state_bits, const AdamPlan& p, const AdamGrads& g, uint32_t first_tensor,
-                             uint32_t first_chunk, uint32_t chunks, bool clipped, const AdamScalars& s, hipStream_t stream) {
+                             uint32_t first_chunk, uint32_t chunks, bool clipped, const AdamScalars& s, float* norm_out,
+          hipStream_t stream) {
     if (param_dtype == BPS_F32)
-        step<F32, F32>(state_bits, p, g, first_tensor, first_chunk, chunks, clipped, s, stream);
+        step<F32, F32>(state_bits, p, g, first_tensor, first_chunk, chunks, clipped, s, norm_out, stream);
     else if (param_dtype == BPS_BF16 && grad_dtype == BPS_BF16)
-        step<Bf16, Bf16>(state_bits, p, g, first_tensor, first_chunk, chunks, clipped, s, stream);
+        step<Bf16, Bf16>(state_bits, p, g, first_tensor, first_chunk, chunks, clipped, s, norm_out, stream);
     else if (param_dtype == BPS_BF16)
-        step<Bf16, F32>(state_bits, p, g, first_tensor, first_chunk, chunks, clipped, s, stream);
+        step<Bf16, F32>(state_bits, p, g, first_tensor, first_chunk, chunks, clipped, s, norm_out, stream);
     else if (grad_dtype == BPS_F16)
-        step<F16, F16>(state_bits, p, g, first_tensor, first_chunk, chunks, clipped, s, stream);
+        step<F16, F16>(state_bits, p, g, first_tensor, first_chunk, chunks, clipped, s, norm_out, stream);
     else
-        step<F16, F32>(state_bits, p, g, first_tensor, first_chunk, chunks, clipped, s, stream);
+        step<F16, F32>(state_bits, p, g, first_tensor, first_chunk, chunks, clipped, s, norm_out, stream);
     return hipGetLastError();
 }
 

@@ -37,7 +37,8 @@ bps_status check_scores(const char* what, const void* logits, int32_t dtype, uin
 struct bps_adamw {
     int device = 0;
     int32_t param_dtype = 0, state_bits = 0;
-    uint32_t seed = 0, all_chunks = 0;
+    uint32_t seed = 0;
+    uint32_t sums = 0;                     // sums of squares that a launch leaves at most
     uint64_t total = 0;
     std::vector<uint32_t> first_chunk;     // of each tensor, and behind the last
     void* block = nullptr;                 // one allocation: tensors, chunks, sums
@@ -156,7 +157,8 @@ bps_status bps_adamw_create(const bps_adamw_config* cfg, bps_adamw** out) {
         h->state_bits = cfg->state_bits;
         h->seed = cfg->seed;
         h->total = cfg->total;
-        h->all_chunks = (uint32_t)chunks;
+        const uint32_t launches = (cfg->tensors + bps::kAdamGrads - 1) / bps::kAdamGrads;
+        h->sums = launches <= bps::kAdamSums / 64 ? bps::kAdamSums / launches : 64;
         std::vector<bps::AdamTensor> tensors(cfg->tensors);
         std::vector<bps::AdamChunk> list;
         list.reserve(chunks);
@@ -168,24 +170,21 @@ bps_status bps_adamw_create(const bps_adamw_config* cfg, bps_adamw** out) {
             for (uint64_t c = 0; c * bps::kAdamChunk < t.count; ++c) list.push_back({i, (uint32_t)c});
         }
         h->first_chunk.push_back((uint32_t)list.size());
-        // tensors | chunks | sums | norm, clip, arrived
+        // tensors | chunks | sums
         const size_t at_chunks = tensors.size() * sizeof(tensors[0]), at_sums = at_chunks + list.size() * sizeof(list[0]);
-        const size_t at_norm = at_sums + (chunks * sizeof(float) + 15) / 16 * 16, bytes = at_norm + 16;
+        const size_t bytes = at_sums + (size_t)launches * h->sums * sizeof(float);
         hipError_t e = hipMalloc(&h->block, bytes);
         if (e != hipSuccess) return fail_here(e == hipErrorOutOfMemory ? BPS_ERR_OOM : BPS_ERR_HIP, "%s: hipMalloc(%zu): %s", what, bytes, hipGetErrorString(e));
         char* b = static_cast<char*>(h->block);
-        const uint32_t zeros[4] = {0, 0, 0, 0};
         e = hipMemcpy(b, tensors.data(), at_chunks, hipMemcpyHostToDevice);
         if (e == hipSuccess) e = hipMemcpy(b + at_chunks, list.data(), list.size() * sizeof(list[0]), hipMemcpyHostToDevice);
-        if (e == hipSuccess) e = hipMemcpy(b + at_norm, zeros, sizeof(zeros), hipMemcpyHostToDevice);
         if (e == hipSuccess) e = hipDeviceSynchronize();
         if (e != hipSuccess) {
             hipFree(h->block);
             return launched(what, e);
         }
-        float* norm = reinterpret_cast<float*>(b + at_norm);
         h->plan = {reinterpret_cast<bps::AdamTensor*>(b), reinterpret_cast<bps::AdamChunk*>(b + at_chunks), cfg->exp_avg, cfg->exp_avg_sq, cfg->exp_avg_exponent,
-                   cfg->exp_avg_sq_exponent, reinterpret_cast<float*>(b + at_sums), reinterpret_cast<uint32_t*>(norm + 2), norm};
+                   cfg->exp_avg_sq_exponent, reinterpret_cast<float*>(b + at_sums)};
         *out = h.release();
         return BPS_OK;
     } catch (const std::bad_alloc&) {
@@ -230,15 +229,21 @@ bps_status bps_adamw_step(bps_adamw* h, const void* const* grads, int32_t grad_d
     s.max_norm = (float)max_norm;
     s.key = bps::mixed(h->seed + (uint32_t)step * bps::kGolden);
     const bool clipped = max_norm > 0.0;
+    // the sums of squares of all gradients first, then the step
     bps::AdamGrads g;
     for (int pass = clipped ? 0 : 1; pass < 2; ++pass)
         for (uint32_t first = 0; first < tensors; first += bps::kAdamGrads) {
             const uint32_t n = tensors - first < bps::kAdamGrads ? tensors - first : bps::kAdamGrads;
             for (uint32_t i = 0; i < bps::kAdamGrads; ++i) g.at[i] = i < n ? grads[first + i] : nullptr;
             const uint32_t chunk = h->first_chunk[first], chunks = h->first_chunk[first + n] - chunk;
-            const hipError_t e = pass == 0 ? bps::launch_adamw_norm(grad_dtype, h->plan, g, first, chunk, chunks, h->all_chunks, s, grad_norm, static_cast<hipStream_t>(stream))
-                                           : bps::launch_adamw_step(h->param_dtype, grad_dtype, h->state_bits, h->plan, g, first, chunk, chunks, clipped, s,
-                                                                    static_cast<hipStream_t>(stream));
+            hipError_t e;
+            if (pass == 0) {
+                const uint32_t groups = chunks < h->sums ? chunks : h->sums;
+                e = bps::launch_adamw_norm(grad_dtype, h->plan, g, first, chunk, chunks, s.partials, groups, s, static_cast<hipStream_t>(stream));
+                s.partials += groups;
+            } else {
+                e = bps::launch_adamw_step(h->param_dtype, grad_dtype, h->state_bits, h->plan, g, first, chunk, chunks, clipped, s, grad_norm, static_cast<hipStream_t>(stream));
+            }
             if (e != hipSuccess) return launched(what, e);
         }
     return BPS_OK;

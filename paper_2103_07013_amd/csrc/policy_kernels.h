@@ -76,6 +76,9 @@ constexpr uint32_t kStateBlock = 256;     // states of a tensor start at a multi
 constexpr uint32_t kAdamGroup = 256;      // threads of a work-group
 constexpr uint32_t kAdamChunk = 4096;     // elements of a work-group
 constexpr uint32_t kAdamGrads = 448;      // gradients of one launch: their addresses travel as kernel arguments
+// Sums of squares of all gradients, in which every work-group of the step finds the norm for itself: a second launch more, or a counter of
+// work-groups with the cache write-backs that it needs (35 us for 5.3e6 parameters), cost more than reading them does (see k_adamw_norm).
+constexpr uint32_t kAdamSums = 1024;
 
 struct AdamTensor {
     void* param;
@@ -95,19 +98,18 @@ struct AdamPlan {             // device memory of a handle
     const AdamChunk* chunks;
     void *exp_avg, *exp_avg_sq;
     uint8_t *exp_avg_exponent, *exp_avg_sq_exponent;
-    float* partial;           // one sum of squares per chunk
-    uint32_t* arrived;        // work-groups whose sum is there, 0 between steps
-    float* norm;              // [0] norm, [1] what gradients are multiplied by
+    float* partial;           // sums of squares
 };
 struct AdamScalars {
     double lr, step_size;     // lr, and lr / (1 - beta1^t)
     float beta1, one_minus_beta1, beta2, one_minus_beta2, root_c2, eps, grad_scale, max_norm;   // root_c2: 1 / sqrt(1 - beta2^t)
     uint32_t key;             // of the dither
+    uint32_t partials;        // sums of squares
 };
 hipError_t launch_adamw_norm(int32_t grad_dtype, const AdamPlan& p, const AdamGrads& g, uint32_t first_tensor, uint32_t first_chunk, uint32_t chunks,
-                             uint32_t all_chunks, const AdamScalars& s, float* norm_out, hipStream_t stream);
+                             uint32_t first_sum, uint32_t groups, const AdamScalars& s, hipStream_t stream);
 hipError_t launch_adamw_step(int32_t param_dtype, int32_t grad_dtype, int32_t state_bits, const AdamPlan& p, const AdamGrads& g, uint32_t first_tensor,
-                             uint32_t first_chunk, uint32_t chunks, bool clipped, const AdamScalars& s, hipStream_t stream);
+                             uint32_t first_chunk, uint32_t chunks, bool clipped, const AdamScalars& s, float* norm_out, hipStream_t stream);
 hipError_t launch_adamw_read(const AdamPlan& p, uint64_t blocks, float* exp_avg, float* exp_avg_sq, hipStream_t stream);
 
 // 32 bits each of which depends on all bits of h; the factors are odd numbers next to 2^32 times the fractional parts

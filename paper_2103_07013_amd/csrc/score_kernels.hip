@@ -33,11 +33,13 @@ __device__ __forceinline__ Part joined(const Part& a, const Part& b, float c) {
     return {m, fmaf(fa, a.z, fb * b.z), fa * fmaf(da, a.z, a.s) + fb * fmaf(db, b.z, b.s)};
 }
 
+// Adds N entries, and returns the largest of them (or the lowest finite value).
 template <int N>
-__device__ __forceinline__ void add(Part& p, const float (&x)[N], float c) {
-    float m = p.m;
+__device__ __forceinline__ float add(Part& p, const float (&x)[N], float c) {
+    float top = kLowest;
 #pragma unroll
-    for (int k = 0; k < N; ++k) m = fmaxf(m, x[k]);
+    for (int k = 0; k < N; ++k) top = fmaxf(top, x[k]);
+    const float m = fmaxf(p.m, top);
     if (m > p.m) {
         const float d = fmaxf((p.m - m) * c, kFar), f = __builtin_amdgcn_exp2f(d);
         p.s = f * fmaf(d, p.z, p.s);
@@ -50,6 +52,7 @@ __device__ __forceinline__ void add(Part& p, const float (&x)[N], float c) {
         p.z += e;
         p.s = fmaf(e, fmaxf(d, kFar), p.s);
     }
+    return top;
 }
 
 // N entries of a row from `at` on; what is masked or behind the row's end is -inf.
@@ -193,11 +196,9 @@ __device__ __forceinline__ uint64_t merged_waves(uint64_t list, uint64_t* held, 
     return list;
 }
 
-// The upper half of an order (see order_of), which the float alone decides, and the float that it stands for; 0 stands for -inf.
+// The upper half of an order (see order_of), which the float alone decides, and the float that it stands for.
 __device__ __forceinline__ uint32_t rank_of(float x) { return (uint32_t)(order_of(x, 0u) >> 32); }
-__device__ __forceinline__ float value_of(uint32_t rank) {
-    return rank == 0u ? -kInf : __uint_as_float((rank & 0x80000000u) ? rank & 0x7FFFFFFFu : ~rank);
-}
+__device__ __forceinline__ float value_of(uint32_t rank) { return __uint_as_float((rank & 0x80000000u) ? rank & 0x7FFFFFFFu : ~rank); }
 
 constexpr uint32_t kWaiting = 128;     // candidates that wait for a sort, per wavefront
 
@@ -205,7 +206,7 @@ struct Best {
     uint64_t list;            // sorted, one per lane
     uint64_t* waiting;        // LDS, kWaiting of this wavefront
     uint32_t count;           // of them, below 64 between calls
-    float least;              // entries below it, or as large and not before least_at, are no candidates
+    float least;              // finite, or NaN, or +inf: entries below it, or as large and behind least_at, are no candidates (nor is -inf ever)
     uint32_t least_at;
 
     __device__ __forceinline__ void raise(float to, uint32_t at) {
@@ -223,7 +224,8 @@ struct Best {
         if (last) raise(value_of((uint32_t)(last >> 32)), ~(uint32_t)last);
     }
     __device__ __forceinline__ void offer(float x, uint32_t at, uint32_t lane, uint32_t k) {
-        const bool is = x > least || (x == least && at < least_at) || x != x;
+        if (!__ballot(!(x < least))) return;
+        const bool is = x > least || (x == least && at <= least_at) || x != x;
         const uint64_t who = __ballot(is);
         if (!who) return;
         if (is) waiting[count + lanes_before(who)] = order_of(x, at);
@@ -259,15 +261,12 @@ __device__ __forceinline__ Part stream(const typename T::raw* row, const uint8_t
 #pragma unroll
             for (int e = 0; e < N; ++e) x[u * N + e] = y[e];
         }
-        add(p, x, c);
+        const float top = add(p, x, c);
         if constexpr (TOP) {
-            float top = -kInf;
-#pragma unroll
-            for (int e = 0; e < U * N; ++e) top = fmaxf(top, x[e]);
             if (first) {
                 // Where at least k lanes' own best reach a bar, the k-th best of all does: the k-th of any wavefront's lanes, and what the
                 // k / WAVES best lanes of every wavefront reach.
-                const uint32_t own = sorted(top != -kInf ? rank_of(top) : 0u, lane);
+                const uint32_t own = sorted(rank_of(top), lane);
                 uint32_t bar = __shfl(own, (int)k - 1, 64);
                 if constexpr (WAVES > 1) {
                     const uint32_t all = __shfl(own, (int)((k + WAVES - 1) / WAVES) - 1, 64);
@@ -285,10 +284,9 @@ __device__ __forceinline__ Part stream(const typename T::raw* row, const uint8_t
                     bar = least > bar ? least : bar;
                 }
                 best.least = value_of(bar);
-                best.least_at = bar ? 0xFFFFFFFFu : 0u;
                 first = false;
             }
-            if (__ballot((top >= best.least && top != -kInf) || p.z != p.z)) {
+            if (__ballot(top >= best.least || p.z != p.z)) {
 #pragma unroll
                 for (int e = 0; e < U * N; ++e) best.offer(x[e], base + ((e / N) * kThreads + tid) * N + e % N, lane, k);
             }
@@ -310,7 +308,7 @@ __global__ __launch_bounds__(WAVES > 4 ? WAVES * 64 : 256) void k_score(ScoreArg
     if (r >= a.rows) return;        // whole wavefronts, and where they share a row whole work-groups
     const typename T::raw* row = static_cast<const typename T::raw*>(a.logits) + (int64_t)r * a.row_stride;
     const uint8_t* mask = MASK ? a.mask + (int64_t)r * a.mask_stride : nullptr;
-    Best best = {0, waiting + (TOP ? wave * kWaiting : 0), 0, -kInf, 0};
+    Best best = {0, waiting + (TOP ? wave * kWaiting : 0), 0, kLowest, 0xFFFFFFFFu};
     Part p = stream<T, MASK, TOP, WAVES>(row, mask, 0, a.entries, threadIdx.x % (64 * WAVES), c, best, a.top_k, bars);
     p = group_part<64>(p, c);
     if constexpr (TOP) best.finish(lane, a.top_k);
@@ -350,7 +348,7 @@ __global__ __launch_bounds__(256) void k_score_piece(ScoreArgs a, Pieces pieces,
     const float c = a.scale * kLog2e;
     const typename T::raw* row = static_cast<const typename T::raw*>(a.logits) + (int64_t)r * a.row_stride;
     const uint8_t* mask = MASK ? a.mask + (int64_t)r * a.mask_stride : nullptr;
-    Best best = {0, waiting + (TOP ? wave * kWaiting : 0), 0, -kInf, 0};
+    Best best = {0, waiting + (TOP ? wave * kWaiting : 0), 0, kLowest, 0xFFFFFFFFu};
     Part p = stream<T, MASK, TOP, 4>(row, mask, from, to, threadIdx.x, c, best, a.top_k, bars);
     p = group_part<64>(p, c);
     if constexpr (TOP) best.finish(lane, a.top_k);
@@ -466,21 +464,26 @@ __global__ __launch_bounds__(GROUP) void k_score_grad(ScoreGradArgs a, uint32_t 
 
 // ---- which kernel
 
-// Rows of up to this many entries are shared by few lanes (see below), longer ones by a wavefront at least.
+// Rows of up to this many entries are shared by few lanes, longer ones by a wavefront at least.
 constexpr uint32_t kShort = 128;
-// Rows of up to kWaveRow entries have one wavefront.
-constexpr uint32_t kWaveRow = 2048;
-constexpr uint32_t kComputeUnits = 256;
+// Rows of up to kWaveRow entries have one wavefront, where there are kWaveRows rows or more those of up to kLongWaveRow too.  Measured
+// with bf16, one wavefront / four: 4096 x 2048 6.4 / 14.8 us, 4096 x 4096 9.8 / 15.1, 4096 x 8192 17.4 / 18.3, 512 x 4096 5.3 / 5.2, 1024 x 8192 8.7 / 6.4.
+constexpr uint32_t kWaveRow = 2048, kLongWaveRow = 8192, kWaveRows = 2048;
+// Longer ones have four wavefronts, or sixteen where they are longer than kLongWaveRow and fewer than kFewRows.  Four / sixteen:
+// 64 x 8192 4.2 / 6.3 us, 1 x 32768 7.1 / 5.6, 192 x 50257 11.4 / 9.7, 512 x 131072 35.3 / 27.2, 1024 x 50257 24.1 / 27.5.
+constexpr uint32_t kFewRows = 1024;
+// Of up to kPieceRows rows, those longer than kLongRow are cut, so that there are about kGroups pieces of not less than 4096 entries.
+// Sixteen wavefronts / pieces: 1 x 32768 5.6 / 5.9 us, 1 x 131072 12.0 / 6.1, 32 x 131072 12.5 / 7.1, 64 x 50257 9.5 / 7.4, 128 x 50257 9.6 / 8.9 (with
+// 20 alternatives 18.4 / 19.4), 192 x 50257 9.7 / 10.5.
+constexpr uint32_t kPieceRows = 64, kLongRow = 32768, kGroups = 512;
 
-// How many pieces a row is cut into: where there is not a work-group of whole rows for each compute unit, but never below 4096 entries.
 Pieces pieces_of(uint64_t rows, uint32_t entries) {
-    if (entries <= 2 * 4096 || rows >= kComputeUnits) return {1, entries};
-    uint64_t n = (2 * kComputeUnits + rows - 1) / rows;
-    const uint32_t most = (entries + 4095) / 4096;
+    if (entries <= kLongRow || rows > kPieceRows || rows == 0) return {1, entries};
+    uint32_t n = kGroups / (uint32_t)rows;
+    const uint32_t most = entries / 4096;
     if (n > most) n = most;
     if (n > kMaxPieces) n = kMaxPieces;
-    uint32_t length = (uint32_t)((entries + n - 1) / n);
-    length = (length + 63) / 64 * 64;
+    const uint32_t length = ((entries + n - 1) / n + 63) / 64 * 64;
     return {(entries + length - 1) / length, length};
 }
 
@@ -502,9 +505,9 @@ hipError_t score(const ScoreArgs& a, hipStream_t stream) {
         uint64_t* lists = reinterpret_cast<uint64_t*>(sums + a.rows * pieces.count);
         hipLaunchKernelGGL((k_score_piece<T, MASK, TOP>), dim3((uint32_t)(a.rows * pieces.count)), dim3(256), 0, stream, a, pieces, sums, lists);
         hipLaunchKernelGGL((k_score_join<T, TOP>), dim3((uint32_t)a.rows), dim3(TOP ? 1024 : 64), 0, stream, a, pieces, sums, lists);
-    } else if (a.entries <= kWaveRow) {
+    } else if (a.entries <= (a.rows < kWaveRows ? kWaveRow : kLongWaveRow)) {
         BPS_ROWS(k_score, 4, 256, TOP, 1);
-    } else if (a.rows >= 2 * kComputeUnits) {
+    } else if (a.entries <= kLongWaveRow || a.rows >= kFewRows) {
         BPS_ROWS(k_score, 1, 256, TOP, 4);
     } else {
         BPS_ROWS(k_score, 1, 1024, TOP, 16);
