@@ -13,37 +13,32 @@ constexpr uint32_t kPerLane = 4, kStep = kAdamGroup * kPerLane;
 static_assert(kStateBlock == 64 * kPerLane, "a wavefront's elements share an exponent");
 static_assert(kAdamChunk % kStep == 0, "a chunk is whole steps");
 
-__device__ __forceinline__ float power(uint32_t biased) { return __uint_as_float(biased << 23); }
-
-// what an 8-bit code of exponent field and 3 mantissa bits stands for; e: the block's exponent byte
+// 8-bit codes are the upper bits of a float32 with a bias of their own: shifted to where those are, subnormal ones included, a code is a float that
+// is a power of two away from what it stands for.  e: the block's exponent byte.
 template <int TOP>
 __device__ __forceinline__ float decoded(uint32_t code, uint32_t e) {
-    const uint32_t field = code >> 3 > 1u ? code >> 3 : 1u;
-    return e == 255u ? __builtin_nanf("") : (float)(code - 8u * (field - 1u)) * power(e - TOP + field - 3u);
+    return __builtin_amdgcn_ldexpf(__uint_as_float(code << 20), (int)e - TOP);
 }
 
-// the block's exponent byte for the largest magnitude's bits: the least that holds it
+// the exponent byte for a magnitude's bits: the least that holds it
 template <uint32_t LEAST>
-__device__ __forceinline__ uint32_t exponent_for(uint32_t largest) {
-    const uint32_t e = (largest + 0x0FFFFFu) >> 23;
+__device__ __forceinline__ uint32_t exponent_for(uint32_t magnitude) {
+    const uint32_t e = (magnitude + 0x0FFFFFu) >> 23;
     return e < LEAST ? LEAST : e > 255u ? 255u : e;
 }
 
+// The other way: the code's place is above 20 bits, to which 20 bits of dither (a 16-bit number, times 16) are added before they are cut off.
 template <int TOP>
-__device__ __forceinline__ uint32_t encoded(float magnitude, uint32_t e, float dither) {
-    if (e == 255u) return 0u;
-    const int f = (int)(__float_as_uint(magnitude) >> 23) - (int)e + TOP;
-    const uint32_t field = f > 1 ? (uint32_t)f : 1u;
-    return 8u * (field - 1u) + (uint32_t)(magnitude * power(254u - (e - TOP + field - 3u)) + dither);
+__device__ __forceinline__ uint32_t encoded(float magnitude, uint32_t e, uint32_t dither) {
+    return (__float_as_uint(__builtin_amdgcn_ldexpf(magnitude, TOP - (int)e)) + (dither << 4)) >> 20;
 }
 
-__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
-#pragma unroll
-    for (int d = 32; d; d >>= 1) {
-        const uint32_t y = __shfl_xor(x, d, 64);
-        x = y > x ? y : x;
-    }
-    return x;
+// The larger of both halves over the wavefront, in all lanes.
+__device__ __forceinline__ uint32_t wave_max_of_halves(uint32_t x) {
+    typedef uint16_t halves __attribute__((ext_vector_type(2)));
+    return group_reduce<64>(x, [](uint32_t a, uint32_t b) {
+        return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(halves, a), __builtin_bit_cast(halves, b)));
+    });
 }
 
 // Sums of squares: each work-group those of every gridDim.x-th chunk.
@@ -146,14 +141,26 @@ __global__ __launch_bounds__(kAdamGroup) void k_adamw(AdamPlan plan, AdamGrads g
         } else {
             code_m = *reinterpret_cast<const uint32_t*>(static_cast<uint8_t*>(plan.exp_avg) + state);
             code_v = *reinterpret_cast<const uint32_t*>(static_cast<uint8_t*>(plan.exp_avg_sq) + state);
-            const uint32_t em = plan.exp_avg_exponent[state / kStateBlock], ev = plan.exp_avg_sq_exponent[state / kStateBlock];
+            // one block for the whole wavefront
+            const uint32_t em = __builtin_amdgcn_readfirstlane(plan.exp_avg_exponent[state / kStateBlock]);
+            const uint32_t ev = __builtin_amdgcn_readfirstlane(plan.exp_avg_sq_exponent[state / kStateBlock]);
 #pragma unroll
             for (uint32_t k = 0; k < kPerLane; ++k) {
                 const uint32_t cm = code_m >> (8 * k) & 255u, cv = code_v >> (8 * k) & 255u;
-                m[k] = decoded<15>(cm & 127u, em);
-                m[k] = cm & 128u ? -m[k] : m[k];
+                m[k] = __uint_as_float(__float_as_uint(decoded<15>(cm & 127u, em)) | (cm & 128u) << 24);
                 v[k] = decoded<31>(cv, ev);
-                if (k >= live) m[k] = v[k] = 0.0f;      // behind the tensor's end: no part of the block's largest
+            }
+            if (em == 255u || ev == 255u) {
+#pragma unroll
+                for (uint32_t k = 0; k < kPerLane; ++k) {
+                    if (em == 255u) m[k] = __builtin_nanf("");
+                    if (ev == 255u) v[k] = __builtin_nanf("");
+                }
+            }
+            if (live != kPerLane) {      // behind the tensor's end: no part of the block's largest
+#pragma unroll
+                for (uint32_t k = 0; k < kPerLane; ++k)
+                    if (k >= live) m[k] = v[k] = 0.0f;
             }
         }
 #pragma unroll
@@ -188,16 +195,17 @@ __global__ __launch_bounds__(kAdamGroup) void k_adamw(AdamPlan plan, AdamGrads g
                 largest_m = bm > largest_m ? bm : largest_m;
                 largest_v = bv > largest_v ? bv : largest_v;
             }
-            const uint32_t em = exponent_for<20>(wave_max(largest_m)), ev = exponent_for<36>(wave_max(largest_v));
+            const uint32_t both = __builtin_amdgcn_readfirstlane(wave_max_of_halves(exponent_for<20>(largest_m) | exponent_for<36>(largest_v) << 16));
+            const uint32_t em = both & 0xFFFFu, ev = both >> 16;
             code_m = code_v = 0;
 #pragma unroll
             for (uint32_t k = 0; k < kPerLane; ++k) {
                 const uint32_t h = mixed(((uint32_t)(state + k) * kGolden) ^ s.key);
-                const uint32_t cm = encoded<15>(fabsf(m[k]), em, (float)(h & 0xFFFFu) * 0x1p-16f) | (m[k] < 0.0f ? 128u : 0u);
-                const uint32_t cv = encoded<31>(v[k], ev, (float)(h >> 16) * 0x1p-16f);
-                code_m |= cm << (8 * k);
-                code_v |= cv << (8 * k);
+                code_m |= (encoded<15>(fabsf(m[k]), em, h & 0xFFFFu) | (m[k] < 0.0f ? 128u : 0u)) << (8 * k);
+                code_v |= encoded<31>(v[k], ev, h >> 16) << (8 * k);
             }
+            if (em == 255u) code_m = 0;
+            if (ev == 255u) code_v = 0;
             *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(plan.exp_avg) + state) = code_m;
             *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(plan.exp_avg_sq) + state) = code_v;
             if ((threadIdx.x & 63u) == 0) {
@@ -218,9 +226,9 @@ __global__ __launch_bounds__(256) void k_adamw_read(AdamPlan plan, uint64_t bloc
 #pragma unroll
         for (uint32_t k = 0; k < kPerLane; ++k) {
             const uint32_t cm = code_m >> (8 * k) & 255u;
-            m[k] = decoded<15>(cm & 127u, em);
-            m[k] = cm & 128u ? -m[k] : m[k];
-            v[k] = decoded<31>(code_v >> (8 * k) & 255u, ev);
+            const float x = decoded<15>(cm & 127u, em), y = decoded<31>(code_v >> (8 * k) & 255u, ev);
+            m[k] = em == 255u ? __builtin_nanf("") : cm & 128u ? -x : x;
+            v[k] = ev == 255u ? __builtin_nanf("") : y;
         }
         store<F32, kPerLane>(exp_avg + at, m);
         store<F32, kPerLane>(exp_avg_sq + at, v);

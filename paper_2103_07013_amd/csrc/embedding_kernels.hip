@@ -323,11 +323,12 @@ __global__ __launch_bounds__(256) void k_embed(EmbedArgs a) {
 
 // ---- gradient
 
-// Tokens of a piece: 64, more where there would be more than kMaxPieces pieces.
+// Tokens of a piece: about count / 2048, so that there are pieces for all compute units, but no fewer than 8, to keep partial sums few, and from
+// 64 on as many as kMaxPieces allow.
 constexpr uint32_t kPiece = 64, kMaxPieces = 4096;
 uint32_t piece_length(uint32_t count) {
-    uint32_t n = kPiece;
-    while ((count + (uint64_t)n - 1) / n > kMaxPieces) n *= 2;
+    uint32_t n = 8;
+    while ((count + (uint64_t)n - 1) / n > (n < kPiece ? kMaxPieces / 2 : kMaxPieces)) n *= 2;
     return n;
 }
 

@@ -156,19 +156,18 @@ __global__ __launch_bounds__(256) void k_score_short(ScoreArgs a) {
 
 // The best 64 of what a wavefront has seen, one in each lane in descending order; 0 = none.
 // A bitonic network: halves that are sorted are joined by a comparison with the mirrored lane, then with lanes at falling distances.
-template <int X, class V>
-__device__ __forceinline__ V exchanged(V v, bool keep_larger) {
-    const V o = bps::from_lane_xor<X>(v);
+template <int X>
+__device__ __forceinline__ uint64_t exchanged(uint64_t v, bool keep_larger) {
+    const uint64_t o = bps::from_lane_xor<X>(v);
     return (o > v) == keep_larger ? o : v;
 }
-template <int X, class V>
-__device__ __forceinline__ V settled(V v, uint32_t lane) {      // comparisons at the distances X, X / 2 .. 1
+template <int X>
+__device__ __forceinline__ uint64_t settled(uint64_t v, uint32_t lane) {      // comparisons at the distances X, X / 2 .. 1
     v = exchanged<X>(v, (lane & X) == 0);
     if constexpr (X > 1) v = settled<X / 2>(v, lane);
     return v;
 }
-template <class V>
-__device__ __forceinline__ V sorted(V v, uint32_t lane) {
+__device__ __forceinline__ uint64_t sorted(uint64_t v, uint32_t lane) {
     v = exchanged<1>(v, (lane & 1) == 0);
     v = settled<1>(exchanged<3>(v, (lane & 2) == 0), lane);
     v = settled<2>(exchanged<7>(v, (lane & 4) == 0), lane);
@@ -196,16 +195,29 @@ __device__ __forceinline__ uint64_t merged_waves(uint64_t list, uint64_t* held, 
     return list;
 }
 
+// A number that k of the wavefront's reach, and no more than the k-th largest's upper 16 bits are above it.
+__device__ __forceinline__ uint32_t reached_by(uint32_t v, uint32_t k) {
+    uint32_t bar = 0;
+#pragma unroll
+    for (int b = 31; b >= 16; --b) {
+        const uint32_t trial = bar | 1u << b;
+        bar = (uint32_t)__popcll(__ballot(v >= trial)) >= k ? trial : bar;
+    }
+    return bar;
+}
+
 // The upper half of an order (see order_of), which the float alone decides, and the float that it stands for.
 __device__ __forceinline__ uint32_t rank_of(float x) { return (uint32_t)(order_of(x, 0u) >> 32); }
-__device__ __forceinline__ float value_of(uint32_t rank) { return __uint_as_float((rank & 0x80000000u) ? rank & 0x7FFFFFFFu : ~rank); }
+__device__ __forceinline__ float value_of(uint32_t rank) { return rank < 0x00800000u ? kLowest : __uint_as_float((rank & 0x80000000u) ? rank & 0x7FFFFFFFu : ~rank); }
 
 constexpr uint32_t kWaiting = 128;     // candidates that wait for a sort, per wavefront
+constexpr uint32_t kCounted = 40;      // up to so many are put in order by counting
 
 struct Best {
     uint64_t list;            // sorted, one per lane
     uint64_t* waiting;        // LDS, kWaiting of this wavefront
     uint32_t count;           // of them, below 64 between calls
+    bool any;                 // in the list
     float least;              // finite, or NaN, or +inf: entries below it, or as large and behind least_at, are no candidates (nor is -inf ever)
     uint32_t least_at;
 
@@ -218,24 +230,53 @@ struct Best {
     __device__ __forceinline__ void take_in(uint32_t lane, uint32_t k, uint32_t n) {
         // the wavefront's own stores, in order before its loads
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        const uint64_t v = lane < n ? waiting[lane] : 0;
-        list = merged(list, sorted(v, lane), lane);
+        uint64_t v = lane < n ? waiting[lane] : 0;
+        if (n <= kCounted) {
+            // few: each goes where the number of larger ones says
+            uint32_t larger = 0;
+            for (uint32_t j = 0; j < n; ++j) {
+                const uint64_t o = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), (int)j) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, (int)j);
+                larger += o > v ? 1u : 0u;
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            if (lane < n) waiting[larger] = v;
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            v = lane < n ? waiting[lane] : 0;
+        } else {
+            v = sorted(v, lane);
+        }
+        list = any ? merged(list, v, lane) : v;
+        any = true;
         const uint64_t last = __shfl((unsigned long long)list, (int)k - 1, 64);
         if (last) raise(value_of((uint32_t)(last >> 32)), ~(uint32_t)last);
     }
-    __device__ __forceinline__ void offer(float x, uint32_t at, uint32_t lane, uint32_t k) {
-        if (!__ballot(!(x < least))) return;
-        const bool is = x > least || (x == least && at <= least_at) || x != x;
-        const uint64_t who = __ballot(is);
-        if (!who) return;
-        if (is) waiting[count + lanes_before(who)] = order_of(x, at);
-        count += (uint32_t)__popcll(who);
-        if (count >= 64) {
-            take_in(lane, k, 64);
-            count -= 64;
-            const uint64_t v = waiting[64 + lane];
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            if (lane < count) waiting[lane] = v;
+    // Entries base + place(e); most wavefronts hold few candidates or none, so that each lane's are told first and then taken one
+    // at a time.
+    template <int N, class Place>
+    __device__ __forceinline__ void offer(const float (&x)[N], uint32_t lane, uint32_t k, Place&& place) {
+        uint32_t hit = 0;
+#pragma unroll
+        for (int e = 0; e < N; ++e) hit += hit + (x[e] < least ? 0u : 1u);
+        hit <<= 32 - N;
+        while (__ballot(hit != 0)) {
+            const uint32_t e = (uint32_t)__builtin_clz(hit | 1u);
+            float y = x[0];
+#pragma unroll
+            for (int j = 1; j < N; ++j) y = e == (uint32_t)j ? x[j] : y;
+            const uint32_t at = place(e);
+            const bool is = hit != 0 && (y > least || (y == least && at <= least_at) || y != y);
+            hit &= 0x7FFFFFFFu >> e;
+            const uint64_t who = __ballot(is);
+            if (!who) continue;
+            if (is) waiting[count + lanes_before(who)] = order_of(y, at);
+            count += (uint32_t)__popcll(who);
+            if (count >= 64) {
+                take_in(lane, k, 64);
+                count -= 64;
+                const uint64_t v = waiting[64 + lane];
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                if (lane < count) waiting[lane] = v;
+            }
         }
     }
     __device__ __forceinline__ void finish(uint32_t lane, uint32_t k) {
@@ -266,10 +307,10 @@ __device__ __forceinline__ Part stream(const typename T::raw* row, const uint8_t
             if (first) {
                 // Where at least k lanes' own best reach a bar, the k-th best of all does: the k-th of any wavefront's lanes, and what the
                 // k / WAVES best lanes of every wavefront reach.
-                const uint32_t own = sorted(rank_of(top), lane);
-                uint32_t bar = __shfl(own, (int)k - 1, 64);
+                const uint32_t own = rank_of(top);
+                uint32_t bar = reached_by(own, k);
                 if constexpr (WAVES > 1) {
-                    const uint32_t all = __shfl(own, (int)((k + WAVES - 1) / WAVES) - 1, 64);
+                    const uint32_t all = reached_by(own, (k + WAVES - 1) / WAVES);
                     if (lane == 0) {
                         bars[wave] = bar;
                         bars[WAVES + wave] = all;
@@ -286,10 +327,8 @@ __device__ __forceinline__ Part stream(const typename T::raw* row, const uint8_t
                 best.least = value_of(bar);
                 first = false;
             }
-            if (__ballot(top >= best.least || p.z != p.z)) {
-#pragma unroll
-                for (int e = 0; e < U * N; ++e) best.offer(x[e], base + ((e / N) * kThreads + tid) * N + e % N, lane, k);
-            }
+            if (__ballot(top >= best.least || p.z != p.z))
+                best.offer(x, lane, k, [&](uint32_t e) { return base + ((e / N) * kThreads + tid) * N + e % N; });
         }
     }
     return p;
@@ -308,7 +347,7 @@ __global__ __launch_bounds__(WAVES > 4 ? WAVES * 64 : 256) void k_score(ScoreArg
     if (r >= a.rows) return;        // whole wavefronts, and where they share a row whole work-groups
     const typename T::raw* row = static_cast<const typename T::raw*>(a.logits) + (int64_t)r * a.row_stride;
     const uint8_t* mask = MASK ? a.mask + (int64_t)r * a.mask_stride : nullptr;
-    Best best = {0, waiting + (TOP ? wave * kWaiting : 0), 0, kLowest, 0xFFFFFFFFu};
+    Best best = {0, waiting + (TOP ? wave * kWaiting : 0), 0, false, kLowest, 0xFFFFFFFFu};
     Part p = stream<T, MASK, TOP, WAVES>(row, mask, 0, a.entries, threadIdx.x % (64 * WAVES), c, best, a.top_k, bars);
     p = group_part<64>(p, c);
     if constexpr (TOP) best.finish(lane, a.top_k);
@@ -348,7 +387,7 @@ __global__ __launch_bounds__(256) void k_score_piece(ScoreArgs a, Pieces pieces,
     const float c = a.scale * kLog2e;
     const typename T::raw* row = static_cast<const typename T::raw*>(a.logits) + (int64_t)r * a.row_stride;
     const uint8_t* mask = MASK ? a.mask + (int64_t)r * a.mask_stride : nullptr;
-    Best best = {0, waiting + (TOP ? wave * kWaiting : 0), 0, kLowest, 0xFFFFFFFFu};
+    Best best = {0, waiting + (TOP ? wave * kWaiting : 0), 0, false, kLowest, 0xFFFFFFFFu};
     Part p = stream<T, MASK, TOP, 4>(row, mask, from, to, threadIdx.x, c, best, a.top_k, bars);
     p = group_part<64>(p, c);
     if constexpr (TOP) best.finish(lane, a.top_k);
