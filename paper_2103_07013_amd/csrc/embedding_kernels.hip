@@ -12,7 +12,7 @@ namespace bps {
 
 namespace {
 
-constexpr uint32_t kSortGroup = 256, kSortTile = 2048, kMaxDigit = 9;
+constexpr uint32_t kSortGroup = 512, kSortTile = 2048, kMaxDigit = 9;
 // Up to this many tokens are sorted by one work-group, in one launch: the passes of a work-group take longer the more there are,
 // those of many pay two launches each.
 constexpr uint32_t kSortOne = 4096, kSortOneGroup = 1024;
@@ -314,7 +314,7 @@ __global__ __launch_bounds__(256) void k_embed(EmbedArgs a) {
             load<T, N>(from + at, x);
 #pragma unroll
             for (int k = 0; k < N; ++k) x[k] = row ? x[k] * a.scale : other;
-            store<T, N>(to + at, x);
+            store<T, N>(to + at, x, a.past != 0);
         } else {
             for (uint32_t k = at; k < a.width; ++k) to[k] = rounded<T>(row ? to_float(from[k]) * a.scale : other);
         }
@@ -346,7 +346,8 @@ struct SumArgs {
     uint32_t count, rows, width, pieces, length;
     uint32_t sum_groups, blocks;      // work-groups that add up, the others write zeros; groups of columns of a row
     float scale;
-    int32_t accumulate;
+    int32_t accumulate, past;
+    uint32_t join_bits;               // 2^join_bits lanes join 4 columns each
 };
 
 template <class O, int N>
@@ -362,7 +363,7 @@ __device__ __forceinline__ void write_sum(const SumArgs& a, uint32_t row, uint32
 #pragma unroll
             for (int k = 0; k < N; ++k) y[k] = sum[k] * a.scale;
         }
-        store<O, N>(to, y);
+        store<O, N>(to, y, a.past != 0);
     } else {
         for (uint32_t k = 0; at + k < a.width; ++k) to[k] = rounded<O>(a.accumulate ? fmaf(sum[k], a.scale, to_float(to[k])) : sum[k] * a.scale);
     }
@@ -378,7 +379,7 @@ __device__ __forceinline__ void write_zeros(const SumArgs& a, uint32_t group, ui
         typename O::raw* to = static_cast<typename O::raw*>(a.out) + (int64_t)row * a.out_stride;
         for (uint32_t at = threadIdx.x % GROUP * N; at < a.width; at += GROUP * N) {
             if (at + N <= a.width) {
-                store<O, N>(to + at, zero);
+                store<O, N>(to + at, zero, a.past != 0);
             } else {
                 for (uint32_t k = at; k < a.width; ++k) to[k] = rounded<O>(0.0f);
             }
@@ -399,8 +400,8 @@ __global__ __launch_bounds__(256) void k_embed_sum(SumArgs a) {
         return;
     }
     const uint32_t lane = threadIdx.x % GROUP, slot = threadIdx.x / GROUP;
-    const uint64_t work = (uint64_t)blockIdx.x * kSlots + slot;
-    const uint32_t piece = (uint32_t)(work / a.blocks), at = ((uint32_t)(work % a.blocks) * GROUP + lane) * N;
+    const uint32_t work = blockIdx.x * kSlots + slot;
+    const uint32_t piece = work / a.blocks, at = (work % a.blocks * GROUP + lane) * N;
     const uint32_t from = piece * a.length;
     const uint32_t end = piece >= a.pieces ? from : a.count - from < a.length ? a.count : from + a.length;
     bool began_before = piece < a.pieces && from > 0 && a.keys[from - 1] == a.keys[from];
@@ -460,65 +461,72 @@ __global__ __launch_bounds__(256) void k_embed_sum(SumArgs a) {
     }
 }
 
-// The rows that are cut.  Each work-group lists the pieces in which such a row begins, and how many partial sums there are of it.  Of rows
-// with few a wavefront adds up 256 columns; of rows with many a work-group does, each wavefront a part of them in order, and then those
-// parts in order.
+// The rows that are cut.  Each work-group lists the pieces in which such a row begins, those of few partial sums and those of many.  2^join_bits
+// lanes, 4 columns each, add up the sums of a row with few; of rows with many all lanes of a work-group do, each such share of
+// them a part of the sums in order, and then those parts in a fixed order.
 template <class O>
 __global__ __launch_bounds__(1024) void k_embed_join(SumArgs a) {
-    constexpr uint32_t kWaves = 16, kColumns = 256, kFew = 32;
-    __shared__ uint64_t through[kMaxPieces / 64 + 1];
-    __shared__ uint16_t begins[kMaxPieces];
-    __shared__ uint32_t counts[kMaxPieces / 64];
-    __shared__ float part[kWaves][kColumns];
+    constexpr uint32_t kFew = 8, kTogether = 8, kWords = kMaxPieces / 64, kRounds = kMaxPieces / 1024;
+    __shared__ uint64_t through[kWords];
+    __shared__ uint16_t list[kMaxPieces];      // of few from the front, of many from the back
+    __shared__ uint32_t counts[2][kWords];
+    __shared__ float part[16][256];
     const uint32_t tid = threadIdx.x, lane = tid & 63u, wave = tid >> 6;
-    uint64_t mine[kMaxPieces / 1024];
+    uint64_t begin_here[kRounds];
 #pragma unroll
-    for (uint32_t k = 0; k < kMaxPieces / 1024; ++k) {
+    for (uint32_t k = 0; k < kRounds; ++k) {
         const uint32_t piece = k * 1024 + tid;
         const uint32_t cut = piece < a.pieces ? a.cuts[piece] : 0u;
-        mine[k] = __ballot(cut == kGoesOn);
+        begin_here[k] = __ballot(cut == kGoesOn);
         const uint64_t with = __ballot(cut == kThrough);
+        if (lane == 0) through[piece / 64] = with;
+    }
+    __syncthreads();
+    // partial sums of the row that begins in a piece: of this one, of those that it goes through, and of the one that it ends in
+    auto partial_sums = [&](uint32_t piece) {
+        const uint32_t at = piece + 1;
+        for (uint32_t word = at / 64; word < kWords; ++word) {
+            const uint64_t ends = ~through[word] & (word == at / 64 ? ~0ull << (at % 64) : ~0ull);
+            if (ends) return word * 64 + (uint32_t)__builtin_ctzll(ends) + 1 - piece;
+        }
+        return kMaxPieces - piece;
+    };
+    uint64_t many_here[kRounds];
+#pragma unroll
+    for (uint32_t k = 0; k < kRounds; ++k) {
+        const uint32_t piece = k * 1024 + tid;
+        many_here[k] = __ballot((begin_here[k] >> lane & 1u) && partial_sums(piece) > kFew);
+        begin_here[k] &= ~many_here[k];
         if (lane == 0) {
-            through[piece / 64] = with;
-            counts[piece / 64] = (uint32_t)__popcll(mine[k]);
+            counts[0][piece / 64] = (uint32_t)__popcll(begin_here[k]);
+            counts[1][piece / 64] = (uint32_t)__popcll(many_here[k]);
         }
     }
     __syncthreads();
-    uint32_t found = 0;
-    if (wave == 0) {
-        const uint32_t n = counts[lane];
-        uint32_t with = n;
+    if (wave < 2) {
+        uint32_t with = counts[wave][lane];
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
             const uint32_t x = __shfl_up(with, d, 64);
             if (lane >= (uint32_t)d) with += x;
         }
-        counts[lane] = with;
+        counts[wave][lane] = with;
     }
     __syncthreads();
-    found = counts[kMaxPieces / 64 - 1];
 #pragma unroll
-    for (uint32_t k = 0; k < kMaxPieces / 1024; ++k) {
+    for (uint32_t k = 0; k < kRounds; ++k) {
         const uint32_t piece = k * 1024 + tid, word = piece / 64;
-        if (mine[k] >> lane & 1u) begins[(word ? counts[word - 1] : 0u) + lanes_before(mine[k])] = (uint16_t)piece;
+        if (begin_here[k] >> lane & 1u) list[(word ? counts[0][word - 1] : 0u) + lanes_before(begin_here[k])] = (uint16_t)piece;
+        if (many_here[k] >> lane & 1u) list[kMaxPieces - 1 - (word ? counts[1][word - 1] : 0u) - lanes_before(many_here[k])] = (uint16_t)piece;
     }
     __syncthreads();
-    // partial sums of the row that begins in a piece: of this one, of those that it goes through, and of the one that it ends in
-    auto partial_sums = [&](uint32_t piece) {
-        uint32_t at = piece + 1;
-        for (uint32_t word = at / 64; word < kMaxPieces / 64; ++word) {
-            const uint64_t ends = ~through[word] & (word == at / 64 ? ~0ull << (at % 64) : ~0ull);
-            if (ends) return word * 64 + (uint32_t)__builtin_ctzll(ends) + 1 - piece;
-        }
-        return (uint32_t)kMaxPieces - piece;
-    };
     auto add = [&](uint32_t piece, uint32_t from, uint32_t to, uint32_t at, float (&sum)[4]) {
 #pragma unroll
         for (int c = 0; c < 4; ++c) sum[c] = 0.0f;
-        for (uint32_t k = from; k < to; k += 4) {
-            float x[4][4];
+        for (uint32_t k = from; k < to; k += kTogether) {
+            float x[kTogether][4];
 #pragma unroll
-            for (uint32_t u = 0; u < 4; ++u) {
+            for (uint32_t u = 0; u < kTogether; ++u) {
                 const float* p = a.partial + ((size_t)(piece + (k + u < to ? k + u : from)) * 2 + ((k + u < to ? k + u : from) == 0)) * a.width + at;
                 if (at + 4 <= a.width) {
                     load<F32, 4>(p, x[u]);
@@ -528,35 +536,46 @@ __global__ __launch_bounds__(1024) void k_embed_join(SumArgs a) {
                 }
             }
 #pragma unroll
-            for (uint32_t u = 0; u < 4; ++u)
+            for (uint32_t u = 0; u < kTogether; ++u)
                 if (k + u < to) {
 #pragma unroll
                     for (int c = 0; c < 4; ++c) sum[c] += x[u][c];
                 }
         }
     };
-    const uint32_t blocks = (a.width + kColumns - 1) / kColumns;
-    const uint64_t all = (uint64_t)found * blocks;
-    for (uint64_t work = (uint64_t)wave * gridDim.x + blockIdx.x; work < all; work += (uint64_t)kWaves * gridDim.x) {
-        const uint32_t piece = begins[work / blocks], n = partial_sums(piece), at = (uint32_t)(work % blocks) * kColumns + lane * 4;
-        if (n > kFew || at >= a.width) continue;
-        float sum[4];
-        add(piece, 0, n, at, sum);
-        write_sum<O, 4>(a, a.keys[(piece + 1) * a.length - 1], at, sum);
+    const uint32_t lanes = 1u << a.join_bits, shares = 1024u >> a.join_bits, share = tid >> a.join_bits, column = (tid & (lanes - 1)) * 4;
+    const uint32_t blocks = (a.width + 4 * lanes - 1) / (4 * lanes);
+    // a gradient of `count` rows fits in memory, so that this and the like stay below 2^32
+    const uint32_t few = counts[0][kWords - 1] * blocks, many = counts[1][kWords - 1] * blocks;
+    // up to half of the work-groups have rows of many sums alone, so that those of few do not wait
+    const uint32_t apart = many < gridDim.x / 2 ? many : 0u;
+    if (blockIdx.x >= apart) {
+        for (uint32_t work = share * (gridDim.x - apart) + blockIdx.x - apart; work < few; work += shares * (gridDim.x - apart)) {
+            const uint32_t piece = list[work / blocks], at = work % blocks * 4 * lanes + column;
+            if (at >= a.width) continue;
+            float sum[4];
+            add(piece, 0, partial_sums(piece), at, sum);
+            write_sum<O, 4>(a, a.keys[(piece + 1) * a.length - 1], at, sum);
+        }
+        if (apart) return;
     }
-    for (uint64_t work = blockIdx.x; work < all; work += gridDim.x) {
-        const uint32_t piece = begins[work / blocks], n = partial_sums(piece), at = (uint32_t)(work % blocks) * kColumns + lane * 4;
-        if (n <= kFew) continue;
-        const uint32_t each = (n + kWaves - 1) / kWaves, begin = wave * each < n ? wave * each : n, stop = begin + each < n ? begin + each : n;
+    for (uint32_t work = blockIdx.x; work < many; work += gridDim.x) {
+        const uint32_t piece = list[kMaxPieces - 1 - work / blocks], n = partial_sums(piece), at = work % blocks * 4 * lanes + column;
+        const uint32_t each = (n + shares - 1) / shares, begin = share * each < n ? share * each : n, stop = begin + each < n ? begin + each : n;
         float sum[4] = {};
         if (at < a.width) add(piece, begin, stop, at, sum);
-        __syncthreads();
-        store<F32, 4>(&part[wave][lane * 4], sum);
-        __syncthreads();
-        if (wave == 0 && at < a.width) {
-            for (uint32_t w = 1; w < kWaves; ++w) {
+        for (uint32_t d = lanes; d < 64; d <<= 1) {      // the shares of a wavefront, then the wavefronts
 #pragma unroll
-                for (int c = 0; c < 4; ++c) sum[c] += part[w][lane * 4 + c];
+            for (int c = 0; c < 4; ++c) sum[c] += __shfl_xor(sum[c], (int)d, 64);
+        }
+        __syncthreads();
+        if (lane < lanes) store<F32, 4>(&part[wave][column], sum);
+        __syncthreads();
+        if (share == 0 && at < a.width) {
+#pragma unroll
+            for (uint32_t w = 1; w < 16; ++w) {
+#pragma unroll
+                for (int c = 0; c < 4; ++c) sum[c] += part[w][column + c];
             }
             write_sum<O, 4>(a, a.keys[(piece + 1) * a.length - 1], at, sum);
         }
@@ -576,7 +595,8 @@ void sum(SumArgs s, hipStream_t stream) {
 
 template <class T, class O>
 hipError_t embed_grad(const EmbedGradArgs& a, hipStream_t stream) {
-    SumArgs s = {nullptr, nullptr, nullptr, a.grad, a.out, nullptr, nullptr, a.grad_stride, a.out_stride, a.count, a.rows, a.width, 0, 0, 0, 0, a.scale, a.accumulate};
+    SumArgs s = {nullptr, nullptr, nullptr, a.grad, a.out, nullptr, nullptr, a.grad_stride, a.out_stride, a.count, a.rows, a.width, 0, 0, 0, 0, a.scale, a.accumulate, past_caches(a.out, a.out_stride, sizeof(typename O::raw), a.rows, a.width), 0};
+    while (s.join_bits < 6 && 4u << s.join_bits < a.width) ++s.join_bits;
     if (!a.count) {
         if (!a.accumulate) hipLaunchKernelGGL((k_embed_zero<O>), dim3((a.rows + 3) / 4 < 16384 ? (a.rows + 3) / 4 : 16384), dim3(256), 0, stream, s);
         return hipGetLastError();
@@ -623,7 +643,11 @@ hipError_t embed_grad(const EmbedGradArgs& a, hipStream_t stream) {
         sum<T, O, 16>(s, stream);
     else
         sum<T, O, 64>(s, stream);
-    if (s.pieces > 1) hipLaunchKernelGGL((k_embed_join<O>), dim3(s.pieces < 256 ? s.pieces : 256), dim3(1024), 0, stream, s);
+    if (s.pieces > 1) {
+        // no more rows are cut than there are rows, or places to cut at
+        const uint64_t cut = (uint64_t)(s.pieces - 1 < a.rows ? s.pieces - 1 : a.rows) * ((a.width + 255) / 256);
+        hipLaunchKernelGGL((k_embed_join<O>), dim3(cut < 256 ? (uint32_t)cut : 256u), dim3(1024), 0, stream, s);
+    }
     return hipGetLastError();
 }
 
@@ -643,11 +667,13 @@ void embed_rows(const EmbedArgs& a, hipStream_t stream) {
 template <class T>
 hipError_t embed(const EmbedArgs& a, hipStream_t stream) {
     const uint32_t lanes = (a.width + T::kPer16 - 1) / T::kPer16;
+    const int32_t past = past_caches(a.out, a.out_stride, sizeof(typename T::raw), a.count, a.width);
     for (uint64_t first = 0; first < a.count; first += kMaxRows) {
         EmbedArgs s = a;
         s.count = a.count - first < kMaxRows ? a.count - first : kMaxRows;
         s.tokens = static_cast<const char*>(a.tokens) + first * (a.tokens64 ? 8 : 4);
         s.out = static_cast<typename T::raw*>(a.out) + (int64_t)first * a.out_stride;
+        s.past = past;
         if (lanes <= 4)
             embed_rows<T, 4>(s, stream);
         else if (lanes <= 16)

@@ -78,7 +78,7 @@ bps_status bps_log_probs_backward(const void* logits, int32_t dtype, uint64_t ro
     if (!aligned(out, size_of(dtype))) return fail_here(BPS_ERR_INVALID_ARG, "%s: misaligned out", what);
     if (rows > 1 && (out_stride < 0 ? -out_stride : out_stride) < (int64_t)entries) return fail_here(BPS_ERR_INVALID_ARG, "%s: rows of out overlap", what);
     const bps::ScoreGradArgs a = {logits, tokens, mask, row_stride, mask_stride, out_stride, rows, entries, scale, token_bits == 64,
-                                  logp, entropy, norm, norm + rows, grad_logp, grad_entropy, out};
+                                  logp, entropy, norm, norm + rows, grad_logp, grad_entropy, out, 0};
     return launched(what, bps::launch_score_grad(dtype, a, static_cast<hipStream_t>(stream)));
 }
 
@@ -93,7 +93,7 @@ bps_status bps_embedding(const void* tokens, int32_t token_bits, uint64_t count,
     if (!tokens || !weight || !out) return fail_here(BPS_ERR_INVALID_ARG, "%s: null argument", what);
     if (!aligned(weight, size_of(dtype)) || !aligned(out, size_of(dtype)) || !aligned(tokens, token_bits / 8)) return fail_here(BPS_ERR_INVALID_ARG, "%s: misaligned argument", what);
     if (count > 1 && (out_stride < 0 ? -out_stride : out_stride) < (int64_t)width) return fail_here(BPS_ERR_INVALID_ARG, "%s: rows of out overlap", what);
-    const bps::EmbedArgs a = {tokens, weight, out, weight_stride, out_stride, count, rows, width, scale, token_bits == 64};
+    const bps::EmbedArgs a = {tokens, weight, out, weight_stride, out_stride, count, rows, width, scale, token_bits == 64, 0};
     return launched(what, bps::launch_embed(dtype, a, static_cast<hipStream_t>(stream)));
 }
 

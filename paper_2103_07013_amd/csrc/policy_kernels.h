@@ -41,6 +41,7 @@ struct ScoreGradArgs {
     int32_t tokens64;
     const float *logp, *entropy, *largest, *ln_z, *grad_logp, *grad_entropy;   // grad_* may be null (zero)
     void* out;
+    int32_t past;             // the launcher's: results are written past the caches
 };
 hipError_t launch_score_grad(int32_t dtype, const ScoreGradArgs& a, hipStream_t stream);
 
@@ -53,6 +54,7 @@ struct EmbedArgs {
     uint32_t rows, width;     // V, D
     float scale;
     int32_t tokens64;
+    int32_t past;             // the launcher's, as above
 };
 hipError_t launch_embed(int32_t dtype, const EmbedArgs& a, hipStream_t stream);
 

@@ -458,9 +458,9 @@ __device__ __forceinline__ void gradient(const RowGrad& g, float scale, uint32_t
     }
 }
 template <class T, int N>
-__device__ __forceinline__ void store_entries(typename T::raw* out, uint32_t at, uint32_t end, const float (&d)[N]) {
+__device__ __forceinline__ void store_entries(typename T::raw* out, uint32_t at, uint32_t end, const float (&d)[N], bool past) {
     if (at + N <= end) {
-        store<T, N>(out + at, d);
+        store<T, N>(out + at, d, past);
     } else {
 #pragma unroll
         for (int k = 0; k < N; ++k)
@@ -477,7 +477,7 @@ __global__ __launch_bounds__(256) void k_score_grad_short(ScoreGradArgs a) {
     float x[N], d[N];
     row_entries<T, N, MASK>(static_cast<const typename T::raw*>(a.logits) + (int64_t)r * a.row_stride, MASK ? a.mask + (int64_t)r * a.mask_stride : nullptr, lane * N, a.entries, x);
     gradient(g, a.scale, lane * N, x, d);
-    store_entries<T, N>(static_cast<typename T::raw*>(a.out) + (int64_t)r * a.out_stride, lane * N, a.entries, d);
+    store_entries<T, N>(static_cast<typename T::raw*>(a.out) + (int64_t)r * a.out_stride, lane * N, a.entries, d, false);
 }
 
 // Work-groups take pieces of rows, the last row first: what of the logits the forward pass read last may still be in a cache.
@@ -497,7 +497,7 @@ __global__ __launch_bounds__(GROUP) void k_score_grad(ScoreGradArgs a, uint32_t 
     for (int u = 0; u < U; ++u) {
         const uint32_t at = from + (u * GROUP + threadIdx.x) * N;
         gradient(g, a.scale, at, x[u], d);
-        store_entries<T, N>(out, at, a.entries, d);
+        store_entries<T, N>(out, at, a.entries, d, a.past != 0);
     }
 }
 
@@ -628,13 +628,16 @@ hipError_t launch_score(int32_t dtype, const ScoreArgs& a, hipStream_t stream) {
 
 hipError_t launch_score_grad(int32_t dtype, const ScoreGradArgs& a, hipStream_t stream) {
     const uint64_t each = kMaxGroups / (1 + a.entries / 4096);
+    const size_t size = dtype == BPS_F32 ? 4 : 2;
+    const int32_t past = past_caches(a.out, a.out_stride, size, a.rows, a.entries);
     for (uint64_t left = a.rows; left;) {      // the last rows first, as within a launch
         const uint64_t n = left < each ? left : each;
         left -= n;
         ScoreGradArgs s = rows_of(a, dtype, left, n);
         if (a.grad_logp) s.grad_logp = a.grad_logp + left;
         if (a.grad_entropy) s.grad_entropy = a.grad_entropy + left;
-        s.out = static_cast<char*>(a.out) + (int64_t)left * a.out_stride * (dtype == BPS_F32 ? 4 : 2);
+        s.out = static_cast<char*>(a.out) + (int64_t)left * a.out_stride * (int64_t)size;
+        s.past = past;
         const hipError_t e = dtype == BPS_F32 ? score_grad<F32>(s, stream) : dtype == BPS_BF16 ? score_grad<Bf16>(s, stream) : score_grad<F16>(s, stream);
         if (e != hipSuccess) return e;
     }
