@@ -582,6 +582,109 @@ __global__ __launch_bounds__(1024) void k_embed_join(SumArgs a) {
     }
 }
 
+// ---- gradient of tables of few rows
+
+// A policy's moves, say: every row has many tokens, and sums of all rows fit in LDS, so that nothing is sorted.  GROUP lanes for N columns each; the
+// groups of a work-group add up a part of its tokens each, in order, into sums of their own, which are joined in order, and
+// the work-groups' sums by a second kernel.
+struct FewArgs {
+    const void *tokens, *grad;
+    void* out;
+    float* partial;           // [part][row][width]
+    int64_t grad_stride, out_stride;
+    uint32_t count, rows, width, parts, length;      // parts: work-groups side by side, length: tokens of one
+    float scale;
+    int32_t tokens64, accumulate;
+};
+
+template <class T, int GROUP>
+__global__ __launch_bounds__(256) void k_embed_few(FewArgs a) {
+    constexpr int N = T::kPer16, kSlots = 256 / GROUP, kAhead = 8;
+    extern __shared__ float sums[];                  // [row][slot][GROUP][N]
+    const uint32_t lane = threadIdx.x % GROUP, slot = threadIdx.x / GROUP, at = (blockIdx.y * GROUP + lane) * N;
+    float zero[N] = {};
+    for (uint32_t r = 0; r < a.rows; ++r) store<F32, N>(sums + ((size_t)r * 256 + threadIdx.x) * N, zero);
+    const uint32_t first = blockIdx.x * a.length, last = a.count - first < a.length ? a.count : first + a.length;
+    const uint32_t each = (a.length + kSlots - 1) / kSlots, from = first + slot * each < last ? first + slot * each : last, to = last - from < each ? last : from + each;
+    if (at < a.width) {
+        for (uint32_t i = from; i < to; i += kAhead) {
+            float x[kAhead][N];
+            int64_t t[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const uint32_t n = i + u < to ? i + u : i;
+                t[u] = i + u < to ? token_at(a.tokens, a.tokens64, n) : -1;
+                const typename T::raw* g = static_cast<const typename T::raw*>(a.grad) + (int64_t)n * a.grad_stride + at;
+                if (at + N <= a.width) {
+                    load<T, N>(g, x[u]);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < N; ++k) x[u][k] = at + k < a.width ? to_float(g[k]) : 0.0f;
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                if (t[u] < 0 || t[u] >= (int64_t)a.rows) continue;
+                float* sum = sums + ((uint32_t)t[u] * 256 + threadIdx.x) * N;
+#pragma unroll
+                for (int k = 0; k < N; ++k) sum[k] += x[u][k];
+            }
+        }
+    }
+    __syncthreads();
+    // lane (r, column) of the joined sums: N consecutive columns of one row to a thread
+    for (uint32_t w = threadIdx.x; w < a.rows * GROUP; w += 256) {
+        const uint32_t r = w / GROUP, l = w % GROUP, column = (blockIdx.y * GROUP + l) * N;
+        if (column >= a.width) continue;
+        float sum[N] = {};
+#pragma unroll 4
+        for (uint32_t g = 0; g < kSlots; ++g) {
+#pragma unroll
+            for (int k = 0; k < N; ++k) sum[k] += sums[(r * 256 + g * GROUP + l) * N + k];
+        }
+        float* p = a.partial + ((size_t)blockIdx.x * a.rows + r) * a.width + column;
+        for (int k = 0; k < N; ++k)
+            if (column + k < a.width) p[k] = sum[k];
+    }
+}
+
+// 16 lanes for a column of a row, each of which adds up every 16th part's sum.
+template <class O>
+__global__ __launch_bounds__(256) void k_embed_few_join(FewArgs a) {
+    __shared__ float part[16][16];
+    const uint32_t cells = a.rows * a.width, cell = blockIdx.x * 16 + (threadIdx.x & 15u), share = threadIdx.x >> 4;
+    float sum = 0.0f;
+    if (cell < cells) {
+#pragma unroll 8
+        for (uint32_t p = share; p < a.parts; p += 16) sum += a.partial[(size_t)p * cells + cell];
+    }
+    part[share][threadIdx.x & 15u] = sum;
+    __syncthreads();
+    if (share || cell >= cells) return;
+#pragma unroll
+    for (uint32_t w = 1; w < 16; ++w) sum += part[w][threadIdx.x];
+    const uint32_t r = cell / a.width;
+    typename O::raw* to = static_cast<typename O::raw*>(a.out) + (int64_t)r * a.out_stride + cell % a.width;
+    *to = rounded<O>(a.accumulate ? fmaf(sum, a.scale, to_float(*to)) : sum * a.scale);
+}
+
+// Sums of so many bytes are held by a work-group, two to a compute unit.
+constexpr uint32_t kFewBytes = 64 << 10, kFewParts = 256;
+// How many work-groups share the tokens of a table of few rows (0: the table has more): for sums not much larger than the gradients, no fewer
+// than 64 tokens for each.
+uint32_t few_parts(uint32_t count, uint32_t rows, uint32_t width, bool wide) {
+    if (rows > 16 || rows * 256u * (wide ? 16u : 32u) > kFewBytes || (uint64_t)rows * width >= 1u << 31) return 0;
+    const uint32_t n = (count + 63) / 64;
+    return n < kFewParts ? n : kFewParts;
+}
+
+template <class T, class O, int GROUP>
+void few(FewArgs f, hipStream_t stream) {
+    const uint32_t blocks = (f.width + GROUP * T::kPer16 - 1) / (GROUP * T::kPer16);
+    hipLaunchKernelGGL((k_embed_few<T, GROUP>), dim3(f.parts, blocks), dim3(256), f.rows * 256 * T::kPer16 * sizeof(float), stream, f);
+    hipLaunchKernelGGL((k_embed_few_join<O>), dim3((uint32_t)(((uint64_t)f.rows * f.width + 15) / 16)), dim3(256), 0, stream, f);
+}
+
 size_t whole(size_t n) { return (n + 255) / 256 * 256; }
 
 template <class T, class O, int GROUP>
@@ -599,6 +702,19 @@ hipError_t embed_grad(const EmbedGradArgs& a, hipStream_t stream) {
     while (s.join_bits < 6 && 4u << s.join_bits < a.width) ++s.join_bits;
     if (!a.count) {
         if (!a.accumulate) hipLaunchKernelGGL((k_embed_zero<O>), dim3((a.rows + 3) / 4 < 16384 ? (a.rows + 3) / 4 : 16384), dim3(256), 0, stream, s);
+        return hipGetLastError();
+    }
+    const uint32_t lanes = (a.width + T::kPer16 - 1) / T::kPer16;
+    if (uint32_t parts = few_parts(a.count, a.rows, a.width, T::kPer16 == 4)) {
+        const uint32_t length = (a.count + parts - 1) / parts;
+        parts = (a.count + length - 1) / length;
+        const FewArgs f = {a.tokens, a.grad, a.out, static_cast<float*>(a.workspace), a.grad_stride, a.out_stride, a.count, a.rows, a.width, parts, length, a.scale, a.tokens64, a.accumulate};
+        if (lanes <= 4)
+            few<T, O, 4>(f, stream);
+        else if (lanes <= 16)
+            few<T, O, 16>(f, stream);
+        else
+            few<T, O, 64>(f, stream);
         return hipGetLastError();
     }
     const SortPlan plan = sort_plan(a.count, a.rows);
@@ -636,7 +752,6 @@ hipError_t embed_grad(const EmbedGradArgs& a, hipStream_t stream) {
     s.marks = sort.marks;
     s.length = piece_length(a.count);
     s.pieces = (uint32_t)((a.count + (uint64_t)s.length - 1) / s.length);
-    const uint32_t lanes = (a.width + T::kPer16 - 1) / T::kPer16;
     if (lanes <= 4)
         sum<T, O, 4>(s, stream);
     else if (lanes <= 16)
@@ -690,7 +805,10 @@ size_t embed_grad_workspace(uint32_t count, uint32_t rows, uint32_t width) {
     if (!count) return 0;
     const SortPlan plan = sort_plan(count, rows);
     const uint32_t length = piece_length(count);
-    return 4 * whole((size_t)count * 4) + whole(((size_t)(plan.row + 1) << plan.digit) * 4) + whole(rows) + kMaxPieces + (count + (size_t)length - 1) / length * 2 * width * 4;
+    // the gradient's type is not known here: enough for either way
+    const size_t few = (size_t)few_parts(count, rows, width, true) * rows * width * 4;
+    const size_t sorted = 4 * whole((size_t)count * 4) + whole(((size_t)(plan.row + 1) << plan.digit) * 4) + whole(rows) + kMaxPieces + (count + (size_t)length - 1) / length * 2 * width * 4;
+    return few > sorted ? few : sorted;
 }
 
 hipError_t launch_embed(int32_t dtype, const EmbedArgs& a, hipStream_t stream) {

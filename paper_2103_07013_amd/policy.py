@@ -140,7 +140,7 @@ def _log_probs(logits, tokens, mask, scale, top_k):
     device = logits.device
     bits = _tokens(tokens, shape, device)
     mask_at, mask_step = _mask(mask, shape, rows, width, device) if mask is not None else (None, 0)
-    held = torch.empty((5, *shape), dtype=torch.float32, device=device)
+    held = torch.empty(5, *shape, dtype=torch.float32, device=device)
     at, size = held.data_ptr(), 4 * rows
     dtype = _TYPES[logits.dtype]
     top_ids = top_logp = ids_at = top_at = space = None
@@ -211,7 +211,7 @@ def log_probs_backward(logits, tokens, result, grad_logp=None, grad_entropy=None
     mask_at, mask_step = _mask(mask, shape, rows, width, device) if mask is not None else (None, 0)
     at, size = _vector(result.held if isinstance(result, LogProbs) else result, (5, *shape), device, "result"), 4 * rows
     if out is None:
-        out = torch.empty(logits.shape, dtype=logits.dtype, device=device)
+        out = torch.empty(*shape, width, dtype=logits.dtype, device=device)
         out_step = width
     else:
         if out.dtype != logits.dtype or out.device != device or out.shape != logits.shape:
@@ -232,7 +232,7 @@ def _embedding(tokens, weight, scale, out):
     device = weight.device
     bits = _tokens(tokens, tokens.shape, device)
     if out is None:
-        out = torch.empty((*tokens.shape, width), dtype=weight.dtype, device=device)
+        out = torch.empty(*tokens.shape, width, dtype=weight.dtype, device=device)
         out_step = width
     else:
         if out.dtype != weight.dtype or out.device != device or out.shape != (*tokens.shape, width):
@@ -286,7 +286,7 @@ def embedding_backward(tokens, grad_out, rows, scale=1.0, dtype=torch.float32, o
         count, width, step = 0, grad_out.shape[-1], grad_out.shape[-1]
     bits = _tokens(tokens, tokens.shape, device)
     if out is None:
-        out = torch.empty((rows, width), dtype=dtype, device=device)
+        out = torch.empty(rows, width, dtype=dtype, device=device)
         out_step = width
     else:
         if out.device != device or out.shape != (rows, width):

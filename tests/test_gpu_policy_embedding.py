@@ -109,6 +109,25 @@ def test_accumulation_leaves_other_rows_alone(N, V, D, to):
     _near(out, both, slack + E * both.abs())
 
 
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("N,V,D", [(3, 16, 5), (70, 8, 17), (1000, 9, 64), (5000, 16, 300), (4097, 17, 40), (66000, 8, 130), (20001, 1, 1025), (65536, 16, 4)])
+@pytest.mark.parametrize("how", ["even", "skewed", "one"])
+def test_gradient_of_tables_of_few_rows(N, V, D, how, dtype):
+    import paper_2103_07013_amd as bps
+    torch = _torch()
+    t = _tokens(N, V, how)
+    g = torch.randn((N, D), generator=torch.Generator().manual_seed(N + V)).to(getattr(torch, dtype)).cuda()
+    ref, slack = _reference(t, g, V, 0.3)
+    first = bps.embedding_backward(t, g, V, scale=0.3)
+    _near(first, ref, slack)
+    assert torch.equal(first, bps.embedding_backward(t.int(), g, V, scale=0.3))
+    held = torch.randn((V, D), device="cuda")
+    out = held.clone()
+    bps.embedding_backward(t, g, V, scale=0.3, out=out, accumulate=True)
+    both = ref + held.cpu().double()
+    _near(out, both, slack + E * both.abs())
+
+
 def test_against_differences():
     """The lookup is linear: the difference quotient of sum(out * c) is exact up to the rounding of the sums."""
     import paper_2103_07013_amd as bps
