@@ -13,9 +13,9 @@ namespace bps {
 namespace {
 
 constexpr uint32_t kSortGroup = 512, kSortTile = 2048, kMaxDigit = 9;
-// Up to this many tokens are sorted by one work-group, in one launch: the passes of a work-group take longer the more there are,
-// those of many pay two launches each.
-constexpr uint32_t kSortOne = 4096, kSortOneGroup = 1024;
+// Up to this many tokens are sorted by one work-group, in one launch.  Measured at 50257 rows (two passes), one work-group / two launches a pass:
+// 4096 tokens 13 / 21 us, 8192 20 / 21, without what the launches take apart.
+constexpr uint32_t kSortOne = 8192, kSortOneGroup = 1024;
 // Up to this many tiles each work-group adds up the counts of those before its own by itself; for more a launch in between does.
 constexpr uint32_t kSumTiles = 32;
 
@@ -58,14 +58,39 @@ struct SortArgs {
     const uint32_t *keys, *places;
     uint32_t *out_keys, *out_places;
     uint32_t* counts;         // [digit][row of tiles], tiles in whole words of 16 bytes; then the digits' totals
-    uint8_t* marks;           // [rows, in whole words], 1 where a row has a token
+    uint8_t* marks;           // [rows, in whole words], 1 where a row has a token; or null
+    void* fill;               // the gradient, where the first launch writes zeros into all of it; or null
+    uint64_t fill_bytes;
     int32_t tokens64;
-    uint32_t count, rows, shift, bits, tiles, row, last;
+    uint32_t count, rows, shift, bits, tiles, row, passes, last;
 };
+
+// Zeros into all of a.fill, 16 bytes at a time, by the threads of `groups` work-groups.
+__device__ __forceinline__ void fill_zeros(const SortArgs& a, uint32_t group, uint32_t groups) {
+    char* p = static_cast<char*>(a.fill);
+    const uint32_t head = (uint32_t)(-reinterpret_cast<uintptr_t>(p) & 15u);
+    const uint64_t at = (uint64_t)group * blockDim.x + threadIdx.x, threads = (uint64_t)groups * blockDim.x;
+    if (a.fill_bytes <= head) {
+        for (uint64_t i = 2 * at; i < a.fill_bytes; i += 2 * threads) *reinterpret_cast<uint16_t*>(p + i) = 0;
+        return;
+    }
+    const uint64_t words = (a.fill_bytes - head) / 16, tail = head + words * 16;
+    if (2 * at < head) *reinterpret_cast<uint16_t*>(p + 2 * at) = 0;
+    if (tail + 2 * at < a.fill_bytes) *reinterpret_cast<uint16_t*>(p + tail + 2 * at) = 0;
+    typedef uint32_t word __attribute__((ext_vector_type(4)));
+    const word zero = {0, 0, 0, 0};
+    for (uint64_t i = at; i < words; i += threads) __builtin_nontemporal_store(zero, reinterpret_cast<word*>(p + head) + i);
+}
+
 __device__ __forceinline__ uint32_t sort_key(const SortArgs& a, uint32_t i) { return a.keys ? a.keys[i] : key_at(a.tokens, a.tokens64, i, a.rows); }
 
+// (Counted by the pass before, with an atomic addition for each pair, the second pass's counts cost 20 to 230 us: tokens in frequent use meet.)
 __global__ __launch_bounds__(kSortGroup) void k_sort_count(SortArgs a) {
     __shared__ uint32_t hist[1u << kMaxDigit];
+    if (blockIdx.x >= a.tiles) {
+        fill_zeros(a, blockIdx.x - a.tiles, gridDim.x - a.tiles);
+        return;
+    }
     const uint32_t bins = 1u << a.bits;
     for (uint32_t b = threadIdx.x; b < bins; b += kSortGroup) hist[b] = 0;
     __syncthreads();
@@ -81,7 +106,7 @@ __global__ __launch_bounds__(kSortGroup) void k_sort_count(SortArgs a) {
         if (first + k * kSortGroup + threadIdx.x < a.count) atomicAdd(&hist[(key[k] >> a.shift) & (bins - 1)], 1u);
     // marks are cleared by the first pass and set by the last
     if (!a.keys && a.marks)
-        for (uint32_t r = blockIdx.x * kSortGroup + threadIdx.x; r < (a.rows + 3) / 4; r += gridDim.x * kSortGroup) reinterpret_cast<uint32_t*>(a.marks)[r] = 0;
+        for (uint32_t r = blockIdx.x * kSortGroup + threadIdx.x; r < (a.rows + 3) / 4; r += a.tiles * kSortGroup) reinterpret_cast<uint32_t*>(a.marks)[r] = 0;
     __syncthreads();
     for (uint32_t b = threadIdx.x; b < bins; b += kSortGroup) a.counts[(size_t)b * a.row + blockIdx.x] = hist[b];
 }
@@ -232,13 +257,18 @@ __global__ __launch_bounds__(kSortGroup) void k_sort_place(SortArgs a) {
     }
 }
 
-// All passes by one work-group, the pairs in LDS between them.  bits: of the whole key, digit: of one pass.
-__global__ __launch_bounds__(kSortOneGroup) void k_sort_one(SortArgs a, uint32_t passes) {
-    constexpr uint32_t kWaves = kSortOneGroup / 64, kEach = kSortOne / kWaves, kRounds = kEach / 64;
+// All passes by one work-group, the pairs in LDS between them; kRounds pairs to a thread.
+template <uint32_t kRounds>
+__global__ __launch_bounds__(kSortOneGroup) void k_sort_one(SortArgs a) {
+    constexpr uint32_t kWaves = kSortOneGroup / 64, kEach = 64 * kRounds;
     __shared__ uint32_t at[kWaves][1u << kMaxDigit];
     __shared__ uint32_t start[1u << kMaxDigit];
     __shared__ uint32_t sums[kWaves];
-    __shared__ uint64_t pairs[kSortOne];
+    __shared__ uint64_t pairs[kWaves * kEach];
+    if (blockIdx.x) {
+        fill_zeros(a, blockIdx.x - 1, gridDim.x - 1);
+        return;
+    }
     const uint32_t bins = 1u << a.bits, lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
     const uint32_t first = wave * kEach;
     uint32_t key[kRounds], place[kRounds], digit[kRounds], to[kRounds];
@@ -252,7 +282,7 @@ __global__ __launch_bounds__(kSortOneGroup) void k_sort_one(SortArgs a, uint32_t
     }
     if (a.marks)
         for (uint32_t r = threadIdx.x; r < (a.rows + 3) / 4; r += kSortOneGroup) reinterpret_cast<uint32_t*>(a.marks)[r] = 0;
-    for (uint32_t p = 0; p < passes; ++p) {
+    for (uint32_t p = 0; p < a.passes; ++p) {
         for (uint32_t b = threadIdx.x; b < kWaves * bins; b += kSortOneGroup) at[b >> a.bits][b & (bins - 1)] = 0;
 #pragma unroll
         for (uint32_t j = 0; j < kRounds; ++j) digit[j] = (key[j] >> (p * a.bits)) & (bins - 1);
@@ -323,12 +353,12 @@ __global__ __launch_bounds__(256) void k_embed(EmbedArgs a) {
 
 // ---- gradient
 
-// Tokens of a piece: about count / 2048, so that there are pieces for all compute units, but no fewer than 8, to keep partial sums few, and from
-// 64 on as many as kMaxPieces allow.
-constexpr uint32_t kPiece = 64, kMaxPieces = 4096;
-uint32_t piece_length(uint32_t count) {
+// Tokens of a piece: so many that there are about 2048 pieces, 4096 of narrow rows, which take few lanes each, so that all compute units have
+// some; but no fewer than 8, to keep partial sums few, and from 64 on as many as kMaxPieces allow.
+constexpr uint32_t kPiece = 64, kMaxPieces = 4096, kNarrow = 64;
+uint32_t piece_length(uint32_t count, uint32_t width) {
     uint32_t n = 8;
-    while ((count + (uint64_t)n - 1) / n > (n < kPiece ? kMaxPieces / 2 : kMaxPieces)) n *= 2;
+    while ((count + (uint64_t)n - 1) / n > (n < kPiece && width > kNarrow ? kMaxPieces / 2 : kMaxPieces)) n *= 2;
     return n;
 }
 
@@ -337,7 +367,7 @@ enum : uint8_t { kGoesOn = 1, kThrough = 2 };
 
 struct SumArgs {
     const uint32_t *keys, *places;
-    const uint8_t* marks;     // null with accumulate
+    const uint8_t* marks;     // null where no zeros are to be written
     const void* grad;
     void* out;
     uint8_t* cuts;            // [piece] what its last row is: kGoesOn, kThrough or 0
@@ -375,7 +405,7 @@ __device__ __forceinline__ void write_zeros(const SumArgs& a, uint32_t group, ui
     constexpr int N = O::kPer16, kRows = 256 / GROUP;
     float zero[N] = {};
     for (uint64_t row = (uint64_t)group * kRows + threadIdx.x / GROUP; row < a.rows; row += (uint64_t)groups * kRows) {
-        if (a.marks && a.marks[row]) continue;
+        if (a.marks && a.marks[row]) continue;      // no marks: no tokens at all
         typename O::raw* to = static_cast<typename O::raw*>(a.out) + (int64_t)row * a.out_stride;
         for (uint32_t at = threadIdx.x % GROUP * N; at < a.width; at += GROUP * N) {
             if (at + N <= a.width) {
@@ -692,7 +722,7 @@ void sum(SumArgs s, hipStream_t stream) {
     constexpr uint32_t kSlots = 256 / GROUP;
     s.blocks = (s.width + GROUP * T::kPer16 - 1) / (GROUP * T::kPer16);
     s.sum_groups = (uint32_t)(((uint64_t)s.pieces * s.blocks + kSlots - 1) / kSlots);
-    const uint32_t zero = s.accumulate ? 0u : (s.rows + kSlots - 1) / kSlots;
+    const uint32_t zero = s.marks ? (s.rows + kSlots - 1) / kSlots : 0u;
     hipLaunchKernelGGL((k_embed_sum<T, O, GROUP>), dim3(s.sum_groups + (zero < 4096 ? zero : 4096)), dim3(256), 0, stream, s);
 }
 
@@ -731,16 +761,24 @@ hipError_t embed_grad(const EmbedGradArgs& a, hipStream_t stream) {
     s.cuts = reinterpret_cast<uint8_t*>(w);
     w += kMaxPieces;
     s.partial = reinterpret_cast<float*>(w);
-    SortArgs sort = {a.tokens, nullptr, nullptr, buffer[0], buffer[1], counts, a.accumulate ? nullptr : marks, a.tokens64, a.count, a.rows, 0, plan.digit, plan.tiles, plan.row, 1};
+    // Where most rows have no token the whole table is cleared by work-groups of the sort's first launch, a contiguous one in whole cache lines;
+    // else the rows that have none are, next to the sums.
+    const bool cleared = !a.accumulate && a.out_stride == a.width && a.count < a.rows / 4;
+    const uint64_t bytes = (uint64_t)a.rows * a.width * sizeof(typename O::raw);
+    SortArgs sort = {a.tokens, nullptr, nullptr, buffer[0], buffer[1], counts, cleared || a.accumulate ? nullptr : marks, cleared ? a.out : nullptr, bytes, a.tokens64, a.count,
+                     a.rows, 0, plan.digit, plan.tiles, plan.row, plan.passes, 0};
+    const uint64_t fill_groups = !cleared ? 0 : (bytes + (64 << 10) - 1) / (64 << 10);
+    const uint32_t fill = (uint32_t)(fill_groups < 2048 ? fill_groups : 2048);
     if (a.count <= kSortOne) {
-        hipLaunchKernelGGL(k_sort_one, dim3(1), dim3(kSortOneGroup), 0, stream, sort, plan.passes);
+        const auto kernel = a.count <= kSortOneGroup ? &k_sort_one<1> : a.count <= 4 * kSortOneGroup ? &k_sort_one<4> : &k_sort_one<8>;
+        hipLaunchKernelGGL(kernel, dim3(1 + fill), dim3(kSortOneGroup), 0, stream, sort);
     } else {
         for (uint32_t p = 0; p < plan.passes; ++p) {
             sort.shift = p * plan.digit;
             sort.last = p + 1 == plan.passes;
             sort.out_keys = buffer[2 * (p & 1)];
             sort.out_places = buffer[2 * (p & 1) + 1];
-            hipLaunchKernelGGL(k_sort_count, dim3(plan.tiles), dim3(kSortGroup), 0, stream, sort);
+            hipLaunchKernelGGL(k_sort_count, dim3(plan.tiles + (p == 0 ? fill : 0u)), dim3(kSortGroup), 0, stream, sort);
             if (plan.tiles > kSumTiles) hipLaunchKernelGGL(k_sort_sum, dim3(((1u << plan.digit) + 3) / 4), dim3(256), 0, stream, sort);
             hipLaunchKernelGGL(k_sort_place, dim3(plan.tiles), dim3(kSortGroup), 0, stream, sort);
             sort.keys = sort.out_keys;
@@ -750,7 +788,7 @@ hipError_t embed_grad(const EmbedGradArgs& a, hipStream_t stream) {
     s.keys = sort.out_keys;
     s.places = sort.out_places;
     s.marks = sort.marks;
-    s.length = piece_length(a.count);
+    s.length = piece_length(a.count, a.width);
     s.pieces = (uint32_t)((a.count + (uint64_t)s.length - 1) / s.length);
     if (lanes <= 4)
         sum<T, O, 4>(s, stream);
@@ -804,7 +842,7 @@ hipError_t embed(const EmbedArgs& a, hipStream_t stream) {
 size_t embed_grad_workspace(uint32_t count, uint32_t rows, uint32_t width) {
     if (!count) return 0;
     const SortPlan plan = sort_plan(count, rows);
-    const uint32_t length = piece_length(count);
+    const uint32_t length = piece_length(count, width);
     // the gradient's type is not known here: enough for either way
     const size_t few = (size_t)few_parts(count, rows, width, true) * rows * width * 4;
     const size_t sorted = 4 * whole((size_t)count * 4) + whole(((size_t)(plan.row + 1) << plan.digit) * 4) + whole(rows) + kMaxPieces + (count + (size_t)length - 1) / length * 2 * width * 4;
