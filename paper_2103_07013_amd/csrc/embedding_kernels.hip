@@ -65,7 +65,9 @@ struct SortArgs {
     uint32_t count, rows, shift, bits, tiles, row, passes, last;
 };
 
-// Zeros into all of a.fill, 16 bytes at a time, by the threads of `groups` work-groups.
+constexpr uint32_t kFill = 4096;      // of 16 bytes
+// Zeros into all of a.fill, 16 bytes at a time, by the threads of `groups` work-groups, 64 KiB after 64 KiB: 1 GiB takes 210 us so, 255 with all
+// work-groups side by side along it, 286 so and past the caches.
 __device__ __forceinline__ void fill_zeros(const SortArgs& a, uint32_t group, uint32_t groups) {
     char* p = static_cast<char*>(a.fill);
     const uint32_t head = (uint32_t)(-reinterpret_cast<uintptr_t>(p) & 15u);
@@ -79,7 +81,8 @@ __device__ __forceinline__ void fill_zeros(const SortArgs& a, uint32_t group, ui
     if (tail + 2 * at < a.fill_bytes) *reinterpret_cast<uint16_t*>(p + tail + 2 * at) = 0;
     typedef uint32_t word __attribute__((ext_vector_type(4)));
     const word zero = {0, 0, 0, 0};
-    for (uint64_t i = at; i < words; i += threads) __builtin_nontemporal_store(zero, reinterpret_cast<word*>(p + head) + i);
+    for (uint64_t from = (uint64_t)group * kFill; from < words; from += (uint64_t)groups * kFill)
+        for (uint64_t i = from + threadIdx.x; i < words && i < from + kFill; i += blockDim.x) reinterpret_cast<word*>(p + head)[i] = zero;
 }
 
 __device__ __forceinline__ uint32_t sort_key(const SortArgs& a, uint32_t i) { return a.keys ? a.keys[i] : key_at(a.tokens, a.tokens64, i, a.rows); }
@@ -354,10 +357,10 @@ __global__ __launch_bounds__(256) void k_embed(EmbedArgs a) {
 // ---- gradient
 
 // Tokens of a piece: so many that there are about 2048 pieces, 4096 of narrow rows, which take few lanes each, so that all compute units have
-// some; but no fewer than 8, to keep partial sums few, and from 64 on as many as kMaxPieces allow.
+// some; but no fewer than 8, to keep partial sums few, and from 64 on as many as kMaxPieces allow.  Up to 32 tokens are one piece: nothing is cut.
 constexpr uint32_t kPiece = 64, kMaxPieces = 4096, kNarrow = 64;
 uint32_t piece_length(uint32_t count, uint32_t width) {
-    uint32_t n = 8;
+    uint32_t n = count <= 32 ? 32 : 8;
     while ((count + (uint64_t)n - 1) / n > (n < kPiece && width > kNarrow ? kMaxPieces / 2 : kMaxPieces)) n *= 2;
     return n;
 }
@@ -767,7 +770,7 @@ hipError_t embed_grad(const EmbedGradArgs& a, hipStream_t stream) {
     const uint64_t bytes = (uint64_t)a.rows * a.width * sizeof(typename O::raw);
     SortArgs sort = {a.tokens, nullptr, nullptr, buffer[0], buffer[1], counts, cleared || a.accumulate ? nullptr : marks, cleared ? a.out : nullptr, bytes, a.tokens64, a.count,
                      a.rows, 0, plan.digit, plan.tiles, plan.row, plan.passes, 0};
-    const uint64_t fill_groups = !cleared ? 0 : (bytes + (64 << 10) - 1) / (64 << 10);
+    const uint64_t fill_groups = !cleared ? 0 : (bytes + 16 * kFill - 1) / (16 * kFill);
     const uint32_t fill = (uint32_t)(fill_groups < 2048 ? fill_groups : 2048);
     if (a.count <= kSortOne) {
         const auto kernel = a.count <= kSortOneGroup ? &k_sort_one<1> : a.count <= 4 * kSortOneGroup ? &k_sort_one<4> : &k_sort_one<8>;

@@ -174,6 +174,7 @@ class _LogProbs(torch.autograd.Function):
         return logp, entropy, *r[2:]
 
     @staticmethod
+    @torch.autograd.function.once_differentiable
     def backward(ctx, grad_logp, grad_entropy, *_):
         logits, tokens, mask, held = ctx.saved_tensors
         plain = [None if g is None else g.to(torch.float32).contiguous() for g in (grad_logp, grad_entropy)]
@@ -251,6 +252,7 @@ class _Embedding(torch.autograd.Function):
         return _embedding(tokens, weight, scale, None)
 
     @staticmethod
+    @torch.autograd.function.once_differentiable
     def backward(ctx, grad_out):
         return None, embedding_backward(ctx.saved_tensors[0], grad_out.contiguous(), ctx.rows, ctx.scale, dtype=ctx.dtype), None
 
