@@ -216,19 +216,31 @@ __global__ __launch_bounds__(kAdamGroup) void k_adamw(AdamPlan plan, AdamGrads g
     }
 }
 
+// 8-bit states as float32: 16 consecutive blocks to a work-group, four to a wavefront.
+constexpr uint32_t kReadBlocks = 16;
 __global__ __launch_bounds__(256) void k_adamw_read(AdamPlan plan, uint64_t blocks, float* exp_avg, float* exp_avg_sq) {
-    for (uint64_t b = (uint64_t)blockIdx.x * 4 + (threadIdx.x >> 6); b < blocks; b += (uint64_t)gridDim.x * 4) {
-        const uint64_t at = b * kStateBlock + (threadIdx.x & 63u) * kPerLane;
-        const uint32_t code_m = *reinterpret_cast<const uint32_t*>(static_cast<uint8_t*>(plan.exp_avg) + at);
-        const uint32_t code_v = *reinterpret_cast<const uint32_t*>(static_cast<uint8_t*>(plan.exp_avg_sq) + at);
-        const uint32_t em = plan.exp_avg_exponent[b], ev = plan.exp_avg_sq_exponent[b];
+    constexpr uint32_t kEach = kReadBlocks / 4;
+    const uint64_t first = (uint64_t)blockIdx.x * kReadBlocks + threadIdx.x / 64 * kEach;
+    uint32_t code_m[kEach], code_v[kEach], em[kEach], ev[kEach];
+#pragma unroll
+    for (uint32_t j = 0; j < kEach; ++j) {
+        const uint64_t b = first + j < blocks ? first + j : blocks - 1, at = b * kStateBlock + (threadIdx.x & 63u) * kPerLane;
+        code_m[j] = *reinterpret_cast<const uint32_t*>(static_cast<uint8_t*>(plan.exp_avg) + at);
+        code_v[j] = *reinterpret_cast<const uint32_t*>(static_cast<uint8_t*>(plan.exp_avg_sq) + at);
+        em[j] = plan.exp_avg_exponent[b];
+        ev[j] = plan.exp_avg_sq_exponent[b];
+    }
+#pragma unroll
+    for (uint32_t j = 0; j < kEach; ++j) {
+        if (first + j >= blocks) return;
+        const uint64_t at = (first + j) * kStateBlock + (threadIdx.x & 63u) * kPerLane;
         float m[kPerLane], v[kPerLane];
 #pragma unroll
         for (uint32_t k = 0; k < kPerLane; ++k) {
-            const uint32_t cm = code_m >> (8 * k) & 255u;
-            const float x = decoded<15>(cm & 127u, em), y = decoded<31>(code_v >> (8 * k) & 255u, ev);
-            m[k] = em == 255u ? __builtin_nanf("") : cm & 128u ? -x : x;
-            v[k] = ev == 255u ? __builtin_nanf("") : y;
+            const uint32_t cm = code_m[j] >> (8 * k) & 255u;
+            const float x = decoded<15>(cm & 127u, em[j]), y = decoded<31>(code_v[j] >> (8 * k) & 255u, ev[j]);
+            m[k] = em[j] == 255u ? __builtin_nanf("") : cm & 128u ? -x : x;
+            v[k] = ev[j] == 255u ? __builtin_nanf("") : y;
         }
         store<F32, kPerLane>(exp_avg + at, m);
         store<F32, kPerLane>(exp_avg_sq + at, v);
@@ -288,8 +300,7 @@ hipError_t launch_adamw_step(int32_t param_dtype, int32_t grad_dtype, int32_t st
 }
 
 hipError_t launch_adamw_read(const AdamPlan& p, uint64_t blocks, float* exp_avg, float* exp_avg_sq, hipStream_t stream) {
-    const uint64_t g = (blocks + 3) / 4;
-    hipLaunchKernelGGL(k_adamw_read, dim3((uint32_t)(g < 16384 ? g : 16384)), dim3(256), 0, stream, p, blocks, exp_avg, exp_avg_sq);
+    hipLaunchKernelGGL(k_adamw_read, dim3((uint32_t)((blocks + kReadBlocks - 1) / kReadBlocks)), dim3(256), 0, stream, p, blocks, exp_avg, exp_avg_sq);
     return hipGetLastError();
 }
 

@@ -378,6 +378,7 @@ struct SumArgs {
     int64_t grad_stride, out_stride;
     uint32_t count, rows, width, pieces, length;
     uint32_t sum_groups, blocks;      // work-groups that add up, the others write zeros; groups of columns of a row
+    uint32_t zero_rows;
     float scale;
     int32_t accumulate, past;
     uint32_t join_bits;               // 2^join_bits lanes join 4 columns each
@@ -402,12 +403,13 @@ __device__ __forceinline__ void write_sum(const SumArgs& a, uint32_t row, uint32
     }
 }
 
-// Zeros in rows that are not marked, GROUP lanes to a row.
+// Zeros in rows that are not marked, GROUP lanes to a row; a work-group takes zero_rows rows that follow one another.
 template <class O, int GROUP>
-__device__ __forceinline__ void write_zeros(const SumArgs& a, uint32_t group, uint32_t groups) {
+__device__ __forceinline__ void write_zeros(const SumArgs& a, uint32_t group) {
     constexpr int N = O::kPer16, kRows = 256 / GROUP;
     float zero[N] = {};
-    for (uint64_t row = (uint64_t)group * kRows + threadIdx.x / GROUP; row < a.rows; row += (uint64_t)groups * kRows) {
+    const uint64_t first = (uint64_t)group * a.zero_rows, last = first + a.zero_rows < a.rows ? first + a.zero_rows : a.rows;
+    for (uint64_t row = first + threadIdx.x / GROUP; row < last; row += kRows) {
         if (a.marks && a.marks[row]) continue;      // no marks: no tokens at all
         typename O::raw* to = static_cast<typename O::raw*>(a.out) + (int64_t)row * a.out_stride;
         for (uint32_t at = threadIdx.x % GROUP * N; at < a.width; at += GROUP * N) {
@@ -419,8 +421,14 @@ __device__ __forceinline__ void write_zeros(const SumArgs& a, uint32_t group, ui
         }
     }
 }
+// How many rows that is: 64 KiB at least.
 template <class O>
-__global__ __launch_bounds__(256) void k_embed_zero(SumArgs a) { write_zeros<O, 64>(a, blockIdx.x, gridDim.x); }
+uint32_t zero_rows(uint32_t width, uint32_t together) {
+    const uint32_t bytes = width * (uint32_t)sizeof(typename O::raw), n = bytes < (64u << 10) ? (64u << 10) / bytes : 1u;
+    return (n + together - 1) / together * together;
+}
+template <class O>
+__global__ __launch_bounds__(256) void k_embed_zero(SumArgs a) { write_zeros<O, 64>(a, blockIdx.x); }
 
 // GROUP lanes for N columns each of a piece; 256 / GROUP pieces (or column blocks of one) to a work-group.  Keys and places are
 // fetched 64 at a time, rows kAhead at a time, so that that many are on their way at once.
@@ -429,7 +437,7 @@ __global__ __launch_bounds__(256) void k_embed_sum(SumArgs a) {
     constexpr int N = T::kPer16, kSlots = 256 / GROUP, kAhead = 8;
     __shared__ uint32_t keys[kSlots][kPiece + 1], places[kSlots][kPiece];
     if (blockIdx.x >= a.sum_groups) {
-        write_zeros<O, GROUP>(a, blockIdx.x - a.sum_groups, gridDim.x - a.sum_groups);
+        write_zeros<O, GROUP>(a, blockIdx.x - a.sum_groups);
         return;
     }
     const uint32_t lane = threadIdx.x % GROUP, slot = threadIdx.x / GROUP;
@@ -725,16 +733,18 @@ void sum(SumArgs s, hipStream_t stream) {
     constexpr uint32_t kSlots = 256 / GROUP;
     s.blocks = (s.width + GROUP * T::kPer16 - 1) / (GROUP * T::kPer16);
     s.sum_groups = (uint32_t)(((uint64_t)s.pieces * s.blocks + kSlots - 1) / kSlots);
-    const uint32_t zero = s.marks ? (s.rows + kSlots - 1) / kSlots : 0u;
-    hipLaunchKernelGGL((k_embed_sum<T, O, GROUP>), dim3(s.sum_groups + (zero < 4096 ? zero : 4096)), dim3(256), 0, stream, s);
+    s.zero_rows = zero_rows<O>(s.width, kSlots);
+    const uint32_t zero = s.marks ? (s.rows + s.zero_rows - 1) / s.zero_rows : 0u;
+    hipLaunchKernelGGL((k_embed_sum<T, O, GROUP>), dim3(s.sum_groups + zero), dim3(256), 0, stream, s);
 }
 
 template <class T, class O>
 hipError_t embed_grad(const EmbedGradArgs& a, hipStream_t stream) {
-    SumArgs s = {nullptr, nullptr, nullptr, a.grad, a.out, nullptr, nullptr, a.grad_stride, a.out_stride, a.count, a.rows, a.width, 0, 0, 0, 0, a.scale, a.accumulate, past_caches(a.out, a.out_stride, sizeof(typename O::raw), a.rows, a.width), 0};
+    SumArgs s = {nullptr, nullptr, nullptr, a.grad, a.out, nullptr, nullptr, a.grad_stride, a.out_stride, a.count, a.rows, a.width, 0, 0, 0, 0, 0, a.scale, a.accumulate, past_caches(a.out, a.out_stride, sizeof(typename O::raw), a.rows, a.width), 0};
     while (s.join_bits < 6 && 4u << s.join_bits < a.width) ++s.join_bits;
     if (!a.count) {
-        if (!a.accumulate) hipLaunchKernelGGL((k_embed_zero<O>), dim3((a.rows + 3) / 4 < 16384 ? (a.rows + 3) / 4 : 16384), dim3(256), 0, stream, s);
+        s.zero_rows = zero_rows<O>(a.width, 4);
+        if (!a.accumulate) hipLaunchKernelGGL((k_embed_zero<O>), dim3((a.rows + s.zero_rows - 1) / s.zero_rows), dim3(256), 0, stream, s);
         return hipGetLastError();
     }
     const uint32_t lanes = (a.width + T::kPer16 - 1) / T::kPer16;
