@@ -4,7 +4,13 @@
 // is cut into pieces of equal length, and one group of lanes walks a piece, adding up gradient rows in float32 in
 // that order.  A row that lies within one piece is written at once.  One that is cut by a piece's bounds leaves a
 // partial sum per piece, which are added in order by a second kernel.  The sort marks the rows that have a token; the others
-// are written as zeros next to the sums.
+// are written as zeros next to the sums, or all of a table that is little used is cleared next to the sort.  Tables of up to 16
+// rows need no sort: sums of all rows fit in LDS.
+//
+// What bounds it, on one MI355X (median kernel times): long batches the memory, the lookup of 262144 rows of 2048 bf16 313 us (5.3 TB/s of what it
+// moves), their sums into 131072 float32 rows 518 us (4.1 TB/s: rows are gathered from all over the batch, 4 KiB at a time), sorting 40 us, joining cut
+// rows 38 us.  Middling ones the launches one after the other, each waiting for a few memory round trips: 16384 tokens and 50257 rows
+// of 769, 23 us of sort, 32 us of sums (5.3 TB/s), 13 us of joining.  Few rows: 32768 tokens of 5 rows of 32 5.4 us and 2.9 us.
 #include "policy_device.h"
 #include "policy_kernels.h"
 
