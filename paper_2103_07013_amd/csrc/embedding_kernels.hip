@@ -11,6 +11,8 @@
 // moves), their sums into 131072 float32 rows 518 us (4.1 TB/s: rows are gathered from all over the batch, 4 KiB at a time), sorting 40 us, joining cut
 // rows 38 us.  Middling ones the launches one after the other, each waiting for a few memory round trips: 16384 tokens and 50257 rows
 // of 769, 23 us of sort, 32 us of sums (5.3 TB/s), 13 us of joining.  Few rows: 32768 tokens of 5 rows of 32 5.4 us and 2.9 us.
+#include <type_traits>
+
 #include "policy_device.h"
 #include "policy_kernels.h"
 
@@ -436,6 +438,26 @@ uint32_t zero_rows(uint32_t width, uint32_t together) {
 template <class O>
 __global__ __launch_bounds__(256) void k_embed_zero(SumArgs a) { write_zeros<O, 64>(a, blockIdx.x); }
 
+// 16 bytes of AHEAD rows, of which `left` columns are the row's, as they lie there: all loads are on their way before the first value is converted.  (A
+// load and its conversion under one condition are waited for there: 519 instead of 429 us for 262144 rows of 2048 bf16.)
+template <class T, int AHEAD>
+__device__ __forceinline__ void rows_ahead(const typename T::raw* const (&g)[AHEAD], uint32_t left, Words (&x)[AHEAD]) {
+    constexpr int N = T::kPer16, kInWord = N / 4;
+    using bits = std::conditional_t<kInWord == 1, uint32_t, uint16_t>;
+    if (left >= (uint32_t)N) {
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) x[u] = load_words<T>(g[u]);
+    } else {
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) x[u] = Words{0, 0, 0, 0};
+#pragma unroll
+        for (int k = 0; k < N - 1; ++k)
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u)
+                x[u][k / kInWord] |= (uint32_t)((uint32_t)k < left ? __builtin_bit_cast(bits, g[u][k]) : bits(0)) << (16 * (k % kInWord));
+    }
+}
+
 // GROUP lanes for N columns each of a piece; 256 / GROUP pieces (or column blocks of one) to a work-group.  Keys and places are
 // fetched 64 at a time, rows kAhead at a time, so that that many are on their way at once.
 template <class T, class O, int GROUP>
@@ -470,24 +492,19 @@ __global__ __launch_bounds__(256) void k_embed_sum(SumArgs a) {
         __syncthreads();
         if (at >= a.width) continue;
         for (uint32_t j = 0; j < n; j += kAhead) {
-            float x[kAhead][N];
+            Words x[kAhead];
+            const typename T::raw* g[kAhead];
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u) {
-                const typename T::raw* g = static_cast<const typename T::raw*>(a.grad) + (j + u < n ? (int64_t)places[slot][j + u] * a.grad_stride : 0) + at;
-                if (at + N <= a.width) {
-                    load<T, N>(g, x[u]);
-                } else {
-#pragma unroll
-                    for (int k = 0; k < N; ++k) x[u][k] = at + k < a.width ? to_float(g[k]) : 0.0f;
-                }
-            }
+            for (int u = 0; u < kAhead; ++u)
+                g[u] = static_cast<const typename T::raw*>(a.grad) + (j + u < n ? (int64_t)places[slot][j + u] * a.grad_stride : 0) + at;
+            rows_ahead<T, kAhead>(g, a.width - at, x);
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
                 if (j + u >= n) continue;
                 const uint32_t key = keys[slot][j + u];
                 if (key >= a.rows) continue;
 #pragma unroll
-                for (int k = 0; k < N; ++k) sum[k] += x[u][k];
+                for (int k = 0; k < N; ++k) sum[k] += word_float<T>(x[u], k);
                 const bool ends = keys[slot][j + u + 1] != key;
                 if (!ends && base + j + u + 1 != end) continue;
                 if (ends && !began_before) {
@@ -655,26 +672,22 @@ __global__ __launch_bounds__(256) void k_embed_few(FewArgs a) {
     const uint32_t each = (a.length + kSlots - 1) / kSlots, from = first + slot * each < last ? first + slot * each : last, to = last - from < each ? last : from + each;
     if (at < a.width) {
         for (uint32_t i = from; i < to; i += kAhead) {
-            float x[kAhead][N];
+            Words x[kAhead];
             int64_t t[kAhead];
+            const typename T::raw* g[kAhead];
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
                 const uint32_t n = i + u < to ? i + u : i;
                 t[u] = i + u < to ? token_at(a.tokens, a.tokens64, n) : -1;
-                const typename T::raw* g = static_cast<const typename T::raw*>(a.grad) + (int64_t)n * a.grad_stride + at;
-                if (at + N <= a.width) {
-                    load<T, N>(g, x[u]);
-                } else {
-#pragma unroll
-                    for (int k = 0; k < N; ++k) x[u][k] = at + k < a.width ? to_float(g[k]) : 0.0f;
-                }
+                g[u] = static_cast<const typename T::raw*>(a.grad) + (int64_t)n * a.grad_stride + at;
             }
+            rows_ahead<T, kAhead>(g, a.width - at, x);
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
                 if (t[u] < 0 || t[u] >= (int64_t)a.rows) continue;
                 float* sum = sums + ((uint32_t)t[u] * 256 + threadIdx.x) * N;
 #pragma unroll
-                for (int k = 0; k < N; ++k) sum[k] += x[u][k];
+                for (int k = 0; k < N; ++k) sum[k] += word_float<T>(x[u], k);
             }
         }
     }

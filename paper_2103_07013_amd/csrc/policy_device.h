@@ -48,6 +48,18 @@ __device__ __forceinline__ void load(const typename T::raw* p, float (&x)[N]) {
 #pragma unroll
     for (int k = 0; k < N; ++k) x[k] = to_float(q.v[k]);
 }
+// The same as they lie in memory, for loads that are to be on their way before the first value is converted.
+typedef uint32_t Words __attribute__((ext_vector_type(4)));
+typedef Words WordsAnywhere __attribute__((aligned(2)));
+template <class T>
+__device__ __forceinline__ Words load_words(const typename T::raw* p) { return *reinterpret_cast<const WordsAnywhere*>(p); }
+template <class T>
+__device__ __forceinline__ float word_float(const Words& w, int k) {
+    if constexpr (sizeof(typename T::raw) == 4)
+        return __uint_as_float(w[k]);
+    else
+        return to_float(__builtin_bit_cast(typename T::raw, (uint16_t)(w[k / 2] >> (16 * (k % 2)))));
+}
 template <class T, int N>
 __device__ __forceinline__ void store(typename T::raw* p, const float (&x)[N]) {
     Pack<typename T::raw, N> q;

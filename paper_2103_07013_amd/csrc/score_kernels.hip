@@ -9,9 +9,9 @@
 // grows, so that one pass over the logits is enough; lanes, wavefronts and pieces of a row are joined by the same rule.  m and ln z are kept
 // apart for the gradient: their sum, lse, loses ln z where logits are large (rows of a type's lowest value).
 //
-// What bounds it, on one MI355X (median kernel times): long rows the memory, 8192 x 131072 bf16 in 370 us (5.8 TB/s, with what the Infinity Cache still
-// holds) and their gradient in 770 us (5.6 TB/s of 4.3 GB); about ten vector instructions and one exponential an entry take a third of
-// that.  Short rows the launch: 32768 x 6 float32 3.5 us, the gradient 3.1.  Alternatives cost what ordering the candidates costs: 192 x 50257 f16 with 5 of them
+// What bounds it, on one MI355X (median kernel times): long rows the memory, 8192 x 131072 bf16 in 361 us (5.9 TB/s, with what the Infinity Cache still
+// holds) and their gradient in 737 us (5.8 TB/s of 4.3 GB); the pass itself is near the vector units' limit too, with nine instructions and one
+// exponential (four times the issue slots) an entry.  Short rows the launch: 32768 x 6 float32 3.5 us, the gradient 3.1.  Alternatives cost what ordering the candidates costs: 192 x 50257 f16 with 5 of them
 // 17 us, 10 without; 1 x 131072 with 20 in pieces 7 us and their join 5.
 #include "policy_device.h"
 #include "policy_kernels.h"
@@ -75,6 +75,35 @@ __device__ __forceinline__ void row_entries(const typename T::raw* row, const ui
     } else {
 #pragma unroll
         for (int k = 0; k < N; ++k) x[k] = at + k < end && (!MASK || mask[at + k]) ? to_float(row[at + k]) : -kInf;
+    }
+}
+
+// U times N entries of a row, the u-th from first + u * apart + lane * N on; `all`: the same for all lanes of the wavefront, says that none of them lies behind
+// the row's end.  Loads under a condition of their own would each be waited for before the next.
+template <class T, int U, int N, bool MASK>
+__device__ __forceinline__ void row_blocks(const typename T::raw* row, const uint8_t* mask, uint32_t first, uint32_t apart, uint32_t lane, uint32_t end, bool all, float (&x)[U * N]) {
+    if (all) {
+        Pack<typename T::raw, N> q[U];
+        Pack<uint8_t, N> may[MASK ? U : 1];
+#pragma unroll
+        for (int u = 0; u < U; ++u) q[u] = *reinterpret_cast<const Pack<typename T::raw, N>*>(row + first + u * apart + lane * N);
+        if (MASK) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) may[u] = *reinterpret_cast<const Pack<uint8_t, N>*>(mask + first + u * apart + lane * N);
+        }
+#pragma unroll
+        for (int e = 0; e < U * N; ++e) {
+            const float y = to_float(q[e / N].v[e % N]);
+            x[e] = !MASK || may[e / N].v[e % N] ? y : -kInf;
+        }
+        return;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        float y[N];
+        row_entries<T, N, MASK>(row, mask, first + u * apart + lane * N, end, y);
+#pragma unroll
+        for (int e = 0; e < N; ++e) x[u * N + e] = y[e];
     }
 }
 
@@ -302,13 +331,7 @@ __device__ __forceinline__ Part stream(const typename T::raw* row, const uint8_t
     bool first = true;
     for (uint32_t base = from; base < to; base += kThreads * N * U) {
         float x[U * N];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            float y[N];
-            row_entries<T, N, MASK>(row, mask, base + (u * kThreads + tid) * N, to, y);
-#pragma unroll
-            for (int e = 0; e < N; ++e) x[u * N + e] = y[e];
-        }
+        row_blocks<T, U, N, MASK>(row, mask, base, kThreads * N, tid, to, base + kThreads * N * U <= to, x);
         const float top = add(p, x, c);
         if constexpr (TOP) {
             if (first) {
@@ -439,29 +462,42 @@ __global__ __launch_bounds__(TOP ? 1024 : 64) void k_score_join(ScoreArgs a, Pie
 
 // ---- gradient
 
+// With l = log2 p_j = c (x_j - m) - log2 z, the gradient is p_j (slope l + base), and token_grad more for the token's entry.  An entry that takes no
+// part has p = 0 and so the gradient 0, but where the row's numbers are not finite: odd, where that has to be asked for.
 struct RowGrad {
-    float m, ln_z, gl, gh, base;
+    float m, log2_z, slope, base, token_grad;
     int64_t t;
+    bool odd;
 };
 __device__ __forceinline__ RowGrad row_grad(const ScoreGradArgs& a, uint64_t r) {
     RowGrad g;
     g.m = a.largest[r];
-    g.ln_z = a.ln_z[r];
+    const float ln_z = a.ln_z[r];
+    g.log2_z = ln_z == -kInf ? 0.0f : ln_z * kLog2e;      // nothing takes part: all entries are -inf
     g.t = token_at(a.tokens, a.tokens64, r);
-    g.gh = a.grad_entropy ? a.grad_entropy[r] : 0.0f;
-    g.gl = !a.grad_logp || g.t == -1 || a.logp[r] == -kInf ? 0.0f : g.t < -1 || g.t >= (int64_t)a.entries ? __builtin_nanf("") : a.grad_logp[r];
-    g.base = fmaf(g.gh, a.entropy[r], g.gl);
+    const float gh = a.grad_entropy ? a.grad_entropy[r] : 0.0f;
+    const float gl = !a.grad_logp || g.t == -1 || a.logp[r] == -kInf ? 0.0f : g.t < -1 || g.t >= (int64_t)a.entries ? __builtin_nanf("") : a.grad_logp[r];
+    g.slope = -gh * a.scale * kLn2;
+    g.base = -fmaf(gh, a.entropy[r], gl) * a.scale;
+    g.token_grad = gl * a.scale;
+    g.odd = !(fabsf(g.log2_z) < kInf && fabsf(g.slope) < kInf && fabsf(g.base) < kInf);
     return g;
 }
 template <int N>
-__device__ __forceinline__ void gradient(const RowGrad& g, float scale, uint32_t at, const float (&x)[N], float (&d)[N]) {
+__device__ __forceinline__ void gradient(const RowGrad& g, float c, uint32_t at, const float* x, float (&d)[N]) {
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-        const float lp = fmaf(x[k] - g.m, scale, -g.ln_z);
-        const float p = __builtin_amdgcn_exp2f(lp * kLog2e);
-        d[k] = -p * fmaf(g.gh, lp, g.base);
-        if (at + k == (uint64_t)g.t) d[k] += g.gl;
-        d[k] = x[k] == -kInf ? 0.0f : d[k] * scale;
+        const float l = fmaf(x[k] - g.m, c, -g.log2_z);
+        d[k] = __builtin_amdgcn_exp2f(l) * fmaf(g.slope, fmaxf(l, kFar), g.base);
+    }
+    if ((uint64_t)g.t - at < (uint64_t)N) {
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+            if (at + k == (uint64_t)g.t && x[k] != -kInf) d[k] += g.token_grad;
+    }
+    if (g.odd) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) d[k] = x[k] == -kInf ? 0.0f : d[k];
     }
 }
 template <class T, int N>
@@ -483,7 +519,7 @@ __global__ __launch_bounds__(256) void k_score_grad_short(ScoreGradArgs a) {
     const RowGrad g = row_grad(a, r);
     float x[N], d[N];
     row_entries<T, N, MASK>(static_cast<const typename T::raw*>(a.logits) + (int64_t)r * a.row_stride, MASK ? a.mask + (int64_t)r * a.mask_stride : nullptr, lane * N, a.entries, x);
-    gradient(g, a.scale, lane * N, x, d);
+    gradient<N>(g, a.scale * kLog2e, lane * N, x, d);
     store_entries<T, N>(static_cast<typename T::raw*>(a.out) + (int64_t)r * a.out_stride, lane * N, a.entries, d, false);
 }
 
@@ -497,13 +533,13 @@ __global__ __launch_bounds__(GROUP) void k_score_grad(ScoreGradArgs a, uint32_t 
     const typename T::raw* row = static_cast<const typename T::raw*>(a.logits) + (int64_t)r * a.row_stride;
     const uint8_t* mask = MASK ? a.mask + (int64_t)r * a.mask_stride : nullptr;
     typename T::raw* out = static_cast<typename T::raw*>(a.out) + (int64_t)r * a.out_stride;
-    float x[U][N], d[N];
-#pragma unroll
-    for (int u = 0; u < U; ++u) row_entries<T, N, MASK>(row, mask, from + (u * GROUP + threadIdx.x) * N, a.entries, x[u]);
+    const float c = a.scale * kLog2e;
+    float x[U * N], d[N];
+    row_blocks<T, U, N, MASK>(row, mask, from, GROUP * N, threadIdx.x, a.entries, from + GROUP * N * U <= a.entries, x);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const uint32_t at = from + (u * GROUP + threadIdx.x) * N;
-        gradient(g, a.scale, at, x[u], d);
+        gradient<N>(g, c, at, x + u * N, d);
         store_entries<T, N>(out, at, a.entries, d, a.past != 0);
     }
 }
@@ -513,20 +549,22 @@ __global__ __launch_bounds__(GROUP) void k_score_grad(ScoreGradArgs a, uint32_t 
 // Rows of up to this many entries are shared by few lanes, longer ones by a wavefront at least.
 constexpr uint32_t kShort = 128;
 // Rows of up to kWaveRow entries have one wavefront, where there are kWaveRows rows or more those of up to kLongWaveRow too.  Measured
-// with bf16, one wavefront / four: 4096 x 2048 6.4 / 14.8 us, 4096 x 4096 9.8 / 15.1, 4096 x 8192 17.4 / 18.3, 512 x 4096 5.3 / 5.2, 1024 x 8192 8.7 / 6.4.
+// with bf16, one wavefront / four: 4096 x 2048 6.0 / 14.6 us, 4096 x 4096 8.5 / 14.9, 4096 x 8192 15.1 / 15.4, 512 x 4096 4.3 / 5.2 (with 20
+// alternatives 10.0 / 8.9), 1024 x 8192 6.3 / 6.1 (16.1 / 12.4).
 constexpr uint32_t kWaveRow = 2048, kLongWaveRow = 8192, kWaveRows = 2048;
-// Longer ones have four wavefronts, or sixteen where they are longer than kLongWaveRow and fewer than kFewRows.  Four / sixteen:
-// 64 x 8192 4.2 / 6.3 us, 1 x 32768 7.1 / 5.6, 192 x 50257 11.4 / 9.7, 512 x 131072 35.3 / 27.2, 1024 x 50257 24.1 / 27.5.
-constexpr uint32_t kFewRows = 1024;
-// Of up to kPieceRows rows, those longer than kLongRow are cut, so that there are about kGroups pieces of not less than 4096 entries.
-// Sixteen wavefronts / pieces: 1 x 32768 5.6 / 5.9 us, 1 x 131072 12.0 / 6.1, 32 x 131072 12.5 / 7.1, 64 x 50257 9.5 / 7.4, 128 x 50257 9.6 / 8.9 (with
-// 20 alternatives 18.4 / 19.4), 192 x 50257 9.7 / 10.5.
-constexpr uint32_t kPieceRows = 64, kLongRow = 32768, kGroups = 512;
+// Longer ones have four wavefronts, or sixteen where they are longer than kLongWaveRow and there is a compute unit for each row.  Four / sixteen, and
+// with 20 alternatives: 64 x 8192 3.8 / 6.2 us, 192 x 50257 9.2 / 9.0 (20.0 / 15.9), 256 x 131072 18.0 / 15.8 (36.8 / 25.6), 384 x 50257 13.5 / 14.7
+// (24.5 / 29.1), 512 x 131072 23.7 / 27.8 (43.4 / 45.9).
+constexpr uint32_t kComputeUnits = 256;
+// Of up to kPieceRows rows, those longer than kLongRow are cut, so that there are up to kGroups pieces of not less than kPieceEntries, what a work-group
+// loads at once.  Sixteen wavefronts / pieces: 1 x 32768 5.4 / 5.2 us (9.9 / 11.2), 1 x 131072 11.2 / 5.5 (21.0 / 11.2), 32 x 131072 11.6 / 6.6
+// (21.8 / 12.9), 64 x 50257 8.7 / 7.4 (15.3 / 13.6), 128 x 50257 8.9 / 8.4 (15.5 / 16.1).
+constexpr uint32_t kPieceRows = 64, kLongRow = 32768, kGroups = 512, kPieceEntries = 8192;
 
 Pieces pieces_of(uint64_t rows, uint32_t entries) {
     if (entries <= kLongRow || rows > kPieceRows || rows == 0) return {1, entries};
     uint32_t n = kGroups / (uint32_t)rows;
-    const uint32_t most = entries / 4096;
+    const uint32_t most = (entries + kPieceEntries - 1) / kPieceEntries;
     if (n > most) n = most;
     if (n > kMaxPieces) n = kMaxPieces;
     const uint32_t length = ((entries + n - 1) / n + 63) / 64 * 64;
@@ -553,7 +591,7 @@ hipError_t score(const ScoreArgs& a, hipStream_t stream) {
         hipLaunchKernelGGL((k_score_join<T, TOP>), dim3((uint32_t)a.rows), dim3(TOP ? 1024 : 64), 0, stream, a, pieces, sums, lists);
     } else if (a.entries <= (a.rows < kWaveRows ? kWaveRow : kLongWaveRow)) {
         BPS_ROWS(k_score, 4, 256, TOP, 1);
-    } else if (a.entries <= kLongWaveRow || a.rows >= kFewRows) {
+    } else if (a.entries <= kLongWaveRow || a.rows > kComputeUnits) {
         BPS_ROWS(k_score, 1, 256, TOP, 4);
     } else {
         BPS_ROWS(k_score, 1, 1024, TOP, 16);
