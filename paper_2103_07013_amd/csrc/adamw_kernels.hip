@@ -16,9 +16,9 @@ namespace bps {
 
 namespace {
 
-constexpr uint32_t kPerLane = 4, kStep = kAdamGroup * kPerLane;
+constexpr uint32_t kPerLane = 4;
 static_assert(kStateBlock == 64 * kPerLane, "a wavefront's elements share an exponent");
-static_assert(kAdamChunk % kStep == 0, "a chunk is whole steps");
+static_assert(kAdamChunk == kAdamGroup * kPerLane, "a chunk is what a work-group takes at once");
 
 // 8-bit codes are the upper bits of a float32 with a bias of their own: shifted to where those are, subnormal ones included, a code is a float that
 // is a power of two away from what it stands for.  e: the block's exponent byte.
@@ -48,33 +48,37 @@ __device__ __forceinline__ uint32_t wave_max_of_halves(uint32_t x) {
     });
 }
 
-// Sums of squares: each work-group those of every gridDim.x-th chunk.
+// Sums of squares: each work-group those of every gridDim.x-th four chunks, so that four loads are on their way at once.
 template <class G>
 __global__ __launch_bounds__(kAdamGroup) void k_adamw_norm(AdamPlan plan, AdamGrads grads, uint32_t first_tensor, uint32_t first_chunk, uint32_t chunks, uint32_t first_sum,
                                                            AdamScalars s) {
     __shared__ float sums[kAdamGroup / 64];
-    constexpr uint32_t kLoads = kAdamChunk / kStep;
-    const uint32_t tid = threadIdx.x;
+    constexpr uint32_t kTogether = 4;
+    const uint32_t tid = threadIdx.x, i = tid * kPerLane;
     float sum = 0.0f;
-    for (uint32_t c = blockIdx.x; c < chunks; c += gridDim.x) {
-        const AdamChunk chunk = plan.chunks[first_chunk + c];
-        const typename G::raw* g = static_cast<const typename G::raw*>(grads.at[chunk.tensor - first_tensor]);
-        if (!g) continue;
-        const uint64_t from = (uint64_t)chunk.index * kAdamChunk, left = plan.tensors[chunk.tensor].count - from;
-        const uint32_t n = left < kAdamChunk ? (uint32_t)left : kAdamChunk;
-        float x[kLoads][kPerLane];
+    for (uint32_t c = blockIdx.x * kTogether; c < chunks; c += gridDim.x * kTogether) {
+        const typename G::raw* g[kTogether];
+        uint32_t n[kTogether];
 #pragma unroll
-        for (uint32_t u = 0; u < kLoads; ++u) {
-            const uint32_t i = u * kStep + tid * kPerLane;
-            if (i + kPerLane <= n) {
-                load<G, kPerLane>(g + from + i, x[u]);
+        for (uint32_t u = 0; u < kTogether; ++u) {
+            const AdamChunk chunk = plan.chunks[first_chunk + (c + u < chunks ? c + u : c)];
+            const uint64_t from = (uint64_t)chunk.index * kAdamChunk, left = plan.tensors[chunk.tensor].count - from;
+            const typename G::raw* grad = static_cast<const typename G::raw*>(grads.at[chunk.tensor - first_tensor]);
+            n[u] = !grad || c + u >= chunks ? 0u : left < kAdamChunk ? (uint32_t)left : kAdamChunk;
+            g[u] = grad ? grad + from : nullptr;
+        }
+        float x[kTogether][kPerLane];
+#pragma unroll
+        for (uint32_t u = 0; u < kTogether; ++u) {
+            if (i + kPerLane <= n[u]) {
+                load<G, kPerLane>(g[u] + i, x[u]);
             } else {
 #pragma unroll
-                for (uint32_t k = 0; k < kPerLane; ++k) x[u][k] = i + k < n ? to_float(g[from + i + k]) : 0.0f;
+                for (uint32_t k = 0; k < kPerLane; ++k) x[u][k] = i + k < n[u] ? to_float(g[u][i + k]) : 0.0f;
             }
         }
 #pragma unroll
-        for (uint32_t u = 0; u < kLoads; ++u)
+        for (uint32_t u = 0; u < kTogether; ++u)
 #pragma unroll
             for (uint32_t k = 0; k < kPerLane; ++k) {
                 const float y = x[u][k] * s.grad_scale;
@@ -123,102 +127,101 @@ __global__ __launch_bounds__(kAdamGroup) void k_adamw(AdamPlan plan, AdamGrads g
     const AdamTensor t = plan.tensors[chunk.tensor];
     const float keep = (float)(1.0 - s.lr * t.lr_scale * t.weight_decay), step_size = (float)(s.step_size * t.lr_scale);
     const uint64_t from = (uint64_t)chunk.index * kAdamChunk, left = t.count - from;
-    const uint32_t n = left < kAdamChunk ? (uint32_t)left : kAdamChunk;
-    for (uint32_t i = threadIdx.x * kPerLane; i / kStateBlock * kStateBlock < n; i += kStep) {
-        const uint64_t at = from + i, state = t.start + at;
-        const uint32_t live = i >= n ? 0u : n - i < kPerLane ? n - i : kPerLane;
-        float x[kPerLane], w[kPerLane], m[kPerLane], v[kPerLane];
-        typename P::raw* param = static_cast<typename P::raw*>(t.param) + at;
-        float* weight = kMaster ? t.master + at : reinterpret_cast<float*>(t.param) + at;
-        if (live == kPerLane) {
-            load<G, kPerLane>(g + at, x);
-            load<F32, kPerLane>(weight, w);
-        } else {
-#pragma unroll
-            for (uint32_t k = 0; k < kPerLane; ++k) {
-                x[k] = k < live ? to_float(g[at + k]) : 0.0f;
-                w[k] = k < live ? weight[k] : 0.0f;
-            }
-        }
-        uint32_t code_m = 0, code_v = 0;
-        if (BITS == 32) {
-            // a state block belongs to one tensor, so that all four are this lane's
-            load<F32, kPerLane>(static_cast<float*>(plan.exp_avg) + state, m);
-            load<F32, kPerLane>(static_cast<float*>(plan.exp_avg_sq) + state, v);
-        } else {
-            code_m = *reinterpret_cast<const uint32_t*>(static_cast<uint8_t*>(plan.exp_avg) + state);
-            code_v = *reinterpret_cast<const uint32_t*>(static_cast<uint8_t*>(plan.exp_avg_sq) + state);
-            // one block for the whole wavefront
-            const uint32_t em = __builtin_amdgcn_readfirstlane(plan.exp_avg_exponent[state / kStateBlock]);
-            const uint32_t ev = __builtin_amdgcn_readfirstlane(plan.exp_avg_sq_exponent[state / kStateBlock]);
-#pragma unroll
-            for (uint32_t k = 0; k < kPerLane; ++k) {
-                const uint32_t cm = code_m >> (8 * k) & 255u, cv = code_v >> (8 * k) & 255u;
-                m[k] = __uint_as_float(__float_as_uint(decoded<15>(cm & 127u, em)) | (cm & 128u) << 24);
-                v[k] = decoded<31>(cv, ev);
-            }
-            if (em == 255u || ev == 255u) {
-#pragma unroll
-                for (uint32_t k = 0; k < kPerLane; ++k) {
-                    if (em == 255u) m[k] = __builtin_nanf("");
-                    if (ev == 255u) v[k] = __builtin_nanf("");
-                }
-            }
-            if (live != kPerLane) {      // behind the tensor's end: no part of the block's largest
-#pragma unroll
-                for (uint32_t k = 0; k < kPerLane; ++k)
-                    if (k >= live) m[k] = v[k] = 0.0f;
-            }
-        }
+    const uint32_t n = left < kAdamChunk ? (uint32_t)left : kAdamChunk, i = threadIdx.x * kPerLane;
+    if (i / kStateBlock * kStateBlock >= n) return;      // whole wavefronts: a state block belongs to one tensor
+    const uint64_t at = from + i, state = t.start + at;
+    const uint32_t live = i >= n ? 0u : n - i < kPerLane ? n - i : kPerLane;
+    float x[kPerLane], w[kPerLane], m[kPerLane], v[kPerLane];
+    typename P::raw* param = static_cast<typename P::raw*>(t.param) + at;
+    float* weight = kMaster ? t.master + at : reinterpret_cast<float*>(t.param) + at;
+    if (live == kPerLane) {
+        load<G, kPerLane>(g + at, x);
+        load<F32, kPerLane>(weight, w);
+    } else {
 #pragma unroll
         for (uint32_t k = 0; k < kPerLane; ++k) {
-            x[k] = x[k] * s.grad_scale;
-            if (CLIP) x[k] = x[k] * clip;
-            m[k] = m[k] * s.beta1 + x[k] * s.one_minus_beta1;
-            v[k] = v[k] * s.beta2 + x[k] * s.one_minus_beta2 * x[k];
-            w[k] = w[k] * keep - m[k] / (sqrtf(v[k]) * s.root_c2 + s.eps) * step_size;
+            x[k] = k < live ? to_float(g[at + k]) : 0.0f;
+            w[k] = k < live ? weight[k] : 0.0f;
         }
-        if (live == kPerLane) {
-            store<F32, kPerLane>(weight, w);
-            if (kMaster) store<P, kPerLane>(param, w);
-        } else {
+    }
+    uint32_t code_m = 0, code_v = 0;
+    if (BITS == 32) {
+        // a state block belongs to one tensor, so that all four are this lane's
+        load<F32, kPerLane>(static_cast<float*>(plan.exp_avg) + state, m);
+        load<F32, kPerLane>(static_cast<float*>(plan.exp_avg_sq) + state, v);
+    } else {
+        code_m = *reinterpret_cast<const uint32_t*>(static_cast<uint8_t*>(plan.exp_avg) + state);
+        code_v = *reinterpret_cast<const uint32_t*>(static_cast<uint8_t*>(plan.exp_avg_sq) + state);
+        // one block for the whole wavefront
+        const uint32_t em = __builtin_amdgcn_readfirstlane(plan.exp_avg_exponent[state / kStateBlock]);
+        const uint32_t ev = __builtin_amdgcn_readfirstlane(plan.exp_avg_sq_exponent[state / kStateBlock]);
+#pragma unroll
+        for (uint32_t k = 0; k < kPerLane; ++k) {
+            const uint32_t cm = code_m >> (8 * k) & 255u, cv = code_v >> (8 * k) & 255u;
+            m[k] = __uint_as_float(__float_as_uint(decoded<15>(cm & 127u, em)) | (cm & 128u) << 24);
+            v[k] = decoded<31>(cv, ev);
+        }
+        if (em == 255u || ev == 255u) {
+#pragma unroll
+            for (uint32_t k = 0; k < kPerLane; ++k) {
+                if (em == 255u) m[k] = __builtin_nanf("");
+                if (ev == 255u) v[k] = __builtin_nanf("");
+            }
+        }
+        if (live != kPerLane) {      // behind the tensor's end: no part of the block's largest
 #pragma unroll
             for (uint32_t k = 0; k < kPerLane; ++k)
-                if (k < live) {
-                    weight[k] = w[k];
-                    if (kMaster) param[k] = rounded<P>(w[k]);
-                }
+                if (k >= live) m[k] = v[k] = 0.0f;
         }
-        if (BITS == 32) {
-            if (live) {
-                store<F32, kPerLane>(static_cast<float*>(plan.exp_avg) + state, m);
-                store<F32, kPerLane>(static_cast<float*>(plan.exp_avg_sq) + state, v);
-            }
-        } else {
-            uint32_t largest_m = 0, largest_v = 0;
+    }
 #pragma unroll
-            for (uint32_t k = 0; k < kPerLane; ++k) {
-                const uint32_t bm = __float_as_uint(m[k]) & 0x7FFFFFFFu, bv = __float_as_uint(v[k]) & 0x7FFFFFFFu;
-                largest_m = bm > largest_m ? bm : largest_m;
-                largest_v = bv > largest_v ? bv : largest_v;
-            }
-            const uint32_t both = __builtin_amdgcn_readfirstlane(wave_max_of_halves(exponent_for<20>(largest_m) | exponent_for<36>(largest_v) << 16));
-            const uint32_t em = both & 0xFFFFu, ev = both >> 16;
-            code_m = code_v = 0;
+    for (uint32_t k = 0; k < kPerLane; ++k) {
+        x[k] = x[k] * s.grad_scale;
+        if (CLIP) x[k] = x[k] * clip;
+        m[k] = m[k] * s.beta1 + x[k] * s.one_minus_beta1;
+        v[k] = v[k] * s.beta2 + x[k] * s.one_minus_beta2 * x[k];
+        w[k] = w[k] * keep - m[k] / (sqrtf(v[k]) * s.root_c2 + s.eps) * step_size;
+    }
+    if (live == kPerLane) {
+        store<F32, kPerLane>(weight, w);
+        if (kMaster) store<P, kPerLane>(param, w);
+    } else {
 #pragma unroll
-            for (uint32_t k = 0; k < kPerLane; ++k) {
-                const uint32_t h = mixed(((uint32_t)(state + k) * kGolden) ^ s.key);
-                code_m |= (encoded<15>(fabsf(m[k]), em, h & 0xFFFFu) | (m[k] < 0.0f ? 128u : 0u)) << (8 * k);
-                code_v |= encoded<31>(v[k], ev, h >> 16) << (8 * k);
+        for (uint32_t k = 0; k < kPerLane; ++k)
+            if (k < live) {
+                weight[k] = w[k];
+                if (kMaster) param[k] = rounded<P>(w[k]);
             }
-            if (em == 255u) code_m = 0;
-            if (ev == 255u) code_v = 0;
-            *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(plan.exp_avg) + state) = code_m;
-            *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(plan.exp_avg_sq) + state) = code_v;
-            if ((threadIdx.x & 63u) == 0) {
-                plan.exp_avg_exponent[state / kStateBlock] = (uint8_t)em;
-                plan.exp_avg_sq_exponent[state / kStateBlock] = (uint8_t)ev;
-            }
+    }
+    if (BITS == 32) {
+        if (live) {
+            store<F32, kPerLane>(static_cast<float*>(plan.exp_avg) + state, m);
+            store<F32, kPerLane>(static_cast<float*>(plan.exp_avg_sq) + state, v);
+        }
+    } else {
+        uint32_t largest_m = 0, largest_v = 0;
+#pragma unroll
+        for (uint32_t k = 0; k < kPerLane; ++k) {
+            const uint32_t bm = __float_as_uint(m[k]) & 0x7FFFFFFFu, bv = __float_as_uint(v[k]) & 0x7FFFFFFFu;
+            largest_m = bm > largest_m ? bm : largest_m;
+            largest_v = bv > largest_v ? bv : largest_v;
+        }
+        const uint32_t both = __builtin_amdgcn_readfirstlane(wave_max_of_halves(exponent_for<20>(largest_m) | exponent_for<36>(largest_v) << 16));
+        const uint32_t em = both & 0xFFFFu, ev = both >> 16;
+        code_m = code_v = 0;
+#pragma unroll
+        for (uint32_t k = 0; k < kPerLane; ++k) {
+            const uint32_t h = mixed(((uint32_t)(state + k) * kGolden) ^ s.key);
+            code_m |= (encoded<15>(fabsf(m[k]), em, h & 0xFFFFu) | (m[k] < 0.0f ? 128u : 0u)) << (8 * k);
+            code_v |= encoded<31>(v[k], ev, h >> 16) << (8 * k);
+        }
+        if (em == 255u) code_m = 0;
+        if (ev == 255u) code_v = 0;
+        *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(plan.exp_avg) + state) = code_m;
+        *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(plan.exp_avg_sq) + state) = code_v;
+        if ((threadIdx.x & 63u) == 0) {
+            plan.exp_avg_exponent[state / kStateBlock] = (uint8_t)em;
+            plan.exp_avg_sq_exponent[state / kStateBlock] = (uint8_t)ev;
         }
     }
 }

@@ -238,7 +238,7 @@ bps_status bps_adamw_step(bps_adamw* h, const void* const* grads, int32_t grad_d
             const uint32_t chunk = h->first_chunk[first], chunks = h->first_chunk[first + n] - chunk;
             hipError_t e;
             if (pass == 0) {
-                const uint32_t groups = chunks < h->sums ? chunks : h->sums;
+                const uint32_t groups = (chunks + 3) / 4 < h->sums ? (chunks + 3) / 4 : h->sums;      // four chunks at a time each
                 e = bps::launch_adamw_norm(grad_dtype, h->plan, g, first, chunk, chunks, s.partials, groups, s, static_cast<hipStream_t>(stream));
                 s.partials += groups;
             } else {
