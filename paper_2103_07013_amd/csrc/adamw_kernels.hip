@@ -5,10 +5,10 @@
 // compute units busy and a launch takes up to kAdamGrads of them.  A lane takes four elements at a time, a wavefront the 256 of a state block,
 // whose largest magnitudes are found across its lanes (both at once, as the halves of one word).
 //
-// What bounds it, on one MI355X (median kernel times): the memory.  4e8 float32 parameters 2.10 ms (5.3 TB/s of the 28 bytes each has to move; a copy reaches
-// 4.9); 1.2e8 bf16 ones with float32 masters and 8-bit states 375 us (5.1 TB/s of 16 bytes each), at 41 % of the vector units' issue
-// slots: the exact root and quotient, three products of the hash and the codes take about 90 instructions an element; read back 213 us
-// (5.6 TB/s).  5.3e6 parameters in 38 tensors with a bound on the norm 6 and 26 us.
+// What bounds it, on one MI355X (median kernel times): the memory.  4e8 float32 parameters 2.03 ms (5.5 TB/s of the 28 bytes each has to move; a copy reaches
+// 4.9); 1.2e8 bf16 ones with float32 masters and 8-bit states 333 us (5.8 TB/s of 16 bytes each), with the vector units near their limit
+// too: the exact root and quotient, three products of the hash and the codes take about 90 instructions an element; read back 210 us
+// (5.7 TB/s).  5.3e6 parameters in 38 tensors with a bound on the norm 7 and 27 us.
 #include "policy_device.h"
 #include "policy_kernels.h"
 
