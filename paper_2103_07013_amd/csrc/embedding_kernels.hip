@@ -338,10 +338,10 @@ __global__ __launch_bounds__(kSortOneGroup) void k_sort_one(SortArgs a) {
     }
 }
 
-// GROUP lanes for a row (or for GROUP * N columns of it), one after the other where there are more columns.
+// GROUP lanes for a row, four blocks of GROUP * N columns at a time.
 template <class T, int GROUP>
 __global__ __launch_bounds__(256) void k_embed(EmbedArgs a) {
-    constexpr int N = T::kPer16, kRows = 256 / GROUP;
+    constexpr int N = T::kPer16, kRows = 256 / GROUP, kAhead = 4;
     const uint64_t n = (uint64_t)blockIdx.x * kRows + threadIdx.x / GROUP;
     if (n >= a.count) return;
     const int64_t t = token_at(a.tokens, a.tokens64, n);
@@ -349,15 +349,24 @@ __global__ __launch_bounds__(256) void k_embed(EmbedArgs a) {
     const float other = t == -1 ? 0.0f : __builtin_nanf("");
     const typename T::raw* from = static_cast<const typename T::raw*>(a.weight) + (row ? t : 0) * a.weight_stride;
     typename T::raw* to = static_cast<typename T::raw*>(a.out) + (int64_t)n * a.out_stride;
-    for (uint32_t at = threadIdx.x % GROUP * N; at < a.width; at += GROUP * N) {
-        if (at + N <= a.width) {
-            float x[N];
-            load<T, N>(from + at, x);
+    for (uint32_t base = threadIdx.x % GROUP * N; base < a.width; base += kAhead * GROUP * N) {
+        Words w[kAhead];
 #pragma unroll
-            for (int k = 0; k < N; ++k) x[k] = row ? x[k] * a.scale : other;
-            store<T, N>(to + at, x, a.past != 0);
-        } else {
-            for (uint32_t k = at; k < a.width; ++k) to[k] = rounded<T>(row ? to_float(from[k]) * a.scale : other);
+        for (int u = 0; u < kAhead; ++u) {
+            w[u] = Words{0, 0, 0, 0};
+            if (base + (u * GROUP + 1) * N <= a.width) w[u] = load_words<T>(from + base + u * GROUP * N);
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const uint32_t at = base + u * GROUP * N;
+            if (at + N <= a.width) {
+                float x[N];
+#pragma unroll
+                for (int k = 0; k < N; ++k) x[k] = row ? word_float<T>(w[u], k) * a.scale : other;
+                store<T, N>(to + at, x, a.past != 0);
+            } else {
+                for (uint32_t k = at; k < a.width; ++k) to[k] = rounded<T>(row ? to_float(from[k]) * a.scale : other);
+            }
         }
     }
 }

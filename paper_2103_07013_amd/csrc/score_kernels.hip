@@ -13,6 +13,8 @@
 // holds) and their gradient in 737 us (5.8 TB/s of 4.3 GB); the pass itself is near the vector units' limit too, with nine instructions and one
 // exponential (four times the issue slots) an entry.  Short rows the launch: 32768 x 6 float32 3.5 us, the gradient 3.1.  Alternatives cost what ordering the candidates costs: 192 x 50257 f16 with 5 of them
 // 17 us, 10 without; 1 x 131072 with 20 in pieces 7 us and their join 5.
+#include <type_traits>
+
 #include "policy_device.h"
 #include "policy_kernels.h"
 
@@ -78,6 +80,17 @@ __device__ __forceinline__ void row_entries(const typename T::raw* row, const ui
     }
 }
 
+// N bytes of a mask that lie anywhere, in two words.
+template <int N>
+__device__ __forceinline__ auto mask_bytes(const uint8_t* p) {
+    typedef uint32_t Bytes __attribute__((ext_vector_type(2)));
+    const Pack<uint8_t, N> q = *reinterpret_cast<const Pack<uint8_t, N>*>(p);
+    if constexpr (N == 8)
+        return __builtin_bit_cast(Bytes, q);
+    else
+        return Bytes{__builtin_bit_cast(uint32_t, q), 0u};
+}
+
 // U times N entries of a row, the u-th from first + u * apart + lane * N on; `all`: the same for all lanes of the wavefront, says that none of them lies behind
 // the row's end.  Loads under a condition of their own would each be waited for before the next.
 template <class T, int U, int N, bool MASK>
@@ -98,12 +111,33 @@ __device__ __forceinline__ void row_blocks(const typename T::raw* row, const uin
         }
         return;
     }
+    // -inf, and allowed, where nothing is loaded; the one lane that the row ends in takes its entries one by one
+    constexpr uint32_t kNone = sizeof(typename T::raw) == 4 ? 0xFF800000u : std::is_same_v<T, Bf16> ? 0xFF80FF80u : 0xFC00FC00u;
+    typedef uint32_t Bytes __attribute__((ext_vector_type(2)));
+    Words q[U];
+    Bytes may[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        float y[N];
-        row_entries<T, N, MASK>(row, mask, first + u * apart + lane * N, end, y);
+        const uint32_t at = first + u * apart + lane * N;
+        q[u] = Words{kNone, kNone, kNone, kNone};
+        may[u] = Bytes{0x01010101u, 0x01010101u};
+        if (at + N <= end) {
+            q[u] = load_words<T>(row + at);
+            if (MASK) may[u] = mask_bytes<N>(mask + at);
+        }
+    }
 #pragma unroll
-        for (int e = 0; e < N; ++e) x[u * N + e] = y[e];
+    for (int e = 0; e < U * N; ++e) {
+        const float y = word_float<T>(q[e / N], e % N);
+        x[e] = !MASK || (may[e / N][e % N / 4] >> (8 * (e % 4)) & 255u) ? y : -kInf;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const uint32_t at = first + u * apart + lane * N;
+        if (at < end && at + N > end) {
+#pragma unroll
+            for (int k = 0; k < N; ++k) x[u * N + k] = at + k < end && (!MASK || mask[at + k]) ? to_float(row[at + k]) : -kInf;
+        }
     }
 }
 
