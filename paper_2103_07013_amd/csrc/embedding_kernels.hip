@@ -7,7 +7,7 @@
 // are written as zeros next to the sums, or all of a table that is little used is cleared next to the sort.  Tables of up to 16
 // rows need no sort: sums of all rows fit in LDS.
 //
-// What bounds it, on one MI355X (median kernel times): long batches the memory, the lookup of 262144 rows of 2048 bf16 313 us (5.3 TB/s of what it
+// What bounds it, on one MI355X (median kernel times): long batches the memory, the lookup of 262144 rows of 2048 bf16 290 us (5.8 TB/s of what it
 // moves), their sums into 131072 float32 rows 415 us (5.1 TB/s), sorting 40 us, joining cut rows
 // 39 us.  Middling ones the launches one after the other, each waiting for a few memory round trips: 16384 tokens and 50257 rows
 // of 769, 24 us of sort, 30 us of sums (5.8 TB/s), 13 us of joining.  Few rows: 32768 tokens of 5 rows of 32 4.8 us and 2.9 us.

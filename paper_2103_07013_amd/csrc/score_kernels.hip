@@ -545,14 +545,18 @@ __device__ __forceinline__ void store_entries(typename T::raw* out, uint32_t at,
     }
 }
 
-template <class T, bool MASK, int G, int N>
+template <class T, int G, int N>
 __global__ __launch_bounds__(256) void k_score_grad_short(ScoreGradArgs a) {
     const uint32_t lane = threadIdx.x & (G - 1);
     const uint64_t r = (uint64_t)blockIdx.x * (256 / G) + threadIdx.x / G;
     if (r >= a.rows) return;
     const RowGrad g = row_grad(a, r);
     float x[N], d[N];
-    row_entries<T, N, MASK>(static_cast<const typename T::raw*>(a.logits) + (int64_t)r * a.row_stride, MASK ? a.mask + (int64_t)r * a.mask_stride : nullptr, lane * N, a.entries, x);
+    const typename T::raw* row = static_cast<const typename T::raw*>(a.logits) + (int64_t)r * a.row_stride;
+    if (a.mask)
+        row_entries<T, N, true>(row, a.mask + (int64_t)r * a.mask_stride, lane * N, a.entries, x);
+    else
+        row_entries<T, N, false>(row, nullptr, lane * N, a.entries, x);
     gradient<N>(g, a.scale * kLog2e, lane * N, x, d);
     store_entries<T, N>(static_cast<typename T::raw*>(a.out) + (int64_t)r * a.out_stride, lane * N, a.entries, d, false);
 }
@@ -580,8 +584,14 @@ __global__ __launch_bounds__(GROUP) void k_score_grad(ScoreGradArgs a, uint32_t 
 
 // ---- which kernel
 
-// Rows of up to this many entries are shared by few lanes, longer ones by a wavefront at least.
-constexpr uint32_t kShort = 128;
+// Rows of up to kShort entries are held by few lanes, those of up to kWide by a wavefront, 8 entries to a lane, if not many alternatives are asked for, which cost a
+// pass over the lanes each; longer ones are streamed.  Measured with 32768 rows of bf16, held / streamed by a wavefront each: 32 entries 3.8 / 25.7 us, 128
+// 5.4 / 25.2 (with 16 alternatives 22 / 68, with 32 37 / 90, but 300 rows of 100 with 32 17 / 11), 256 15.7 / 24.2 (with 3 alternatives 29 / 41; float32 29 / 29, with
+// 5 36 / 30).
+constexpr uint32_t kShort = 128, kShortTop = 16, kManyRows = 8192, kShortTopOfMany = 32, kWide = 512, kWideTop = 3;
+bool held(uint64_t rows, uint32_t entries, uint32_t top_k) {
+    return entries <= kShort ? top_k <= (rows < kManyRows ? kShortTop : kShortTopOfMany) : entries <= kWide && top_k <= kWideTop;
+}
 // Rows of up to kWaveRow entries have one wavefront, where there are kWaveRows rows or more those of up to kLongWaveRow too.  Measured
 // with bf16, one wavefront / four: 4096 x 2048 6.0 / 14.6 us, 4096 x 4096 8.5 / 14.9, 4096 x 8192 15.1 / 15.4, 512 x 4096 4.3 / 5.2 (with 20
 // alternatives 10.0 / 8.9), 1024 x 8192 6.3 / 6.1 (16.1 / 12.4).
@@ -606,29 +616,31 @@ Pieces pieces_of(uint64_t rows, uint32_t entries) {
 }
 
 #define BPS_ROWS(kernel, per_group, threads, ...) \
-    hipLaunchKernelGGL((kernel<T, MASK, __VA_ARGS__>), dim3((uint32_t)((a.rows + (per_group) - 1) / (per_group))), dim3(threads), 0, stream, a)
+    hipLaunchKernelGGL((kernel<T, __VA_ARGS__>), dim3((uint32_t)((a.rows + (per_group) - 1) / (per_group))), dim3(threads), 0, stream, a)
 
 template <class T, bool MASK, bool TOP>
 hipError_t score(const ScoreArgs& a, hipStream_t stream) {
     const Pieces pieces = pieces_of(a.rows, a.entries);
-    if (a.entries <= kShort && a.top_k <= 8) {
+    if (held(a.rows, a.entries, a.top_k)) {
         if (a.entries <= 8)
-            BPS_ROWS(k_score_short, 64, 256, TOP, 4, 2);
+            BPS_ROWS(k_score_short, 64, 256, MASK, TOP, 4, 2);
         else if (a.entries <= 32)
-            BPS_ROWS(k_score_short, 32, 256, TOP, 8, 4);
+            BPS_ROWS(k_score_short, 32, 256, MASK, TOP, 8, 4);
+        else if (a.entries <= kShort)
+            BPS_ROWS(k_score_short, 16, 256, MASK, TOP, 16, 8);
         else
-            BPS_ROWS(k_score_short, 16, 256, TOP, 16, 8);
+            BPS_ROWS(k_score_short, 4, 256, MASK, TOP, 64, 8);
     } else if (pieces.count > 1) {
         PieceSums* sums = static_cast<PieceSums*>(a.workspace);
         uint64_t* lists = reinterpret_cast<uint64_t*>(sums + a.rows * pieces.count);
         hipLaunchKernelGGL((k_score_piece<T, MASK, TOP>), dim3((uint32_t)(a.rows * pieces.count)), dim3(256), 0, stream, a, pieces, sums, lists);
         hipLaunchKernelGGL((k_score_join<T, TOP>), dim3((uint32_t)a.rows), dim3(TOP ? 1024 : 64), 0, stream, a, pieces, sums, lists);
     } else if (a.entries <= (a.rows < kWaveRows ? kWaveRow : kLongWaveRow)) {
-        BPS_ROWS(k_score, 4, 256, TOP, 1);
+        BPS_ROWS(k_score, 4, 256, MASK, TOP, 1);
     } else if (a.entries <= kLongWaveRow || a.rows > kComputeUnits) {
-        BPS_ROWS(k_score, 1, 256, TOP, 4);
+        BPS_ROWS(k_score, 1, 256, MASK, TOP, 4);
     } else {
-        BPS_ROWS(k_score, 1, 1024, TOP, 16);
+        BPS_ROWS(k_score, 1, 1024, MASK, TOP, 16);
     }
     return hipGetLastError();
 }
@@ -646,6 +658,8 @@ hipError_t score_grad_masked(const ScoreGradArgs& a, hipStream_t stream) {
         BPS_ROWS(k_score_grad_short, 32, 256, 8, 4);
     } else if (a.entries <= kShort) {
         BPS_ROWS(k_score_grad_short, 16, 256, 16, 8);
+    } else if (a.entries <= kWide) {
+        BPS_ROWS(k_score_grad_short, 4, 256, 64, 8);
     } else {
         const uint32_t wave = 64 * T::kPer16 * 4, group = 4 * wave;
         const uint32_t pieces = a.entries <= wave ? 1 : (a.entries + group - 1) / group;
