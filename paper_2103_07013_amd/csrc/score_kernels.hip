@@ -618,10 +618,11 @@ Pieces pieces_of(uint64_t rows, uint32_t entries) {
 #define BPS_ROWS(kernel, per_group, threads, ...) \
     hipLaunchKernelGGL((kernel<T, __VA_ARGS__>), dim3((uint32_t)((a.rows + (per_group) - 1) / (per_group))), dim3(threads), 0, stream, a)
 
+// all: rows of the whole call, which decide for each of its launches: the workspace was sized for them
 template <class T, bool MASK, bool TOP>
-hipError_t score(const ScoreArgs& a, hipStream_t stream) {
-    const Pieces pieces = pieces_of(a.rows, a.entries);
-    if (held(a.rows, a.entries, a.top_k)) {
+hipError_t score(const ScoreArgs& a, uint64_t all, hipStream_t stream) {
+    const Pieces pieces = pieces_of(all, a.entries);
+    if (held(all, a.entries, a.top_k)) {
         if (a.entries <= 8)
             BPS_ROWS(k_score_short, 64, 256, MASK, TOP, 4, 2);
         else if (a.entries <= 32)
@@ -635,9 +636,9 @@ hipError_t score(const ScoreArgs& a, hipStream_t stream) {
         uint64_t* lists = reinterpret_cast<uint64_t*>(sums + a.rows * pieces.count);
         hipLaunchKernelGGL((k_score_piece<T, MASK, TOP>), dim3((uint32_t)(a.rows * pieces.count)), dim3(256), 0, stream, a, pieces, sums, lists);
         hipLaunchKernelGGL((k_score_join<T, TOP>), dim3((uint32_t)a.rows), dim3(TOP ? 1024 : 64), 0, stream, a, pieces, sums, lists);
-    } else if (a.entries <= (a.rows < kWaveRows ? kWaveRow : kLongWaveRow)) {
+    } else if (a.entries <= (all < kWaveRows ? kWaveRow : kLongWaveRow)) {
         BPS_ROWS(k_score, 4, 256, MASK, TOP, 1);
-    } else if (a.entries <= kLongWaveRow || a.rows > kComputeUnits) {
+    } else if (a.entries <= kLongWaveRow || all > kComputeUnits) {
         BPS_ROWS(k_score, 1, 256, MASK, TOP, 4);
     } else {
         BPS_ROWS(k_score, 1, 1024, MASK, TOP, 16);
@@ -645,9 +646,9 @@ hipError_t score(const ScoreArgs& a, hipStream_t stream) {
     return hipGetLastError();
 }
 template <class T>
-hipError_t score(const ScoreArgs& a, hipStream_t stream) {
-    if (a.mask) return a.top_k ? score<T, true, true>(a, stream) : score<T, true, false>(a, stream);
-    return a.top_k ? score<T, false, true>(a, stream) : score<T, false, false>(a, stream);
+hipError_t score(const ScoreArgs& a, uint64_t all, hipStream_t stream) {
+    if (a.mask) return a.top_k ? score<T, true, true>(a, all, stream) : score<T, true, false>(a, all, stream);
+    return a.top_k ? score<T, false, true>(a, all, stream) : score<T, false, false>(a, all, stream);
 }
 
 template <class T, bool MASK>
@@ -705,7 +706,8 @@ size_t score_workspace(int32_t, uint64_t rows, uint32_t entries, uint32_t top_k)
 }
 
 hipError_t launch_score(int32_t dtype, const ScoreArgs& a, hipStream_t stream) {
-    // rows that are cut into pieces are few, others have at most one work-group each
+    // rows of a call that cuts them into pieces are few, so that it has one launch of all of them; others have at most one work-group each
+    static_assert(kPieceRows <= kMaxGroups, "calls that need the workspace are not split");
     for (uint64_t first = 0; first < a.rows; first += kMaxGroups) {
         ScoreArgs s = rows_of(a, dtype, first, a.rows - first < kMaxGroups ? a.rows - first : kMaxGroups);
         s.lse = a.lse + first;
@@ -713,7 +715,7 @@ hipError_t launch_score(int32_t dtype, const ScoreArgs& a, hipStream_t stream) {
             s.top_ids = a.top_ids + first * a.top_k;
             s.top_logp = a.top_logp + first * a.top_k;
         }
-        const hipError_t e = dtype == BPS_F32 ? score<F32>(s, stream) : dtype == BPS_BF16 ? score<Bf16>(s, stream) : score<F16>(s, stream);
+        const hipError_t e = dtype == BPS_F32 ? score<F32>(s, a.rows, stream) : dtype == BPS_BF16 ? score<Bf16>(s, a.rows, stream) : score<F16>(s, a.rows, stream);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;

@@ -1,0 +1,19 @@
+/* The stand-in for the HIP runtime (fake_hip.c) with a line for every launch that says how large it is, and with what the runtime
+ * refuses: a grid of 2^32 threads or more. */
+#define hipLaunchKernel fake_plain_launch
+#include "fake_hip.c"
+#undef hipLaunchKernel
+
+static char g_launches[1 << 16];
+static size_t g_launches_at;
+const char* fake_launches(void) { return g_launches; }
+void fake_clear_launches(void) { g_launches[g_launches_at = 0] = 0; }
+
+hipError_t hipLaunchKernel(const void* f, dim3 grid, dim3 block, void** args, size_t shared, hipStream_t stream) {
+    (void)args; (void)stream;
+    const size_t room = sizeof(g_launches) - g_launches_at;
+    const int n = snprintf(g_launches + g_launches_at, room, "%s grid=%ux%u threads=%u lds=%zu\n", kernel_name(f), grid.x, grid.y, block.x, shared);
+    if (n < 0 || (size_t)n >= room) abort();
+    g_launches_at += (size_t)n;
+    return (uint64_t)grid.x * grid.y * block.x >> 32 ? hipErrorInvalidConfiguration : hipSuccess;
+}

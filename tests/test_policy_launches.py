@@ -1,0 +1,68 @@
+"""Which kernels the policy's operators launch, without a GPU: libbps.so runs on a stand-in for the HIP runtime
+(fake_hip_launches.c) that notes every launch, and no kernel runs."""
+import os
+import re
+import subprocess
+import sys
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+PRELUDE = """
+import ctypes, sys
+fake = ctypes.CDLL(sys.argv[1], mode=ctypes.RTLD_GLOBAL)      # found before the real runtime
+fake.fake_launches.restype = ctypes.c_char_p
+import paper_2103_07013_amd as bps          # without torch, whose kernels the stand-in has no room for
+lib = bps.load_library()
+p, i, u, l, f = ctypes.c_void_p, ctypes.c_int32, ctypes.c_uint32, ctypes.c_uint64, ctypes.c_float
+lib.bps_log_probs_workspace.restype, lib.bps_log_probs_workspace.argtypes = ctypes.c_size_t, [i, l, u, u]
+lib.bps_log_probs.argtypes = [p, i, l, u, l, p, i, p, l, f, u, p, p, p, p, p, p, p, l, p]
+P = 4096          # an address that nothing looks behind
+
+def scores(rows, entries, k=0, dtype=1):
+    size = lib.bps_log_probs_workspace(dtype, rows, entries, k)
+    top = P if k else None
+    fake.fake_clear_launches()
+    status = lib.bps_log_probs(P, dtype, rows, entries, 0, P, 64, None, 0, 1.0, k, P, P, P, P, top, top, P if size else None, size, None)
+    assert status == 0, bps.bps_last_error()
+    print("workspace=%d" % size)
+    print(fake.fake_launches().decode(), end="")
+"""
+
+
+@pytest.fixture(scope="module")
+def fake(tmp_path_factory):
+    so = str(tmp_path_factory.mktemp("fake") / "fake_hip_launches.so")
+    subprocess.run(["gcc", "-O1", "-shared", "-fPIC", "-I/opt/rocm/include", os.path.join(ROOT, "tests", "fake_hip_launches.c"), "-o", so], check=True)
+    return so
+
+
+def _calls(fake, code):
+    """What the calls in `code` print and launch: (what was printed before, [(kernel, work-groups, threads of each)]) of each call."""
+    p = subprocess.run([sys.executable, "-c", PRELUDE + code, fake], cwd=ROOT, capture_output=True, text=True, timeout=300)
+    assert p.returncode == 0, p.stdout + p.stderr
+    calls = []
+    for line in p.stdout.splitlines():
+        m = re.match(r"_ZN3bps\S*?\d(k_[a-z_]+)I?\S* grid=(\d+)x(\d+) threads=(\d+)", line)
+        if m:
+            calls[-1][1].append((m[1], int(m[2]) * int(m[3]), int(m[4])))
+        else:
+            calls.append((line, []))
+    return calls
+
+
+@pytest.mark.parametrize("k", [0, 20])
+@pytest.mark.parametrize("parts,left", [(1, 1), (1, 10), (1, 64), (2, 3), (1, 65), (1, 5000)])
+def test_rows_behind_a_launch_are_cut_into_pieces_only_with_a_workspace(fake, parts, left, k):
+    """A call of more rows than a launch takes has many rows, however few the last launch is left with: no row is cut into pieces, whose sums would
+    need the workspace that such a call does not have, and all launches run the same kernel."""
+    (said, launches), = _calls(fake, f"scores({parts} * 2 ** 21 + {left}, 40000, {k})")
+    assert said == "workspace=0"
+    assert [name for name, _, _ in launches] == ["k_score"] * (parts + 1)
+    assert launches[-1][1:] == (left, launches[0][2])
+
+
+def test_few_long_rows_are_cut_into_pieces(fake):
+    (said, launches), = _calls(fake, "scores(10, 40000, 3)")
+    assert int(said.split("=")[1]) > 0 and [name for name, _, _ in launches] == ["k_score_piece", "k_score_join"]
