@@ -2,9 +2,9 @@
 embedding of tokens, and AdamW over many tensors.  Marshalling only; tensors are torch's, on the GPU.
 
 Calls take their device from the tensors and torch's current stream of it, unless `stream` names another (a
-torch.cuda.Stream or a raw hipStream_t), which is then current for the call: what it allocates belongs to that stream.  A tensor
-that is used on another stream than its own has to be complete, and to be kept alive or recorded on that stream,
-by the caller, as for every operator of torch.
+torch.cuda.Stream or a raw hipStream_t, 0 = the default stream), which is then current for the call: what it
+allocates belongs to that stream.  A tensor that is used on another stream than its own has to be complete, and
+to be kept alive or recorded on that stream, by the caller, as for every operator of torch.
 """
 from __future__ import annotations
 
@@ -78,7 +78,10 @@ def _on(index, call, *arguments):
 
 def _stream(stream, device):
     """A context in which `stream` is current."""
-    return torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device) if isinstance(stream, int) else stream)
+    if isinstance(stream, int):
+        # the default stream's handle is 0, which ExternalStream would take for none given
+        stream = torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
+    return torch.cuda.stream(stream)
 
 
 def _rows(t, name, width=None):
