@@ -81,6 +81,8 @@ def _stream(stream, device):
     if isinstance(stream, int):
         # the default stream's handle is 0, which ExternalStream would take for none given
         stream = torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
+    elif stream.device != device:
+        raise ValueError(f"stream: need one of {device}, got one of {stream.device}")
     return torch.cuda.stream(stream)
 
 

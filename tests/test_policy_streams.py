@@ -51,3 +51,15 @@ def test_calls_on_the_default_stream():
         assert torch.allclose(r.lse.cpu().double(), torch.logsumexp(x, 1), rtol=1e-5)
         assert torch.isfinite(dx).all() and (rows == k).all() and (dw == k).all()
     opt.close()
+
+
+def test_a_stream_of_another_device_is_refused(monkeypatch):
+    """Made current, it would be another device's stream, and the call would run on this one's, unordered with it."""
+    import types
+    import torch
+    from paper_2103_07013_amd import policy
+    monkeypatch.setattr(torch.cuda, "stream", lambda s: s)
+    here, there = (types.SimpleNamespace(device=torch.device("cuda", k)) for k in range(2))
+    assert policy._stream(here, torch.device("cuda", 0)) is here
+    with pytest.raises(ValueError, match="stream"):
+        policy._stream(there, torch.device("cuda", 0))
