@@ -318,7 +318,9 @@ class AdamW:
     max_grad_norm > 0: gradients are scaled down to this 2-norm over all tensors; a step whose norm is not finite changes nothing
 
     lr, betas, eps and max_grad_norm may be changed between steps.  State: master (or None), exp_avg, exp_avg_sq,
-    with 8 bits exp_avg_exponent and exp_avg_sq_exponent, and steps; a tensor's part of them begins at starts[i].
+    with 8 bits exp_avg_exponent and exp_avg_sq_exponent, and steps; a tensor's part of them begins at starts[i].  The
+    library has the tensors' addresses: saved states are copied into them (exp_avg.copy_(saved)), and a step or states() after one of
+    them was replaced is refused.
     """
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, lr_scale=1.0, state_bits=32, max_grad_norm=0.0, seed=0):
@@ -369,6 +371,13 @@ class AdamW:
             _checked(_library().bps_adamw_create(ctypes.byref(config), ctypes.byref(handle)))
         self._handle = handle
         self._grads = (ctypes.c_void_p * n)()
+        self._kept = [(name, t, t.data_ptr()) for name in ("master", "exp_avg", "exp_avg_sq", "exp_avg_exponent", "exp_avg_sq_exponent", "grad_norm")
+                      if (t := getattr(self, name)) is not None]
+
+    def _check_kept(self):
+        for name, t, place in self._kept:
+            if getattr(self, name) is not t or t.data_ptr() != place:
+                raise ValueError(f"{name} was replaced: this optimiser works on the one that it was made with, into which values can be copied")
 
     def step(self, grads=None, grad_scale=1.0, stream=None):
         """One step with the parameters' gradients, or with `grads`: one contiguous tensor (or None) for each, of the
@@ -380,6 +389,7 @@ class AdamW:
             raise ValueError("this optimiser is closed")
         if [p.data_ptr() for p in self.params] != self._places:
             raise ValueError("a parameter's memory is no longer where it was when this optimiser was made")
+        self._check_kept()
         grads = [p.grad for p in self.params] if grads is None else list(grads)
         if len(grads) != len(self.params):
             raise ValueError("grads: one for each parameter")
@@ -409,6 +419,7 @@ class AdamW:
         if stream is not None:
             with _stream(stream, self.device):
                 return self.states()
+        self._check_kept()
         if self.state_bits == 32:
             return self.exp_avg, self.exp_avg_sq
         if self._handle is None:
