@@ -66,6 +66,8 @@ def _checked(status):
 
 
 _current_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+# The library writes through addresses: autograd is told of tensors that were there before, so that graphs that saved them are refused.
+_written = torch.autograd.graph.increment_version
 
 
 def _on(index, call, *arguments):
@@ -216,7 +218,8 @@ def log_probs_backward(logits, tokens, result, grad_logp=None, grad_entropy=None
     bits = _tokens(tokens, shape, device)
     mask_at, mask_step = _mask(mask, shape, rows, width, device) if mask is not None else (None, 0)
     at, size = _vector(result.held if isinstance(result, LogProbs) else result, (5, *shape), device, "result"), 4 * rows
-    if out is None:
+    given = out is not None
+    if not given:
         out = torch.empty(*shape, width, dtype=logits.dtype, device=device)
         out_step = width
     else:
@@ -227,6 +230,8 @@ def log_probs_backward(logits, tokens, result, grad_logp=None, grad_entropy=None
                  at, at + size, at + 3 * size, _vector(grad_logp, shape, device, "grad_logp"), _vector(grad_entropy, shape, device, "grad_entropy"), out.data_ptr(), out_step)
     if status:
         _checked(status)
+    if given:
+        _written(out)
     return out
 
 
@@ -237,7 +242,8 @@ def _embedding(tokens, weight, scale, out):
     _, rows, width, step = _rows(weight, "weight")
     device = weight.device
     bits = _tokens(tokens, tokens.shape, device)
-    if out is None:
+    given = out is not None
+    if not given:
         out = torch.empty(*tokens.shape, width, dtype=weight.dtype, device=device)
         out_step = width
     else:
@@ -246,6 +252,8 @@ def _embedding(tokens, weight, scale, out):
         out_step = _rows(out, "out", width)[3] if out.numel() else width
     _checked(_on(device.index, lib.bps_embedding, tokens.data_ptr(), bits, tokens.numel(), weight.data_ptr(), _TYPES[weight.dtype], rows, width, step, scale,
                  out.data_ptr(), out_step))
+    if given:
+        _written(out)
     return out
 
 
@@ -292,7 +300,8 @@ def embedding_backward(tokens, grad_out, rows, scale=1.0, dtype=torch.float32, o
     else:
         count, width, step = 0, grad_out.shape[-1], grad_out.shape[-1]
     bits = _tokens(tokens, tokens.shape, device)
-    if out is None:
+    given = out is not None
+    if not given:
         out = torch.empty(rows, width, dtype=dtype, device=device)
         out_step = width
     else:
@@ -305,6 +314,8 @@ def embedding_backward(tokens, grad_out, rows, scale=1.0, dtype=torch.float32, o
     space = torch.empty(size, dtype=torch.uint8, device=device) if size else None
     _checked(_on(device.index, lib.bps_embedding_backward, tokens.data_ptr(), bits, count, grad_out.data_ptr(), _TYPES[grad_out.dtype], rows, width, step, scale,
                  out.data_ptr(), _TYPES[out.dtype], out_step, int(accumulate), space.data_ptr() if size else None, size))
+    if given:
+        _written(out)
     return out
 
 
@@ -413,6 +424,7 @@ class AdamW:
         except BpsError:
             self.steps -= 1
             raise
+        _written([p for p, g in zip(self.params, grads) if g is not None] + [t for _, t, _ in self._kept])
 
     def states(self, stream=None):
         """(exp_avg, exp_avg_sq) as float32: the arrays themselves with 32 bits, what their codes stand for with 8."""
