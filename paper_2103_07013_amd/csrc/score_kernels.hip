@@ -24,8 +24,9 @@ namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr float kLowest = -3.402823466e38f;
-// stands for differences below it where they are multiplied by a probability that is zero
-constexpr float kFar = -1e30f;
+// Stands for differences below it where they are multiplied by a probability, which is zero there (2^-149 is the least float), so that the product
+// is too: near enough to zero that neither the number of entries nor the gradients that come in make it infinite first.
+constexpr float kFar = -256.0f;
 constexpr float kInf = __builtin_inff();
 
 // A part of a row: the largest entry, the sum of 2^d and of d 2^d, d = (x - m) scale log2 e.  m starts at the lowest
@@ -497,7 +498,7 @@ __global__ __launch_bounds__(TOP ? 1024 : 64) void k_score_join(ScoreArgs a, Pie
 // ---- gradient
 
 // With l = log2 p_j = c (x_j - m) - log2 z, the gradient is p_j (slope l + base), and token_grad more for the token's entry.  An entry that takes no
-// part has p = 0 and so the gradient 0, but where the row's numbers are not finite: odd, where that has to be asked for.
+// part has p = 0 and so the gradient 0, but where the bracket may not be finite: odd, where that has to be asked for, and p multiplied first.
 struct RowGrad {
     float m, log2_z, slope, base, token_grad;
     int64_t t;
@@ -514,7 +515,7 @@ __device__ __forceinline__ RowGrad row_grad(const ScoreGradArgs& a, uint64_t r) 
     g.slope = -gh * a.scale * kLn2;
     g.base = -fmaf(gh, a.entropy[r], gl) * a.scale;
     g.token_grad = gl * a.scale;
-    g.odd = !(fabsf(g.log2_z) < kInf && fabsf(g.slope) < kInf && fabsf(g.base) < kInf);
+    g.odd = !(fabsf(g.log2_z) < kInf && fmaf(fabsf(g.slope), -kFar, fabsf(g.base)) < kInf);
     return g;
 }
 template <int N>
@@ -524,14 +525,17 @@ __device__ __forceinline__ void gradient(const RowGrad& g, float c, uint32_t at,
         const float l = fmaf(x[k] - g.m, c, -g.log2_z);
         d[k] = __builtin_amdgcn_exp2f(l) * fmaf(g.slope, fmaxf(l, kFar), g.base);
     }
+    if (g.odd) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const float l = fmaf(x[k] - g.m, c, -g.log2_z), p = __builtin_amdgcn_exp2f(l);
+            d[k] = x[k] == -kInf ? 0.0f : fmaf(p * g.slope, fmaxf(l, kFar), p * g.base);
+        }
+    }
     if ((uint64_t)g.t - at < (uint64_t)N) {
 #pragma unroll
         for (int k = 0; k < N; ++k)
             if (at + k == (uint64_t)g.t && x[k] != -kInf) d[k] += g.token_grad;
-    }
-    if (g.odd) {
-#pragma unroll
-        for (int k = 0; k < N; ++k) d[k] = x[k] == -kInf ? 0.0f : d[k];
     }
 }
 template <class T, int N>

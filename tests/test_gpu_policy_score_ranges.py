@@ -1,0 +1,83 @@
+"""Scores and their gradient at the ends of what their arguments may be: gradients and scales that are large, entries that are far below the
+largest, very many of them."""
+import math
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+E = 2.0 ** -24
+
+
+def _inputs(N, V, dtype, seed=0):
+    import torch
+    g = torch.Generator().manual_seed(seed + N + V)
+    logits = (torch.randn((N, V), generator=g) * 3).to(getattr(torch, dtype))
+    logits[torch.rand((N, V), generator=g) < 0.1] = -math.inf
+    logits[torch.rand((N, V), generator=g) < 0.1] = torch.finfo(logits.dtype).min
+    logits[:, V // 2] = 1.0
+    mask = torch.rand((N, V), generator=g) < 0.7
+    mask[:, V // 2] = True
+    tokens = torch.full((N,), V // 2)
+    tokens[::2] = -1
+    return logits, tokens, mask
+
+
+@pytest.mark.parametrize("size", [1e8, 1e9, 1e20, 1e33, 1e37])
+@pytest.mark.parametrize("masked", [False, True])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("N,V", [(5, 7), (3, 60), (4, 300), (3, 3000), (2, 20001)])
+def test_gradients_of_any_size(N, V, dtype, masked, size):
+    """Entries that take no part have the gradient 0, others the formula's, however large the gradient is that comes in (a loss scale, say).  e (8
+    |ln p| + 16 ln V + 64 + V / 128) bounds what ln p and the entropy may be off, absolutely, and p relative to itself."""
+    import torch
+    import paper_2103_07013_amd as bps
+    logits, tokens, mask = _inputs(N, V, dtype)
+    given = mask.cuda() if masked else None
+    r = bps.log_probs(logits.cuda(), tokens.cuda(), mask=given)
+    gl, gh = torch.full((N,), size), torch.full((N,), -size)
+    gh[1::2] *= -0.5
+    dx = bps.log_probs_backward(logits.cuda(), tokens.cuda(), r, gl.cuda(), gh.cuda(), mask=given).cpu().double()
+    x = logits.double()
+    part = (x > -math.inf) & (mask if masked else torch.ones_like(mask))
+    x = torch.where(part, x, -math.inf)
+    lp = torch.where(part, x - torch.logsumexp(x, 1, keepdim=True), 0.0)
+    p = torch.where(part, lp.exp(), 0.0)
+    entropy = -(p * lp).sum(1, keepdim=True)
+    at = torch.arange(V)[None] == tokens[:, None]
+    gl, gh = torch.where(tokens < 0, 0.0, gl.double())[:, None], gh.double()[:, None]
+    ref = gl * (at.double() - p) - gh * p * (lp + entropy)
+    assert (dx[~part] == 0).all()
+    slack = E * (8 * torch.where(p > 0, lp.abs(), 0.0) + 16 * math.log(V) + 64 + V / 128)
+    slack = 4 * slack * (gl.abs() * (p + at) + gh.abs() * p * (1 + lp.abs() + entropy)) + 1e-30 * size
+    half = 2.0 ** -8 if dtype == "bfloat16" else 0.0
+    assert torch.isfinite(dx).all() and ((dx - ref).abs() <= slack + half * (ref.abs() + slack))[part].all()
+
+
+@pytest.mark.parametrize("scale", [1e6, 1e12, 1e30])
+@pytest.mark.parametrize("V", [7, 60, 300, 3000, 50001])
+def test_large_scales(V, scale):
+    """The largest entry is all there is, so that the gradient is 0 wherever ln p is not 0, masked or not."""
+    import torch
+    import paper_2103_07013_amd as bps
+    logits, tokens, mask = _inputs(4, V, "float32")
+    logits[:, V // 2] = 20.0
+    one = torch.ones(4, device="cuda")
+    for m in (None, mask.cuda()):
+        r = bps.log_probs(logits.cuda(), tokens.cuda(), mask=m, scale=scale, top_k=1)
+        assert (r.logp == 0).all() and (r.entropy == 0).all() and (r.top_ids == V // 2).all() and (r.top_logp == 0).all()
+        dx = bps.log_probs_backward(logits.cuda(), tokens.cuda(), r, one, 1000 * one, mask=m, scale=scale)
+        assert (dx == 0).all()
+
+
+def test_very_many_entries_far_below_the_largest():
+    """7.5e8 entries of the type's lowest value and one of 0 behind them: nothing but that one counts."""
+    import torch
+    import paper_2103_07013_amd as bps
+    V = 750_000_000
+    logits = torch.full((1, V), torch.finfo(torch.bfloat16).min, dtype=torch.bfloat16, device="cuda")
+    logits[0, -1] = 0.0
+    r = bps.log_probs(logits, torch.tensor([V - 1], device="cuda"), top_k=2)
+    assert r.logp.item() == 0 and r.lse.item() == 0 and r.entropy.item() == 0
+    assert r.top_ids.tolist() == [[V - 1, 0]]
+    dx = bps.log_probs_backward(logits, torch.tensor([V - 1], device="cuda"), r, *torch.ones((2, 1), device="cuda"), out=logits)
+    assert int(torch.count_nonzero(dx)) == 0
