@@ -251,7 +251,7 @@ enum { BPS_F32 = 0, BPS_BF16 = 1, BPS_F16 = 2 };
  *   logits    [rows][entries], rows row_stride elements apart (any sign; 0 = the same row for all)
  *   tokens    [rows]  which entry was taken, -1 = none
  *   mask      uint8 [rows][entries], rows mask_stride bytes apart (0 = one for all rows), or NULL; 0 = the entry is forbidden
- *   scale     > 0, multiplies the logits (1 / temperature)
+ *   scale     > 0, at most 2^127; multiplies the logits (1 / temperature)
  * An entry takes part when its mask allows it and its logit is not -inf; what the logit of a forbidden entry is does not
  * matter.  With y = scale * logit over the entries that take part:
  *   lse       float32 [rows]  ln sum e^y, -inf where nothing takes part

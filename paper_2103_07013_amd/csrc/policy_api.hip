@@ -26,7 +26,8 @@ bps_status check_scores(const char* what, const void* logits, int32_t dtype, uin
     if (!known(dtype)) return fail_here(BPS_ERR_INVALID_ARG, "%s: unknown element type %d", what, dtype);
     if (token_bits != 32 && token_bits != 64) return fail_here(BPS_ERR_INVALID_ARG, "%s: tokens of %d bits (32 or 64)", what, token_bits);
     if (entries == 0 || entries >= kMaxEntries) return fail_here(BPS_ERR_INVALID_ARG, "%s: entries=%u must be 1 .. 2^30 - 1", what, entries);
-    if (!(scale > 0.0f) || !std::isfinite(scale)) return fail_here(BPS_ERR_INVALID_ARG, "%s: scale must be positive and finite", what);
+    // exponents are taken to the base 2, and scale * log2 e has to be finite
+    if (!(scale > 0.0f) || !(scale <= 0x1p127f)) return fail_here(BPS_ERR_INVALID_ARG, "%s: scale must be positive and at most 2^127", what);
     if (!logits || !tokens) return fail_here(BPS_ERR_INVALID_ARG, "%s: null argument", what);
     if (!aligned(logits, size_of(dtype)) || !aligned(tokens, token_bits / 8)) return fail_here(BPS_ERR_INVALID_ARG, "%s: misaligned logits or tokens", what);
     return BPS_OK;

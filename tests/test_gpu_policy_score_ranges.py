@@ -81,3 +81,17 @@ def test_very_many_entries_far_below_the_largest():
     assert r.top_ids.tolist() == [[V - 1, 0]]
     dx = bps.log_probs_backward(logits, torch.tensor([V - 1], device="cuda"), r, *torch.ones((2, 1), device="cuda"), out=logits)
     assert int(torch.count_nonzero(dx)) == 0
+
+
+def test_the_largest_scale():
+    import torch
+    import paper_2103_07013_amd as bps
+    logits, tokens = torch.tensor([[0.0, 0.0, -1.0]], device="cuda"), torch.tensor([1], device="cuda")
+    r = bps.log_probs(logits, tokens, scale=2.0 ** 127, top_k=3)
+    half = torch.tensor([math.log(0.5)]).double()
+    assert torch.allclose(r.logp.cpu().double(), half, rtol=1e-6) and torch.allclose(r.entropy.cpu().double(), -half, rtol=1e-6)
+    assert r.top_ids.tolist() == [[0, 1, 2]] and r.top_logp[0, 2] == -2.0 ** 127
+    dx = bps.log_probs_backward(logits, tokens, r, torch.ones(1, device="cuda"), scale=2.0 ** 127)
+    assert torch.allclose(dx.cpu().double(), torch.tensor([[-0.5, 0.5, 0.0]]).double() * 2.0 ** 127, rtol=1e-6)
+    with pytest.raises(bps.BpsError):
+        bps.log_probs(logits, tokens, scale=3e38)
