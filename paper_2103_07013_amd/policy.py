@@ -95,6 +95,8 @@ def _rows(t, name, width=None):
     shape, strides = t.shape, t.stride()
     if not shape or shape[-1] == 0 or (width is not None and shape[-1] != width):
         raise ValueError(f"{name}: the last dimension must be {'at least 1' if width is None else width}, got shape {tuple(shape)}")
+    if 0 in shape:
+        return shape[:-1], 0, shape[-1], shape[-1]
     if strides[-1] != 1 and shape[-1] != 1:
         raise ValueError(f"{name}: the last dimension must be contiguous")
     if len(shape) == 2:
