@@ -286,8 +286,8 @@ bps_status bps_embedding(const void *tokens, int32_t token_bits, uint64_t count,
 /* Its gradient: grad_weight[v] = scale * sum of grad_out[n] over the n with tokens[n] = v; every row is written, zeros where
  * a row has no token.  With accumulate the sums are added to what grad_weight holds, and other rows are not touched.
  *   grad_out [count][width] of grad_dtype; grad_weight [rows][width] of weight_dtype.  Tokens that are no row are left out.
- * Tokens are sorted by row first; each row's sum is taken in the tokens' order, in float32, over pieces of that order
- * whose bounds depend on `count`, `rows` and `width` alone, and rounded once.  count < 2^31.
+ * Each row's sum is taken in the tokens' order, in float32, over pieces of that order (of the tokens sorted by row, or as they
+ * are where `rows` is small) whose bounds depend on `count`, `rows`, `width` and grad_dtype alone, and rounded once.  count < 2^31.
  *   workspace  device memory of bps_embedding_backward_workspace bytes, 16-byte aligned */
 size_t bps_embedding_backward_workspace(uint64_t count, uint32_t rows, uint32_t width);
 bps_status bps_embedding_backward(const void *tokens, int32_t token_bits, uint64_t count, const void *grad_out, int32_t grad_dtype, uint32_t rows,

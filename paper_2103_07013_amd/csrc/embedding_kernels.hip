@@ -663,6 +663,7 @@ __global__ __launch_bounds__(1024) void k_embed_join(SumArgs a) {
 struct FewArgs {
     const void *tokens, *grad;
     void* out;
+    uint32_t* used;           // [part][wavefront], with accumulate: bit r is set where row r had a token
     float* partial;           // [part][row][width]
     int64_t grad_stride, out_stride;
     uint32_t count, rows, width, parts, length;      // parts: work-groups side by side, length: tokens of one
@@ -678,6 +679,7 @@ __global__ __launch_bounds__(256) void k_embed_few(FewArgs a) {
     float zero[N] = {};
     for (uint32_t r = 0; r < a.rows; ++r) store<F32, N>(sums + ((size_t)r * 256 + threadIdx.x) * N, zero);
     const uint32_t first = blockIdx.x * a.length, last = a.count - first < a.length ? a.count : first + a.length;
+    uint32_t used = 0;
     const uint32_t each = (a.length + kSlots - 1) / kSlots, from = first + slot * each < last ? first + slot * each : last, to = last - from < each ? last : from + each;
     if (at < a.width) {
         for (uint32_t i = from; i < to; i += kAhead) {
@@ -694,11 +696,16 @@ __global__ __launch_bounds__(256) void k_embed_few(FewArgs a) {
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
                 if (t[u] < 0 || t[u] >= (int64_t)a.rows) continue;
+                used |= 1u << t[u];
                 float* sum = sums + ((uint32_t)t[u] * 256 + threadIdx.x) * N;
 #pragma unroll
                 for (int k = 0; k < N; ++k) sum[k] += word_float<T>(x[u], k);
             }
         }
+    }
+    if (a.accumulate && blockIdx.y == 0) {      // a slot's first lane has seen all of its tokens
+        used = group_reduce<64>(used, [](uint32_t u, uint32_t v) { return u | v; });
+        if ((threadIdx.x & 63u) == 0) a.used[blockIdx.x * 4 + threadIdx.x / 64] = used;
     }
     __syncthreads();
     // lane (r, column) of the joined sums: N consecutive columns of one row to a thread
@@ -717,10 +724,18 @@ __global__ __launch_bounds__(256) void k_embed_few(FewArgs a) {
     }
 }
 
-// 16 lanes for a column of a row, each of which adds up every 16th part's sum.
+// 16 lanes for a column of a row, each of which adds up every 16th part's sum.  With accumulate, rows that had no token are not written.
 template <class O>
 __global__ __launch_bounds__(256) void k_embed_few_join(FewArgs a) {
     __shared__ float part[16][16];
+    __shared__ uint32_t used;
+    if (a.accumulate) {
+        uint32_t mine = 0;
+        for (uint32_t i = threadIdx.x; i < 4 * a.parts; i += 256) mine |= a.used[i];
+        if (threadIdx.x == 0) used = 0;
+        __syncthreads();
+        if (mine) atomicOr(&used, mine);
+    }
     const uint32_t cells = a.rows * a.width, cell = blockIdx.x * 16 + (threadIdx.x & 15u), share = threadIdx.x >> 4;
     float sum = 0.0f;
     if (cell < cells) {
@@ -733,6 +748,7 @@ __global__ __launch_bounds__(256) void k_embed_few_join(FewArgs a) {
 #pragma unroll
     for (uint32_t w = 1; w < 16; ++w) sum += part[w][threadIdx.x];
     const uint32_t r = cell / a.width;
+    if (a.accumulate && !(used >> r & 1u)) return;
     typename O::raw* to = static_cast<typename O::raw*>(a.out) + (int64_t)r * a.out_stride + cell % a.width;
     *to = rounded<O>(a.accumulate ? fmaf(sum, a.scale, to_float(*to)) : sum * a.scale);
 }
@@ -779,7 +795,8 @@ hipError_t embed_grad(const EmbedGradArgs& a, hipStream_t stream) {
     if (uint32_t parts = few_parts(a.count, a.rows, a.width, T::kPer16 == 4)) {
         const uint32_t length = (a.count + parts - 1) / parts;
         parts = (a.count + length - 1) / length;
-        const FewArgs f = {a.tokens, a.grad, a.out, static_cast<float*>(a.workspace), a.grad_stride, a.out_stride, a.count, a.rows, a.width, parts, length, a.scale, a.tokens64, a.accumulate};
+        uint32_t* used = static_cast<uint32_t*>(a.workspace);
+        const FewArgs f = {a.tokens, a.grad, a.out, used, reinterpret_cast<float*>(used + 4 * parts), a.grad_stride, a.out_stride, a.count, a.rows, a.width, parts, length, a.scale, a.tokens64, a.accumulate};
         if (lanes <= 4)
             few<T, O, 4>(f, stream);
         else if (lanes <= 16)
@@ -885,7 +902,7 @@ size_t embed_grad_workspace(uint32_t count, uint32_t rows, uint32_t width) {
     const SortPlan plan = sort_plan(count, rows);
     const uint32_t length = piece_length(count, width);
     // the gradient's type is not known here: enough for either way
-    const size_t few = (size_t)few_parts(count, rows, width, true) * rows * width * 4;
+    const size_t few = (size_t)few_parts(count, rows, width, true) * ((size_t)rows * width * 4 + 16);
     const size_t sorted = 4 * whole((size_t)count * 4) + whole(((size_t)(plan.row + 1) << plan.digit) * 4) + whole(rows) + kMaxPieces + (count + (size_t)length - 1) / length * 2 * width * 4;
     return few > sorted ? few : sorted;
 }
