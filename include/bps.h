@@ -298,7 +298,8 @@ bps_status bps_embedding_backward(const void *tokens, int32_t token_bits, uint64
  *   m = beta1 m + (1 - beta1) g';   v = beta2 v + ((1 - beta2) g') g'
  *   w = w (1 - lr weight_decay) - (lr / (1 - beta1^t)) m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
  * in float32, each operation rounded by itself; clip = max_norm / norm where norm, the 2-norm of all gradients times
- * grad_scale, is over max_norm > 0, else 1.  With max_norm > 0 a step whose norm is not finite changes nothing.
+ * grad_scale (summed in 64 bits, rounded to float32), is over max_norm > 0, else 1.  With max_norm > 0 a step whose norm is not finite
+ * changes nothing; whether its number counts is the caller's to say.
  *
  * The states of all tensors lie in one array each, a tensor's at `start` elements, a multiple of 256, in total elements, a multiple
  * of 256 too; what lies between tensors belongs to nobody.  state_bits 32: exp_avg (m) and exp_avg_sq (v) are float32.  state_bits 8:

@@ -48,14 +48,21 @@ __device__ __forceinline__ uint32_t wave_max_of_halves(uint32_t x) {
     });
 }
 
-// Sums of squares: each work-group those of every gridDim.x-th four chunks, so that four loads are on their way at once.
+__device__ __forceinline__ double wave_sum(double x) {
+#pragma unroll
+    for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d, 64);
+    return x;
+}
+
+// Sums of squares: each work-group those of every gridDim.x-th four chunks, so that four loads are on their way at once.  In 64 bits, since the
+// square of a float32 from 1.8e19 on is none, nor is that of one below 1e-23; the memory bounds it either way.
 template <class G>
 __global__ __launch_bounds__(kAdamGroup) void k_adamw_norm(AdamPlan plan, AdamGrads grads, uint32_t first_tensor, uint32_t first_chunk, uint32_t chunks, uint32_t first_sum,
                                                            AdamScalars s) {
-    __shared__ float sums[kAdamGroup / 64];
+    __shared__ double sums[kAdamGroup / 64];
     constexpr uint32_t kTogether = 4;
     const uint32_t tid = threadIdx.x, i = tid * kPerLane;
-    float sum = 0.0f;
+    double sum = 0.0;
     for (uint32_t c = blockIdx.x * kTogether; c < chunks; c += gridDim.x * kTogether) {
         const typename G::raw* g[kTogether];
         uint32_t n[kTogether];
@@ -81,8 +88,8 @@ __global__ __launch_bounds__(kAdamGroup) void k_adamw_norm(AdamPlan plan, AdamGr
         for (uint32_t u = 0; u < kTogether; ++u)
 #pragma unroll
             for (uint32_t k = 0; k < kPerLane; ++k) {
-                const float y = x[u][k] * s.grad_scale;
-                sum = fmaf(y, y, sum);
+                const double y = x[u][k] * s.grad_scale;
+                sum = fma(y, y, sum);
             }
     }
     sum = wave_sum(sum);
@@ -91,19 +98,18 @@ __global__ __launch_bounds__(kAdamGroup) void k_adamw_norm(AdamPlan plan, AdamGr
     if (tid == 0) plan.partial[first_sum + blockIdx.x] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
 }
 
-// The 2-norm from the sums of squares, by every work-group of the step for itself: in 64 bits, in an order that all share.
-__device__ __forceinline__ float norm_of(const float* partial, uint32_t n, double* total) {
+// The 2-norm from the sums of squares, by every work-group of the step for itself, in an order that all share.
+__device__ __forceinline__ float norm_of(const double* partial, uint32_t n, double* total) {
     const uint32_t tid = threadIdx.x;
     double all = 0.0;
     for (uint32_t i = 0; i < n; i += 4 * kAdamGroup) {
-        float x[4];
+        double x[4];
 #pragma unroll
-        for (uint32_t u = 0; u < 4; ++u) x[u] = i + u * kAdamGroup + tid < n ? partial[i + u * kAdamGroup + tid] : 0.0f;
+        for (uint32_t u = 0; u < 4; ++u) x[u] = i + u * kAdamGroup + tid < n ? partial[i + u * kAdamGroup + tid] : 0.0;
 #pragma unroll
-        for (uint32_t u = 0; u < 4; ++u) all += (double)x[u];
+        for (uint32_t u = 0; u < 4; ++u) all += x[u];
     }
-#pragma unroll
-    for (int d = 32; d; d >>= 1) all += __shfl_xor(all, d, 64);
+    all = wave_sum(all);
     if ((tid & 63u) == 0) total[tid >> 6] = all;
     __syncthreads();
     return (float)sqrt((total[0] + total[1]) + (total[2] + total[3]));

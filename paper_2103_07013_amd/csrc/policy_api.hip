@@ -172,8 +172,9 @@ bps_status bps_adamw_create(const bps_adamw_config* cfg, bps_adamw** out) {
         }
         h->first_chunk.push_back((uint32_t)list.size());
         // tensors | chunks | sums
+        static_assert(sizeof(bps::AdamTensor) % alignof(double) == 0 && sizeof(bps::AdamChunk) % alignof(double) == 0, "the sums are aligned");
         const size_t at_chunks = tensors.size() * sizeof(tensors[0]), at_sums = at_chunks + list.size() * sizeof(list[0]);
-        const size_t bytes = at_sums + (size_t)launches * h->sums * sizeof(float);
+        const size_t bytes = at_sums + (size_t)launches * h->sums * sizeof(double);
         hipError_t e = hipMalloc(&h->block, bytes);
         if (e != hipSuccess) return fail_here(e == hipErrorOutOfMemory ? BPS_ERR_OOM : BPS_ERR_HIP, "%s: hipMalloc(%zu): %s", what, bytes, hipGetErrorString(e));
         char* b = static_cast<char*>(h->block);
@@ -185,7 +186,7 @@ bps_status bps_adamw_create(const bps_adamw_config* cfg, bps_adamw** out) {
             return launched(what, e);
         }
         h->plan = {reinterpret_cast<bps::AdamTensor*>(b), reinterpret_cast<bps::AdamChunk*>(b + at_chunks), cfg->exp_avg, cfg->exp_avg_sq, cfg->exp_avg_exponent,
-                   cfg->exp_avg_sq_exponent, reinterpret_cast<float*>(b + at_sums)};
+                   cfg->exp_avg_sq_exponent, reinterpret_cast<double*>(b + at_sums)};
         *out = h.release();
         return BPS_OK;
     } catch (const std::bad_alloc&) {

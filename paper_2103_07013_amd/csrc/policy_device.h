@@ -1,4 +1,4 @@
-// What the kernels of a policy's operators share: element types, loads of 16 bytes, sums over a wavefront.
+// What the kernels of a policy's operators share: element types, loads of 16 bytes, what lanes of a wavefront exchange.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -139,9 +139,6 @@ __device__ __forceinline__ X group_reduce(X x, F f) {
     if constexpr (G > 16) x = f(x, from_lane_xor<16>(x));
     if constexpr (G > 32) x = f(x, from_lane_xor<32>(x));
     return x;
-}
-__device__ __forceinline__ float wave_sum(float x) {
-    return group_reduce<64>(x, [](float a, float b) { return a + b; });
 }
 
 }  // namespace bps

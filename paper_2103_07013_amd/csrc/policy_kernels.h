@@ -102,7 +102,7 @@ struct AdamPlan {             // device memory of a handle
     const AdamChunk* chunks;
     void *exp_avg, *exp_avg_sq;
     uint8_t *exp_avg_exponent, *exp_avg_sq_exponent;
-    float* partial;           // sums of squares
+    double* partial;          // sums of squares
 };
 struct AdamScalars {
     double lr, step_size;     // lr, and lr / (1 - beta1^t)
