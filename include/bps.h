@@ -313,7 +313,7 @@ bps_status bps_embedding_backward(const void *tokens, int32_t token_bits, uint64
  * The step itself uses m and v before they are rounded.
  *
  * float32 parameters are updated in place; BF16 and F16 ones need a float32 `master` (may not be NULL), which is
- * updated, and get its value rounded.  Tensors are contiguous. */
+ * updated, and get its value rounded.  Tensors are contiguous, and do not overlap. */
 typedef struct bps_adamw bps_adamw;
 
 typedef struct {

@@ -1,4 +1,5 @@
 // Host side of the policy's operators (include/bps.h): checks of arguments, and the handle of an AdamW plan.
+#include <algorithm>
 #include <cmath>
 #include <memory>
 #include <new>
@@ -31,6 +32,25 @@ bps_status check_scores(const char* what, const void* logits, int32_t dtype, uin
     if (!logits || !tokens) return fail_here(BPS_ERR_INVALID_ARG, "%s: null argument", what);
     if (!aligned(logits, size_of(dtype)) || !aligned(tokens, token_bits / 8)) return fail_here(BPS_ERR_INVALID_ARG, "%s: misaligned logits or tokens", what);
     return BPS_OK;
+}
+
+// Whether parameters or masters of a plan share memory, where work-groups would write to it in no order.
+bool share_memory(const bps_adamw_config& cfg) {
+    struct Span {
+        uintptr_t begin, end;
+    };
+    std::vector<Span> spans;
+    spans.reserve(2 * (size_t)cfg.tensors);
+    for (uint32_t i = 0; i < cfg.tensors; ++i) {
+        const bps_adamw_tensor& t = cfg.tensor[i];
+        const uintptr_t param = reinterpret_cast<uintptr_t>(t.param), master = reinterpret_cast<uintptr_t>(t.master);
+        spans.push_back({param, param + t.count * size_of(cfg.param_dtype)});
+        if (t.master) spans.push_back({master, master + t.count * sizeof(float)});
+    }
+    std::sort(spans.begin(), spans.end(), [](const Span& a, const Span& b) { return a.begin < b.begin; });
+    for (size_t i = 1; i < spans.size(); ++i)
+        if (spans[i].begin < spans[i - 1].end) return true;
+    return false;
 }
 
 }  // namespace
@@ -152,6 +172,7 @@ bps_status bps_adamw_create(const bps_adamw_config* cfg, bps_adamw** out) {
     if (hipGetDeviceCount(&ndev) != hipSuccess || ndev <= 0 || hipGetDevice(&device) != hipSuccess)
         return fail_here(BPS_ERR_HIP, "%s: no HIP device available (this library has no CPU path)", what);
     try {
+        if (share_memory(*cfg)) return fail_here(BPS_ERR_INVALID_ARG, "%s: tensors overlap in memory", what);
         std::unique_ptr<bps_adamw> h(new bps_adamw());
         h->device = device;
         h->param_dtype = cfg->param_dtype;

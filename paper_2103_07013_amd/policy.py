@@ -324,7 +324,7 @@ def embedding_backward(tokens, grad_out, rows, scale=1.0, dtype=torch.float32, o
 class AdamW:
     """One AdamW step over all of a model's tensors at once (include/bps.h states the rule).
 
-    params        contiguous tensors of one type on one GPU, each with at least one element; float32 ones are updated in place,
+    params        contiguous tensors of one type on one GPU, each with at least one element, that share no memory; float32 ones are updated in place,
                   bfloat16 and float16 ones get the rounded values of float32 masters that are kept here
     weight_decay, lr_scale   one number, or one for each tensor
     state_bits    32, or 8: a byte and a 256th per state, rounded up or down so that the mean is kept (seed)

@@ -82,3 +82,16 @@ def test_a_step_after_a_refusal():
         opt.step(g)
         # equal gradients: each step goes by lr
         assert torch.allclose(p[0], torch.full_like(p[0], 0.5), atol=1e-5) and opt.steps == 2
+
+
+@pytest.mark.gpu
+def test_parameters_that_share_memory():
+    import torch
+    import paper_2103_07013_amd as bps
+    flat = torch.zeros(1000, device="cuda")
+    for params in ([flat, flat], [flat[:600], flat[500:]], [flat[500:], flat, flat.clone()]):
+        with pytest.raises(bps.BpsError, match="overlap"):
+            bps.AdamW(params)
+    with bps.AdamW([flat[500:], flat[:500]], lr=0.5, weight_decay=0.0) as opt:
+        opt.step([torch.ones(500, device="cuda")] * 2)
+        assert torch.allclose(flat, torch.full_like(flat, -0.5), atol=1e-5)

@@ -66,3 +66,34 @@ def test_rows_behind_a_launch_are_cut_into_pieces_only_with_a_workspace(fake, pa
 def test_few_long_rows_are_cut_into_pieces(fake):
     (said, launches), = _calls(fake, "scores(10, 40000, 3)")
     assert int(said.split("=")[1]) > 0 and [name for name, _, _ in launches] == ["k_score_piece", "k_score_join"]
+
+
+ADAMW = """
+class Tensor(ctypes.Structure):
+    _fields_ = [("param", p), ("master", p), ("count", l), ("start", l), ("weight_decay", f), ("lr_scale", f)]
+
+class Config(ctypes.Structure):
+    _fields_ = [("param_dtype", i), ("state_bits", i), ("tensors", u), ("seed", u), ("total", l), ("tensor", ctypes.POINTER(Tensor)), ("exp_avg", p), ("exp_avg_sq", p),
+                ("exp_avg_exponent", p), ("exp_avg_sq_exponent", p)]
+
+def create(*tensors, dtype=0):
+    '''tensors: (address, master's address, elements)'''
+    rows, start = [], 0
+    for at, master, n in tensors:
+        rows.append(Tensor(at, master, n, start, 0.0, 1.0))
+        start += -(-n // 256) * 256
+    out = p()
+    status = lib.bps_adamw_create(ctypes.byref(Config(dtype, 32, len(rows), 0, start, (Tensor * len(rows))(*rows), P, P, None, None)), ctypes.byref(out))
+    print(status, bps.bps_last_error() if status else "")
+    lib.bps_adamw_destroy(out)
+"""
+
+
+@pytest.mark.parametrize("tensors,dtype,fits", [("(P, None, 10), (P + 40, None, 10)", 0, True), ("(P + 40, None, 300), (P, None, 10)", 0, True), ("(P, None, 10), (P, None, 10)", 0, False),
+                                                ("(P, None, 10), (P + 36, None, 10)", 0, False), ("(P + 4000, None, 1), (P, None, 1001), (P + 8000, None, 9)", 0, False),
+                                                ("(P, 2 * P, 10), (P + 20, 2 * P + 40, 10)", 1, True), ("(P, 2 * P, 10), (P + 18, 2 * P + 40, 10)", 1, False),
+                                                ("(P, 2 * P, 10), (P + 20, 2 * P + 36, 10)", 1, False), ("(P, P + 4, 10),", 1, False)])
+def test_tensors_that_share_memory_are_refused(fake, tensors, dtype, fits):
+    """A step would write to shared elements from two work-groups, in no order."""
+    (said, _), = _calls(fake, ADAMW + f"create({tensors} dtype={dtype})" if tensors.endswith(",") else ADAMW + f"create({tensors}, dtype={dtype})")
+    assert said.startswith("0" if fits else "-1") and ("overlap" in said) == (not fits)
