@@ -168,9 +168,12 @@ bps_status bps_adamw_create(const bps_adamw_config* cfg, bps_adamw** out) {
         chunks += (t.count + bps::kAdamChunk - 1) / bps::kAdamChunk;
     }
     if (chunks >= 1ull << 23) return fail_here(BPS_ERR_UNSUPPORTED, "%s: too many elements", what);
+    // failures are told by the status; the runtime's last error, which the next launch would be taken to have failed with, is cleared
     int ndev = 0, device = 0;
-    if (hipGetDeviceCount(&ndev) != hipSuccess || ndev <= 0 || hipGetDevice(&device) != hipSuccess)
+    if (hipGetDeviceCount(&ndev) != hipSuccess || ndev <= 0 || hipGetDevice(&device) != hipSuccess) {
+        (void)hipGetLastError();
         return fail_here(BPS_ERR_HIP, "%s: no HIP device available (this library has no CPU path)", what);
+    }
     try {
         if (share_memory(*cfg)) return fail_here(BPS_ERR_INVALID_ARG, "%s: tensors overlap in memory", what);
         std::unique_ptr<bps_adamw> h(new bps_adamw());
@@ -197,13 +200,17 @@ bps_status bps_adamw_create(const bps_adamw_config* cfg, bps_adamw** out) {
         const size_t at_chunks = tensors.size() * sizeof(tensors[0]), at_sums = at_chunks + list.size() * sizeof(list[0]);
         const size_t bytes = at_sums + (size_t)launches * h->sums * sizeof(double);
         hipError_t e = hipMalloc(&h->block, bytes);
-        if (e != hipSuccess) return fail_here(e == hipErrorOutOfMemory ? BPS_ERR_OOM : BPS_ERR_HIP, "%s: hipMalloc(%zu): %s", what, bytes, hipGetErrorString(e));
+        if (e != hipSuccess) {
+            (void)hipGetLastError();
+            return fail_here(e == hipErrorOutOfMemory ? BPS_ERR_OOM : BPS_ERR_HIP, "%s: hipMalloc(%zu): %s", what, bytes, hipGetErrorString(e));
+        }
         char* b = static_cast<char*>(h->block);
         e = hipMemcpy(b, tensors.data(), at_chunks, hipMemcpyHostToDevice);
         if (e == hipSuccess) e = hipMemcpy(b + at_chunks, list.data(), list.size() * sizeof(list[0]), hipMemcpyHostToDevice);
         if (e == hipSuccess) e = hipDeviceSynchronize();
         if (e != hipSuccess) {
-            hipFree(h->block);
+            (void)hipFree(h->block);
+            (void)hipGetLastError();
             return launched(what, e);
         }
         h->plan = {reinterpret_cast<bps::AdamTensor*>(b), reinterpret_cast<bps::AdamChunk*>(b + at_chunks), cfg->exp_avg, cfg->exp_avg_sq, cfg->exp_avg_exponent,

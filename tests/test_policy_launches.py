@@ -97,3 +97,13 @@ def test_tensors_that_share_memory_are_refused(fake, tensors, dtype, fits):
     """A step would write to shared elements from two work-groups, in no order."""
     (said, _), = _calls(fake, ADAMW + f"create({tensors} dtype={dtype})" if tensors.endswith(",") else ADAMW + f"create({tensors}, dtype={dtype})")
     assert said.startswith("0" if fits else "-1") and ("overlap" in said) == (not fits)
+
+
+def test_a_plan_that_does_not_fit_leaves_no_error_behind(fake):
+    """The runtime keeps the last error until it is read: the next launch, the library's or torch's, would be taken for a failure."""
+    (failed, _), (said, launches) = _calls(fake, ADAMW + """
+fake.fake_largest(0, ctypes.c_size_t(0))
+create((P, None, 10))
+scores(10, 100)
+""")
+    assert failed.startswith("-3") and "hipMalloc" in failed and said == "workspace=0" and len(launches) == 1
