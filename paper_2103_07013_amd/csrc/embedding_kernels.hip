@@ -757,17 +757,25 @@ __global__ __launch_bounds__(256) void k_embed_few_join(FewArgs a) {
 constexpr uint32_t kFewBytes = 64 << 10, kFewParts = 256;
 // How many work-groups share the tokens of a table of few rows (0: the table has more): for sums not much larger than the gradients, no fewer
 // than 64 tokens for each.
-uint32_t few_parts(uint32_t count, uint32_t rows, uint32_t width, bool wide) {
-    if (rows > 16 || rows * 256u * (wide ? 16u : 32u) > kFewBytes || (uint64_t)rows * width >= 1u << 31) return 0;
+uint32_t few_parts(uint32_t count, uint32_t rows, bool wide) {
+    if (rows > 16 || rows * 256u * (wide ? 16u : 32u) > kFewBytes) return 0;
     const uint32_t n = (count + 63) / 64;
     return n < kFewParts ? n : kFewParts;
 }
 
+// Columns of one launch: a grid has less than 2^32 threads, and up to 65535 work-groups along its second axis.
+constexpr uint32_t kFewColumns = 1u << 22;
 template <class T, class O, int GROUP>
-void few(FewArgs f, hipStream_t stream) {
-    const uint32_t blocks = (f.width + GROUP * T::kPer16 - 1) / (GROUP * T::kPer16);
-    hipLaunchKernelGGL((k_embed_few<T, GROUP>), dim3(f.parts, blocks), dim3(256), f.rows * 256 * T::kPer16 * sizeof(float), stream, f);
-    hipLaunchKernelGGL((k_embed_few_join<O>), dim3((uint32_t)(((uint64_t)f.rows * f.width + 15) / 16)), dim3(256), 0, stream, f);
+void few(const FewArgs& a, hipStream_t stream) {
+    FewArgs f = a;
+    for (uint32_t first = 0; first < a.width; first += kFewColumns) {
+        f.width = a.width - first < kFewColumns ? a.width - first : kFewColumns;
+        f.grad = static_cast<const typename T::raw*>(a.grad) + first;
+        f.out = static_cast<typename O::raw*>(a.out) + first;
+        const uint32_t blocks = (f.width + GROUP * T::kPer16 - 1) / (GROUP * T::kPer16);
+        hipLaunchKernelGGL((k_embed_few<T, GROUP>), dim3(f.parts, blocks), dim3(256), f.rows * 256 * T::kPer16 * sizeof(float), stream, f);
+        hipLaunchKernelGGL((k_embed_few_join<O>), dim3((f.rows * f.width + 15) / 16), dim3(256), 0, stream, f);
+    }
 }
 
 size_t whole(size_t n) { return (n + 255) / 256 * 256; }
@@ -792,7 +800,7 @@ hipError_t embed_grad(const EmbedGradArgs& a, hipStream_t stream) {
         return hipGetLastError();
     }
     const uint32_t lanes = (a.width + T::kPer16 - 1) / T::kPer16;
-    if (uint32_t parts = few_parts(a.count, a.rows, a.width, T::kPer16 == 4)) {
+    if (uint32_t parts = few_parts(a.count, a.rows, T::kPer16 == 4)) {
         const uint32_t length = (a.count + parts - 1) / parts;
         parts = (a.count + length - 1) / length;
         uint32_t* used = static_cast<uint32_t*>(a.workspace);
@@ -902,7 +910,7 @@ size_t embed_grad_workspace(uint32_t count, uint32_t rows, uint32_t width) {
     const SortPlan plan = sort_plan(count, rows);
     const uint32_t length = piece_length(count, width);
     // the gradient's type is not known here: enough for either way
-    const size_t few = (size_t)few_parts(count, rows, width, true) * ((size_t)rows * width * 4 + 16);
+    const size_t few = (size_t)few_parts(count, rows, true) * ((size_t)rows * (width < kFewColumns ? width : kFewColumns) * 4 + 16);
     const size_t sorted = 4 * whole((size_t)count * 4) + whole(((size_t)(plan.row + 1) << plan.digit) * 4) + whole(rows) + kMaxPieces + (count + (size_t)length - 1) / length * 2 * width * 4;
     return few > sorted ? few : sorted;
 }

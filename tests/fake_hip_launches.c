@@ -1,5 +1,5 @@
 /* The stand-in for the HIP runtime (fake_hip.c) with a line for every launch that says how large it is, with what the runtime
- * refuses (a grid of 2^32 threads or more), and with the last error, which stays until it is read. */
+ * refuses (a grid of 2^32 threads or more along x, or more than 65535 work-groups along y), and with the last error, which stays until it is read. */
 #define hipLaunchKernel fake_plain_launch
 #define hipGetLastError fake_no_last_error
 #define hipMalloc fake_plain_malloc
@@ -31,6 +31,6 @@ hipError_t hipLaunchKernel(const void* f, dim3 grid, dim3 block, void** args, si
     const int n = snprintf(g_launches + g_launches_at, room, "%s grid=%ux%u threads=%u lds=%zu\n", kernel_name(f), grid.x, grid.y, block.x, shared);
     if (n < 0 || (size_t)n >= room) abort();
     g_launches_at += (size_t)n;
-    return kept((uint64_t)grid.x * grid.y * block.x >> 32 ? hipErrorInvalidConfiguration : hipSuccess);
+    return kept((uint64_t)grid.x * block.x >> 32 || grid.y > 65535 ? hipErrorInvalidConfiguration : hipSuccess);
 }
 hipError_t hipGetDevice(int* device) { *device = 0; return hipSuccess; }

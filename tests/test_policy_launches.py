@@ -107,3 +107,35 @@ create((P, None, 10))
 scores(10, 100)
 """)
     assert failed.startswith("-3") and "hipMalloc" in failed and said == "workspace=0" and len(launches) == 1
+
+
+EMBEDDING = """
+lib.bps_embedding_backward_workspace.restype, lib.bps_embedding_backward_workspace.argtypes = ctypes.c_size_t, [l, u, u]
+lib.bps_embedding_backward.argtypes = [p, i, l, p, i, u, u, l, f, p, i, l, i, p, l, p]
+
+def gradient(count, rows, width, dtype=0, accumulate=0):
+    size = lib.bps_embedding_backward_workspace(count, rows, width)
+    fake.fake_clear_launches()
+    status = lib.bps_embedding_backward(P, 32, count, P, dtype, rows, width, width, 1.0, P, 0, width, accumulate, P if size else None, size, None)
+    assert status == 0, bps.bps_last_error()
+    print("workspace=%d" % size)
+    print(fake.fake_launches().decode(), end="")
+"""
+
+
+@pytest.mark.parametrize("dtype,rows", [(0, 1), (0, 16), (1, 8)])
+@pytest.mark.parametrize("count", [5, 16384])
+@pytest.mark.parametrize("width", [1 << 20, 20_000_000, 300_000_000, (1 << 30) - 1])
+def test_tables_of_few_rows_of_any_width(fake, width, count, rows, dtype):
+    """No launch is larger than the runtime takes, however wide the rows are, and the workspace does not grow without end."""
+    (said, launches), = _calls(fake, EMBEDDING + f"gradient({count}, {rows}, {width}, {dtype})")
+    assert {name for name, _, _ in launches} == {"k_embed_few", "k_embed_few_join"}
+    # a work-group takes 64 lanes of columns of a part of the tokens, or 16 sums of the result: all of them are there
+    lanes = 64 * (8 if dtype else 4)
+    assert sum(n for name, n, _ in launches if name == "k_embed_few") >= -(-width // lanes) * (1 if count == 5 else 256)
+    assert sum(n for name, n, _ in launches if name == "k_embed_few_join") >= -(-rows * width // 16)
+
+
+@pytest.mark.parametrize("count,rows,width", [(1, 1, 1), (33, 1000, 1), (9000, 17, 3), (1 << 20, (1 << 30) - 1, 1), ((1 << 31) - 1, 40, 1), (20000, 100, 1 << 20), (0, (1 << 30) - 1, 8)])
+def test_sorted_gradients_of_any_size(fake, count, rows, width):
+    _calls(fake, EMBEDDING + f"gradient({count}, {rows}, {width})\ngradient({count}, {rows}, {width}, accumulate=1)")
