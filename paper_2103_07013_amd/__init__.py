@@ -12,15 +12,18 @@ from .binding import (BpsError, Renderer, bps_create, bps_destroy, bps_last_erro
 
 __all__ = ["BpsError", "Renderer", "bps_create", "bps_destroy", "bps_last_error", "bps_last_kernel_ms", "bps_kernel_ms_total", "bps_kernel_ms_each", "bps_set_diagnostics", "bps_read_diagnostics",
            "bps_load_scene", "bps_load_scene_async", "bps_load_scene_textured", "bps_scene_ready", "bps_pack_clusters", "bps_query", "bps_render", "bps_render_static", "bps_set_profiling", "bps_unload_scene", "load_library",
-           "MODE_DEPTH", "MODE_RGBD", "FLAG_NO_CLUSTER_CULL", "FLAG_NO_OCCLUSION_CULL", "FLAG_NO_DISPATCH_ORDER", "FLAG_INPUTS_READY", "FLAG_BILINEAR", "EXPORTS",
-           "log_probs", "log_probs_backward", "LogProbs", "embedding", "embedding_backward", "AdamW"]
+           "MODE_DEPTH", "MODE_RGBD", "FLAG_NO_CLUSTER_CULL", "FLAG_NO_OCCLUSION_CULL", "FLAG_NO_DISPATCH_ORDER", "FLAG_INPUTS_READY", "FLAG_BILINEAR", "EXPORTS"]
 
-
+# The policy's operators need torch from the start, the renderer only where it is given torch's tensors: they are imported when they are
+# first asked for, and not by `import *`.
 _POLICY = ("log_probs", "log_probs_backward", "LogProbs", "embedding", "embedding_backward", "AdamW")
 
 
+def __dir__():
+    return sorted({*globals(), *_POLICY})
+
+
 def __getattr__(name):
-    # the policy's operators need torch from the start, the renderer only where it is given torch's tensors
     if name in _POLICY:
         from . import policy
         globals().update((n, getattr(policy, n)) for n in _POLICY)
