@@ -604,8 +604,8 @@ constexpr uint32_t kWaveRow = 2048, kLongWaveRow = 8192, kWaveRows = 2048;
 // with 20 alternatives: 64 x 8192 3.8 / 6.2 us, 192 x 50257 9.2 / 9.0 (20.0 / 15.9), 256 x 131072 18.0 / 15.8 (36.8 / 25.6), 384 x 50257 13.5 / 14.7
 // (24.5 / 29.1), 512 x 131072 23.7 / 27.8 (43.4 / 45.9).
 constexpr uint32_t kComputeUnits = 256;
-// Of up to kPieceRows rows, those longer than kLongRow are cut, so that there are up to kGroups pieces of not less than kPieceEntries, what a work-group
-// loads at once.  Sixteen wavefronts / pieces: 1 x 32768 5.4 / 5.2 us (9.9 / 11.2), 1 x 131072 11.2 / 5.5 (21.0 / 11.2), 32 x 131072 11.6 / 6.6
+// Of up to kPieceRows rows, those longer than kLongRow are cut, so that there are up to kGroups pieces, and as many of a row at most as it has blocks
+// of kPieceEntries, what a work-group loads at once of 16-bit entries (half of that of float32 ones).  Sixteen wavefronts / pieces: 1 x 32768 5.4 / 5.2 us (9.9 / 11.2), 1 x 131072 11.2 / 5.5 (21.0 / 11.2), 32 x 131072 11.6 / 6.6
 // (21.8 / 12.9), 64 x 50257 8.7 / 7.4 (15.3 / 13.6), 128 x 50257 8.9 / 8.4 (15.5 / 16.1).
 constexpr uint32_t kPieceRows = 64, kLongRow = 32768, kGroups = 512, kPieceEntries = 8192;
 
