@@ -241,7 +241,8 @@ bps_status bps_query(bps_renderer *r, bps_scene scene, int32_t what, uint64_t *v
  * `stream` (a hipStream_t of that device, NULL = default stream) and return; all buffers must stay alive until the
  * stream reaches the end of the call.  Nothing is allocated (bps_adamw_create aside) and nothing is copied from
  * the host, so that calls can be captured into a graph.  Their failures' texts are those of bps_last_error(NULL)
- * on the calling thread.  A call that fails has enqueued nothing, unless its status is BPS_ERR_HIP.
+ * on the calling thread.  A call that fails has enqueued nothing, unless its status is BPS_ERR_HIP.  Results share no memory
+ * with inputs, unless a call says that they may.
  * Element types are BPS_F32, BPS_BF16 and BPS_F16; sums are held in float32 whatever the type.  A row may start at any
  * element: rows of odd widths need no padding.  Tokens are int32 or int64 (token_bits 32 or 64).  No results depend on
  * the order in which work-groups run: the same call gives the same bits. */
@@ -341,7 +342,10 @@ typedef struct {
  * bps_adamw_destroy.  Calls on one handle must not overlap: on the host, and on the device (one stream, or ordered streams). */
 bps_status bps_adamw_create(const bps_adamw_config *cfg, bps_adamw **out);
 void bps_adamw_destroy(bps_adamw *h);    /* waits for the device; NULL is ignored */
-/* One step.  grads: HOST array of `tensors` device pointers, each to `count` elements of grad_dtype (param_dtype or BPS_F32),
+/* One step.  A captured step replays with the step number, lr and factors that it was captured with, and with 8 bits with the same
+ * dither every time, which then no longer keeps the mean over many steps: capture each step anew, or use 32 bits and a
+ * number late enough for the bias corrections.
+ * grads: HOST array of `tensors` device pointers, each to `count` elements of grad_dtype (param_dtype or BPS_F32),
  * NULL = no gradient: that tensor and its states are left as they are.  The addresses are consumed during the call.
  * grad_norm: device float32 [1] or NULL, receives the norm where max_norm > 0. */
 bps_status bps_adamw_step(bps_adamw *h, const void *const *grads, int32_t grad_dtype, uint64_t step, double lr, double beta1, double beta2, double eps,

@@ -1,14 +1,17 @@
-// AdamW over many tensors at once; states in 32 or in 8 bits.  The rule is in include/bps.h: every operation is rounded by itself
-// (the library is built without contraction), so that what 8-bit states are rounded to can be reproduced bit for bit.
+// AdamW over many tensors at once; states in 32 or in 8 bits.  The rule is in include/bps.h: every operation is
+// rounded by itself (the library is built without contraction), so that what 8-bit states are rounded to can be
+// reproduced bit for bit.
 //
-// A work-group takes a chunk of kAdamChunk elements of one tensor; a table made with the handle says which, so that tensors of any size keep all
-// compute units busy and a launch takes up to kAdamGrads of them.  A lane takes four elements at a time, a wavefront the 256 of a state block,
-// whose largest magnitudes are found across its lanes (both at once, as the halves of one word).
+// A work-group takes a chunk of kAdamChunk elements of one tensor; a table made with the handle says which, so
+// that tensors of any size keep all compute units busy and a launch takes up to kAdamGrads of them.  A lane
+// takes four elements at a time, a wavefront the 256 of a state block, whose largest magnitudes are found
+// across its lanes (both at once, as the halves of one word).
 //
-// What bounds it, on one MI355X (median kernel times): the memory.  4e8 float32 parameters 2.03 ms (5.5 TB/s of the 28 bytes each has to move; a copy reaches
-// 4.9); 1.2e8 bf16 ones with float32 masters and 8-bit states 333 us (5.8 TB/s of 16 bytes each), with the vector units near their limit
-// too: the exact root and quotient, three products of the hash and the codes take about 90 instructions an element; read back 210 us
-// (5.7 TB/s).  5.3e6 parameters in 38 tensors with a bound on the norm 7 and 27 us.
+// What bounds it, on one MI355X (median kernel times): the memory.  4e8 float32 parameters 2.03 ms (5.5 TB/s of
+// the 28 bytes each has to move; a copy reaches 4.9); 1.2e8 bf16 ones with float32 masters and 8-bit states 333
+// us (5.8 TB/s of 16 bytes each), with the vector units near their limit too: the exact root and quotient,
+// three products of the hash and the codes take about 90 instructions an element; read back 210 us (5.7 TB/s).
+// 5.3e6 parameters in 38 tensors with a bound on the norm 7 and 26 us.
 #include "policy_device.h"
 #include "policy_kernels.h"
 
@@ -20,8 +23,9 @@ constexpr uint32_t kPerLane = 4;
 static_assert(kStateBlock == 64 * kPerLane, "a wavefront's elements share an exponent");
 static_assert(kAdamChunk == kAdamGroup * kPerLane, "a chunk is what a work-group takes at once");
 
-// 8-bit codes are the upper bits of a float32 with a bias of their own: shifted to where those are, subnormal ones included, a code is a float that
-// is a power of two away from what it stands for.  e: the block's exponent byte.
+// 8-bit codes are the upper bits of a float32 with a bias of their own: shifted to where those are, subnormal
+// ones included, a code is a float that is a power of two away from what it stands for.  e: the block's
+// exponent byte.
 template <int TOP>
 __device__ __forceinline__ float decoded(uint32_t code, uint32_t e) {
     return __builtin_amdgcn_ldexpf(__uint_as_float(code << 20), (int)e - TOP);
@@ -34,7 +38,8 @@ __device__ __forceinline__ uint32_t exponent_for(uint32_t magnitude) {
     return e < LEAST ? LEAST : e > 255u ? 255u : e;
 }
 
-// The other way: the code's place is above 20 bits, to which 20 bits of dither (a 16-bit number, times 16) are added before they are cut off.
+// The other way: the code's place is above 20 bits, to which 20 bits of dither (a 16-bit number, times 16) are
+// added before they are cut off.
 template <int TOP>
 __device__ __forceinline__ uint32_t encoded(float magnitude, uint32_t e, uint32_t dither) {
     return (__float_as_uint(__builtin_amdgcn_ldexpf(magnitude, TOP - (int)e)) + (dither << 4)) >> 20;
@@ -54,8 +59,9 @@ __device__ __forceinline__ double wave_sum(double x) {
     return x;
 }
 
-// Sums of squares: each work-group those of every gridDim.x-th four chunks, so that four loads are on their way at once.  In 64 bits, since the
-// square of a float32 from 1.8e19 on is none, nor is that of one below 1e-23; the memory bounds it either way.
+// Sums of squares: each work-group those of every gridDim.x-th four chunks, so that four loads are on their way
+// at once.  In 64 bits, since the square of a float32 from 1.8e19 on is none, nor is that of one below 1e-23;
+// the memory bounds it either way.
 template <class G>
 __global__ __launch_bounds__(kAdamGroup) void k_adamw_norm(AdamPlan plan, AdamGrads grads, uint32_t first_tensor, uint32_t first_chunk, uint32_t chunks, uint32_t first_sum,
                                                            AdamScalars s) {

@@ -1,16 +1,17 @@
 // Embedding lookup with scaling, and its gradient by sorted tokens.
 //
-// Gradient: (row, token) pairs are sorted by row, stably, by digits of a few bits from the lowest up; the sorted order
-// is cut into pieces of equal length, and one group of lanes walks a piece, adding up gradient rows in float32 in
-// that order.  A row that lies within one piece is written at once.  One that is cut by a piece's bounds leaves a
-// partial sum per piece, which are added in order by a second kernel.  The sort marks the rows that have a token; the others
-// are written as zeros next to the sums, or all of a table that is little used is cleared next to the sort.  Tables of up to 16
-// rows need no sort: sums of all rows fit in LDS.
+// Gradient: (row, token) pairs are sorted by row, stably, by digits of a few bits from the lowest up; the
+// sorted order is cut into pieces of equal length, and one group of lanes walks a piece, adding up gradient
+// rows in float32 in that order.  A row that lies within one piece is written at once.  One that is cut by a
+// piece's bounds leaves a partial sum per piece, which are added in order by a second kernel.  The sort marks
+// the rows that have a token; the others are written as zeros next to the sums, or all of a table that is
+// little used is cleared next to the sort.  Tables of up to 16 rows need no sort: sums of all rows fit in LDS.
 //
-// What bounds it, on one MI355X (median kernel times): long batches the memory, the lookup of 262144 rows of 2048 bf16 290 us (5.8 TB/s of what it
-// moves), their sums into 131072 float32 rows 415 us (5.1 TB/s), sorting 40 us, joining cut rows
-// 39 us.  Middling ones the launches one after the other, each waiting for a few memory round trips: 16384 tokens and 50257 rows
-// of 769, 24 us of sort, 30 us of sums (5.8 TB/s), 13 us of joining.  Few rows: 32768 tokens of 5 rows of 32 4.8 us and 2.9 us.
+// What bounds it, on one MI355X (median kernel times): long batches the memory, the lookup of 262144 rows of
+// 2048 bf16 290 us (5.8 TB/s of what it moves), their sums into 131072 float32 rows 415 us (5.3 TB/s), sorting
+// 40 us, joining cut rows 40 us.  Middling ones the launches one after the other, each waiting for a few memory
+// round trips: 16384 tokens and 50257 rows of 769, 23 us of sort, 30 us of sums (6.3 TB/s), 13 us of joining (8
+// MB; each work-group lists the cut rows first).  Few rows: 32768 tokens of 5 rows of 32 4.8 us and 2.9 us.
 #include <type_traits>
 
 #include "policy_device.h"
@@ -21,10 +22,11 @@ namespace bps {
 namespace {
 
 constexpr uint32_t kSortGroup = 512, kSortTile = 2048, kMaxDigit = 9;
-// Up to this many tokens are sorted by one work-group, in one launch.  Measured at 50257 rows (two passes), one work-group / two launches a pass:
-// 4096 tokens 13 / 21 us, 8192 20 / 21, without what the launches take apart.
+// Up to this many tokens are sorted by one work-group, in one launch.  Measured at 50257 rows (two passes), one
+// work-group / two launches a pass: 4096 tokens 13 / 21 us, 8192 20 / 21, without what the launches take apart.
 constexpr uint32_t kSortOne = 8192, kSortOneGroup = 1024;
-// Up to this many tiles each work-group adds up the counts of those before its own by itself; for more a launch in between does.
+// Up to this many tiles each work-group adds up the counts of those before its own by itself; for more a launch
+// in between does.
 constexpr uint32_t kSumTiles = 32;
 
 uint32_t bits_of(uint32_t v) {
@@ -74,8 +76,8 @@ struct SortArgs {
 };
 
 constexpr uint32_t kFill = 4096;      // of 16 bytes
-// Zeros into all of a.fill, 16 bytes at a time, by the threads of `groups` work-groups, 64 KiB after 64 KiB: 1 GiB takes 210 us so, 255 with all
-// work-groups side by side along it, 286 so and past the caches.
+// Zeros into all of a.fill, 16 bytes at a time, by the threads of `groups` work-groups, 64 KiB after 64 KiB: 1
+// GiB takes 210 us so, 255 with all work-groups side by side along it, 286 so and past the caches.
 __device__ __forceinline__ void fill_zeros(const SortArgs& a, uint32_t group, uint32_t groups) {
     char* p = static_cast<char*>(a.fill);
     const uint32_t head = (uint32_t)(-reinterpret_cast<uintptr_t>(p) & 15u);
@@ -95,7 +97,8 @@ __device__ __forceinline__ void fill_zeros(const SortArgs& a, uint32_t group, ui
 
 __device__ __forceinline__ uint32_t sort_key(const SortArgs& a, uint32_t i) { return a.keys ? a.keys[i] : key_at(a.tokens, a.tokens64, i, a.rows); }
 
-// (Counted by the pass before, with an atomic addition for each pair, the second pass's counts cost 20 to 230 us: tokens in frequent use meet.)
+// (Counted by the pass before, with an atomic addition for each pair, the second pass's counts cost 20 to 230
+// us: tokens in frequent use meet.)
 __global__ __launch_bounds__(kSortGroup) void k_sort_count(SortArgs a) {
     __shared__ uint32_t hist[1u << kMaxDigit];
     if (blockIdx.x >= a.tiles) {
@@ -171,9 +174,10 @@ __device__ __forceinline__ void exclusive_sums(uint32_t* v, uint32_t bins, uint3
     __syncthreads();
 }
 
-// Where the pairs of ROUNDS * 64 consecutive places that a wavefront holds go, 64 at a time: among the lanes of equal digits the rank
-// is the number of lanes before, so that pairs of equal digits keep their order.  at[wave][digit]: first how many the
-// wavefront has, then, after `spread` has turned counts into places, the next free one.
+// Where the pairs of ROUNDS * 64 consecutive places that a wavefront holds go, 64 at a time: among the lanes of
+// equal digits the rank is the number of lanes before, so that pairs of equal digits keep their order.
+// at[wave][digit]: first how many the wavefront has, then, after `spread` has turned counts into places, the
+// next free one.
 template <uint32_t ROUNDS>
 struct Ranks {
     uint64_t same[ROUNDS];
@@ -373,8 +377,9 @@ __global__ __launch_bounds__(256) void k_embed(EmbedArgs a) {
 
 // ---- gradient
 
-// Tokens of a piece: so many that there are about 2048 pieces, 4096 of narrow rows, which take few lanes each, so that all compute units have
-// some; but no fewer than 8, to keep partial sums few, and from 64 on as many as kMaxPieces allow.  Up to 32 tokens are one piece: nothing is cut.
+// Tokens of a piece: so many that there are about 2048 pieces, 4096 of narrow rows, which take few lanes each,
+// so that all compute units have some; but no fewer than 8, to keep partial sums few, and from 64 on as many as
+// kMaxPieces allow.  Up to 32 tokens are one piece: nothing is cut.
 constexpr uint32_t kPiece = 64, kMaxPieces = 4096, kNarrow = 64;
 uint32_t piece_length(uint32_t count, uint32_t width) {
     uint32_t n = count <= 32 ? 32 : 8;
@@ -447,8 +452,9 @@ uint32_t zero_rows(uint32_t width, uint32_t together) {
 template <class O>
 __global__ __launch_bounds__(256) void k_embed_zero(SumArgs a) { write_zeros<O, 64>(a, blockIdx.x); }
 
-// 16 bytes of AHEAD rows, of which `left` columns are the row's, as they lie there: all loads are on their way before the first value is converted.  (A
-// load and its conversion under one condition are waited for there: 519 instead of 429 us for 262144 rows of 2048 bf16.)
+// 16 bytes of AHEAD rows, of which `left` columns are the row's, as they lie there: all loads are on their way
+// before the first value is converted.  (A load and its conversion under one condition are waited for there:
+// 519 instead of 429 us for 262144 rows of 2048 bf16.)
 template <class T, int AHEAD>
 __device__ __forceinline__ void rows_ahead(const typename T::raw* const (&g)[AHEAD], uint32_t left, Words (&x)[AHEAD]) {
     constexpr int N = T::kPer16, kInWord = N / 4;
@@ -467,8 +473,8 @@ __device__ __forceinline__ void rows_ahead(const typename T::raw* const (&g)[AHE
     }
 }
 
-// GROUP lanes for N columns each of a piece; 256 / GROUP pieces (or column blocks of one) to a work-group.  Keys and places are
-// fetched 64 at a time, rows kAhead at a time, so that that many are on their way at once.
+// GROUP lanes for N columns each of a piece; 256 / GROUP pieces (or column blocks of one) to a work-group.
+// Keys and places are fetched 64 at a time, rows kAhead at a time, so that that many are on their way at once.
 template <class T, class O, int GROUP>
 __global__ __launch_bounds__(256) void k_embed_sum(SumArgs a) {
     constexpr int N = T::kPer16, kSlots = 256 / GROUP, kAhead = 8;
@@ -534,9 +540,10 @@ __global__ __launch_bounds__(256) void k_embed_sum(SumArgs a) {
     }
 }
 
-// The rows that are cut.  Each work-group lists the pieces in which such a row begins, those of few partial sums and those of many.  2^join_bits
-// lanes, 4 columns each, add up the sums of a row with few; of rows with many all lanes of a work-group do, each such share of
-// them a part of the sums in order, and then those parts in a fixed order.
+// The rows that are cut.  Each work-group lists the pieces in which such a row begins, those of few partial
+// sums and those of many.  2^join_bits lanes, 4 columns each, add up the sums of a row with few; of rows with
+// many all lanes of a work-group do, each such share of them a part of the sums in order, and then those parts
+// in a fixed order.
 template <class O>
 __global__ __launch_bounds__(1024) void k_embed_join(SumArgs a) {
     constexpr uint32_t kFew = 8, kTogether = 8, kWords = kMaxPieces / 64, kRounds = kMaxPieces / 1024;
@@ -555,7 +562,8 @@ __global__ __launch_bounds__(1024) void k_embed_join(SumArgs a) {
         if (lane == 0) through[piece / 64] = with;
     }
     __syncthreads();
-    // partial sums of the row that begins in a piece: of this one, of those that it goes through, and of the one that it ends in
+    // partial sums of the row that begins in a piece: of this one, of those that it goes through, and of the
+    // one that it ends in
     auto partial_sums = [&](uint32_t piece) {
         const uint32_t at = piece + 1;
         for (uint32_t word = at / 64; word < kWords; ++word) {
@@ -657,9 +665,9 @@ __global__ __launch_bounds__(1024) void k_embed_join(SumArgs a) {
 
 // ---- gradient of tables of few rows
 
-// A policy's moves, say: every row has many tokens, and sums of all rows fit in LDS, so that nothing is sorted.  GROUP lanes for N columns each; the
-// groups of a work-group add up a part of its tokens each, in order, into sums of their own, which are joined in order, and
-// the work-groups' sums by a second kernel.
+// A policy's moves, say: every row has many tokens, and sums of all rows fit in LDS, so that nothing is sorted.
+// GROUP lanes for N columns each; the groups of a work-group add up a part of its tokens each, in order, into
+// sums of their own, which are joined in order, and the work-groups' sums by a second kernel.
 struct FewArgs {
     const void *tokens, *grad;
     void* out;
@@ -724,7 +732,8 @@ __global__ __launch_bounds__(256) void k_embed_few(FewArgs a) {
     }
 }
 
-// 16 lanes for a column of a row, each of which adds up every 16th part's sum.  With accumulate, rows that had no token are not written.
+// 16 lanes for a column of a row, each of which adds up every 16th part's sum.  With accumulate, rows that had
+// no token are not written.
 template <class O>
 __global__ __launch_bounds__(256) void k_embed_few_join(FewArgs a) {
     __shared__ float part[16][16];
@@ -755,8 +764,8 @@ __global__ __launch_bounds__(256) void k_embed_few_join(FewArgs a) {
 
 // Sums of so many bytes are held by a work-group, two to a compute unit.
 constexpr uint32_t kFewBytes = 64 << 10, kFewParts = 256;
-// How many work-groups share the tokens of a table of few rows (0: the table has more): for sums not much larger than the gradients, no fewer
-// than 64 tokens for each.
+// How many work-groups share the tokens of a table of few rows (0: the table has more): for sums not much
+// larger than the gradients, no fewer than 64 tokens for each.
 uint32_t few_parts(uint32_t count, uint32_t rows, bool wide) {
     if (rows > 16 || rows * 256u * (wide ? 16u : 32u) > kFewBytes) return 0;
     const uint32_t n = (count + 63) / 64;
@@ -827,8 +836,8 @@ hipError_t embed_grad(const EmbedGradArgs& a, hipStream_t stream) {
     s.cuts = reinterpret_cast<uint8_t*>(w);
     w += kMaxPieces;
     s.partial = reinterpret_cast<float*>(w);
-    // Where most rows have no token the whole table is cleared by work-groups of the sort's first launch, a contiguous one in whole cache lines;
-    // else the rows that have none are, next to the sums.
+    // Where most rows have no token the whole table is cleared by work-groups of the sort's first launch, a
+    // contiguous one in whole cache lines; else the rows that have none are, next to the sums.
     const bool cleared = !a.accumulate && a.out_stride == a.width && a.count < a.rows / 4;
     const uint64_t bytes = (uint64_t)a.rows * a.width * sizeof(typename O::raw);
     SortArgs sort = {a.tokens, nullptr, nullptr, buffer[0], buffer[1], counts, cleared || a.accumulate ? nullptr : marks, cleared ? a.out : nullptr, bytes, a.tokens64, a.count,

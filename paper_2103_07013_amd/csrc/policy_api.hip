@@ -168,7 +168,8 @@ bps_status bps_adamw_create(const bps_adamw_config* cfg, bps_adamw** out) {
         chunks += (t.count + bps::kAdamChunk - 1) / bps::kAdamChunk;
     }
     if (chunks >= 1ull << 23) return fail_here(BPS_ERR_UNSUPPORTED, "%s: too many elements", what);
-    // failures are told by the status; the runtime's last error, which the next launch would be taken to have failed with, is cleared
+    // failures are told by the status; the runtime's last error, which the next launch would be taken to have
+    // failed with, is cleared
     int ndev = 0, device = 0;
     if (hipGetDeviceCount(&ndev) != hipSuccess || ndev <= 0 || hipGetDevice(&device) != hipSuccess) {
         (void)hipGetLastError();

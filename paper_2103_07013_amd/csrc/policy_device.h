@@ -1,4 +1,5 @@
-// What the kernels of a policy's operators share: element types, loads of 16 bytes, what lanes of a wavefront exchange.
+// What the kernels of a policy's operators share: element types, loads of 16 bytes, what lanes of a wavefront
+// exchange.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -92,10 +93,12 @@ __device__ __forceinline__ void store(typename T::raw* p, const float (&x)[N], b
         store<T, N>(p, x);
 }
 
-// Whether results of `rows` rows are better written past the caches: where they do not fit the Infinity Cache (256 MiB), so that inputs may stay there, and
-// all rows begin at whole cache lines, since parts of lines are not joined on the way.  Measured, through / past the caches: gradient of 8192 x
-// 131072 bf16 logits 826 / 780 us, and the pass before it, which then finds some of the logits, 405 / 371; 262144 rows of 2048 bf16 332 / 312;
-// 50257 rows of 769 float32 (not whole lines) 31 / 45; state of 1.2e8 parameters as float32 251 / 270 (there it stays as it was).
+// Whether results of `rows` rows are better written past the caches: where they do not fit the Infinity Cache
+// (256 MiB), so that inputs may stay there, and all rows begin at whole cache lines, since parts of lines are
+// not joined on the way.  Measured, through / past the caches: gradient of 8192 x 131072 bf16 logits 826 / 780
+// us, and the pass before it, which then finds some of the logits, 405 / 371; 262144 rows of 2048 bf16 332 /
+// 312; 50257 rows of 769 float32 (not whole lines) 31 / 45; state of 1.2e8 parameters as float32 251 / 270
+// (there it stays as it was).
 inline bool past_caches(const void* p, int64_t stride, size_t size, uint64_t rows, uint64_t width) {
     return rows * width * size > 256u << 20 && (reinterpret_cast<uintptr_t>(p) % 128) == 0 && stride * (int64_t)size % 128 == 0;
 }

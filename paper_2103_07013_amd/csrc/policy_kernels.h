@@ -76,12 +76,13 @@ hipError_t launch_embed_grad(int32_t grad_dtype, int32_t out_dtype, const EmbedG
 
 constexpr uint32_t kStateBlock = 256;     // states of a tensor start at a multiple of this; 8-bit states share an exponent over as many
 constexpr uint32_t kAdamGroup = 256;      // threads of a work-group
-// Elements of a work-group: four to a thread, at once.  Chunks of 1024 / 2048 / 4096: 1.92e8 float32 parameters 965 / 1008 / 1012 us, 1.2e8 bf16 ones
-// with 8-bit states 331 / 369 / 378.
+// Elements of a work-group: four to a thread, at once.  Chunks of 1024 / 2048 / 4096: 1.92e8 float32 parameters
+// 965 / 1008 / 1012 us, 1.2e8 bf16 ones with 8-bit states 331 / 369 / 378.
 constexpr uint32_t kAdamChunk = 1024;
 constexpr uint32_t kAdamGrads = 448;      // gradients of one launch: their addresses travel as kernel arguments
-// Sums of squares of all gradients, in which every work-group of the step finds the norm for itself: a second launch more, or a counter of
-// work-groups with the cache write-backs that it needs (35 us for 5.3e6 parameters), cost more than reading them does (see k_adamw_norm).
+// Sums of squares of all gradients, in which every work-group of the step finds the norm for itself: a second
+// launch more, or a counter of work-groups with the cache write-backs that it needs (35 us for 5.3e6
+// parameters), cost more than reading them does (see k_adamw_norm).
 constexpr uint32_t kAdamSums = 1024;
 
 struct AdamTensor {

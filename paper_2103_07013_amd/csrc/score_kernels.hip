@@ -5,14 +5,17 @@
 //   lse = scale m + ln z,  logp = scale (x_t - m) - ln z,  entropy = ln z - s / z
 //   d logp / dx_j = scale (d_jt - p_j),  d entropy / dx_j = -scale p_j (ln p_j + entropy)
 //
-// All sums are held in float32 and exponents taken to the base 2.  A lane keeps m, z and s of what it has seen, and rescales z and s when m
-// grows, so that one pass over the logits is enough; lanes, wavefronts and pieces of a row are joined by the same rule.  m and ln z are kept
-// apart for the gradient: their sum, lse, loses ln z where logits are large (rows of a type's lowest value).
+// All sums are held in float32 and exponents taken to the base 2.  A lane keeps m, z and s of what it has seen,
+// and rescales z and s when m grows, so that one pass over the logits is enough; lanes, wavefronts and pieces
+// of a row are joined by the same rule.  m and ln z are kept apart for the gradient: their sum, lse, loses ln z
+// where logits are large (rows of a type's lowest value).
 //
-// What bounds it, on one MI355X (median kernel times): long rows the memory, 8192 x 131072 bf16 in 361 us (5.9 TB/s, with what the Infinity Cache still
-// holds) and their gradient in 737 us (5.8 TB/s of 4.3 GB); the pass itself is near the vector units' limit too, with nine instructions and one
-// exponential (four times the issue slots) an entry.  Short rows the launch: 32768 x 6 float32 3.5 us, the gradient 3.1.  Alternatives cost what ordering the candidates costs: 192 x 50257 f16 with 5 of them
-// 17 us, 10 without; 1 x 131072 with 20 in pieces 7 us and their join 5.
+// What bounds it, on one MI355X (median kernel times): long rows the memory, 8192 x 131072 bf16 in 361 us (5.9
+// TB/s, with what the Infinity Cache still holds) and their gradient in 730 to 750 us (5.8 TB/s of 4.3 GB); the
+// pass itself is near the vector units' limit too, with nine instructions and one exponential (four times the
+// issue slots) an entry.  Short rows the launch: 32768 x 6 float32 3.5 us, the gradient 3.1.  Alternatives cost
+// what ordering the candidates costs: 192 x 50257 f16 with 5 of them 17 us, 10 without; 1 x 131072 with 20 in
+// pieces 7 us and their join 5.
 #include <type_traits>
 
 #include "policy_device.h"
@@ -24,8 +27,9 @@ namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr float kLowest = -3.402823466e38f;
-// Stands for differences below it where they are multiplied by a probability, which is zero there (2^-149 is the least float), so that the product
-// is too: near enough to zero that neither the number of entries nor the gradients that come in make it infinite first.
+// Stands for differences below it where they are multiplied by a probability, which is zero there (2^-149 is
+// the least float), so that the product is too: near enough to zero that neither the number of entries nor the
+// gradients that come in make it infinite first.
 constexpr float kFar = -256.0f;
 constexpr float kInf = __builtin_inff();
 
@@ -92,8 +96,9 @@ __device__ __forceinline__ auto mask_bytes(const uint8_t* p) {
         return Bytes{__builtin_bit_cast(uint32_t, q), 0u};
 }
 
-// U times N entries of a row, the u-th from first + u * apart + lane * N on; `all`: the same for all lanes of the wavefront, says that none of them lies behind
-// the row's end.  Loads under a condition of their own would each be waited for before the next.
+// U times N entries of a row, the u-th from first + u * apart + lane * N on; `all`: the same for all lanes of
+// the wavefront, says that none of them lies behind the row's end.  Loads under a condition of their own would
+// each be waited for before the next.
 template <class T, int U, int N, bool MASK>
 __device__ __forceinline__ void row_blocks(const typename T::raw* row, const uint8_t* mask, uint32_t first, uint32_t apart, uint32_t lane, uint32_t end, bool all, float (&x)[U * N]) {
     if (all) {
@@ -225,8 +230,9 @@ __global__ __launch_bounds__(256) void k_score_short(ScoreArgs a) {
 
 // ---- longer rows: a wavefront, or a work-group, streams a row or a piece of one
 
-// The best 64 of what a wavefront has seen, one in each lane in descending order; 0 = none.
-// A bitonic network: halves that are sorted are joined by a comparison with the mirrored lane, then with lanes at falling distances.
+// The best 64 of what a wavefront has seen, one in each lane in descending order; 0 = none. A bitonic network:
+// halves that are sorted are joined by a comparison with the mirrored lane, then with lanes at falling
+// distances.
 template <int X>
 __device__ __forceinline__ uint64_t exchanged(uint64_t v, bool keep_larger) {
     const uint64_t o = bps::from_lane_xor<X>(v);
@@ -321,8 +327,8 @@ struct Best {
         const uint64_t last = __shfl((unsigned long long)list, (int)k - 1, 64);
         if (last) raise(value_of((uint32_t)(last >> 32)), ~(uint32_t)last);
     }
-    // Entries base + place(e); most wavefronts hold few candidates or none, so that each lane's are told first and then taken one
-    // at a time.
+    // Entries base + place(e); most wavefronts hold few candidates or none, so that each lane's are told first
+    // and then taken one at a time.
     template <int N, class Place>
     __device__ __forceinline__ void offer(const float (&x)[N], uint32_t lane, uint32_t k, Place&& place) {
         uint32_t hit = 0;
@@ -370,8 +376,8 @@ __device__ __forceinline__ Part stream(const typename T::raw* row, const uint8_t
         const float top = add(p, x, c);
         if constexpr (TOP) {
             if (first) {
-                // Where at least k lanes' own best reach a bar, the k-th best of all does: the k-th of any wavefront's lanes, and what the
-                // k / WAVES best lanes of every wavefront reach.
+                // Where at least k lanes' own best reach a bar, the k-th best of all does: the k-th of any
+                // wavefront's lanes, and what the k / WAVES best lanes of every wavefront reach.
                 const uint32_t own = rank_of(top);
                 uint32_t bar = reached_by(own, k);
                 if constexpr (WAVES > 1) {
@@ -497,8 +503,9 @@ __global__ __launch_bounds__(TOP ? 1024 : 64) void k_score_join(ScoreArgs a, Pie
 
 // ---- gradient
 
-// With l = log2 p_j = c (x_j - m) - log2 z, the gradient is p_j (slope l + base), and token_grad more for the token's entry.  An entry that takes no
-// part has p = 0 and so the gradient 0, but where the bracket may not be finite: odd, where that has to be asked for, and p multiplied first.
+// With l = log2 p_j = c (x_j - m) - log2 z, the gradient is p_j (slope l + base), and token_grad more for the
+// token's entry.  An entry that takes no part has p = 0 and so the gradient 0, but where the bracket may not be
+// finite: odd, where that has to be asked for, and p multiplied first.
 struct RowGrad {
     float m, log2_z, slope, base, token_grad;
     int64_t t;
@@ -565,7 +572,8 @@ __global__ __launch_bounds__(256) void k_score_grad_short(ScoreGradArgs a) {
     store_entries<T, N>(static_cast<typename T::raw*>(a.out) + (int64_t)r * a.out_stride, lane * N, a.entries, d, false);
 }
 
-// Work-groups take pieces of rows, the last row first: what of the logits the forward pass read last may still be in a cache.
+// Work-groups take pieces of rows, the last row first: what of the logits the forward pass read last may still
+// be in a cache.
 template <class T, bool MASK, int GROUP>
 __global__ __launch_bounds__(GROUP) void k_score_grad(ScoreGradArgs a, uint32_t pieces) {
     constexpr int N = T::kPer16, U = 4;
@@ -588,25 +596,30 @@ __global__ __launch_bounds__(GROUP) void k_score_grad(ScoreGradArgs a, uint32_t 
 
 // ---- which kernel
 
-// Rows of up to kShort entries are held by few lanes, those of up to kWide by a wavefront, 8 entries to a lane, if not many alternatives are asked for, which cost a
-// pass over the lanes each; longer ones are streamed.  Measured with 32768 rows of bf16, held / streamed by a wavefront each: 32 entries 3.8 / 25.7 us, 128
-// 5.4 / 25.2 (with 16 alternatives 22 / 68, with 32 37 / 90, but 300 rows of 100 with 32 17 / 11), 256 15.7 / 24.2 (with 3 alternatives 29 / 41; float32 29 / 29, with
-// 5 36 / 30).
+// Rows of up to kShort entries are held by few lanes, those of up to kWide by a wavefront, 8 entries to a lane,
+// if not many alternatives are asked for, which cost a pass over the lanes each; longer ones are streamed.
+// Measured with 32768 rows of bf16, held / streamed by a wavefront each: 32 entries 3.8 / 25.7 us, 128 5.4 /
+// 25.2 (with 16 alternatives 22 / 68, with 32 37 / 90, but 300 rows of 100 with 32 17 / 11), 256 15.7 / 24.2
+// (with 3 alternatives 29 / 41; float32 29 / 29, with 5 36 / 30).
 constexpr uint32_t kShort = 128, kShortTop = 16, kManyRows = 8192, kShortTopOfMany = 32, kWide = 512, kWideTop = 3;
 bool held(uint64_t rows, uint32_t entries, uint32_t top_k) {
     return entries <= kShort ? top_k <= (rows < kManyRows ? kShortTop : kShortTopOfMany) : entries <= kWide && top_k <= kWideTop;
 }
-// Rows of up to kWaveRow entries have one wavefront, where there are kWaveRows rows or more those of up to kLongWaveRow too.  Measured
-// with bf16, one wavefront / four: 4096 x 2048 6.0 / 14.6 us, 4096 x 4096 8.5 / 14.9, 4096 x 8192 15.1 / 15.4, 512 x 4096 4.3 / 5.2 (with 20
-// alternatives 10.0 / 8.9), 1024 x 8192 6.3 / 6.1 (16.1 / 12.4).
+// Rows of up to kWaveRow entries have one wavefront, where there are kWaveRows rows or more those of up to
+// kLongWaveRow too.  Measured with bf16, one wavefront / four: 4096 x 2048 6.0 / 14.6 us, 4096 x 4096 8.5 /
+// 14.9, 4096 x 8192 15.1 / 15.4, 512 x 4096 4.3 / 5.2 (with 20 alternatives 10.0 / 8.9), 1024 x 8192 6.3 / 6.1
+// (16.1 / 12.4).
 constexpr uint32_t kWaveRow = 2048, kLongWaveRow = 8192, kWaveRows = 2048;
-// Longer ones have four wavefronts, or sixteen where they are longer than kLongWaveRow and there is a compute unit for each row.  Four / sixteen, and
-// with 20 alternatives: 64 x 8192 3.8 / 6.2 us, 192 x 50257 9.2 / 9.0 (20.0 / 15.9), 256 x 131072 18.0 / 15.8 (36.8 / 25.6), 384 x 50257 13.5 / 14.7
-// (24.5 / 29.1), 512 x 131072 23.7 / 27.8 (43.4 / 45.9).
+// Longer ones have four wavefronts, or sixteen where they are longer than kLongWaveRow and there is a compute
+// unit for each row.  Four / sixteen, and with 20 alternatives: 64 x 8192 3.8 / 6.2 us, 192 x 50257 9.2 / 9.0
+// (20.0 / 15.9), 256 x 131072 18.0 / 15.8 (36.8 / 25.6), 384 x 50257 13.5 / 14.7 (24.5 / 29.1), 512 x 131072
+// 23.7 / 27.8 (43.4 / 45.9).
 constexpr uint32_t kComputeUnits = 256;
-// Of up to kPieceRows rows, those longer than kLongRow are cut, so that there are up to kGroups pieces, and as many of a row at most as it has blocks
-// of kPieceEntries, what a work-group loads at once of 16-bit entries (half of that of float32 ones).  Sixteen wavefronts / pieces: 1 x 32768 5.4 / 5.2 us (9.9 / 11.2), 1 x 131072 11.2 / 5.5 (21.0 / 11.2), 32 x 131072 11.6 / 6.6
-// (21.8 / 12.9), 64 x 50257 8.7 / 7.4 (15.3 / 13.6), 128 x 50257 8.9 / 8.4 (15.5 / 16.1).
+// Of up to kPieceRows rows, those longer than kLongRow are cut, so that there are up to kGroups pieces, and as
+// many of a row at most as it has blocks of kPieceEntries, what a work-group loads at once of 16-bit entries
+// (half of that of float32 ones).  Sixteen wavefronts / pieces: 1 x 32768 5.4 / 5.2 us (9.9 / 11.2), 1 x 131072
+// 11.2 / 5.5 (21.0 / 11.2), 32 x 131072 11.6 / 6.6 (21.8 / 12.9), 64 x 50257 8.7 / 7.4 (15.3 / 13.6), 128 x
+// 50257 8.9 / 8.4 (15.5 / 16.1).
 constexpr uint32_t kPieceRows = 64, kLongRow = 32768, kGroups = 512, kPieceEntries = 8192;
 
 Pieces pieces_of(uint64_t rows, uint32_t entries) {
@@ -710,7 +723,8 @@ size_t score_workspace(int32_t, uint64_t rows, uint32_t entries, uint32_t top_k)
 }
 
 hipError_t launch_score(int32_t dtype, const ScoreArgs& a, hipStream_t stream) {
-    // rows of a call that cuts them into pieces are few, so that it has one launch of all of them; others have at most one work-group each
+    // rows of a call that cuts them into pieces are few, so that it has one launch of all of them; others have
+    // at most one work-group each
     static_assert(kPieceRows <= kMaxGroups, "calls that need the workspace are not split");
     for (uint64_t first = 0; first < a.rows; first += kMaxGroups) {
         ScoreArgs s = rows_of(a, dtype, first, a.rows - first < kMaxGroups ? a.rows - first : kMaxGroups);

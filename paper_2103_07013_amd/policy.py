@@ -195,7 +195,9 @@ def log_probs(logits, tokens, mask=None, scale=1.0, top_k=0, stream=None):
 
     logits  float32, bfloat16 or float16 [..., entries]; tokens int32 or int64 [...], -1 = none; mask bool [..., entries] or
     [entries], False = the entry is forbidden.  -> LogProbs(logp, entropy, lse, top_ids, top_logp, held), float32 [...] (top_ids int32,
-    [..., top_k]; both None without top_k; held [5, ...], which the gradient needs).  logp and entropy carry a gradient to the logits; the rest is for reading.
+    [..., top_k]; both None without top_k; held [5, ...], which the gradient needs).  logp and entropy carry a gradient to the
+    logits; the rest is for reading.  Where no gradient is recorded logp, entropy and lse are parts of held: what is written to
+    them is what log_probs_backward finds there.
     """
     if stream is not None:
         with _stream(stream, logits.device):
@@ -275,7 +277,7 @@ class _Embedding(torch.autograd.Function):
 def embedding(tokens, weight, scale=1.0, out=None, stream=None):
     """Rows of `weight` [rows, width] for int32 or int64 tokens [...], times scale; zeros for token -1. -> [..., width]
 
-    Carries a gradient to the weight, unless `out` is given."""
+    Carries a gradient to the weight, unless `out` is given, which shares no memory with it."""
     if stream is not None:
         with _stream(stream, weight.device):
             return embedding(tokens, weight, scale, out)
@@ -329,6 +331,7 @@ class AdamW:
     weight_decay, lr_scale   one number, or one for each tensor
     state_bits    32, or 8: a byte and a 256th per state, rounded up or down so that the mean is kept (seed)
     max_grad_norm > 0: gradients are scaled down to this 2-norm over all tensors; a step whose norm is not finite changes nothing
+                  (but it counts among `steps`)
 
     lr, betas, eps and max_grad_norm may be changed between steps.  State: master (or None), exp_avg, exp_avg_sq,
     with 8 bits exp_avg_exponent and exp_avg_sq_exponent, and steps; a tensor's part of them begins at starts[i].  The
@@ -394,7 +397,8 @@ class AdamW:
 
     def step(self, grads=None, grad_scale=1.0, stream=None):
         """One step with the parameters' gradients, or with `grads`: one contiguous tensor (or None) for each, of the
-        parameters' type or all float32, times grad_scale (one over a loss scale).  grad_norm receives the norm."""
+        parameters' type or all float32, times grad_scale (one over a loss scale).  With max_grad_norm > 0 grad_norm receives the
+        norm.  Captured into a graph, it replays with the step number, and the rounding of 8-bit states, that it was captured with."""
         if stream is not None:
             with _stream(stream, self.device):
                 return self.step(grads, grad_scale)
