@@ -423,13 +423,9 @@ class AdamW:
         if kind is None:
             return
         self._grads[:] = [None if g is None else g.data_ptr() for g in grads]
+        _checked(_on(self.device.index, _library().bps_adamw_step, self._handle, self._grads, _TYPES[kind], self.steps + 1, self.lr, *self.betas, self.eps, grad_scale,
+                     self.max_grad_norm, self.grad_norm.data_ptr()))
         self.steps += 1
-        try:
-            _checked(_on(self.device.index, _library().bps_adamw_step, self._handle, self._grads, _TYPES[kind], self.steps, self.lr, *self.betas, self.eps, grad_scale,
-                         self.max_grad_norm, self.grad_norm.data_ptr()))
-        except BpsError:
-            self.steps -= 1
-            raise
         _written([p for p, g in zip(self.params, grads) if g is not None] + [t for _, t, _ in self._kept])
 
     def states(self, stream=None):

@@ -95,3 +95,28 @@ def test_parameters_that_share_memory():
     with bps.AdamW([flat[500:], flat[:500]], lr=0.5, weight_decay=0.0) as opt:
         opt.step([torch.ones(500, device="cuda")] * 2)
         assert torch.allclose(flat, torch.full_like(flat, -0.5), atol=1e-5)
+
+
+@pytest.mark.parametrize("failure", [TypeError, KeyboardInterrupt, "status"])
+def test_a_step_that_fails_does_not_count(on_host, monkeypatch, failure):
+    """Whatever ends the call: an argument of another kind (an lr that is no number, say), or the library's status."""
+    import paper_2103_07013_amd as bps
+    from paper_2103_07013_amd import policy
+    make, calls = on_host
+    opt, grads = make()
+    opt.step(grads)
+    working = policy._on
+
+    def failing(*a):
+        if failure == "status":
+            return -1
+        raise failure()
+
+    monkeypatch.setattr(policy, "_on", failing)
+    monkeypatch.setattr(policy, "bps_last_error", lambda: "")
+    with pytest.raises(bps.BpsError if failure == "status" else failure):
+        opt.step(grads)
+    assert opt.steps == 1
+    monkeypatch.setattr(policy, "_on", working)
+    opt.step(grads)
+    assert opt.steps == 2
