@@ -17,15 +17,17 @@ __all__ = ["BpsError", "Renderer", "bps_create", "bps_destroy", "bps_last_error"
 # The policy's operators need torch from the start, the renderer only where it is given torch's tensors: they are imported when they are
 # first asked for, and not by `import *`.
 _POLICY = ("log_probs", "log_probs_backward", "LogProbs", "embedding", "embedding_backward", "AdamW")
+_MEMORY = ("causal_conv", "causal_conv_backward", "causal_conv_step", "CausalConv", "ConvGrads", "selective_scan", "selective_scan_backward", "selective_scan_step", "SelectiveScan",
+           "ScanGrads", "residual_norm", "residual_norm_backward", "ResidualNorm", "NormGrads")
 
 
 def __dir__():
-    return sorted({*globals(), *_POLICY})
+    return sorted({*globals(), *_POLICY, *_MEMORY})
 
 
 def __getattr__(name):
-    if name in _POLICY:
-        from . import policy
-        globals().update((n, getattr(policy, n)) for n in _POLICY)
+    if name in _POLICY or name in _MEMORY:
+        from . import memory, policy
+        globals().update((n, getattr(module, n)) for module, names in ((policy, _POLICY), (memory, _MEMORY)) for n in names)
         return globals()[name]
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

@@ -1,15 +1,18 @@
 """Builds libbps.so (the C-ABI batch renderer) for gfx950 with hipcc, in-tree."""
 from __future__ import annotations
 
+import concurrent.futures
 import os
 import subprocess
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libbps.so")
 SOURCES = ["bps_api.hip", "raster_kernels.hip", "shade_kernels.hip", "clusters.cpp",
-           "policy_api.hip", "score_kernels.hip", "embedding_kernels.hip", "adamw_kernels.hip"]
-HEADERS = ["raster_kernels.h", "raster_device.h", "clusters.h", "policy_kernels.h", "policy_device.h", os.path.join("..", "..", "include", "bps.h")]
+           "policy_api.hip", "score_kernels.hip", "embedding_kernels.hip", "adamw_kernels.hip",
+           "memory_api.hip", "conv_kernels.hip", "scan_kernels.hip", "norm_kernels.hip"]
+HEADERS = ["raster_kernels.h", "raster_device.h", "clusters.h", "policy_kernels.h", "policy_device.h", "memory_kernels.h", "memory_device.h", os.path.join("..", "..", "include", "bps.h")]
 # -ffp-contract=off: the numeric rule fixes where fused multiply-adds happen.
 # packed FP32 instructions are switched off on purpose (hipcc's host pass does not know the
 # feature and says so; that message is harmless).
@@ -38,12 +41,19 @@ def build(force: bool = True, verbose: bool = False) -> str:
 def compile_hip(sources, lib: str, verbose: bool = False) -> str:
     """Compile HIP sources into one shared library with the flags that the numeric rule needs."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    cmd = [hipcc, *HIPCC_FLAGS, *sources, "-o", lib]
-    res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
-    if verbose or res.returncode != 0:
-        print(res.stdout)
-    if res.returncode != 0:
-        raise RuntimeError("hipcc failed building %s:\n" % os.path.basename(lib) + res.stdout)
+
+    def run(arguments):
+        res = subprocess.run([hipcc, *HIPCC_FLAGS, *arguments], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+        if verbose or res.returncode != 0:
+            print(res.stdout)
+        if res.returncode != 0:
+            raise RuntimeError("hipcc failed building %s:\n" % os.path.basename(lib) + res.stdout)
+
+    # each source by itself, as many at a time as there are processors to give, then one link
+    with tempfile.TemporaryDirectory() as objects, concurrent.futures.ThreadPoolExecutor(min(8, os.cpu_count() or 1)) as pool:
+        made = [os.path.join(objects, "%d.o" % k) for k in range(len(sources))]
+        list(pool.map(lambda pair: run(["-c", pair[0], "-o", pair[1]]), zip(sources, made)))
+        run([*made, "-o", lib])
     return lib
 
 

@@ -1,0 +1,313 @@
+// Causal convolution over time, each channel by itself, and its gradient (include/bps.h states the rule).
+//
+// A thread holds 16 bytes of channels and walks over a run of steps with the last inputs in registers, so that every input is
+// read once, and once more by the next run's thread for its first taps - 1 windows.
+#include "memory_device.h"
+#include "memory_kernels.h"
+
+namespace bps {
+
+namespace {
+
+constexpr uint32_t kGroup = 256;
+constexpr uint32_t kThreads = 131072;     // that a launch has at least, where there is work for as many
+
+template <class T, int K>
+struct Window {
+    static constexpr int V = T::kPer16, kBefore = K > 1 ? K - 1 : 1;
+    float before[kBefore][V];             // inputs of the steps before the present one, the oldest first
+
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int k = 0; k < kBefore; ++k)
+#pragma unroll
+            for (int v = 0; v < V; ++v) before[k][v] = 0.0f;
+    }
+    __device__ __forceinline__ void push(const float (&x)[V]) {
+        if constexpr (K > 1) {
+#pragma unroll
+            for (int k = 0; k + 1 < kBefore; ++k)
+#pragma unroll
+                for (int v = 0; v < V; ++v) before[k][v] = before[k + 1][v];
+#pragma unroll
+            for (int v = 0; v < V; ++v) before[kBefore - 1][v] = x[v];
+        }
+    }
+};
+
+// The window before step `first` of sequence b.
+template <class T, int K>
+__device__ __forceinline__ void open_window(const bps_conv& a, uint32_t b, int64_t first, uint32_t c, uint32_t n, Window<T, K>& w) {
+    constexpr int V = T::kPer16;
+    using raw = typename T::raw;
+    w.clear();
+#pragma unroll
+    for (int i = K - 1; i >= 1; --i) {
+        const int64_t t = first - i;
+        float x[V];
+        if (t < 0) {
+            if (!a.state) continue;
+            load_part<T, V>(static_cast<const raw*>(a.state) + b * a.state_stride + (K - 1 + t) * (int64_t)a.channels + c, n, x);
+        } else {
+            if (a.starts.at && a.starts.at[b * a.starts.batch_stride + t * a.starts.step_stride]) w.clear();
+            load_part<T, V>(static_cast<const raw*>(a.x.at) + b * a.x.batch_stride + t * a.x.step_stride + c, n, x);
+        }
+        w.push(x);
+    }
+}
+
+template <class T, int K>
+__device__ __forceinline__ void load_taps(const bps_conv& a, uint32_t c, uint32_t n, float (&w)[K][T::kPer16], float (&bias)[T::kPer16]) {
+    constexpr int V = T::kPer16;
+    const bool wide = a.weight_dtype == BPS_F32;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        float x[K];
+        load_weights<T, K>(a.weight, (uint64_t)(c + (v < (int)n ? v : 0)) * K, wide, K, x);
+#pragma unroll
+        for (int k = 0; k < K; ++k) w[k][v] = x[k];
+        bias[v] = 0.0f;
+    }
+    if (a.bias) load_weights<T, V>(a.bias, c, wide, n, bias);
+}
+
+__device__ __forceinline__ int64_t steps_of(const int32_t* lengths, uint32_t b, uint32_t steps) {
+    if (!lengths) return steps;
+    const int32_t n = lengths[b];
+    return n < 0 ? 0 : (uint32_t)n < steps ? n : steps;
+}
+
+template <class T, int K>
+__global__ __launch_bounds__(kGroup) void k_conv(const bps_conv a, const uint32_t run, const uint32_t runs) {
+    constexpr int V = T::kPer16;
+    using raw = typename T::raw;
+    const uint32_t vectors = (a.channels + V - 1) / V;
+    const uint64_t id = (uint64_t)blockIdx.x * kGroup + threadIdx.x, item = id / vectors;
+    if (item >= (uint64_t)a.batch * runs) return;
+    const uint32_t c = (uint32_t)(id % vectors) * V, n = min(a.channels - c, (uint32_t)V), b = (uint32_t)(item / runs);
+    const int64_t first = (int64_t)(item % runs) * run, last = min(first + run, (int64_t)a.steps), end = steps_of(a.lengths, b, a.steps);
+    float w[K][V], bias[V];
+    load_taps<T, K>(a, c, n, w, bias);
+    Window<T, K> window;
+    open_window<T, K>(a, b, first, c, n, window);
+    const raw* x_at = static_cast<const raw*>(a.x.at) + b * a.x.batch_stride + first * a.x.step_stride + c;
+    raw* out_at = static_cast<raw*>(a.out.at) + b * a.out.batch_stride + first * a.out.step_stride + c;
+    const uint8_t* start_at = a.starts.at ? a.starts.at + b * a.starts.batch_stride + first * a.starts.step_stride : nullptr;
+    const int64_t stop = min(last, end);
+    for (int64_t t = first; t < stop; ++t) {
+        if (start_at) {
+            if (*start_at) window.clear();
+            start_at += a.starts.step_stride;
+        }
+        float x[V], u[V];
+        load_part<T, V>(x_at, n, x);
+        x_at += a.x.step_stride;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            u[v] = __builtin_fmaf(w[K - 1][v], x[v], bias[v]);
+#pragma unroll
+            for (int k = 0; k + 1 < K; ++k) u[v] = __builtin_fmaf(w[k][v], window.before[k][v], u[v]);
+            if (a.silu) u[v] *= sigmoid(u[v]);
+        }
+        store_part<T, V>(out_at, n, u);
+        out_at += a.out.step_stride;
+        window.push(x);
+    }
+    if (a.state_out && ((first < end && end <= last) || (end == 0 && first == 0))) {
+        if constexpr (K > 1) {
+            raw* s = static_cast<raw*>(a.state_out) + b * a.state_out_stride + c;
+#pragma unroll
+            for (int k = 0; k < K - 1; ++k) store_part<T, V>(s + k * (uint64_t)a.channels, n, window.before[k]);
+        }
+    }
+    float zero[V] = {};
+    for (int64_t t = max(first, end); t < last; ++t, out_at += a.out.step_stride) store_part<T, V>(out_at, n, zero);
+}
+
+// With du = grad_out * slope(u):  grad_x[t] = sum over i < K of weight[K - 1 - i] du[t + i], as far as step t + i is of step t's episode;
+// grad_weight[k] = sum of du[t] x[t - K + 1 + k].  A run's thread goes on over K - 1 steps of the next run for its last
+// steps' sums.  The sums of weight and bias are left for each part of the runs.
+template <class T, int K>
+__global__ __launch_bounds__(kGroup) void k_conv_grad(const bps_conv a, const uint32_t run, const uint32_t runs, const uint32_t parts, float* sums) {
+    constexpr int V = T::kPer16;
+    using raw = typename T::raw;
+    const uint32_t vectors = (a.channels + V - 1) / V;
+    const uint64_t id = (uint64_t)blockIdx.x * kGroup + threadIdx.x, part = id / vectors;
+    if (part >= parts) return;
+    const uint32_t c = (uint32_t)(id % vectors) * V, n = min(a.channels - c, (uint32_t)V);
+    float w[K][V], bias[V], dw[K][V], db[V];
+    load_taps<T, K>(a, c, n, w, bias);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        db[v] = 0.0f;
+#pragma unroll
+        for (int k = 0; k < K; ++k) dw[k][v] = 0.0f;
+    }
+    for (uint64_t item = part; item < (uint64_t)a.batch * runs; item += parts) {
+        const uint32_t b = (uint32_t)(item / runs);
+        const int64_t first = (int64_t)(item % runs) * run, last = min(first + run, (int64_t)a.steps), end = steps_of(a.lengths, b, a.steps);
+        Window<T, K> window;
+        open_window<T, K>(a, b, first, c, n, window);
+        float sum[K][V];                  // of grad_x, of the step that is i steps back
+#pragma unroll
+        for (int i = 0; i < K; ++i)
+#pragma unroll
+            for (int v = 0; v < V; ++v) sum[i][v] = 0.0f;
+        const raw* x_at = static_cast<const raw*>(a.x.at) + b * a.x.batch_stride + first * a.x.step_stride + c;
+        const raw* g_at = static_cast<const raw*>(a.grad_out.at) + b * a.grad_out.batch_stride + first * a.grad_out.step_stride + c;
+        raw* dx_at = static_cast<raw*>(a.grad_x.at) + b * a.grad_x.batch_stride + first * a.grad_x.step_stride + c;
+        int age = K;                      // steps since the episode began, as far as they matter
+        for (int64_t t = first; t < last + K - 1; ++t) {
+            float x[V];
+#pragma unroll
+            for (int v = 0; v < V; ++v) x[v] = 0.0f;
+            if (t < end) {
+                age = min(age + 1, K);
+                if (a.starts.at && a.starts.at[b * a.starts.batch_stride + t * a.starts.step_stride]) {
+                    window.clear();
+                    age = 0;
+                }
+                float g[V];
+                load_part<T, V>(x_at + (t - first) * a.x.step_stride, n, x);
+                load_part<T, V>(g_at + (t - first) * a.grad_out.step_stride, n, g);
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    float u = __builtin_fmaf(w[K - 1][v], x[v], bias[v]);
+#pragma unroll
+                    for (int k = 0; k + 1 < K; ++k) u = __builtin_fmaf(w[k][v], window.before[k][v], u);
+                    if (a.silu) g[v] *= silu_slope(u, sigmoid(u));
+                }
+                if (t < last) {
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
+                        db[v] += g[v];
+                        dw[K - 1][v] = __builtin_fmaf(g[v], x[v], dw[K - 1][v]);
+#pragma unroll
+                        for (int k = 0; k + 1 < K; ++k) dw[k][v] = __builtin_fmaf(g[v], window.before[k][v], dw[k][v]);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < K; ++i)
+                    if (i <= age)
+#pragma unroll
+                        for (int v = 0; v < V; ++v) sum[i][v] = __builtin_fmaf(w[K - 1 - i][v], g[v], sum[i][v]);
+            }
+            if (t - (K - 1) >= first) {
+                store_part<T, V>(dx_at, n, sum[K - 1]);
+                dx_at += a.grad_x.step_stride;
+            }
+#pragma unroll
+            for (int i = K - 1; i >= 1; --i)
+#pragma unroll
+                for (int v = 0; v < V; ++v) sum[i][v] = sum[i - 1][v];
+#pragma unroll
+            for (int v = 0; v < V; ++v) sum[0][v] = 0.0f;
+            window.push(x);
+        }
+    }
+    float* s = sums + part * (K + 1) * (uint64_t)a.channels + c;
+#pragma unroll
+    for (int k = 0; k < K; ++k) store_part<F32, V>(s + k * (uint64_t)a.channels, n, dw[k]);
+    store_part<F32, V>(s + K * (uint64_t)a.channels, n, db);
+}
+
+constexpr uint32_t kJoinColumns = 64, kJoinSlices = 16;
+
+// A column of sums for each of 64 lanes, the parts dealt out to 16 wavefronts.
+__global__ __launch_bounds__(kJoinColumns* kJoinSlices) void k_join_parts(const float* parts, uint32_t count, size_t stride, uint32_t width, uint32_t inner, int32_t dtype, void* out) {
+    __shared__ float all[kJoinSlices][kJoinColumns];
+    const uint32_t lane = threadIdx.x % kJoinColumns, slice = threadIdx.x / kJoinColumns;
+    const uint64_t columns = (uint64_t)width * inner, column = (uint64_t)blockIdx.x * kJoinColumns + lane;
+    float sum = 0.0f;
+    if (column < columns)
+        for (uint32_t p = slice; p < count; p += kJoinSlices) sum += parts[p * stride + column];
+    all[slice][lane] = sum;
+    __syncthreads();
+    if (slice || column >= columns) return;
+#pragma unroll
+    for (uint32_t p = 1; p < kJoinSlices; ++p) sum += all[p][lane];
+    const uint64_t at = column % width * inner + column / width;
+    if (dtype == BPS_F32)
+        static_cast<float*>(out)[at] = sum;
+    else if (dtype == BPS_BF16)
+        static_cast<uint16_t*>(out)[at] = rounded<Bf16>(sum);
+    else
+        static_cast<_Float16*>(out)[at] = rounded<F16>(sum);
+}
+
+// Steps of a run: as many as leave the launch kThreads threads, at most 64, at least 8.
+uint32_t run_of(const bps_conv& a, uint32_t vectors) {
+    uint32_t run = 64;
+    while (run > 8 && (uint64_t)a.batch * ((a.steps + run - 1) / run) * vectors < kThreads) run /= 2;
+    return run;
+}
+uint32_t vectors_of(const bps_conv& a) {
+    const uint32_t per = a.dtype == BPS_F32 ? 4 : 8;
+    return (a.channels + per - 1) / per;
+}
+uint32_t runs_of(const bps_conv& a, uint32_t run) { return a.steps ? (a.steps - 1) / run + 1 : 1; }
+uint32_t parts_of(const bps_conv& a) {
+    const uint32_t vectors = vectors_of(a);
+    const uint64_t items = a.steps ? (uint64_t)a.batch * runs_of(a, run_of(a, vectors)) : 0, most = kThreads / vectors;
+    return (uint32_t)(items < most ? items : most ? most : 1);
+}
+
+template <class T>
+hipError_t conv(const bps_conv& a, hipStream_t stream) {
+    const uint32_t vectors = vectors_of(a), run = run_of(a, vectors), runs = runs_of(a, run);
+    const uint64_t threads = (uint64_t)a.batch * runs * vectors;
+    const dim3 grid((uint32_t)((threads + kGroup - 1) / kGroup));
+    switch (a.taps) {
+        case 1: k_conv<T, 1><<<grid, kGroup, 0, stream>>>(a, run, runs); break;
+        case 2: k_conv<T, 2><<<grid, kGroup, 0, stream>>>(a, run, runs); break;
+        case 3: k_conv<T, 3><<<grid, kGroup, 0, stream>>>(a, run, runs); break;
+        case 4: k_conv<T, 4><<<grid, kGroup, 0, stream>>>(a, run, runs); break;
+        case 5: k_conv<T, 5><<<grid, kGroup, 0, stream>>>(a, run, runs); break;
+        case 6: k_conv<T, 6><<<grid, kGroup, 0, stream>>>(a, run, runs); break;
+        case 7: k_conv<T, 7><<<grid, kGroup, 0, stream>>>(a, run, runs); break;
+        default: k_conv<T, 8><<<grid, kGroup, 0, stream>>>(a, run, runs); break;
+    }
+    return hipGetLastError();
+}
+
+template <class T>
+hipError_t conv_grad(const bps_conv& a, float* sums, hipStream_t stream) {
+    const uint32_t vectors = vectors_of(a), run = run_of(a, vectors), runs = runs_of(a, run), parts = parts_of(a);
+    const dim3 grid((uint32_t)(((uint64_t)parts * vectors + kGroup - 1) / kGroup));
+    if (parts) switch (a.taps) {
+        case 1: k_conv_grad<T, 1><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, sums); break;
+        case 2: k_conv_grad<T, 2><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, sums); break;
+        case 3: k_conv_grad<T, 3><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, sums); break;
+        case 4: k_conv_grad<T, 4><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, sums); break;
+        case 5: k_conv_grad<T, 5><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, sums); break;
+        case 6: k_conv_grad<T, 6><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, sums); break;
+        case 7: k_conv_grad<T, 7><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, sums); break;
+        default: k_conv_grad<T, 8><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, sums); break;
+    }
+    // sums of no parts are zero
+    if (hipError_t e = hipGetLastError()) return e;
+    const size_t stride = (size_t)(a.taps + 1) * a.channels;
+    if (hipError_t e = launch_join_parts(sums, parts, stride, a.channels, a.taps, a.weight_dtype, a.grad_weight, stream)) return e;
+    return a.grad_bias ? launch_join_parts(sums + (size_t)a.taps * a.channels, parts, stride, a.channels, 1, a.weight_dtype, a.grad_bias, stream) : hipSuccess;
+}
+
+}  // namespace
+
+hipError_t launch_join_parts(const float* parts, uint32_t count, size_t stride, uint32_t width, uint32_t inner, int32_t dtype, void* out, hipStream_t stream) {
+    const uint64_t columns = (uint64_t)width * inner;
+    k_join_parts<<<(uint32_t)((columns + kJoinColumns - 1) / kJoinColumns), kJoinColumns * kJoinSlices, 0, stream>>>(parts, count, stride, width, inner, dtype, out);
+    return hipGetLastError();
+}
+
+hipError_t launch_conv(const bps_conv& a, hipStream_t stream) {
+    return a.dtype == BPS_F32 ? conv<F32>(a, stream) : a.dtype == BPS_BF16 ? conv<Bf16>(a, stream) : conv<F16>(a, stream);
+}
+
+size_t conv_grad_workspace(const bps_conv& a) { return (size_t)parts_of(a) * (a.taps + 1) * a.channels * sizeof(float); }
+
+hipError_t launch_conv_grad(const bps_conv& a, void* workspace, hipStream_t stream) {
+    float* sums = static_cast<float*>(workspace);
+    return a.dtype == BPS_F32 ? conv_grad<F32>(a, sums, stream) : a.dtype == BPS_BF16 ? conv_grad<Bf16>(a, sums, stream) : conv_grad<F16>(a, sums, stream);
+}
+
+}  // namespace bps

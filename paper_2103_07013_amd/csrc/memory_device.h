@@ -1,0 +1,61 @@
+// What the kernels of a policy's memory share: the functions of one value that they apply, and parts of rows.
+#pragma once
+#include "policy_device.h"
+
+namespace bps {
+
+constexpr float kLog2e = 1.44269504088896340736f;
+
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
+// 1 / (1 + e^-x): 0 and 1 at the ends, where e^-x is infinite or nothing
+__device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.0f + exp_of(-x)); }
+// d/dx of x sigmoid(x)
+__device__ __forceinline__ float silu_slope(float x, float s) { return s * __builtin_fmaf(x, 1.0f - s, 1.0f); }
+
+// ln(1 + e^v) = max(v, 0) + ln(1 + e) with e = e^-|v| <= 1, and ln(1 + e) = 2 artanh(s) with s = e / (2 + e) <= 1/3, by its
+// series to s^15: the next term is 3^-16 / 17 of the sum, under half a step.  Small results keep their relative precision, which
+// 1 + e would not: steps of a thousandth are usual.
+__device__ __forceinline__ float softplus(float v) {
+    const float e = exp_of(-__builtin_fabsf(v));
+    const float s = e * __builtin_amdgcn_rcpf(2.0f + e), q = s * s;
+    float p = 1.0f / 15.0f;
+    p = __builtin_fmaf(p, q, 1.0f / 13.0f);
+    p = __builtin_fmaf(p, q, 1.0f / 11.0f);
+    p = __builtin_fmaf(p, q, 1.0f / 9.0f);
+    p = __builtin_fmaf(p, q, 1.0f / 7.0f);
+    p = __builtin_fmaf(p, q, 1.0f / 5.0f);
+    p = __builtin_fmaf(p, q, 1.0f / 3.0f);
+    p = __builtin_fmaf(p, q, 1.0f);
+    return __builtin_fmaf(2.0f * s, p, fmaxf(v, 0.0f));
+}
+
+// The first n of N elements (n = N: all of them, at once); the others read as zero and are not written.
+template <class T, int N>
+__device__ __forceinline__ void load_part(const typename T::raw* p, uint32_t n, float (&x)[N]) {
+    if (n >= N) {
+        load<T, N>(p, x);
+    } else {
+#pragma unroll
+        for (int k = 0; k < N; ++k) x[k] = k < (int)n ? to_float(p[k]) : 0.0f;
+    }
+}
+template <class T, int N>
+__device__ __forceinline__ void store_part(typename T::raw* p, uint32_t n, const float (&x)[N]) {
+    if (n >= N) {
+        store<T, N>(p, x);
+    } else {
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+            if (k < (int)n) p[k] = rounded<T>(x[k]);
+    }
+}
+// The same of a type known when the kernel runs: F32 where `wide`.
+template <class T, int N>
+__device__ __forceinline__ void load_weights(const void* p, uint64_t at, bool wide, uint32_t n, float (&x)[N]) {
+    if (wide)
+        load_part<F32, N>(static_cast<const float*>(p) + at, n, x);
+    else
+        load_part<T, N>(static_cast<const typename T::raw*>(p) + at, n, x);
+}
+
+}  // namespace bps

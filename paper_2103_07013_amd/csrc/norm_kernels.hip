@@ -1,0 +1,286 @@
+// The norms around a block with its gate, its scale and the residual sum, and their gradient (include/bps.h states the rule).
+//
+// W wavefronts hold a row in registers, P vectors of 16 bytes of the block's type to a lane: each input is read once and each
+// result written once.  Work-groups go on to further rows, with the weights kept.
+#include "memory_device.h"
+#include "memory_kernels.h"
+
+namespace bps {
+
+namespace {
+
+// The sum over the work-group's W wavefronts; `shared` is not used again before the next barrier.
+template <int W>
+__device__ __forceinline__ float row_sum(float x, float* shared) {
+    x = group_reduce<64>(x, [](float p, float q) { return p + q; });
+    if constexpr (W > 1) {
+        __syncthreads();
+        if (threadIdx.x % 64 == 0) shared[threadIdx.x / 64] = x;
+        __syncthreads();
+        x = shared[0];
+#pragma unroll
+        for (int k = 1; k < W; ++k) x += shared[k];
+    }
+    return x;
+}
+
+template <class T, int W, int P>
+__device__ __forceinline__ void load_vector(const void* p, bool wide, uint32_t width, float (&x)[P][T::kPer16], float otherwise) {
+    constexpr int V = T::kPer16;
+#pragma unroll
+    for (int j = 0; j < P; ++j) {
+        const uint32_t c = (j * W * 64 + threadIdx.x) * V;
+#pragma unroll
+        for (int v = 0; v < V; ++v) x[j][v] = otherwise;
+        if (p && c < width) load_weights<T, V>(p, c, wide, width - c, x[j]);
+    }
+}
+
+template <class T, class R, int W, int P>
+__global__ __launch_bounds__(W * 64) void k_norm(const bps_norm a) {
+    constexpr int V = T::kPer16;
+    using raw = typename T::raw;
+    using stream_raw = typename R::raw;
+    __shared__ float shared[W];
+    const bool wide = a.weight_dtype == BPS_F32;
+    const float share = 1.0f / (float)a.width;
+    float post[P][V], scale[P][V], pre[P][V];
+    load_vector<T, W, P>(a.post_weight, wide, a.width, post, 1.0f);
+    load_vector<T, W, P>(a.scale, wide, a.width, scale, 1.0f);
+    load_vector<T, W, P>(a.pre_weight, wide, a.width, pre, 1.0f);
+    for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        float b[P][V], r[P][V], g[P][V];
+        const raw* block = static_cast<const raw*>(a.block) + (int64_t)row * a.block_stride;
+        const raw* gate = static_cast<const raw*>(a.gate) + (int64_t)row * a.gate_stride;
+        const stream_raw* residual = static_cast<const stream_raw*>(a.residual) + (int64_t)row * a.residual_stride;
+        float sum = 0.0f;
+#pragma unroll
+        for (int j = 0; j < P; ++j) {
+            const uint32_t c = (j * W * 64 + threadIdx.x) * V;
+#pragma unroll
+            for (int v = 0; v < V; ++v) b[j][v] = r[j][v] = g[j][v] = 0.0f;
+            if (c < a.width) {
+                load_part<T, V>(block + c, a.width - c, b[j]);
+                load_part<R, V>(residual + c, a.width - c, r[j]);
+                if (a.gate) load_part<T, V>(gate + c, a.width - c, g[j]);
+            }
+#pragma unroll
+            for (int v = 0; v < V; ++v) sum = __builtin_fmaf(b[j][v], b[j][v], sum);
+        }
+        float root = 1.0f;
+        if (a.post_weight) root = __builtin_amdgcn_rsqf(__builtin_fmaf(row_sum<W>(sum, shared), share, a.eps));
+        float square = 0.0f;
+#pragma unroll
+        for (int j = 0; j < P; ++j) {
+            const uint32_t c = (j * W * 64 + threadIdx.x) * V;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                float m = b[j][v] * root * post[j][v];
+                if (a.gate) {
+                    const float s = sigmoid(g[j][v]);
+                    m *= a.activation ? g[j][v] * s : s;
+                }
+                r[j][v] = __builtin_fmaf(m, scale[j][v], r[j][v]);
+                square = __builtin_fmaf(r[j][v], r[j][v], square);
+            }
+            if (a.residual_out && c < a.width) store_part<R, V>(static_cast<stream_raw*>(a.residual_out) + (int64_t)row * a.residual_out_stride + c, a.width - c, r[j]);
+        }
+        float last = 1.0f;
+        if (a.pre_weight) {
+            last = __builtin_amdgcn_rsqf(__builtin_fmaf(row_sum<W>(square, shared), share, a.eps));
+#pragma unroll
+            for (int j = 0; j < P; ++j) {
+                const uint32_t c = (j * W * 64 + threadIdx.x) * V;
+#pragma unroll
+                for (int v = 0; v < V; ++v) r[j][v] = r[j][v] * last * pre[j][v];
+                if (c < a.width) store_part<T, V>(static_cast<raw*>(a.out) + (int64_t)row * a.out_stride + c, a.width - c, r[j]);
+            }
+        }
+        if (a.roots && threadIdx.x == 0) {
+            a.roots[row] = root;
+            a.roots[a.rows + row] = last;
+        }
+    }
+}
+
+// With h = (residual + m) / root, w = grad_out pre_weight:  d = grad_residual_out + (w - h mean(w h)) / root is the gradient of the
+// sum, and so of the residual; that of m's factors follows, and through the block's norm in the same way.  What the forward pass computed is
+// computed again from its inputs.  Sums over rows are left for each work-group: those of post_weight, scale and pre_weight, as far as
+// there are such.
+template <class T, class R, int W, int P>
+__global__ __launch_bounds__(W * 64) void k_norm_grad(const bps_norm a, float* sums) {
+    constexpr int V = T::kPer16;
+    using raw = typename T::raw;
+    using stream_raw = typename R::raw;
+    __shared__ float shared[W];
+    const bool wide = a.weight_dtype == BPS_F32;
+    const float share = 1.0f / (float)a.width;
+    float post[P][V], scale[P][V], pre[P][V], d_post[P][V] = {}, d_scale[P][V] = {}, d_pre[P][V] = {};
+    load_vector<T, W, P>(a.post_weight, wide, a.width, post, 1.0f);
+    load_vector<T, W, P>(a.scale, wide, a.width, scale, 1.0f);
+    load_vector<T, W, P>(a.pre_weight, wide, a.width, pre, 1.0f);
+    const bool through = a.pre_weight && a.grad_out;
+    for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        float b[P][V], r[P][V], g[P][V], f[P][V], d[P][V], go[P][V];
+        const float root = a.post_weight ? a.roots[row] : 1.0f, last = a.pre_weight ? a.roots[a.rows + row] : 1.0f;
+        float sum = 0.0f;
+#pragma unroll
+        for (int j = 0; j < P; ++j) {
+            const uint32_t c = (j * W * 64 + threadIdx.x) * V;
+#pragma unroll
+            for (int v = 0; v < V; ++v) b[j][v] = r[j][v] = g[j][v] = d[j][v] = go[j][v] = 0.0f;
+            if (c < a.width) {
+                const uint32_t n = a.width - c;
+                load_part<T, V>(static_cast<const raw*>(a.block) + (int64_t)row * a.block_stride + c, n, b[j]);
+                if (a.gate) load_part<T, V>(static_cast<const raw*>(a.gate) + (int64_t)row * a.gate_stride + c, n, g[j]);
+                if (through) {
+                    load_part<R, V>(static_cast<const stream_raw*>(a.residual) + (int64_t)row * a.residual_stride + c, n, r[j]);
+                    load_part<T, V>(static_cast<const raw*>(a.grad_out) + (int64_t)row * a.grad_out_stride + c, n, go[j]);
+                }
+                if (a.grad_residual_out) load_part<R, V>(static_cast<const stream_raw*>(a.grad_residual_out) + (int64_t)row * a.grad_residual_out_stride + c, n, d[j]);
+            }
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                b[j][v] *= root;
+                f[j][v] = 1.0f;
+                if (a.gate) {
+                    const float s = sigmoid(g[j][v]);
+                    f[j][v] = a.activation ? g[j][v] * s : s;
+                    g[j][v] = a.activation ? silu_slope(g[j][v], s) : s * (1.0f - s);
+                }
+                // the sum over its root, and what reaches it
+                r[j][v] = __builtin_fmaf(b[j][v] * post[j][v] * f[j][v], scale[j][v], r[j][v]) * last;
+                d_pre[j][v] = __builtin_fmaf(go[j][v], r[j][v], d_pre[j][v]);
+                go[j][v] *= pre[j][v];
+                sum = __builtin_fmaf(go[j][v], r[j][v], sum);
+            }
+        }
+        if (through) sum = row_sum<W>(sum, shared) * share;
+        float inner = 0.0f;
+#pragma unroll
+        for (int j = 0; j < P; ++j) {
+            const uint32_t c = (j * W * 64 + threadIdx.x) * V;
+            if (through) {
+#pragma unroll
+                for (int v = 0; v < V; ++v) d[j][v] = __builtin_fmaf(__builtin_fmaf(-r[j][v], sum, go[j][v]), last, d[j][v]);
+            }
+            if (c < a.width) store_part<R, V>(static_cast<stream_raw*>(a.grad_residual) + (int64_t)row * a.grad_residual_stride + c, a.width - c, d[j]);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const float n = b[j][v] * post[j][v];
+                d_scale[j][v] = __builtin_fmaf(d[j][v], f[j][v] * n, d_scale[j][v]);
+                d[j][v] *= scale[j][v];
+                g[j][v] *= d[j][v] * n;
+                d[j][v] *= f[j][v];
+                d_post[j][v] = __builtin_fmaf(d[j][v], b[j][v], d_post[j][v]);
+                d[j][v] *= post[j][v];
+                inner = __builtin_fmaf(d[j][v], b[j][v], inner);
+            }
+            if (a.gate && c < a.width) store_part<T, V>(static_cast<raw*>(a.grad_gate) + (int64_t)row * a.grad_gate_stride + c, a.width - c, g[j]);
+        }
+        if (a.post_weight) inner = row_sum<W>(inner, shared) * share;
+#pragma unroll
+        for (int j = 0; j < P; ++j) {
+            const uint32_t c = (j * W * 64 + threadIdx.x) * V;
+            if (a.post_weight) {
+#pragma unroll
+                for (int v = 0; v < V; ++v) d[j][v] = __builtin_fmaf(-b[j][v], inner, d[j][v]) * root;
+            }
+            if (c < a.width) store_part<T, V>(static_cast<raw*>(a.grad_block) + (int64_t)row * a.grad_block_stride + c, a.width - c, d[j]);
+        }
+    }
+    const uint32_t vectors = (a.post_weight ? 1 : 0) + (a.scale ? 1 : 0) + (a.pre_weight ? 1 : 0);
+    float* s = sums + (uint64_t)blockIdx.x * vectors * a.width;
+#pragma unroll
+    for (int j = 0; j < P; ++j) {
+        const uint32_t c = (j * W * 64 + threadIdx.x) * V;
+        if (c >= a.width) continue;
+        uint64_t at = c;
+        if (a.post_weight) {
+            store_part<F32, V>(s + at, a.width - c, d_post[j]);
+            at += a.width;
+        }
+        if (a.scale) {
+            store_part<F32, V>(s + at, a.width - c, d_scale[j]);
+            at += a.width;
+        }
+        if (a.pre_weight) store_part<F32, V>(s + at, a.width - c, d_pre[j]);
+    }
+}
+
+uint32_t waves_of(const bps_norm& a) {
+    const uint32_t vectors = (a.width + (a.dtype == BPS_F32 ? 3 : 7)) / (a.dtype == BPS_F32 ? 4 : 8);
+    return vectors <= 128 ? 1 : vectors <= 512 ? 4 : 16;
+}
+uint32_t groups_of(const bps_norm& a) {
+    const uint32_t most = 4096 / waves_of(a);
+    return a.rows < most ? (uint32_t)a.rows : most;
+}
+uint32_t sums_of(const bps_norm& a) { return (a.post_weight ? 1 : 0) + (a.scale ? 1 : 0) + (a.pre_weight ? 1 : 0); }
+
+template <class T, class R>
+hipError_t norm(const bps_norm& a, float* sums, hipStream_t stream) {
+    const uint32_t vectors = (a.width + T::kPer16 - 1) / T::kPer16, waves = waves_of(a);
+    const dim3 grid(sums ? groups_of(a) : (uint32_t)(a.rows < 16384 ? a.rows : 16384));
+    auto go = [&](auto w, auto p) {
+        constexpr int W = decltype(w)::value, P = decltype(p)::value;
+        if (sums)
+            k_norm_grad<T, R, W, P><<<grid, W * 64, 0, stream>>>(a, sums);
+        else
+            k_norm<T, R, W, P><<<grid, W * 64, 0, stream>>>(a);
+    };
+    const std::integral_constant<int, 1> one;
+    const std::integral_constant<int, 2> two;
+    const std::integral_constant<int, 4> four;
+    const std::integral_constant<int, 16> sixteen;
+    if (waves == 1) {
+        if (vectors <= 64)
+            go(one, one);
+        else
+            go(one, two);
+    } else if (waves == 4) {
+        if (vectors <= 256)
+            go(four, one);
+        else
+            go(four, two);
+    } else {
+        if (vectors <= 1024)
+            go(sixteen, one);
+        else if (vectors <= 2048)
+            go(sixteen, two);
+        else
+            go(sixteen, four);
+    }
+    return hipGetLastError();
+}
+
+hipError_t any_norm(const bps_norm& a, float* sums, hipStream_t stream) {
+    if (a.dtype == BPS_F32) return norm<F32, F32>(a, sums, stream);
+    if (a.dtype == BPS_BF16) return a.residual_dtype == BPS_F32 ? norm<Bf16, F32>(a, sums, stream) : norm<Bf16, Bf16>(a, sums, stream);
+    return a.residual_dtype == BPS_F32 ? norm<F16, F32>(a, sums, stream) : norm<F16, F16>(a, sums, stream);
+}
+
+}  // namespace
+
+hipError_t launch_norm(const bps_norm& a, hipStream_t stream) { return any_norm(a, nullptr, stream); }
+
+// Not 0 where there are rows, so that the sums' address tells the gradient.
+size_t norm_grad_workspace(const bps_norm& a) { return (size_t)groups_of(a) * (sums_of(a) ? sums_of(a) : 1) * a.width * sizeof(float); }
+
+hipError_t launch_norm_grad(const bps_norm& a, void* workspace, hipStream_t stream) {
+    float* sums = static_cast<float*>(workspace);
+    if (a.rows)
+        if (hipError_t e = any_norm(a, sums, stream)) return e;
+    const uint32_t groups = groups_of(a);
+    const size_t stride = (size_t)sums_of(a) * a.width;
+    const void* weight[3] = {a.post_weight, a.scale, a.pre_weight};
+    void* out[3] = {a.grad_post_weight, a.grad_scale, a.grad_pre_weight};
+    for (int k = 0; k < 3; ++k) {
+        if (!weight[k]) continue;
+        if (hipError_t e = launch_join_parts(sums, groups, stride, a.width, 1, a.weight_dtype, out[k], stream)) return e;
+        sums += a.width;
+    }
+    return hipSuccess;
+}
+
+}  // namespace bps
