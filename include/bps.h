@@ -406,7 +406,7 @@ bps_status bps_causal_conv_backward(const bps_conv *args, void *workspace, size_
  *   d = delta + delta_bias, or ln(1 + e^that) with softplus
  *   h[n] = e^(d A[n]) h[n] + d x B[n];   y = sum over n of C[n] h[n] + D x;   out = y gate / (1 + e^-gate), or y without a gate
  * B and C are shared by the channels / groups channels of a group.  h is float32, 0 before an episode, the state's before step 0.
- * 1 <= states <= 32, channels < 2^24 and a multiple of groups, steps < 2^31. */
+ * 1 <= states <= 32, channels < 2^24 and a multiple of groups, steps < 2^31, 0 <= step_stride < 2^26. */
 typedef struct {
     int32_t dtype;                       /* of x, delta, gate, B, C, out and their gradients */
     int32_t softplus;
@@ -418,7 +418,7 @@ typedef struct {
     const float *state;                  /* [batch][states][channels], batches state_stride apart; NULL = zeros */
     float *state_out;                    /* the state behind the last step, or NULL; may be `state` */
     int64_t state_stride, state_out_stride;
-    float *held;                         /* [batch][ceil(steps / 8)][states][channels]: states that the gradient needs, or NULL */
+    float *held;                         /* [batch][ceil(steps / 16)][states][channels]: states that the gradient needs, or NULL */
     /* the gradient's */
     bps_sequence grad_out, grad_x, grad_delta, grad_gate, grad_B, grad_C;
     float *grad_A, *grad_D, *grad_delta_bias;

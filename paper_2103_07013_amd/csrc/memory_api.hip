@@ -8,6 +8,7 @@ using bps::fail_here;
 namespace {
 
 constexpr uint32_t kMaxChannels = 1u << 24;
+constexpr int64_t kMaxStride = 1 << 26;          // of a scan's steps: places within 16 rows fit 32 bits
 constexpr uint64_t kMaxThreads = 1ull << 32;     // that a launch takes
 
 bool known(int32_t dtype) { return dtype == BPS_F32 || dtype == BPS_BF16 || dtype == BPS_F16; }
@@ -99,6 +100,8 @@ bps_status check_scan(const char* what, const bps_scan& a, bool grad) {
     if (a.batch * tiles >= kMaxThreads / 64 - 4096 || (grad && (uint64_t)a.batch * a.steps * a.groups * 2 * bps::kMaxStates >= kMaxThreads - 256))
         return fail_here(BPS_ERR_UNSUPPORTED, "%s: too many elements for one launch", what);
     Checks c{what, a.batch, a.steps};
+    for (const bps_sequence* s : {&a.x, &a.delta, &a.gate, &a.B, &a.C, &a.out, &a.grad_out, &a.grad_x, &a.grad_delta, &a.grad_gate, &a.grad_B, &a.grad_C})
+        if (s->at && a.steps > 1 && (s->step_stride < 0 || s->step_stride >= kMaxStride)) return fail_here(BPS_ERR_INVALID_ARG, "%s: step strides must be 0 .. 2^26 - 1", what);
     const uint64_t kept = (uint64_t)a.states * a.channels, shared = (uint64_t)a.groups * a.states;
     c.pointer("A", a.A, 4, true);
     c.pointer("D", a.D, 4, false);

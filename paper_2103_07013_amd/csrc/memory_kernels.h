@@ -14,7 +14,7 @@ bps_status fail_here(bps_status code, const char* fmt, ...) __attribute__((forma
 constexpr uint32_t kMaxTaps = 8;
 constexpr uint32_t kMaxStates = 32;
 constexpr uint32_t kMaxNormWidth = 16384;
-constexpr uint32_t kHeldSteps = 8;        // a scan's states are held before each step whose number is a multiple of this
+constexpr uint32_t kHeldSteps = 16;       // a scan's states are held before each step whose number is a multiple of this
 
 hipError_t launch_conv(const bps_conv& a, hipStream_t stream);
 size_t conv_grad_workspace(const bps_conv& a);

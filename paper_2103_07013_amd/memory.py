@@ -28,7 +28,7 @@ ScanGrads = collections.namedtuple("ScanGrads", "x delta A B C D gate delta_bias
 ResidualNorm = collections.namedtuple("ResidualNorm", "residual out held")
 NormGrads = collections.namedtuple("NormGrads", "residual block post_weight gate scale pre_weight")
 
-HELD_STEPS = 8
+HELD_STEPS = 16
 _ACTIVATIONS = {"sigmoid": 0, "silu": 1}
 _p, _i32, _u32, _i64, _u64, _f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_uint32, ctypes.c_int64, ctypes.c_uint64, ctypes.c_float
 
@@ -333,7 +333,7 @@ def selective_scan(x, delta, A, B, C, D=None, gate=None, delta_bias=None, softpl
     decay; D, delta_bias float32 [channels]; starts bool [batch, steps], where an episode begins (with a state of zero); lengths int32
     [batch], where padded sequences end; state float32 [batch, states, channels] (None: zeros).
     -> SelectiveScan(out, state, held): out is zero behind a sequence's end and carries a gradient to all inputs but the state; state is the next
-    call's; held float32 [batch, ceil(steps / 8), states, channels], with hold or where a gradient is recorded, is for
+    call's; held float32 [batch, ceil(steps / 16), states, channels], with hold or where a gradient is recorded, is for
     selective_scan_backward."""
     if stream is not None:
         with _stream(stream, x.device):
