@@ -10,11 +10,14 @@ namespace bps {
 namespace {
 
 constexpr uint32_t kGroup = 256;
+constexpr int kGradWidth = 4;             // channels of a thread of the gradient, whose sums take registers
+constexpr int kAhead = 4;                 // steps whose inputs are loaded together
+constexpr uint32_t kGradThreads = 262144; // of the gradient's launch
 constexpr uint32_t kThreads = 131072;     // that a launch has at least, where there is work for as many
 
-template <class T, int K>
+template <class T, int K, int V>
 struct Window {
-    static constexpr int V = T::kPer16, kBefore = K > 1 ? K - 1 : 1;
+    static constexpr int kBefore = K > 1 ? K - 1 : 1;
     float before[kBefore][V];             // inputs of the steps before the present one, the oldest first
 
     __device__ __forceinline__ void clear() {
@@ -36,9 +39,8 @@ struct Window {
 };
 
 // The window before step `first` of sequence b.
-template <class T, int K>
-__device__ __forceinline__ void open_window(const bps_conv& a, uint32_t b, int64_t first, uint32_t c, uint32_t n, Window<T, K>& w) {
-    constexpr int V = T::kPer16;
+template <class T, int K, int V>
+__device__ __forceinline__ void open_window(const bps_conv& a, uint32_t b, int64_t first, uint32_t c, uint32_t n, Window<T, K, V>& w) {
     using raw = typename T::raw;
     w.clear();
 #pragma unroll
@@ -56,18 +58,19 @@ __device__ __forceinline__ void open_window(const bps_conv& a, uint32_t b, int64
     }
 }
 
-template <class T, int K>
-__device__ __forceinline__ void load_taps(const bps_conv& a, uint32_t c, uint32_t n, float (&w)[K][T::kPer16], float (&bias)[T::kPer16]) {
-    constexpr int V = T::kPer16;
+template <class T, int K, int V>
+__device__ __forceinline__ void load_taps(const bps_conv& a, uint32_t c, uint32_t n, float (&w)[K][V], float (&bias)[V]) {
     const bool wide = a.weight_dtype == BPS_F32;
+    // a channel's taps lie together, and so do those of the thread's channels
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        float x[K];
-        load_weights<T, K>(a.weight, (uint64_t)(c + (v < (int)n ? v : 0)) * K, wide, K, x);
+    for (int i = 0; i < K; ++i) {
+        float x[V];
+        load_weights<T, V>(a.weight, (uint64_t)c * K + i * V, wide, n * K > (uint32_t)(i * V) ? n * K - i * V : 0, x);
 #pragma unroll
-        for (int k = 0; k < K; ++k) w[k][v] = x[k];
-        bias[v] = 0.0f;
+        for (int v = 0; v < V; ++v) w[(i * V + v) % K][(i * V + v) / K] = x[v];
     }
+#pragma unroll
+    for (int v = 0; v < V; ++v) bias[v] = 0.0f;
     if (a.bias) load_weights<T, V>(a.bias, c, wide, n, bias);
 }
 
@@ -77,9 +80,32 @@ __device__ __forceinline__ int64_t steps_of(const int32_t* lengths, uint32_t b, 
     return n < 0 ? 0 : (uint32_t)n < steps ? n : steps;
 }
 
-template <class T, int K>
+// Inputs of kAhead steps, on their way together; those from `left` on are the last one before them.
+template <class T, int V>
+__device__ __forceinline__ void load_steps(const typename T::raw* p, int64_t stride, int left, uint32_t n, float (&x)[kAhead][V]) {
+    if (n >= V) {
+        Pack<typename T::raw, V> q[kAhead];
+#pragma unroll
+        for (int s = 0; s < kAhead; ++s) q[s] = *reinterpret_cast<const Pack<typename T::raw, V>*>(p + min(s, left - 1) * stride);
+#pragma unroll
+        for (int s = 0; s < kAhead; ++s)
+#pragma unroll
+            for (int v = 0; v < V; ++v) x[s][v] = to_float(q[s].v[v]);
+    } else {
+#pragma unroll
+        for (int s = 0; s < kAhead; ++s) load_part<T, V>(p + min(s, left - 1) * stride, n, x[s]);
+    }
+}
+// Which of them begin an episode, a bit each.
+__device__ __forceinline__ uint32_t load_starts(const bps_starts& s, uint32_t b, int64_t t, int left) {
+    uint32_t bits = 0;
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) bits |= (uint32_t)(k < left && s.at[b * s.batch_stride + (t + min(k, left - 1)) * s.step_stride]) << k;
+    return bits;
+}
+
+template <class T, int K, int V>
 __global__ __launch_bounds__(kGroup) void k_conv(const bps_conv a, const uint32_t run, const uint32_t runs) {
-    constexpr int V = T::kPer16;
     using raw = typename T::raw;
     const uint32_t vectors = (a.channels + V - 1) / V;
     const uint64_t id = (uint64_t)blockIdx.x * kGroup + threadIdx.x, item = id / vectors;
@@ -87,31 +113,35 @@ __global__ __launch_bounds__(kGroup) void k_conv(const bps_conv a, const uint32_
     const uint32_t c = (uint32_t)(id % vectors) * V, n = min(a.channels - c, (uint32_t)V), b = (uint32_t)(item / runs);
     const int64_t first = (int64_t)(item % runs) * run, last = min(first + run, (int64_t)a.steps), end = steps_of(a.lengths, b, a.steps);
     float w[K][V], bias[V];
-    load_taps<T, K>(a, c, n, w, bias);
-    Window<T, K> window;
-    open_window<T, K>(a, b, first, c, n, window);
+    load_taps<T, K, V>(a, c, n, w, bias);
+    Window<T, K, V> window;
+    open_window<T, K, V>(a, b, first, c, n, window);
     const raw* x_at = static_cast<const raw*>(a.x.at) + b * a.x.batch_stride + first * a.x.step_stride + c;
     raw* out_at = static_cast<raw*>(a.out.at) + b * a.out.batch_stride + first * a.out.step_stride + c;
-    const uint8_t* start_at = a.starts.at ? a.starts.at + b * a.starts.batch_stride + first * a.starts.step_stride : nullptr;
     const int64_t stop = min(last, end);
-    for (int64_t t = first; t < stop; ++t) {
-        if (start_at) {
-            if (*start_at) window.clear();
-            start_at += a.starts.step_stride;
-        }
-        float x[V], u[V];
-        load_part<T, V>(x_at, n, x);
-        x_at += a.x.step_stride;
+    for (int64_t t = first; t < stop; t += kAhead) {
+        const int left = (int)min(stop - t, (int64_t)kAhead);
+        float x[kAhead][V];
+        uint32_t starts = 0;
+        load_steps<T, V>(x_at, a.x.step_stride, left, n, x);
+        x_at += kAhead * a.x.step_stride;
+        if (a.starts.at) starts = load_starts(a.starts, b, t, left);
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            u[v] = __builtin_fmaf(w[K - 1][v], x[v], bias[v]);
+        for (int s = 0; s < kAhead; ++s) {
+            if (s >= left) break;
+            if (starts >> s & 1) window.clear();
+            float u[V];
 #pragma unroll
-            for (int k = 0; k + 1 < K; ++k) u[v] = __builtin_fmaf(w[k][v], window.before[k][v], u[v]);
-            if (a.silu) u[v] *= sigmoid(u[v]);
+            for (int v = 0; v < V; ++v) {
+                u[v] = __builtin_fmaf(w[K - 1][v], x[s][v], bias[v]);
+#pragma unroll
+                for (int k = 0; k + 1 < K; ++k) u[v] = __builtin_fmaf(w[k][v], window.before[k][v], u[v]);
+                if (a.silu) u[v] *= sigmoid(u[v]);
+            }
+            store_part<T, V>(out_at, n, u);
+            out_at += a.out.step_stride;
+            window.push(x[s]);
         }
-        store_part<T, V>(out_at, n, u);
-        out_at += a.out.step_stride;
-        window.push(x);
     }
     if (a.state_out && ((first < end && end <= last) || (end == 0 && first == 0))) {
         if constexpr (K > 1) {
@@ -127,16 +157,15 @@ __global__ __launch_bounds__(kGroup) void k_conv(const bps_conv a, const uint32_
 // With du = grad_out * slope(u):  grad_x[t] = sum over i < K of weight[K - 1 - i] du[t + i], as far as step t + i is of step t's episode;
 // grad_weight[k] = sum of du[t] x[t - K + 1 + k].  A run's thread goes on over K - 1 steps of the next run for its last
 // steps' sums.  The sums of weight and bias are left for each part of the runs.
-template <class T, int K>
+template <class T, int K, int V>
 __global__ __launch_bounds__(kGroup) void k_conv_grad(const bps_conv a, const uint32_t run, const uint32_t runs, const uint32_t parts, float* sums) {
-    constexpr int V = T::kPer16;
     using raw = typename T::raw;
     const uint32_t vectors = (a.channels + V - 1) / V;
     const uint64_t id = (uint64_t)blockIdx.x * kGroup + threadIdx.x, part = id / vectors;
     if (part >= parts) return;
     const uint32_t c = (uint32_t)(id % vectors) * V, n = min(a.channels - c, (uint32_t)V);
     float w[K][V], bias[V], dw[K][V], db[V];
-    load_taps<T, K>(a, c, n, w, bias);
+    load_taps<T, K, V>(a, c, n, w, bias);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         db[v] = 0.0f;
@@ -146,8 +175,8 @@ __global__ __launch_bounds__(kGroup) void k_conv_grad(const bps_conv a, const ui
     for (uint64_t item = part; item < (uint64_t)a.batch * runs; item += parts) {
         const uint32_t b = (uint32_t)(item / runs);
         const int64_t first = (int64_t)(item % runs) * run, last = min(first + run, (int64_t)a.steps), end = steps_of(a.lengths, b, a.steps);
-        Window<T, K> window;
-        open_window<T, K>(a, b, first, c, n, window);
+        Window<T, K, V> window;
+        open_window<T, K, V>(a, b, first, c, n, window);
         float sum[K][V];                  // of grad_x, of the step that is i steps back
 #pragma unroll
         for (int i = 0; i < K; ++i)
@@ -155,54 +184,62 @@ __global__ __launch_bounds__(kGroup) void k_conv_grad(const bps_conv a, const ui
             for (int v = 0; v < V; ++v) sum[i][v] = 0.0f;
         const raw* x_at = static_cast<const raw*>(a.x.at) + b * a.x.batch_stride + first * a.x.step_stride + c;
         const raw* g_at = static_cast<const raw*>(a.grad_out.at) + b * a.grad_out.batch_stride + first * a.grad_out.step_stride + c;
-        raw* dx_at = static_cast<raw*>(a.grad_x.at) + b * a.grad_x.batch_stride + first * a.grad_x.step_stride + c;
+        raw* dx_at = static_cast<raw*>(a.grad_x.at) + b * a.grad_x.batch_stride + (first - (K - 1)) * a.grad_x.step_stride + c;
         int age = K;                      // steps since the episode began, as far as they matter
-        for (int64_t t = first; t < last + K - 1; ++t) {
-            float x[V];
+        // the run's steps, and K - 1 behind it: beyond the sequence's end nothing is left to add
+        const int64_t stop = last + K - 1;
+        for (int64_t t = first; t < stop; t += kAhead) {
+            const int left = (int)min(stop - t, (int64_t)kAhead), inside = (int)min(end - t, (int64_t)kAhead);
+            float x[kAhead][V] = {}, g[kAhead][V] = {};
+            uint32_t starts = 0;
+            if (inside > 0) {
+                load_steps<T, V>(x_at, a.x.step_stride, inside, n, x);
+                load_steps<T, V>(g_at, a.grad_out.step_stride, inside, n, g);
+                if (a.starts.at) starts = load_starts(a.starts, b, t, inside);
+            }
+            x_at += kAhead * a.x.step_stride;
+            g_at += kAhead * a.grad_out.step_stride;
 #pragma unroll
-            for (int v = 0; v < V; ++v) x[v] = 0.0f;
-            if (t < end) {
-                age = min(age + 1, K);
-                if (a.starts.at && a.starts.at[b * a.starts.batch_stride + t * a.starts.step_stride]) {
-                    window.clear();
-                    age = 0;
-                }
-                float g[V];
-                load_part<T, V>(x_at + (t - first) * a.x.step_stride, n, x);
-                load_part<T, V>(g_at + (t - first) * a.grad_out.step_stride, n, g);
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    float u = __builtin_fmaf(w[K - 1][v], x[v], bias[v]);
-#pragma unroll
-                    for (int k = 0; k + 1 < K; ++k) u = __builtin_fmaf(w[k][v], window.before[k][v], u);
-                    if (a.silu) g[v] *= silu_slope(u, sigmoid(u));
-                }
-                if (t < last) {
+            for (int s = 0; s < kAhead; ++s) {
+                if (s >= left) break;
+                if (s < inside) {
+                    age = min(age + 1, K);
+                    if (starts >> s & 1) {
+                        window.clear();
+                        age = 0;
+                    }
 #pragma unroll
                     for (int v = 0; v < V; ++v) {
-                        db[v] += g[v];
-                        dw[K - 1][v] = __builtin_fmaf(g[v], x[v], dw[K - 1][v]);
+                        float u = __builtin_fmaf(w[K - 1][v], x[s][v], bias[v]);
 #pragma unroll
-                        for (int k = 0; k + 1 < K; ++k) dw[k][v] = __builtin_fmaf(g[v], window.before[k][v], dw[k][v]);
+                        for (int k = 0; k + 1 < K; ++k) u = __builtin_fmaf(w[k][v], window.before[k][v], u);
+                        if (a.silu) g[s][v] *= silu_slope(u, sigmoid(u));
                     }
+                    if (t + s < last) {
+#pragma unroll
+                        for (int v = 0; v < V; ++v) {
+                            db[v] += g[s][v];
+                            dw[K - 1][v] = __builtin_fmaf(g[s][v], x[s][v], dw[K - 1][v]);
+#pragma unroll
+                            for (int k = 0; k + 1 < K; ++k) dw[k][v] = __builtin_fmaf(g[s][v], window.before[k][v], dw[k][v]);
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < K; ++i)
+                        if (i <= age)
+#pragma unroll
+                            for (int v = 0; v < V; ++v) sum[i][v] = __builtin_fmaf(w[K - 1 - i][v], g[s][v], sum[i][v]);
                 }
-#pragma unroll
-                for (int i = 0; i < K; ++i)
-                    if (i <= age)
-#pragma unroll
-                        for (int v = 0; v < V; ++v) sum[i][v] = __builtin_fmaf(w[K - 1 - i][v], g[v], sum[i][v]);
-            }
-            if (t - (K - 1) >= first) {
-                store_part<T, V>(dx_at, n, sum[K - 1]);
+                if (t + s - (K - 1) >= first) store_part<T, V>(dx_at, n, sum[K - 1]);
                 dx_at += a.grad_x.step_stride;
+#pragma unroll
+                for (int i = K - 1; i >= 1; --i)
+#pragma unroll
+                    for (int v = 0; v < V; ++v) sum[i][v] = sum[i - 1][v];
+#pragma unroll
+                for (int v = 0; v < V; ++v) sum[0][v] = 0.0f;
+                window.push(x[s]);
             }
-#pragma unroll
-            for (int i = K - 1; i >= 1; --i)
-#pragma unroll
-                for (int v = 0; v < V; ++v) sum[i][v] = sum[i - 1][v];
-#pragma unroll
-            for (int v = 0; v < V; ++v) sum[0][v] = 0.0f;
-            window.push(x);
         }
     }
     float* s = sums + part * (K + 1) * (uint64_t)a.channels + c;
@@ -211,91 +248,108 @@ __global__ __launch_bounds__(kGroup) void k_conv_grad(const bps_conv a, const ui
     store_part<F32, V>(s + K * (uint64_t)a.channels, n, db);
 }
 
-constexpr uint32_t kJoinColumns = 64, kJoinSlices = 16;
+constexpr uint32_t kJoinColumns = 64, kJoinSlices = 16, kJoinAhead = 8;
 
-// A column of sums for each of 64 lanes, the parts dealt out to 16 wavefronts.
-__global__ __launch_bounds__(kJoinColumns* kJoinSlices) void k_join_parts(const float* parts, uint32_t count, size_t stride, uint32_t width, uint32_t inner, int32_t dtype, void* out) {
+// A column of sums for each of 64 lanes, the parts dealt out to 16 wavefronts, which have 8 of them on their way at a time.
+__global__ __launch_bounds__(kJoinColumns* kJoinSlices) void k_join_parts(const JoinJobs jobs, uint32_t count, size_t stride) {
     __shared__ float all[kJoinSlices][kJoinColumns];
+    const JoinJob& job = jobs.job[blockIdx.y];
     const uint32_t lane = threadIdx.x % kJoinColumns, slice = threadIdx.x / kJoinColumns;
-    const uint64_t columns = (uint64_t)width * inner, column = (uint64_t)blockIdx.x * kJoinColumns + lane;
+    const uint64_t columns = (uint64_t)job.width * job.inner, column = (uint64_t)blockIdx.x * kJoinColumns + lane;
+    if ((uint64_t)blockIdx.x * kJoinColumns >= columns) return;
     float sum = 0.0f;
-    if (column < columns)
-        for (uint32_t p = slice; p < count; p += kJoinSlices) sum += parts[p * stride + column];
+    if (column < columns) {
+        const float* p = job.parts + column;
+        uint32_t k = slice;
+        for (; k + (kJoinAhead - 1) * kJoinSlices < count; k += kJoinAhead * kJoinSlices) {
+            float x[kJoinAhead];
+#pragma unroll
+            for (uint32_t i = 0; i < kJoinAhead; ++i) x[i] = p[(k + i * kJoinSlices) * stride];
+#pragma unroll
+            for (uint32_t i = 0; i < kJoinAhead; ++i) sum += x[i];
+        }
+        for (; k < count; k += kJoinSlices) sum += p[k * stride];
+    }
     all[slice][lane] = sum;
     __syncthreads();
     if (slice || column >= columns) return;
 #pragma unroll
     for (uint32_t p = 1; p < kJoinSlices; ++p) sum += all[p][lane];
-    const uint64_t at = column % width * inner + column / width;
-    if (dtype == BPS_F32)
-        static_cast<float*>(out)[at] = sum;
-    else if (dtype == BPS_BF16)
-        static_cast<uint16_t*>(out)[at] = rounded<Bf16>(sum);
+    const uint64_t at = column % job.width * job.inner + column / job.width;
+    if (job.dtype == BPS_F32)
+        static_cast<float*>(job.out)[at] = sum;
+    else if (job.dtype == BPS_BF16)
+        static_cast<uint16_t*>(job.out)[at] = rounded<Bf16>(sum);
     else
-        static_cast<_Float16*>(out)[at] = rounded<F16>(sum);
+        static_cast<_Float16*>(job.out)[at] = rounded<F16>(sum);
 }
 
 // Steps of a run: as many as leave the launch kThreads threads, at most 64, at least 8.
-uint32_t run_of(const bps_conv& a, uint32_t vectors) {
+uint32_t run_of(const bps_conv& a, uint32_t vectors, uint32_t threads) {
     uint32_t run = 64;
-    while (run > 8 && (uint64_t)a.batch * ((a.steps + run - 1) / run) * vectors < kThreads) run /= 2;
+    while (run > 8 && (uint64_t)a.batch * ((a.steps + run - 1) / run) * vectors < threads) run /= 2;
     return run;
 }
-uint32_t vectors_of(const bps_conv& a) {
-    const uint32_t per = a.dtype == BPS_F32 ? 4 : 8;
-    return (a.channels + per - 1) / per;
-}
+uint32_t vectors_of(const bps_conv& a, uint32_t per) { return (a.channels + per - 1) / per; }
 uint32_t runs_of(const bps_conv& a, uint32_t run) { return a.steps ? (a.steps - 1) / run + 1 : 1; }
 uint32_t parts_of(const bps_conv& a) {
-    const uint32_t vectors = vectors_of(a);
-    const uint64_t items = a.steps ? (uint64_t)a.batch * runs_of(a, run_of(a, vectors)) : 0, most = kThreads / vectors;
+    const uint32_t vectors = vectors_of(a, kGradWidth);
+    const uint64_t items = a.steps ? (uint64_t)a.batch * runs_of(a, run_of(a, vectors, kGradThreads)) : 0, most = kGradThreads / vectors;
     return (uint32_t)(items < most ? items : most ? most : 1);
 }
 
 template <class T>
 hipError_t conv(const bps_conv& a, hipStream_t stream) {
-    const uint32_t vectors = vectors_of(a), run = run_of(a, vectors), runs = runs_of(a, run);
+    constexpr int V = T::kPer16;
+    const uint32_t vectors = vectors_of(a, V), run = run_of(a, vectors, kThreads), runs = runs_of(a, run);
     const uint64_t threads = (uint64_t)a.batch * runs * vectors;
     const dim3 grid((uint32_t)((threads + kGroup - 1) / kGroup));
     switch (a.taps) {
-        case 1: k_conv<T, 1><<<grid, kGroup, 0, stream>>>(a, run, runs); break;
-        case 2: k_conv<T, 2><<<grid, kGroup, 0, stream>>>(a, run, runs); break;
-        case 3: k_conv<T, 3><<<grid, kGroup, 0, stream>>>(a, run, runs); break;
-        case 4: k_conv<T, 4><<<grid, kGroup, 0, stream>>>(a, run, runs); break;
-        case 5: k_conv<T, 5><<<grid, kGroup, 0, stream>>>(a, run, runs); break;
-        case 6: k_conv<T, 6><<<grid, kGroup, 0, stream>>>(a, run, runs); break;
-        case 7: k_conv<T, 7><<<grid, kGroup, 0, stream>>>(a, run, runs); break;
-        default: k_conv<T, 8><<<grid, kGroup, 0, stream>>>(a, run, runs); break;
+        case 1: k_conv<T, 1, V><<<grid, kGroup, 0, stream>>>(a, run, runs); break;
+        case 2: k_conv<T, 2, V><<<grid, kGroup, 0, stream>>>(a, run, runs); break;
+        case 3: k_conv<T, 3, V><<<grid, kGroup, 0, stream>>>(a, run, runs); break;
+        case 4: k_conv<T, 4, V><<<grid, kGroup, 0, stream>>>(a, run, runs); break;
+        case 5: k_conv<T, 5, V><<<grid, kGroup, 0, stream>>>(a, run, runs); break;
+        case 6: k_conv<T, 6, V><<<grid, kGroup, 0, stream>>>(a, run, runs); break;
+        case 7: k_conv<T, 7, V><<<grid, kGroup, 0, stream>>>(a, run, runs); break;
+        default: k_conv<T, 8, V><<<grid, kGroup, 0, stream>>>(a, run, runs); break;
     }
     return hipGetLastError();
 }
 
 template <class T>
 hipError_t conv_grad(const bps_conv& a, float* sums, hipStream_t stream) {
-    const uint32_t vectors = vectors_of(a), run = run_of(a, vectors), runs = runs_of(a, run), parts = parts_of(a);
+    constexpr int V = kGradWidth;
+    const uint32_t vectors = vectors_of(a, V), run = run_of(a, vectors, kGradThreads), runs = runs_of(a, run), parts = parts_of(a);
     const dim3 grid((uint32_t)(((uint64_t)parts * vectors + kGroup - 1) / kGroup));
     if (parts) switch (a.taps) {
-        case 1: k_conv_grad<T, 1><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, sums); break;
-        case 2: k_conv_grad<T, 2><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, sums); break;
-        case 3: k_conv_grad<T, 3><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, sums); break;
-        case 4: k_conv_grad<T, 4><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, sums); break;
-        case 5: k_conv_grad<T, 5><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, sums); break;
-        case 6: k_conv_grad<T, 6><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, sums); break;
-        case 7: k_conv_grad<T, 7><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, sums); break;
-        default: k_conv_grad<T, 8><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, sums); break;
+        case 1: k_conv_grad<T, 1, V><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, sums); break;
+        case 2: k_conv_grad<T, 2, V><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, sums); break;
+        case 3: k_conv_grad<T, 3, V><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, sums); break;
+        case 4: k_conv_grad<T, 4, V><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, sums); break;
+        case 5: k_conv_grad<T, 5, V><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, sums); break;
+        case 6: k_conv_grad<T, 6, V><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, sums); break;
+        case 7: k_conv_grad<T, 7, V><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, sums); break;
+        default: k_conv_grad<T, 8, V><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, sums); break;
     }
     // sums of no parts are zero
     if (hipError_t e = hipGetLastError()) return e;
-    const size_t stride = (size_t)(a.taps + 1) * a.channels;
-    if (hipError_t e = launch_join_parts(sums, parts, stride, a.channels, a.taps, a.weight_dtype, a.grad_weight, stream)) return e;
-    return a.grad_bias ? launch_join_parts(sums + (size_t)a.taps * a.channels, parts, stride, a.channels, 1, a.weight_dtype, a.grad_bias, stream) : hipSuccess;
+    JoinJobs jobs;
+    jobs.add(sums, a.channels, a.taps, a.weight_dtype, a.grad_weight);
+    if (a.grad_bias) jobs.add(sums + (size_t)a.taps * a.channels, a.channels, 1, a.weight_dtype, a.grad_bias);
+    return launch_join_parts(jobs, parts, (size_t)(a.taps + 1) * a.channels, stream);
 }
 
 }  // namespace
 
-hipError_t launch_join_parts(const float* parts, uint32_t count, size_t stride, uint32_t width, uint32_t inner, int32_t dtype, void* out, hipStream_t stream) {
-    const uint64_t columns = (uint64_t)width * inner;
-    k_join_parts<<<(uint32_t)((columns + kJoinColumns - 1) / kJoinColumns), kJoinColumns * kJoinSlices, 0, stream>>>(parts, count, stride, width, inner, dtype, out);
+hipError_t launch_join_parts(const JoinJobs& jobs, uint32_t count, size_t stride, hipStream_t stream) {
+    uint64_t columns = 0;
+    for (uint32_t k = 0; k < jobs.count; ++k) {
+        const uint64_t mine = (uint64_t)jobs.job[k].width * jobs.job[k].inner;
+        if (mine > columns) columns = mine;
+    }
+    if (!columns) return hipSuccess;
+    k_join_parts<<<dim3((uint32_t)((columns + kJoinColumns - 1) / kJoinColumns), jobs.count), kJoinColumns * kJoinSlices, 0, stream>>>(jobs, count, stride);
     return hipGetLastError();
 }
 

@@ -29,7 +29,19 @@ hipError_t launch_norm(const bps_norm& a, hipStream_t stream);
 size_t norm_grad_workspace(const bps_norm& a);
 hipError_t launch_norm_grad(const bps_norm& a, void* workspace, hipStream_t stream);
 
-// out[d * inner + k] = sum over the parts of parts[p][k][d], for d < width and k < inner, as `dtype`; parts are `stride` floats apart.
-hipError_t launch_join_parts(const float* parts, uint32_t count, size_t stride, uint32_t width, uint32_t inner, int32_t dtype, void* out, hipStream_t stream);
+// Sums of what work-groups left in parts, `stride` floats apart: out[d * inner + k] = sum over the parts of parts[p][k][d], for d < width
+// and k < inner, as `dtype`.
+struct JoinJob {
+    const float* parts;
+    void* out;
+    uint32_t width, inner;
+    int32_t dtype;
+};
+struct JoinJobs {
+    JoinJob job[3];
+    uint32_t count = 0;
+    void add(const float* parts, uint32_t width, uint32_t inner, int32_t dtype, void* out) { job[count++] = {parts, out, width, inner, dtype}; }
+};
+hipError_t launch_join_parts(const JoinJobs& jobs, uint32_t count, size_t stride, hipStream_t stream);
 
 }  // namespace bps

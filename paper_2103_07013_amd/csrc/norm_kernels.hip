@@ -1,7 +1,9 @@
 // The norms around a block with its gate, its scale and the residual sum, and their gradient (include/bps.h states the rule).
 //
 // W wavefronts hold a row in registers, P vectors of 16 bytes of the block's type to a lane: each input is read once and each
-// result written once.  Work-groups go on to further rows, with the weights kept.
+// result written once.  Work-groups, of four such rows where one wavefront holds a row, go on to further rows, with the weights kept.
+#include <type_traits>
+
 #include "memory_device.h"
 #include "memory_kernels.h"
 
@@ -9,7 +11,10 @@ namespace bps {
 
 namespace {
 
-// The sum over the work-group's W wavefronts; `shared` is not used again before the next barrier.
+template <int W>
+constexpr int kSlots = W == 1 ? 4 : 1;    // rows that a work-group has at a time
+
+// The sum over the W wavefronts of a row; `shared` is not used again before the next barrier.
 template <int W>
 __device__ __forceinline__ float row_sum(float x, float* shared) {
     x = group_reduce<64>(x, [](float p, float q) { return p + q; });
@@ -29,7 +34,7 @@ __device__ __forceinline__ void load_vector(const void* p, bool wide, uint32_t w
     constexpr int V = T::kPer16;
 #pragma unroll
     for (int j = 0; j < P; ++j) {
-        const uint32_t c = (j * W * 64 + threadIdx.x) * V;
+        const uint32_t c = (j * W * 64 + threadIdx.x % (W * 64)) * V;
 #pragma unroll
         for (int v = 0; v < V; ++v) x[j][v] = otherwise;
         if (p && c < width) load_weights<T, V>(p, c, wide, width - c, x[j]);
@@ -37,7 +42,7 @@ __device__ __forceinline__ void load_vector(const void* p, bool wide, uint32_t w
 }
 
 template <class T, class R, int W, int P>
-__global__ __launch_bounds__(W * 64) void k_norm(const bps_norm a) {
+__global__ __launch_bounds__(W * 64 * kSlots<W>) void k_norm(const bps_norm a) {
     constexpr int V = T::kPer16;
     using raw = typename T::raw;
     using stream_raw = typename R::raw;
@@ -48,7 +53,7 @@ __global__ __launch_bounds__(W * 64) void k_norm(const bps_norm a) {
     load_vector<T, W, P>(a.post_weight, wide, a.width, post, 1.0f);
     load_vector<T, W, P>(a.scale, wide, a.width, scale, 1.0f);
     load_vector<T, W, P>(a.pre_weight, wide, a.width, pre, 1.0f);
-    for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    for (uint64_t row = (uint64_t)blockIdx.x * kSlots<W> + threadIdx.x / (W * 64); row < a.rows; row += (uint64_t)gridDim.x * kSlots<W>) {
         float b[P][V], r[P][V], g[P][V];
         const raw* block = static_cast<const raw*>(a.block) + (int64_t)row * a.block_stride;
         const raw* gate = static_cast<const raw*>(a.gate) + (int64_t)row * a.gate_stride;
@@ -56,7 +61,7 @@ __global__ __launch_bounds__(W * 64) void k_norm(const bps_norm a) {
         float sum = 0.0f;
 #pragma unroll
         for (int j = 0; j < P; ++j) {
-            const uint32_t c = (j * W * 64 + threadIdx.x) * V;
+            const uint32_t c = (j * W * 64 + threadIdx.x % (W * 64)) * V;
 #pragma unroll
             for (int v = 0; v < V; ++v) b[j][v] = r[j][v] = g[j][v] = 0.0f;
             if (c < a.width) {
@@ -72,7 +77,7 @@ __global__ __launch_bounds__(W * 64) void k_norm(const bps_norm a) {
         float square = 0.0f;
 #pragma unroll
         for (int j = 0; j < P; ++j) {
-            const uint32_t c = (j * W * 64 + threadIdx.x) * V;
+            const uint32_t c = (j * W * 64 + threadIdx.x % (W * 64)) * V;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 float m = b[j][v] * root * post[j][v];
@@ -90,13 +95,13 @@ __global__ __launch_bounds__(W * 64) void k_norm(const bps_norm a) {
             last = __builtin_amdgcn_rsqf(__builtin_fmaf(row_sum<W>(square, shared), share, a.eps));
 #pragma unroll
             for (int j = 0; j < P; ++j) {
-                const uint32_t c = (j * W * 64 + threadIdx.x) * V;
+                const uint32_t c = (j * W * 64 + threadIdx.x % (W * 64)) * V;
 #pragma unroll
                 for (int v = 0; v < V; ++v) r[j][v] = r[j][v] * last * pre[j][v];
                 if (c < a.width) store_part<T, V>(static_cast<raw*>(a.out) + (int64_t)row * a.out_stride + c, a.width - c, r[j]);
             }
         }
-        if (a.roots && threadIdx.x == 0) {
+        if (a.roots && threadIdx.x % (W * 64) == 0) {
             a.roots[row] = root;
             a.roots[a.rows + row] = last;
         }
@@ -108,7 +113,7 @@ __global__ __launch_bounds__(W * 64) void k_norm(const bps_norm a) {
 // computed again from its inputs.  Sums over rows are left for each work-group: those of post_weight, scale and pre_weight, as far as
 // there are such.
 template <class T, class R, int W, int P>
-__global__ __launch_bounds__(W * 64) void k_norm_grad(const bps_norm a, float* sums) {
+__global__ __launch_bounds__(W * 64 * kSlots<W>) void k_norm_grad(const bps_norm a, float* sums) {
     constexpr int V = T::kPer16;
     using raw = typename T::raw;
     using stream_raw = typename R::raw;
@@ -116,17 +121,26 @@ __global__ __launch_bounds__(W * 64) void k_norm_grad(const bps_norm a, float* s
     const bool wide = a.weight_dtype == BPS_F32;
     const float share = 1.0f / (float)a.width;
     float post[P][V], scale[P][V], pre[P][V], d_post[P][V] = {}, d_scale[P][V] = {}, d_pre[P][V] = {};
-    load_vector<T, W, P>(a.post_weight, wide, a.width, post, 1.0f);
-    load_vector<T, W, P>(a.scale, wide, a.width, scale, 1.0f);
-    load_vector<T, W, P>(a.pre_weight, wide, a.width, pre, 1.0f);
+    auto load_weights = [&] {
+        load_vector<T, W, P>(a.post_weight, wide, a.width, post, 1.0f);
+        load_vector<T, W, P>(a.scale, wide, a.width, scale, 1.0f);
+        load_vector<T, W, P>(a.pre_weight, wide, a.width, pre, 1.0f);
+    };
+    // the 128 registers of a lane of 16 wavefronts have no room for them beside their gradients
+    constexpr bool kKeep = W < 16;
+    if constexpr (kKeep) load_weights();
     const bool through = a.pre_weight && a.grad_out;
-    for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    for (uint64_t row = (uint64_t)blockIdx.x * kSlots<W> + threadIdx.x / (W * 64); row < a.rows; row += (uint64_t)gridDim.x * kSlots<W>) {
         float b[P][V], r[P][V], g[P][V], f[P][V], d[P][V], go[P][V];
+        if constexpr (!kKeep) {
+            __asm__ volatile("" ::: "memory");
+            load_weights();
+        }
         const float root = a.post_weight ? a.roots[row] : 1.0f, last = a.pre_weight ? a.roots[a.rows + row] : 1.0f;
         float sum = 0.0f;
 #pragma unroll
         for (int j = 0; j < P; ++j) {
-            const uint32_t c = (j * W * 64 + threadIdx.x) * V;
+            const uint32_t c = (j * W * 64 + threadIdx.x % (W * 64)) * V;
 #pragma unroll
             for (int v = 0; v < V; ++v) b[j][v] = r[j][v] = g[j][v] = d[j][v] = go[j][v] = 0.0f;
             if (c < a.width) {
@@ -159,7 +173,7 @@ __global__ __launch_bounds__(W * 64) void k_norm_grad(const bps_norm a, float* s
         float inner = 0.0f;
 #pragma unroll
         for (int j = 0; j < P; ++j) {
-            const uint32_t c = (j * W * 64 + threadIdx.x) * V;
+            const uint32_t c = (j * W * 64 + threadIdx.x % (W * 64)) * V;
             if (through) {
 #pragma unroll
                 for (int v = 0; v < V; ++v) d[j][v] = __builtin_fmaf(__builtin_fmaf(-r[j][v], sum, go[j][v]), last, d[j][v]);
@@ -181,7 +195,7 @@ __global__ __launch_bounds__(W * 64) void k_norm_grad(const bps_norm a, float* s
         if (a.post_weight) inner = row_sum<W>(inner, shared) * share;
 #pragma unroll
         for (int j = 0; j < P; ++j) {
-            const uint32_t c = (j * W * 64 + threadIdx.x) * V;
+            const uint32_t c = (j * W * 64 + threadIdx.x % (W * 64)) * V;
             if (a.post_weight) {
 #pragma unroll
                 for (int v = 0; v < V; ++v) d[j][v] = __builtin_fmaf(-b[j][v], inner, d[j][v]) * root;
@@ -191,47 +205,67 @@ __global__ __launch_bounds__(W * 64) void k_norm_grad(const bps_norm a, float* s
     }
     const uint32_t vectors = (a.post_weight ? 1 : 0) + (a.scale ? 1 : 0) + (a.pre_weight ? 1 : 0);
     float* s = sums + (uint64_t)blockIdx.x * vectors * a.width;
+    auto leave = [&](float (&d)[P][V]) {
+        if constexpr (kSlots<W> > 1) {
+            // the rows' sums meet in LDS, in the rows' order
+            __shared__ float other[kSlots<W>][P * V][64];
+            __syncthreads();
 #pragma unroll
-    for (int j = 0; j < P; ++j) {
-        const uint32_t c = (j * W * 64 + threadIdx.x) * V;
-        if (c >= a.width) continue;
-        uint64_t at = c;
-        if (a.post_weight) {
-            store_part<F32, V>(s + at, a.width - c, d_post[j]);
-            at += a.width;
+            for (int j = 0; j < P; ++j)
+#pragma unroll
+                for (int v = 0; v < V; ++v) other[threadIdx.x / 64][j * V + v][threadIdx.x % 64] = d[j][v];
+            __syncthreads();
+            if (threadIdx.x < 64)
+#pragma unroll
+            for (int j = 0; j < P; ++j)
+#pragma unroll
+                for (int v = 0; v < V; ++v)
+#pragma unroll
+                    for (int k = 1; k < kSlots<W>; ++k) d[j][v] += other[k][j * V + v][threadIdx.x];
         }
-        if (a.scale) {
-            store_part<F32, V>(s + at, a.width - c, d_scale[j]);
-            at += a.width;
+#pragma unroll
+        for (int j = 0; j < P; ++j) {
+            const uint32_t c = (j * W * 64 + threadIdx.x % (W * 64)) * V;
+            if (c < a.width && (kSlots<W> == 1 || threadIdx.x < 64)) store_part<F32, V>(s + c, a.width - c, d[j]);
         }
-        if (a.pre_weight) store_part<F32, V>(s + at, a.width - c, d_pre[j]);
-    }
+        s += a.width;
+    };
+    if (a.post_weight) leave(d_post);
+    if (a.scale) leave(d_scale);
+    if (a.pre_weight) leave(d_pre);
 }
 
+uint32_t vectors_of(const bps_norm& a) { return (a.width + (a.dtype == BPS_F32 ? 3 : 7)) / (a.dtype == BPS_F32 ? 4 : 8); }
+// Wavefronts of a row: with one vector to a lane as far as 16 of them go.
 uint32_t waves_of(const bps_norm& a) {
-    const uint32_t vectors = (a.width + (a.dtype == BPS_F32 ? 3 : 7)) / (a.dtype == BPS_F32 ? 4 : 8);
-    return vectors <= 128 ? 1 : vectors <= 512 ? 4 : 16;
+    const uint32_t vectors = vectors_of(a);
+    return vectors <= 128 ? 1 : vectors <= 256 ? 4 : vectors <= 512 ? 8 : 16;
 }
+uint32_t slots_of(const bps_norm& a) { return waves_of(a) == 1 ? kSlots<1> : 1; }
+// Work-groups of the gradient: 4096 wavefronts at most.
 uint32_t groups_of(const bps_norm& a) {
-    const uint32_t most = 4096 / waves_of(a);
-    return a.rows < most ? (uint32_t)a.rows : most;
+    const uint32_t slots = slots_of(a), most = 4096 / (waves_of(a) * slots);
+    const uint64_t all = (a.rows + slots - 1) / slots;
+    return all < most ? (uint32_t)all : most;
 }
 uint32_t sums_of(const bps_norm& a) { return (a.post_weight ? 1 : 0) + (a.scale ? 1 : 0) + (a.pre_weight ? 1 : 0); }
 
 template <class T, class R>
 hipError_t norm(const bps_norm& a, float* sums, hipStream_t stream) {
-    const uint32_t vectors = (a.width + T::kPer16 - 1) / T::kPer16, waves = waves_of(a);
-    const dim3 grid(sums ? groups_of(a) : (uint32_t)(a.rows < 16384 ? a.rows : 16384));
+    const uint32_t vectors = vectors_of(a), waves = waves_of(a), slots = slots_of(a);
+    const uint64_t all = (a.rows + slots - 1) / slots;
+    const dim3 grid(sums ? groups_of(a) : (uint32_t)(all < 16384 ? all : 16384));
     auto go = [&](auto w, auto p) {
         constexpr int W = decltype(w)::value, P = decltype(p)::value;
         if (sums)
-            k_norm_grad<T, R, W, P><<<grid, W * 64, 0, stream>>>(a, sums);
+            k_norm_grad<T, R, W, P><<<grid, W * 64 * kSlots<W>, 0, stream>>>(a, sums);
         else
-            k_norm<T, R, W, P><<<grid, W * 64, 0, stream>>>(a);
+            k_norm<T, R, W, P><<<grid, W * 64 * kSlots<W>, 0, stream>>>(a);
     };
     const std::integral_constant<int, 1> one;
     const std::integral_constant<int, 2> two;
     const std::integral_constant<int, 4> four;
+    const std::integral_constant<int, 8> eight;
     const std::integral_constant<int, 16> sixteen;
     if (waves == 1) {
         if (vectors <= 64)
@@ -239,17 +273,15 @@ hipError_t norm(const bps_norm& a, float* sums, hipStream_t stream) {
         else
             go(one, two);
     } else if (waves == 4) {
-        if (vectors <= 256)
-            go(four, one);
-        else
-            go(four, two);
-    } else {
-        if (vectors <= 1024)
-            go(sixteen, one);
-        else if (vectors <= 2048)
-            go(sixteen, two);
-        else
-            go(sixteen, four);
+        go(four, one);
+    } else if (waves == 8) {
+        go(eight, one);
+    } else if (vectors <= 1024) {
+        go(sixteen, one);
+    } else if (T::kPer16 == 8 || vectors <= 2048) {
+        go(sixteen, two);
+    } else if constexpr (T::kPer16 == 4) {
+        go(sixteen, four);
     }
     return hipGetLastError();
 }
@@ -275,12 +307,13 @@ hipError_t launch_norm_grad(const bps_norm& a, void* workspace, hipStream_t stre
     const size_t stride = (size_t)sums_of(a) * a.width;
     const void* weight[3] = {a.post_weight, a.scale, a.pre_weight};
     void* out[3] = {a.grad_post_weight, a.grad_scale, a.grad_pre_weight};
+    JoinJobs jobs;
     for (int k = 0; k < 3; ++k) {
         if (!weight[k]) continue;
-        if (hipError_t e = launch_join_parts(sums, groups, stride, a.width, 1, a.weight_dtype, out[k], stream)) return e;
+        jobs.add(sums, a.width, 1, a.weight_dtype, out[k]);
         sums += a.width;
     }
-    return hipSuccess;
+    return launch_join_parts(jobs, groups, stride, stream);
 }
 
 }  // namespace bps

@@ -891,14 +891,12 @@ hipError_t scan_grad(const ScanArgs& a, hipStream_t stream) {
         k_scan_grad_shared<T, L * M><<<(uint32_t)(((uint64_t)a.batch * a.steps * a.groups * 2 * L * M + 255) / 256), 256, 0, stream>>>(a);
         if (hipError_t e = hipGetLastError()) return e;
     }
-    const size_t stride = (size_t)(a.states + 2) * a.channels;
     const uint32_t count = a.batch && a.steps ? a.parts : 0;      // sums of nothing are zero
-    if (hipError_t e = launch_join_parts(a.sums, count, stride, a.channels * a.states, 1, BPS_F32, a.grad_A, stream)) return e;
-    if (a.D)
-        if (hipError_t e = launch_join_parts(a.sums + (size_t)a.states * a.channels, count, stride, a.channels, 1, BPS_F32, a.grad_D, stream)) return e;
-    if (a.delta_bias)
-        if (hipError_t e = launch_join_parts(a.sums + (size_t)(a.states + 1) * a.channels, count, stride, a.channels, 1, BPS_F32, a.grad_delta_bias, stream)) return e;
-    return hipSuccess;
+    JoinJobs jobs;
+    jobs.add(a.sums, a.channels * a.states, 1, BPS_F32, a.grad_A);
+    if (a.D) jobs.add(a.sums + (size_t)a.states * a.channels, a.channels, 1, BPS_F32, a.grad_D);
+    if (a.delta_bias) jobs.add(a.sums + (size_t)(a.states + 1) * a.channels, a.channels, 1, BPS_F32, a.grad_delta_bias);
+    return launch_join_parts(jobs, count, (size_t)(a.states + 2) * a.channels, stream);
 }
 
 template <class T, int L, int M>
