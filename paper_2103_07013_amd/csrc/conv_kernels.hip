@@ -2,6 +2,8 @@
 //
 // A thread holds 16 bytes of channels and walks over a run of steps with the last inputs in registers, so that every input is
 // read once, and once more by the next run's thread for its first taps - 1 windows.
+#include <type_traits>
+
 #include "memory_device.h"
 #include "memory_kernels.h"
 
@@ -10,9 +12,7 @@ namespace bps {
 namespace {
 
 constexpr uint32_t kGroup = 256;
-constexpr int kGradWidth = 4;             // channels of a thread of the gradient, whose sums take registers
 constexpr int kAhead = 4;                 // steps whose inputs are loaded together
-constexpr uint32_t kGradThreads = 262144; // of the gradient's launch
 constexpr uint32_t kThreads = 131072;     // that a launch has at least, where there is work for as many
 
 template <class T, int K, int V>
@@ -80,22 +80,26 @@ __device__ __forceinline__ int64_t steps_of(const int32_t* lengths, uint32_t b, 
     return n < 0 ? 0 : (uint32_t)n < steps ? n : steps;
 }
 
-// Inputs of kAhead steps, on their way together; those from `left` on are the last one before them.
+// Inputs of kAhead steps as they lie in memory, on their way together; those from `left` on are the last one before them.
 template <class T, int V>
-__device__ __forceinline__ void load_steps(const typename T::raw* p, int64_t stride, int left, uint32_t n, float (&x)[kAhead][V]) {
-    if (n >= V) {
-        Pack<typename T::raw, V> q[kAhead];
+struct Steps {
+    Pack<typename T::raw, V> q[kAhead];
+    __device__ __forceinline__ void load(const typename T::raw* p, int64_t stride, int left, uint32_t n) {
+        if (n >= V) {
 #pragma unroll
-        for (int s = 0; s < kAhead; ++s) q[s] = *reinterpret_cast<const Pack<typename T::raw, V>*>(p + min(s, left - 1) * stride);
+            for (int s = 0; s < kAhead; ++s) q[s] = *reinterpret_cast<const Pack<typename T::raw, V>*>(p + min(s, left - 1) * stride);
+        } else {
 #pragma unroll
-        for (int s = 0; s < kAhead; ++s)
+            for (int s = 0; s < kAhead; ++s)
 #pragma unroll
-            for (int v = 0; v < V; ++v) x[s][v] = to_float(q[s].v[v]);
-    } else {
-#pragma unroll
-        for (int s = 0; s < kAhead; ++s) load_part<T, V>(p + min(s, left - 1) * stride, n, x[s]);
+                for (int v = 0; v < V; ++v) q[s].v[v] = v < (int)n ? p[min(s, left - 1) * stride + v] : typename T::raw(0);
+        }
     }
-}
+    __device__ __forceinline__ void get(int s, float (&x)[V]) const {
+#pragma unroll
+        for (int v = 0; v < V; ++v) x[v] = to_float(q[s].v[v]);
+    }
+};
 // Which of them begin an episode, a bit each.
 __device__ __forceinline__ uint32_t load_starts(const bps_starts& s, uint32_t b, int64_t t, int left) {
     uint32_t bits = 0;
@@ -119,29 +123,37 @@ __global__ __launch_bounds__(kGroup) void k_conv(const bps_conv a, const uint32_
     const raw* x_at = static_cast<const raw*>(a.x.at) + b * a.x.batch_stride + first * a.x.step_stride + c;
     raw* out_at = static_cast<raw*>(a.out.at) + b * a.out.batch_stride + first * a.out.step_stride + c;
     const int64_t stop = min(last, end);
+    Steps<T, V> next;
+    if (first < stop) next.load(x_at, a.x.step_stride, (int)min(stop - first, (int64_t)kAhead), n);
     for (int64_t t = first; t < stop; t += kAhead) {
         const int left = (int)min(stop - t, (int64_t)kAhead);
-        float x[kAhead][V];
-        uint32_t starts = 0;
-        load_steps<T, V>(x_at, a.x.step_stride, left, n, x);
+        const Steps<T, V> now = next;
         x_at += kAhead * a.x.step_stride;
-        if (a.starts.at) starts = load_starts(a.starts, b, t, left);
+        if (t + kAhead < stop) next.load(x_at, a.x.step_stride, (int)min(stop - t - kAhead, (int64_t)kAhead), n);
+        const uint32_t starts = a.starts.at ? load_starts(a.starts, b, t, left) : 0;
+        auto walk = [&](auto plain) {
 #pragma unroll
-        for (int s = 0; s < kAhead; ++s) {
-            if (s >= left) break;
-            if (starts >> s & 1) window.clear();
-            float u[V];
+            for (int s = 0; s < kAhead; ++s) {
+                if (!plain && s >= left) break;
+                if (!plain && (starts >> s & 1)) window.clear();
+                float x[V], u[V];
+                now.get(s, x);
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                u[v] = __builtin_fmaf(w[K - 1][v], x[s][v], bias[v]);
+                for (int v = 0; v < V; ++v) {
+                    u[v] = __builtin_fmaf(w[K - 1][v], x[v], bias[v]);
 #pragma unroll
-                for (int k = 0; k + 1 < K; ++k) u[v] = __builtin_fmaf(w[k][v], window.before[k][v], u[v]);
-                if (a.silu) u[v] *= sigmoid(u[v]);
+                    for (int k = 0; k + 1 < K; ++k) u[v] = __builtin_fmaf(w[k][v], window.before[k][v], u[v]);
+                    if (a.silu) u[v] *= sigmoid(u[v]);
+                }
+                store_part<T, V>(out_at, n, u);
+                out_at += a.out.step_stride;
+                window.push(x);
             }
-            store_part<T, V>(out_at, n, u);
-            out_at += a.out.step_stride;
-            window.push(x[s]);
-        }
+        };
+        if (left == kAhead && !starts)
+            walk(std::true_type());
+        else
+            walk(std::false_type());
     }
     if (a.state_out && ((first < end && end <= last) || (end == 0 && first == 0))) {
         if constexpr (K > 1) {
@@ -190,56 +202,71 @@ __global__ __launch_bounds__(kGroup) void k_conv_grad(const bps_conv a, const ui
         const int64_t stop = last + K - 1;
         for (int64_t t = first; t < stop; t += kAhead) {
             const int left = (int)min(stop - t, (int64_t)kAhead), inside = (int)min(end - t, (int64_t)kAhead);
-            float x[kAhead][V] = {}, g[kAhead][V] = {};
-            uint32_t starts = 0;
+            float x_now[kAhead][V] = {}, g_now[kAhead][V] = {};
             if (inside > 0) {
-                load_steps<T, V>(x_at, a.x.step_stride, inside, n, x);
-                load_steps<T, V>(g_at, a.grad_out.step_stride, inside, n, g);
-                if (a.starts.at) starts = load_starts(a.starts, b, t, inside);
+                Steps<T, V> x, g;
+                x.load(x_at, a.x.step_stride, inside, n);
+                g.load(g_at, a.grad_out.step_stride, inside, n);
+#pragma unroll
+                for (int s = 0; s < kAhead; ++s) {
+                    x.get(s, x_now[s]);
+                    g.get(s, g_now[s]);
+                }
             }
             x_at += kAhead * a.x.step_stride;
             g_at += kAhead * a.grad_out.step_stride;
+            const uint32_t starts = a.starts.at && inside > 0 ? load_starts(a.starts, b, t, inside) : 0;
+            auto walk = [&](auto plain) {
 #pragma unroll
-            for (int s = 0; s < kAhead; ++s) {
-                if (s >= left) break;
-                if (s < inside) {
-                    age = min(age + 1, K);
-                    if (starts >> s & 1) {
-                        window.clear();
-                        age = 0;
-                    }
-#pragma unroll
-                    for (int v = 0; v < V; ++v) {
-                        float u = __builtin_fmaf(w[K - 1][v], x[s][v], bias[v]);
-#pragma unroll
-                        for (int k = 0; k + 1 < K; ++k) u = __builtin_fmaf(w[k][v], window.before[k][v], u);
-                        if (a.silu) g[s][v] *= silu_slope(u, sigmoid(u));
-                    }
-                    if (t + s < last) {
+                for (int s = 0; s < kAhead; ++s) {
+                    if (!plain && s >= left) break;
+                    float(&x)[V] = x_now[s], (&g)[V] = g_now[s];
+                    if (plain || s < inside) {
+                        if (!plain) {
+                            age = min(age + 1, K);
+                            if (starts >> s & 1) {
+                                window.clear();
+                                age = 0;
+                            }
+                        }
 #pragma unroll
                         for (int v = 0; v < V; ++v) {
-                            db[v] += g[s][v];
-                            dw[K - 1][v] = __builtin_fmaf(g[s][v], x[s][v], dw[K - 1][v]);
+                            float u = __builtin_fmaf(w[K - 1][v], x[v], bias[v]);
 #pragma unroll
-                            for (int k = 0; k + 1 < K; ++k) dw[k][v] = __builtin_fmaf(g[s][v], window.before[k][v], dw[k][v]);
+                            for (int k = 0; k + 1 < K; ++k) u = __builtin_fmaf(w[k][v], window.before[k][v], u);
+                            if (a.silu) g[v] *= silu_slope(u, sigmoid(u));
                         }
+                        if (plain || t + s < last) {
+#pragma unroll
+                            for (int v = 0; v < V; ++v) {
+                                db[v] += g[v];
+                                dw[K - 1][v] = __builtin_fmaf(g[v], x[v], dw[K - 1][v]);
+#pragma unroll
+                                for (int k = 0; k + 1 < K; ++k) dw[k][v] = __builtin_fmaf(g[v], window.before[k][v], dw[k][v]);
+                            }
+                        }
+#pragma unroll
+                        for (int i = 0; i < K; ++i)
+                            if (plain || i <= age)
+#pragma unroll
+                                for (int v = 0; v < V; ++v) sum[i][v] = __builtin_fmaf(w[K - 1 - i][v], g[v], sum[i][v]);
                     }
+                    if (plain || t + s - (K - 1) >= first) store_part<T, V>(dx_at, n, sum[K - 1]);
+                    dx_at += a.grad_x.step_stride;
 #pragma unroll
-                    for (int i = 0; i < K; ++i)
-                        if (i <= age)
+                    for (int i = K - 1; i >= 1; --i)
 #pragma unroll
-                            for (int v = 0; v < V; ++v) sum[i][v] = __builtin_fmaf(w[K - 1 - i][v], g[s][v], sum[i][v]);
+                        for (int v = 0; v < V; ++v) sum[i][v] = sum[i - 1][v];
+#pragma unroll
+                    for (int v = 0; v < V; ++v) sum[0][v] = 0.0f;
+                    window.push(x);
                 }
-                if (t + s - (K - 1) >= first) store_part<T, V>(dx_at, n, sum[K - 1]);
-                dx_at += a.grad_x.step_stride;
-#pragma unroll
-                for (int i = K - 1; i >= 1; --i)
-#pragma unroll
-                    for (int v = 0; v < V; ++v) sum[i][v] = sum[i - 1][v];
-#pragma unroll
-                for (int v = 0; v < V; ++v) sum[0][v] = 0.0f;
-                window.push(x[s]);
-            }
+            };
+            // most steps: inside the run and its sequence, with no episode that begins in or just before them
+            if (inside == kAhead && !starts && age >= K && t - first >= K - 1 && t + kAhead <= last)
+                walk(std::true_type());
+            else
+                walk(std::false_type());
         }
     }
     float* s = sums + part * (K + 1) * (uint64_t)a.channels + c;
@@ -285,23 +312,26 @@ __global__ __launch_bounds__(kJoinColumns* kJoinSlices) void k_join_parts(const 
 }
 
 // Steps of a run: as many as leave the launch kThreads threads, at most 64, at least 8.
-uint32_t run_of(const bps_conv& a, uint32_t vectors, uint32_t threads) {
+uint32_t run_of(const bps_conv& a, uint32_t vectors) {
     uint32_t run = 64;
-    while (run > 8 && (uint64_t)a.batch * ((a.steps + run - 1) / run) * vectors < threads) run /= 2;
+    while (run > 8 && (uint64_t)a.batch * ((a.steps + run - 1) / run) * vectors < kThreads) run /= 2;
     return run;
 }
-uint32_t vectors_of(const bps_conv& a, uint32_t per) { return (a.channels + per - 1) / per; }
+uint32_t vectors_of(const bps_conv& a) {
+    const uint32_t per = a.dtype == BPS_F32 ? 4 : 8;
+    return (a.channels + per - 1) / per;
+}
 uint32_t runs_of(const bps_conv& a, uint32_t run) { return a.steps ? (a.steps - 1) / run + 1 : 1; }
 uint32_t parts_of(const bps_conv& a) {
-    const uint32_t vectors = vectors_of(a, kGradWidth);
-    const uint64_t items = a.steps ? (uint64_t)a.batch * runs_of(a, run_of(a, vectors, kGradThreads)) : 0, most = kGradThreads / vectors;
+    const uint32_t vectors = vectors_of(a);
+    const uint64_t items = a.steps ? (uint64_t)a.batch * runs_of(a, run_of(a, vectors)) : 0, most = kThreads / vectors;
     return (uint32_t)(items < most ? items : most ? most : 1);
 }
 
 template <class T>
 hipError_t conv(const bps_conv& a, hipStream_t stream) {
     constexpr int V = T::kPer16;
-    const uint32_t vectors = vectors_of(a, V), run = run_of(a, vectors, kThreads), runs = runs_of(a, run);
+    const uint32_t vectors = vectors_of(a), run = run_of(a, vectors), runs = runs_of(a, run);
     const uint64_t threads = (uint64_t)a.batch * runs * vectors;
     const dim3 grid((uint32_t)((threads + kGroup - 1) / kGroup));
     switch (a.taps) {
@@ -319,8 +349,8 @@ hipError_t conv(const bps_conv& a, hipStream_t stream) {
 
 template <class T>
 hipError_t conv_grad(const bps_conv& a, float* sums, hipStream_t stream) {
-    constexpr int V = kGradWidth;
-    const uint32_t vectors = vectors_of(a, V), run = run_of(a, vectors, kGradThreads), runs = runs_of(a, run), parts = parts_of(a);
+    constexpr int V = T::kPer16;
+    const uint32_t vectors = vectors_of(a), run = run_of(a, vectors), runs = runs_of(a, run), parts = parts_of(a);
     const dim3 grid((uint32_t)(((uint64_t)parts * vectors + kGroup - 1) / kGroup));
     if (parts) switch (a.taps) {
         case 1: k_conv_grad<T, 1, V><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, sums); break;
