@@ -17,9 +17,7 @@ FLAG_BILINEAR = 16
 EXPORTS = ["bps_create", "bps_destroy", "bps_load_scene", "bps_load_scene_async", "bps_load_scene_textured", "bps_scene_ready", "bps_pack_clusters", "bps_unload_scene", "bps_render", "bps_render_static", "bps_set_profiling",
            "bps_last_kernel_ms", "bps_kernel_ms_total", "bps_kernel_ms_each", "bps_set_diagnostics", "bps_read_diagnostics", "bps_query", "bps_last_error",
            "bps_log_probs_workspace", "bps_log_probs", "bps_log_probs_backward", "bps_embedding", "bps_embedding_backward_workspace", "bps_embedding_backward",
-           "bps_adamw_create", "bps_adamw_destroy", "bps_adamw_step", "bps_adamw_read_states",
-           "bps_causal_conv", "bps_causal_conv_backward_workspace", "bps_causal_conv_backward", "bps_selective_scan_workspace", "bps_selective_scan",
-           "bps_selective_scan_backward_workspace", "bps_selective_scan_backward", "bps_residual_norm", "bps_residual_norm_backward_workspace", "bps_residual_norm_backward"]
+           "bps_adamw_create", "bps_adamw_destroy", "bps_adamw_step", "bps_adamw_read_states"]
 
 
 class BpsError(RuntimeError):

@@ -1,4 +1,4 @@
-// Causal convolution over time, each channel by itself, and its gradient (include/bps.h states the rule).
+// Causal convolution over time, each channel by itself, and its gradient (include/bps_memory.h states the rule).
 //
 // A thread holds 16 bytes of channels and walks over a run of steps with the last inputs in registers, so that every input is
 // read once, and once more by the next run's thread for its first taps - 1 windows.

@@ -1,4 +1,4 @@
-// Host side of the operators of the policy's memory (include/bps.h): checks of arguments.
+// Host side of the operators of the policy's memory (include/bps_memory.h): checks of arguments.
 #include <cmath>
 
 #include "memory_kernels.h"
@@ -51,9 +51,8 @@ struct Checks {
             x = count;
             count = others, others = x;
         }
-        if (count > 1 && near < width) fail(name, "has rows that overlap");
-        // the division keeps the product in range
-        if (others > 1 && (far < width || (count > 1 && (far - width) / near < count - 1))) fail(name, "has rows that overlap");
+        // the division, by no less than the width, keeps the product in range
+        if ((count > 1 && near < width) || (others > 1 && (far < width || (count > 1 && (far - width) / near < count - 1)))) fail(name, "has rows that overlap");
     }
     void state(const char* name, const void* p, uint32_t size, int64_t stride, uint64_t width, bool written) {
         pointer(name, p, size, false);

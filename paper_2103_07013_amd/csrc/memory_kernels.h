@@ -5,7 +5,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
-#include "../../include/bps.h"
+#include "../../include/bps_memory.h"
 
 namespace bps {
 

@@ -1,4 +1,4 @@
-// The norms around a block with its gate, its scale and the residual sum, and their gradient (include/bps.h states the rule).
+// The norms around a block with its gate, its scale and the residual sum, and their gradient (include/bps_memory.h states the rule).
 //
 // W wavefronts hold a row in registers, P vectors of 16 bytes of the block's type to a lane: each input is read once and each
 // result written once.  Work-groups, of four such rows where one wavefront holds a row, go on to further rows, with the weights kept.

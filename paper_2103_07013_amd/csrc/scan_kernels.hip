@@ -1,4 +1,4 @@
-// Selective scan over time and its gradient (include/bps.h states the rule).
+// Selective scan over time and its gradient (include/bps_memory.h states the rule).
 //
 // L lanes of a wavefront, 64 / L apart, hold a channel, a share of M of its states each in registers, and walk over time.  What is
 // computed once for a step and a channel (the step's size, the gate) each of the L does for one of L steps, and hands it to the others;

@@ -1,4 +1,4 @@
-"""Operators of the memory of a policy that consumes the frames, over the C ABI of include/bps.h: a causal convolution, a selective state
+"""Operators of the memory of a policy that consumes the frames, over the C ABI of include/bps_memory.h: a causal convolution, a selective state
 space scan, and the norms around a block.  Marshalling only; tensors are torch's, on the GPU.
 
 Sequences are [batch, steps, channels] with any strides over batch and steps, so that rollouts gathered step by step are used as they
@@ -12,9 +12,11 @@ from __future__ import annotations
 
 import collections
 import ctypes
+import os
 
 import torch
 
+from . import build as _build
 from .binding import load_library
 from .policy import _TYPES, _checked, _on, _rows, _stream, _written
 
@@ -28,6 +30,8 @@ ScanGrads = collections.namedtuple("ScanGrads", "x delta A B C D gate delta_bias
 ResidualNorm = collections.namedtuple("ResidualNorm", "residual out held")
 NormGrads = collections.namedtuple("NormGrads", "residual block post_weight gate scale pre_weight")
 
+EXPORTS = ["bps_causal_conv", "bps_causal_conv_backward_workspace", "bps_causal_conv_backward", "bps_selective_scan_workspace", "bps_selective_scan",
+           "bps_selective_scan_backward_workspace", "bps_selective_scan_backward", "bps_residual_norm", "bps_residual_norm_backward_workspace", "bps_residual_norm_backward"]
 HELD_STEPS = 16
 _ACTIVATIONS = {"sigmoid": 0, "silu": 1}
 _p, _i32, _u32, _i64, _u64, _f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_uint32, ctypes.c_int64, ctypes.c_uint64, ctypes.c_float
@@ -64,7 +68,10 @@ _lib = None
 def _library():
     global _lib
     if _lib is None:
-        lib = load_library()
+        load_library()
+        if not os.path.exists(_build.MEMORY_LIB):
+            _build.build(force=True)
+        lib = ctypes.CDLL(_build.MEMORY_LIB)
         size = ctypes.c_size_t
         for name, args, back, forth in (("bps_causal_conv", _Conv, True, False), ("bps_selective_scan", _Scan, True, True), ("bps_residual_norm", _Norm, True, False)):
             for f, space in ((name, forth), (name + "_backward", back)):
@@ -131,15 +138,22 @@ def _state(state, shape, dtype, device):
         return None, 0
     if state.dtype != dtype or state.device != device or state.shape != shape:
         raise ValueError(f"state: need a {dtype} tensor of shape {tuple(shape)} on {device}")
-    if state.numel() and not (state.is_contiguous() or state[0].is_contiguous()):
+    if not state.is_contiguous() and state.numel() and not state[0].is_contiguous():
         raise ValueError("state: each sequence's must be contiguous")
     if state.requires_grad and torch.is_grad_enabled():
         raise ValueError("state: no gradient goes through states (detach it)")
     return state.data_ptr(), state.stride(0)
 
 
+def _any_grad(*tensors):
+    for t in tensors:
+        if t is not None and t.requires_grad:
+            return True
+    return False
+
+
 def _no_gradient(what, *tensors):
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+    if torch.is_grad_enabled() and _any_grad(*tensors):
         raise ValueError(f"{what} has no gradient: call it under torch.no_grad(), or the call for sequences")
 
 
@@ -151,7 +165,7 @@ def _three(x, name):
 
 def _call(index, f, args, size, device):
     space = torch.empty(size, dtype=torch.uint8, device=device) if size else None
-    status = _on(index, f, ctypes.byref(args), None if space is None else space.data_ptr(), size)
+    status = _on(index, f, args, None if space is None else space.data_ptr(), size)
     if status:
         _checked(status)
 
@@ -183,7 +197,7 @@ def _causal_conv(x, weight, bias, silu, starts, lengths, state):
     last = torch.empty(batch, taps - 1, channels, dtype=x.dtype, device=x.device)
     a.out, a.out_batch_stride, a.out_step_stride = out.data_ptr(), steps * channels, channels
     a.state_out, a.state_out_stride = last.data_ptr(), (taps - 1) * channels
-    status = _on(x.device.index, lib.bps_causal_conv, ctypes.byref(a))
+    status = _on(x.device.index, lib.bps_causal_conv, a)
     if status:
         _checked(status)
     return CausalConv(out, last)
@@ -222,7 +236,7 @@ def causal_conv(x, weight, bias=None, silu=True, starts=None, lengths=None, stat
     if stream is not None:
         with _stream(stream, x.device):
             return causal_conv(x, weight, bias, silu, starts, lengths, state)
-    if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad or (bias is not None and bias.requires_grad)):
+    if torch.is_grad_enabled() and _any_grad(x, weight, bias):
         return CausalConv(*_CausalConv.apply(x, weight, bias, silu, starts, lengths, state))
     return _causal_conv(x, weight, bias, silu, starts, lengths, state)
 
@@ -261,7 +275,7 @@ def causal_conv_step(x, state, weight, bias=None, silu=True, starts=None, stream
     out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
     a.out, a.out_batch_stride = out.data_ptr(), x.shape[1]
     a.state_out, a.state_out_stride = a.state, a.state_stride
-    status = _on(x.device.index, lib.bps_causal_conv, ctypes.byref(a))
+    status = _on(x.device.index, lib.bps_causal_conv, a)
     if status:
         _checked(status)
     _written(state)
@@ -338,7 +352,7 @@ def selective_scan(x, delta, A, B, C, D=None, gate=None, delta_bias=None, softpl
     if stream is not None:
         with _stream(stream, x.device):
             return selective_scan(x, delta, A, B, C, D, gate, delta_bias, softplus, starts, lengths, state, hold)
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, delta, A, B, C, D, gate, delta_bias)):
+    if torch.is_grad_enabled() and _any_grad(x, delta, A, B, C, D, gate, delta_bias):
         return SelectiveScan(*_SelectiveScan.apply(x, delta, A, B, C, D, gate, delta_bias, softplus, starts, lengths, state))
     return _selective_scan(x, delta, A, B, C, D, gate, delta_bias, softplus, starts, lengths, state, hold)
 
@@ -389,7 +403,7 @@ def selective_scan_step(x, delta, state, A, B, C, D=None, gate=None, delta_bias=
     out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
     a.out, a.out_batch_stride = out.data_ptr(), x.shape[1]
     a.state_out, a.state_out_stride = a.state, a.state_stride
-    status = _on(x.device.index, lib.bps_selective_scan, ctypes.byref(a), None, 0)
+    status = _on(x.device.index, lib.bps_selective_scan, a, None, 0)
     if status:
         _checked(status)
     _written(state)
@@ -398,34 +412,46 @@ def selective_scan_step(x, delta, state, A, B, C, D=None, gate=None, delta_bias=
 
 # ---------------------------------------------------------------------------------------------- norms around a block
 
+def _row_step(t, name, shape, kinds, device):
+    """Elements from row to row"""
+    if t.dtype not in kinds or t.device != device or t.shape != shape:
+        raise ValueError(f"{name}: need a {' or '.join(str(k) for k in kinds)} tensor of shape {tuple(shape)} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return shape[-1] if t.is_contiguous() else _rows(t, name)[3]
+
+
 def _norm_args(residual, block, post_weight, gate, scale, pre_weight, eps, activation, roots):
     shape, rows, width, step = _rows(block, "block")
     device, dtype = block.device, block.dtype
-    if residual.dtype not in (dtype, torch.float32) or residual.device != device or residual.shape != block.shape:
-        raise ValueError(f"residual: need a {dtype} or float32 tensor of shape {tuple(block.shape)} on {device}")
-    if gate is not None and (gate.dtype != dtype or gate.device != device or gate.shape != block.shape):
-        raise ValueError(f"gate: need a {dtype} tensor of shape {tuple(block.shape)} on {device}")
+    shape = block.shape
+    gate_at, gate_step = (None, 0) if gate is None else (gate.data_ptr(), _row_step(gate, "gate", shape, (dtype,), device))
     if activation not in _ACTIVATIONS:
         raise ValueError("activation: 'sigmoid' or 'silu'")
-    kinds = {w.dtype for w in (post_weight, scale, pre_weight) if w is not None}
-    if len(kinds) > 1 or not kinds <= {dtype, torch.float32}:
-        raise ValueError(f"post_weight, scale and pre_weight must be of one type, {dtype} or float32")
-    kind = kinds.pop() if kinds else dtype
-    weights = (_plain(w, n, (width,), (kind,), device) for w, n in ((post_weight, "post_weight"), (scale, "scale"), (pre_weight, "pre_weight")))
-    gate_step = 0 if gate is None else _rows(gate, "gate")[3]
-    return _Norm(_TYPES[dtype], _TYPES[residual.dtype], _TYPES[kind], _ACTIVATIONS[activation], rows, width, eps, residual.data_ptr(), block.data_ptr(),
-                 None if gate is None else gate.data_ptr(), _rows(residual, "residual")[3], step, gate_step, *weights, None, None, width, width, roots)
+    kind, at = None, []
+    for w, name in ((post_weight, "post_weight"), (scale, "scale"), (pre_weight, "pre_weight")):
+        if w is None:
+            at.append(None)
+            continue
+        if kind is None:
+            kind = w.dtype
+        if w.dtype != kind or kind not in (dtype, torch.float32):
+            raise ValueError(f"post_weight, scale and pre_weight must be of one type, {dtype} or float32")
+        at.append(_plain(w, name, (width,), (kind,), device))
+    return _Norm(_TYPES[dtype], _TYPES.get(residual.dtype, -1), _TYPES[kind or dtype], _ACTIVATIONS[activation], rows, width, eps, residual.data_ptr(), block.data_ptr(),
+                 gate_at, _row_step(residual, "residual", shape, (dtype, torch.float32), device), step, gate_step, *at, None, None, width, width, roots)
 
 
 def _residual_norm(residual, block, post_weight, gate, scale, pre_weight, eps, activation):
     lib = _lib or _library()
     a = _norm_args(residual, block, post_weight, gate, scale, pre_weight, eps, activation, None)
-    device = block.device
-    held = torch.empty(2, *block.shape[:-1], dtype=torch.float32, device=device)
-    total = torch.empty(block.shape, dtype=residual.dtype, device=device)
-    out = None if pre_weight is None else torch.empty(block.shape, dtype=block.dtype, device=device)
-    a.residual_out, a.out, a.roots = total.data_ptr(), None if out is None else out.data_ptr(), held.data_ptr()
-    status = _on(device.index, lib.bps_residual_norm, ctypes.byref(a))
+    device, shape = block.device, block.shape
+    held = torch.empty(2, *shape[:-1], dtype=torch.float32, device=device)
+    total = torch.empty(shape, dtype=residual.dtype, device=device)
+    out = None
+    a.residual_out, a.roots = total.data_ptr(), held.data_ptr()
+    if pre_weight is not None:
+        out = torch.empty(shape, dtype=block.dtype, device=device)
+        a.out = out.data_ptr()
+    status = _on(device.index, lib.bps_residual_norm, a)
     if status:
         _checked(status)
     return ResidualNorm(total, out, held)
@@ -462,7 +488,7 @@ def residual_norm(residual, block, post_weight=None, gate=None, scale=None, pre_
     if stream is not None:
         with _stream(stream, block.device):
             return residual_norm(residual, block, post_weight, gate, scale, pre_weight, eps, activation)
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (residual, block, post_weight, gate, scale, pre_weight)):
+    if torch.is_grad_enabled() and _any_grad(residual, block, post_weight, gate, scale, pre_weight):
         return ResidualNorm(*_ResidualNorm.apply(residual, block, post_weight, gate, scale, pre_weight, eps, activation))
     return _residual_norm(residual, block, post_weight, gate, scale, pre_weight, eps, activation)
 
@@ -478,15 +504,12 @@ def residual_norm_backward(residual, block, result, grad_residual=None, grad_out
     device = block.device
     held = _plain(result.held if isinstance(result, ResidualNorm) else result, "result", (2, *block.shape[:-1]), (torch.float32,), device)
     a = _norm_args(residual, block, post_weight, gate, scale, pre_weight, eps, activation, held)
-    for name, g, like in (("grad_residual", grad_residual, residual), ("grad_out", grad_out, block)):
-        if g is not None and (g.dtype != like.dtype or g.device != device or g.shape != block.shape):
-            raise ValueError(f"{name}: need a {like.dtype} tensor of shape {tuple(block.shape)} on {device}")
     if grad_out is not None and pre_weight is None:
         raise ValueError("grad_out: without pre_weight there is no out")
     if grad_residual is not None:
-        a.grad_residual_out, a.grad_residual_out_stride = grad_residual.data_ptr(), _rows(grad_residual, "grad_residual")[3]
+        a.grad_residual_out, a.grad_residual_out_stride = grad_residual.data_ptr(), _row_step(grad_residual, "grad_residual", block.shape, (residual.dtype,), device)
     if grad_out is not None:
-        a.grad_out, a.grad_out_stride = grad_out.data_ptr(), _rows(grad_out, "grad_out")[3]
+        a.grad_out, a.grad_out_stride = grad_out.data_ptr(), _row_step(grad_out, "grad_out", block.shape, (block.dtype,), device)
     gr, gb, gz = (None if t is None else torch.empty(block.shape, dtype=t.dtype, device=device) for t in (residual, block, gate))
     gp, gs, gn = (None if t is None else torch.empty_like(t) for t in (post_weight, scale, pre_weight))
     a.grad_residual, a.grad_block, a.grad_gate = gr.data_ptr(), gb.data_ptr(), None if gz is None else gz.data_ptr()
