@@ -5,7 +5,10 @@ forbidden where the frame shows something close ahead.  One step of all environm
 previous actions, scores the moves and draws one; one update runs PPO (paper Sec. 3.4, Table A4: clip 0.2, entropy bonus, gradient
 norm 1.0) over the steps gathered, with the gradient of the scores and of the embedding, and an AdamW step.
 
-    python examples/depth_policy.py --envs 1024 --steps 32 --updates 10
+With --memory the policy remembers: a recurrent block of a causal convolution and a selective scan, its output normed, gated and
+joined to the stream, moves its states on from step to step, episodes begin anew now and then, and updates go back through whole rollouts.
+
+    python examples/depth_policy.py --envs 1024 --steps 32 --updates 10 [--memory]
 """
 import argparse
 import math
@@ -24,10 +27,51 @@ FORWARD, LEFT, RIGHT, WAIT = range(4)
 MOVES, STEP, TURN, NEAR, HEIGHT = 4, 0.25, math.radians(10.0), 0.45, 1.25
 
 
-class Policy(torch.nn.Module):
-    """Patches of the frame and the previous action in, scores of the moves and the value of the state out."""
+class Memory(torch.nn.Module):
+    """A recurrent block over [environments, steps, width], or one step over [environments, width] whose states move on in place."""
 
-    def __init__(self, size=64, patch=8, hidden=256, state_width=32):
+    def __init__(self, width, inner=128, states=8, taps=4):
+        super().__init__()
+        ones = lambda *shape: torch.nn.Parameter(torch.ones(shape))  # noqa: E731
+        self.shapes = (taps - 1, inner), (states, inner)
+        self.up = torch.nn.Linear(width, 2 * inner)
+        self.taps = torch.nn.Parameter(torch.randn(inner, taps) * taps ** -0.5)
+        self.taps_bias = torch.nn.Parameter(torch.zeros(inner))
+        self.read = torch.nn.Linear(inner, inner + 2 * states, bias=False)
+        # rates 1 .. states, steps of 0.001 .. 0.1: memories of ten to a thousand steps
+        self.log_rate = torch.nn.Parameter(torch.log(torch.arange(1.0, states + 1))[:, None].repeat(1, inner))
+        self.size_bias = torch.nn.Parameter(torch.expm1(torch.exp(torch.rand(inner) * math.log(100.0) + math.log(0.001))).log())
+        self.skip = ones(inner)
+        self.down = torch.nn.Linear(inner, width)
+        self.gate = torch.nn.Linear(width, width)
+        self.first, self.after, self.scale, self.last = ones(width), ones(width), ones(width), ones(width)
+
+    def start(self, n):
+        return tuple(torch.zeros((n, *shape), device="cuda") for shape in self.shapes)
+
+    def forward(self, x, starts, states):
+        x = x.contiguous()
+        n = bps.residual_norm(torch.zeros_like(x), x, pre_weight=self.first).out
+        y, gate = self.up(n).chunk(2, -1)
+        step = x.dim() == 2
+        if step:
+            y = bps.causal_conv_step(y, states[0], self.taps, self.taps_bias, starts=starts)
+        else:
+            y = bps.causal_conv(y, self.taps, self.taps_bias, starts=starts, state=states[0]).out
+        size, write, read = self.read(y).split((self.shapes[0][1], self.shapes[1][0], self.shapes[1][0]), -1)
+        rest = dict(D=self.skip, gate=gate, delta_bias=self.size_bias, starts=starts)
+        if step:
+            y = bps.selective_scan_step(y, size, states[1], -self.log_rate.exp(), write, read, **rest)
+        else:
+            y = bps.selective_scan(y, size, -self.log_rate.exp(), write, read, state=states[1], **rest).out
+        return bps.residual_norm(x, self.down(y), post_weight=self.after, gate=self.gate(n), scale=self.scale, pre_weight=self.last).out
+
+
+class Policy(torch.nn.Module):
+    """Patches of the frame and the previous action in, scores of the moves and the value of the state out.  With memory, frames of
+    [environments, ...] are one step, those of [environments, steps, ...] whole rollouts."""
+
+    def __init__(self, size=64, patch=8, hidden=256, state_width=32, memory=False):
         super().__init__()
         self.patch = patch
         self.patches = torch.nn.Linear(patch * patch, 32)
@@ -36,21 +80,26 @@ class Policy(torch.nn.Module):
         self.previous = torch.nn.Parameter(torch.randn(MOVES + 1, state_width) * 0.1)
         self.hidden = torch.nn.Linear(hidden + state_width, hidden)
         self.heads = torch.nn.Linear(hidden, MOVES + 1)
+        self.memory = Memory(hidden) if memory else None
 
-    def forward(self, depth, previous):
+    def forward(self, depth, previous, starts=None, states=None):
+        rows = depth.shape[:-2]
+        depth, previous = depth.flatten(0, -3), previous.flatten().contiguous()
         n, h, w = depth.shape
         p = self.patch
         x = torch.clamp(depth * 0.2, max=2.0).view(n, h // p, p, w // p, p).transpose(2, 3).reshape(n, -1, p * p)
         x = torch.relu(self.frame(torch.relu(self.patches(x)).flatten(1)))
         x = torch.relu(self.hidden(torch.cat([x, bps.embedding(previous, self.previous)], 1)))
+        if self.memory is not None:
+            x = self.memory(x.view(*rows, -1), starts, states)
         out = self.heads(x)
-        return out[:, :MOVES], out[:, MOVES]
+        return out[..., :MOVES], out[..., MOVES]
 
 
 class Environments:
     """Poses of `n` agents in the scenes of a workload, and their frames."""
 
-    def __init__(self, n, config=1, seed=0):
+    def __init__(self, n, config=1, seed=0, restart=0.0):
         w = synth.build_config(config, B=n)
         self.renderer = bps.Renderer(max_batch=n, height=w.H, width=w.W, background_depth=20.0)
         handles = [self.renderer.load_scene(s.vertices, s.indices) for s in w.scenes]
@@ -59,7 +108,9 @@ class Environments:
         for k, s in enumerate(w.scenes):
             mine = np.nonzero(w.scene_ids == k)[0]
             poses[mine] = synth.make_cameras(s, len(mine), seed=77 + 13 * k + seed)[1]
-        self.x, self.z, self.yaw = torch.tensor(poses, dtype=torch.float32, device="cuda").T.contiguous()
+        self.first = torch.tensor(poses, dtype=torch.float32, device="cuda").T.contiguous()
+        self.x, self.z, self.yaw = self.first
+        self.restart = restart           # share of the steps that end an episode
         self.projection = torch.tensor(synth.perspective(aspect=w.W / w.H), dtype=torch.float32, device="cuda")
         self.previous = torch.full((n,), MOVES, dtype=torch.int64, device="cuda")
 
@@ -85,45 +136,59 @@ class Environments:
         self.z = self.z - forward * STEP * self.yaw.cos()
         self.yaw = self.yaw + TURN * ((action == LEFT).float() - (action == RIGHT).float())
         self.previous = action
+        if self.restart:
+            over = torch.rand(len(action), device="cuda") < self.restart
+            self.x, self.z, self.yaw = torch.where(over, self.first, torch.stack([self.x, self.z, self.yaw]))
+            self.previous = torch.where(over, MOVES, action)
         return forward
 
     def close(self):
         self.renderer.close()
 
 
-def train(envs=256, steps=16, updates=8, lr=1e-3, state_bits=32, gamma=0.9, clip=0.2, bonus=0.05, seed=0, report=print):
+def train(envs=256, steps=16, updates=8, lr=1e-3, state_bits=32, gamma=0.9, clip=0.2, bonus=0.05, seed=0, report=print, memory=False):
     """Mean rewards of the updates' steps, and the policy."""
     torch.manual_seed(seed)
-    world = Environments(envs, seed=seed)
-    policy = Policy().cuda()
+    world = Environments(envs, seed=seed, restart=1 / 64 if memory else 0.0)
+    policy = Policy(memory=memory).cuda()
+    states = policy.memory.start(envs) if memory else None
+    # an environment's first step has no previous one
+    begins = (lambda previous: previous == MOVES) if memory else (lambda previous: None)
     optimiser = bps.AdamW(policy.parameters(), lr=lr, betas=(0.9, 0.99), eps=1e-5, weight_decay=0.0, state_bits=state_bits, max_grad_norm=1.0, seed=seed)
     rewards = []
     for update in range(updates):
         torch.cuda.synchronize()
         began = time.perf_counter()
+        before = tuple(s.clone() for s in states) if memory else None
         seen = {k: [] for k in ("depth", "allowed", "previous", "action", "logp", "value", "reward")}
         with torch.no_grad():
             for _ in range(steps):
                 depth, allowed = world.observe()
                 previous = world.previous
-                logits, value = policy(depth, previous)
+                logits, value = policy(depth, previous, begins(previous), states)
                 noise = -torch.log(-torch.log(torch.rand_like(logits).clamp(1e-9, 1 - 1e-7)))
                 action = (logits + noise).masked_fill(~allowed, -math.inf).argmax(1)
                 logp = bps.log_probs(logits, action, mask=allowed).logp
                 for k, v in zip(seen, (depth, allowed, previous, action, logp, value, world.move(action))):
                     seen[k].append(v)
-            last = policy(world.observe()[0], world.previous)[1]
+            # the next rollout takes this step again
+            last = policy(world.observe()[0], world.previous, begins(world.previous), tuple(s.clone() for s in states) if memory else None)[1]
             returns, gathered = [], last
-            for reward in reversed(seen["reward"]):
-                gathered = reward + gamma * gathered
+            following = world.previous
+            for reward, previous in zip(reversed(seen["reward"]), reversed(seen["previous"])):
+                # what is gathered behind an episode's end is another one's
+                gathered = reward + gamma * (torch.where(begins(following), 0.0, gathered) if memory else gathered)
+                following = previous
                 returns.append(gathered)
-            batch = {k: torch.cat(v) for k, v in seen.items()}
-            target = torch.cat(returns[::-1])
+            # with memory, environments first: [envs, steps, ...]
+            join = (lambda v: torch.stack(v, 1)) if memory else torch.cat
+            batch = {k: join(v) for k, v in seen.items()}
+            target = join(returns[::-1])
             advantage = target - batch["value"]
             advantage = (advantage - advantage.mean()) / (advantage.std() + 1e-5)
         for _ in range(2):
-            logits, value = policy(batch["depth"], batch["previous"])
-            scores = bps.log_probs(logits, batch["action"], mask=batch["allowed"])
+            logits, value = policy(batch["depth"], batch["previous"], begins(batch["previous"]), before)
+            scores = bps.log_probs(logits.contiguous() if memory else logits, batch["action"], mask=batch["allowed"])
             ratio = (scores.logp - batch["logp"]).exp()
             gain = torch.minimum(ratio * advantage, ratio.clamp(1 - clip, 1 + clip) * advantage)
             loss = -gain.mean() - bonus * scores.entropy.mean() + 0.5 * (value - target).square().mean()
@@ -145,5 +210,6 @@ if __name__ == "__main__":
     ap.add_argument("--steps", type=int, default=16)
     ap.add_argument("--updates", type=int, default=8)
     ap.add_argument("--state-bits", type=int, default=32, choices=(32, 8))
+    ap.add_argument("--memory", action="store_true")
     a = ap.parse_args()
-    train(a.envs, a.steps, a.updates, state_bits=a.state_bits)
+    train(a.envs, a.steps, a.updates, state_bits=a.state_bits, memory=a.memory)
