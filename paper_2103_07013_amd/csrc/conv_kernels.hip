@@ -12,6 +12,7 @@ namespace bps {
 namespace {
 
 constexpr uint32_t kGroup = 256;
+constexpr uint32_t kManyTaps = 6;
 constexpr int kAhead = 4;                 // steps whose inputs are loaded together
 constexpr uint32_t kThreads = 131072;     // that a launch has at least, where there is work for as many
 
@@ -317,13 +318,12 @@ uint32_t run_of(const bps_conv& a, uint32_t vectors) {
     while (run > 8 && (uint64_t)a.batch * ((a.steps + run - 1) / run) * vectors < kThreads) run /= 2;
     return run;
 }
-uint32_t vectors_of(const bps_conv& a) {
-    const uint32_t per = a.dtype == BPS_F32 ? 4 : 8;
-    return (a.channels + per - 1) / per;
-}
+// Channels of a thread: 16 bytes of them, but four of the gradient's from 6 taps on, whose sums take too many registers otherwise.
+uint32_t width_of(const bps_conv& a, bool grad) { return a.dtype == BPS_F32 || (grad && a.taps >= kManyTaps) ? 4 : 8; }
+uint32_t vectors_of(const bps_conv& a, bool grad) { return (a.channels + width_of(a, grad) - 1) / width_of(a, grad); }
 uint32_t runs_of(const bps_conv& a, uint32_t run) { return a.steps ? (a.steps - 1) / run + 1 : 1; }
 uint32_t parts_of(const bps_conv& a) {
-    const uint32_t vectors = vectors_of(a);
+    const uint32_t vectors = vectors_of(a, true);
     const uint64_t items = a.steps ? (uint64_t)a.batch * runs_of(a, run_of(a, vectors)) : 0, most = kThreads / vectors;
     return (uint32_t)(items < most ? items : most ? most : 1);
 }
@@ -331,7 +331,7 @@ uint32_t parts_of(const bps_conv& a) {
 template <class T>
 hipError_t conv(const bps_conv& a, hipStream_t stream) {
     constexpr int V = T::kPer16;
-    const uint32_t vectors = vectors_of(a), run = run_of(a, vectors), runs = runs_of(a, run);
+    const uint32_t vectors = vectors_of(a, false), run = run_of(a, vectors), runs = runs_of(a, run);
     const uint64_t threads = (uint64_t)a.batch * runs * vectors;
     const dim3 grid((uint32_t)((threads + kGroup - 1) / kGroup));
     switch (a.taps) {
@@ -350,7 +350,7 @@ hipError_t conv(const bps_conv& a, hipStream_t stream) {
 template <class T>
 hipError_t conv_grad(const bps_conv& a, float* sums, hipStream_t stream) {
     constexpr int V = T::kPer16;
-    const uint32_t vectors = vectors_of(a), run = run_of(a, vectors), runs = runs_of(a, run), parts = parts_of(a);
+    const uint32_t vectors = vectors_of(a, true), run = run_of(a, vectors), runs = runs_of(a, run), parts = parts_of(a);
     const dim3 grid((uint32_t)(((uint64_t)parts * vectors + kGroup - 1) / kGroup));
     if (parts) switch (a.taps) {
         case 1: k_conv_grad<T, 1, V><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, sums); break;
@@ -358,9 +358,9 @@ hipError_t conv_grad(const bps_conv& a, float* sums, hipStream_t stream) {
         case 3: k_conv_grad<T, 3, V><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, sums); break;
         case 4: k_conv_grad<T, 4, V><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, sums); break;
         case 5: k_conv_grad<T, 5, V><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, sums); break;
-        case 6: k_conv_grad<T, 6, V><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, sums); break;
-        case 7: k_conv_grad<T, 7, V><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, sums); break;
-        default: k_conv_grad<T, 8, V><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, sums); break;
+        case 6: k_conv_grad<T, 6, 4><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, sums); break;
+        case 7: k_conv_grad<T, 7, 4><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, sums); break;
+        default: k_conv_grad<T, 8, 4><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, sums); break;
     }
     // sums of no parts are zero
     if (hipError_t e = hipGetLastError()) return e;

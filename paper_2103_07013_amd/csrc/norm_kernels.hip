@@ -42,7 +42,7 @@ __device__ __forceinline__ void load_vector(const void* p, bool wide, uint32_t w
 }
 
 template <class T, class R, int W, int P>
-__global__ __launch_bounds__(W * 64 * kSlots<W>) void k_norm(const bps_norm a) {
+__global__ __launch_bounds__(W * 64 * kSlots<W>, W == 8 ? 4 : 1) void k_norm(const bps_norm a) {
     constexpr int V = T::kPer16;
     using raw = typename T::raw;
     using stream_raw = typename R::raw;
@@ -239,12 +239,12 @@ uint32_t vectors_of(const bps_norm& a) { return (a.width + (a.dtype == BPS_F32 ?
 // Wavefronts of a row: with one vector to a lane as far as 16 of them go.
 uint32_t waves_of(const bps_norm& a) {
     const uint32_t vectors = vectors_of(a);
-    return vectors <= 128 ? 1 : vectors <= 256 ? 4 : vectors <= 512 ? 8 : 16;
+    return vectors <= 64 ? 1 : vectors <= 128 ? 2 : vectors <= 256 ? 4 : vectors <= 512 ? 8 : 16;
 }
 uint32_t slots_of(const bps_norm& a) { return waves_of(a) == 1 ? kSlots<1> : 1; }
-// Work-groups of the gradient: 4096 wavefronts at most.
+// Work-groups of the gradient: 2048 wavefronts at most, but one for each compute unit.
 uint32_t groups_of(const bps_norm& a) {
-    const uint32_t slots = slots_of(a), most = 4096 / (waves_of(a) * slots);
+    const uint32_t slots = slots_of(a), waves = waves_of(a) * slots, most = waves <= 8 ? 2048 / waves : 256;
     const uint64_t all = (a.rows + slots - 1) / slots;
     return all < most ? (uint32_t)all : most;
 }
@@ -268,16 +268,18 @@ hipError_t norm(const bps_norm& a, float* sums, hipStream_t stream) {
     const std::integral_constant<int, 8> eight;
     const std::integral_constant<int, 16> sixteen;
     if (waves == 1) {
-        if (vectors <= 64)
-            go(one, one);
-        else
-            go(one, two);
+        go(one, one);
+    } else if (waves == 2) {
+        go(two, one);
     } else if (waves == 4) {
         go(four, one);
     } else if (waves == 8) {
         go(eight, one);
     } else if (vectors <= 1024) {
-        go(sixteen, one);
+        if (sums)
+            go(sixteen, one);
+        else
+            k_norm<T, R, 8, 2><<<grid, 512, 0, stream>>>(a);
     } else if (T::kPer16 == 8 || vectors <= 2048) {
         go(sixteen, two);
     } else if constexpr (T::kPer16 == 4) {

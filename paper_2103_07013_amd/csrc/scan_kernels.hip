@@ -622,7 +622,7 @@ template <class T, int L, int M>
 __global__ __launch_bounds__(64 * L, 2) void k_scan_grad(const ScanArgs a) {
     using raw = typename T::raw;
     constexpr int kRow = Shared<T, L, M>::kRow, kOwn = kTile / L;
-    // decays of 8 states of a lane would leave no room for a second wavefront: they are computed again
+    // decays of 4 states of a lane would leave no room for a second wavefront: they are computed again
     constexpr bool kKeep = M <= 2;
     __shared__ float shared[kTile][kRow];
     __shared__ float across[L][kTile][kRow];
@@ -899,18 +899,15 @@ hipError_t scan_grad(const ScanArgs& a, hipStream_t stream) {
     return launch_join_parts(jobs, count, (size_t)(a.states + 2) * a.channels, stream);
 }
 
-template <class T, int L, int M>
-hipError_t one_scan(const ScanArgs& a, bool grad, hipStream_t stream) {
-    return grad ? scan_grad<T, L, M>(a, stream) : scan<T, L, M>(a, stream);
-}
-
 template <class T>
 hipError_t scan_of(const ScanArgs& a, bool grad, hipStream_t stream) {
     switch (room(a.states)) {
-        case 4: return one_scan<T, 4, 1>(a, grad, stream);
-        case 8: return one_scan<T, 4, 2>(a, grad, stream);
-        case 16: return one_scan<T, 4, 4>(a, grad, stream);
-        default: return one_scan<T, 4, 8>(a, grad, stream);
+        case 4: return grad ? scan_grad<T, 4, 1>(a, stream) : scan<T, 4, 1>(a, stream);
+        case 8: return grad ? scan_grad<T, 4, 2>(a, stream) : scan<T, 4, 2>(a, stream);
+        case 16: return grad ? scan_grad<T, 4, 4>(a, stream) : scan<T, 4, 4>(a, stream);
+        // 16 steps' states of 8 states a lane do not fit its registers in the gradient: 8 x 1024 x 1024 with 32 states takes 563 us with four lanes
+        // to a channel and 305 with eight; forward, where only the present ones are held, 77 and 83
+        default: return grad ? scan_grad<T, 8, 4>(a, stream) : scan<T, 4, 8>(a, stream);
     }
 }
 hipError_t any_scan(const bps_scan& s, const ScanArgs& a, bool grad, hipStream_t stream) {

@@ -145,6 +145,11 @@ def _state(state, shape, dtype, device):
     return state.data_ptr(), state.stride(0)
 
 
+def _like(t):
+    """A contiguous tensor of t's shape, type and device."""
+    return torch.empty_like(t) if t.is_contiguous() else torch.empty(t.shape, dtype=t.dtype, device=t.device)
+
+
 def _any_grad(*tensors):
     for t in tensors:
         if t is not None and t.requires_grad:
@@ -193,7 +198,7 @@ def _causal_conv(x, weight, bias, silu, starts, lengths, state):
     _three(x, "x")
     a, taps = _conv_args(x, weight, bias, silu, starts, lengths, state)
     batch, steps, channels = x.shape
-    out = torch.empty(batch, steps, channels, dtype=x.dtype, device=x.device)
+    out = _like(x)
     last = torch.empty(batch, taps - 1, channels, dtype=x.dtype, device=x.device)
     a.out, a.out_batch_stride, a.out_step_stride = out.data_ptr(), steps * channels, channels
     a.state_out, a.state_out_stride = last.data_ptr(), (taps - 1) * channels
@@ -251,7 +256,7 @@ def causal_conv_backward(grad_out, x, weight, bias=None, silu=True, starts=None,
     a, taps = _conv_args(x, weight, bias, silu, starts, lengths, state)
     batch, steps, channels = x.shape
     a.grad_out, a.grad_out_batch_stride, a.grad_out_step_stride = _sequence(grad_out, "grad_out", x.shape, x.dtype, x.device)
-    grads = ConvGrads(torch.empty(batch, steps, channels, dtype=x.dtype, device=x.device), torch.empty_like(weight), None if bias is None else torch.empty_like(bias))
+    grads = ConvGrads(_like(x), torch.empty_like(weight), None if bias is None else torch.empty_like(bias))
     a.grad_x, a.grad_x_batch_stride, a.grad_x_step_stride = grads.x.data_ptr(), steps * channels, channels
     a.grad_weight, a.grad_bias = grads.weight.data_ptr(), None if bias is None else grads.bias.data_ptr()
     _call(x.device.index, lib.bps_causal_conv_backward, a, lib.bps_causal_conv_backward_workspace(a), x.device)
@@ -272,7 +277,7 @@ def causal_conv_step(x, state, weight, bias=None, silu=True, starts=None, stream
     a, taps = _conv_args(x, weight, bias, silu, starts, None, state)
     if state is None:
         raise ValueError("a step needs a state")
-    out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    out = _like(x)
     a.out, a.out_batch_stride = out.data_ptr(), x.shape[1]
     a.state_out, a.state_out_stride = a.state, a.state_stride
     status = _on(x.device.index, lib.bps_causal_conv, a)
@@ -307,7 +312,7 @@ def _selective_scan(x, delta, A, B, C, D, gate, delta_bias, softplus, starts, le
     a = _scan_args(x, delta, A, B, C, D, gate, delta_bias, softplus, starts, lengths, state)
     batch, steps, channels = x.shape
     device, states = x.device, a.states
-    out = torch.empty(batch, steps, channels, dtype=x.dtype, device=device)
+    out = _like(x)
     last = torch.empty(batch, states, channels, dtype=torch.float32, device=device)
     held = torch.empty(batch, -(-steps // HELD_STEPS), states, channels, dtype=torch.float32, device=device) if hold else None
     a.out, a.out_batch_stride, a.out_step_stride = out.data_ptr(), steps * channels, channels
@@ -373,9 +378,7 @@ def selective_scan_backward(grad_out, x, delta, A, B, C, result, D=None, gate=No
         raise ValueError("result: need what selective_scan returned with hold=True")
     a.held = _plain(held, "result", (batch, -(-steps // HELD_STEPS), states, channels), (torch.float32,), device)
     a.grad_out, a.grad_out_batch_stride, a.grad_out_step_stride = _sequence(grad_out, "grad_out", x.shape, dtype, device)
-    gx, gd, gz = (None if t is None else torch.empty(batch, steps, channels, dtype=dtype, device=device) for t in (x, delta, gate))
-    gb, gc = (torch.empty(t.shape, dtype=dtype, device=device) for t in (B, C))
-    ga, g_skip, g_bias = (None if t is None else torch.empty(t.shape, dtype=torch.float32, device=device) for t in (A, D, delta_bias))
+    gx, gd, gz, gb, gc, ga, g_skip, g_bias = (None if t is None else _like(t) for t in (x, delta, gate, B, C, A, D, delta_bias))
     for name, g, width in (("grad_x", gx, channels), ("grad_delta", gd, channels), ("grad_gate", gz, channels), ("grad_B", gb, groups * states), ("grad_C", gc, groups * states)):
         if g is not None:
             setattr(a, name, g.data_ptr())
@@ -400,7 +403,7 @@ def selective_scan_step(x, delta, state, A, B, C, D=None, gate=None, delta_bias=
     a = _scan_args(x, delta, A, B, C, D, gate, delta_bias, softplus, starts, None, state)
     if state is None:
         raise ValueError("a step needs a state")
-    out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    out = _like(x)
     a.out, a.out_batch_stride = out.data_ptr(), x.shape[1]
     a.state_out, a.state_out_stride = a.state, a.state_stride
     status = _on(x.device.index, lib.bps_selective_scan, a, None, 0)
@@ -445,11 +448,11 @@ def _residual_norm(residual, block, post_weight, gate, scale, pre_weight, eps, a
     a = _norm_args(residual, block, post_weight, gate, scale, pre_weight, eps, activation, None)
     device, shape = block.device, block.shape
     held = torch.empty(2, *shape[:-1], dtype=torch.float32, device=device)
-    total = torch.empty(shape, dtype=residual.dtype, device=device)
+    total = _like(residual)
     out = None
     a.residual_out, a.roots = total.data_ptr(), held.data_ptr()
     if pre_weight is not None:
-        out = torch.empty(shape, dtype=block.dtype, device=device)
+        out = _like(block)
         a.out = out.data_ptr()
     status = _on(device.index, lib.bps_residual_norm, a)
     if status:
@@ -510,8 +513,7 @@ def residual_norm_backward(residual, block, result, grad_residual=None, grad_out
         a.grad_residual_out, a.grad_residual_out_stride = grad_residual.data_ptr(), _row_step(grad_residual, "grad_residual", block.shape, (residual.dtype,), device)
     if grad_out is not None:
         a.grad_out, a.grad_out_stride = grad_out.data_ptr(), _row_step(grad_out, "grad_out", block.shape, (block.dtype,), device)
-    gr, gb, gz = (None if t is None else torch.empty(block.shape, dtype=t.dtype, device=device) for t in (residual, block, gate))
-    gp, gs, gn = (None if t is None else torch.empty_like(t) for t in (post_weight, scale, pre_weight))
+    gr, gb, gz, gp, gs, gn = (None if t is None else _like(t) for t in (residual, block, gate, post_weight, scale, pre_weight))
     a.grad_residual, a.grad_block, a.grad_gate = gr.data_ptr(), gb.data_ptr(), None if gz is None else gz.data_ptr()
     a.grad_residual_stride = a.grad_block_stride = a.grad_gate_stride = a.width
     a.grad_post_weight, a.grad_scale, a.grad_pre_weight = (None if g is None else g.data_ptr() for g in (gp, gs, gn))
