@@ -17,7 +17,6 @@ namespace bps {
 namespace {
 
 constexpr int kTile = (int)kHeldSteps;    // steps whose inputs are loaded together
-constexpr uint32_t kWide = 64;            // channels of a work-group: of L wavefronts
 
 // A tensor of sequences as kernels have it.
 struct Seq {
@@ -38,7 +37,7 @@ struct ScanArgs {
     float *grad_A, *grad_D, *grad_delta_bias;
     uint32_t batch, steps, channels, states, groups;
     int32_t softplus;
-    uint32_t tiles;                       // work-groups for a group's channels
+    uint32_t waves, tiles;                // wavefronts of a work-group, of 64 / L channels each; work-groups for a group's channels
     uint32_t chunks, chunk_steps;
     uint32_t parts;                       // the gradient's work-groups that share the pieces of a tile among them
     float *ends, *spans;                  // [chunks][batch][states][channels], [chunks][batch][2][channels]: with more than one chunk
@@ -50,11 +49,11 @@ struct Place {
     uint32_t group, channel, share;
     bool on;
 };
-template <int L>
+template <int L, int W>
 __device__ __forceinline__ Place place_of(const ScanArgs& a, uint32_t tile) {
     constexpr uint32_t kLanes = 64 / L;
     const uint32_t each = a.channels / a.groups, group = tile / a.tiles, lane = threadIdx.x % 64;
-    const uint32_t c = tile % a.tiles * kWide + threadIdx.x / 64 * kLanes + lane % kLanes;
+    const uint32_t c = (tile % a.tiles * W + threadIdx.x / 64) * kLanes + lane % kLanes;
     return {group, group * each + min(c, each - 1), lane / kLanes, c < each};
 }
 
@@ -104,9 +103,9 @@ struct Inputs {
 
 // B and C of kTile steps, a work-group's threads' parts of them on their way to LDS as float32, [step][B of L M states, C of L M
 // states]; those of states that there are not are 0.
-template <class T, int L, int M>
+template <class T, int L, int M, int W>
 struct Shared {
-    static constexpr int kStates = L * M, kRow = 2 * kStates, kThreads = 64 * L, kMost = (kTile * kStates + kThreads - 1) / kThreads;
+    static constexpr int kStates = L * M, kRow = 2 * kStates, kThreads = 64 * W, kMost = (kTile * kStates + kThreads - 1) / kThreads;
     typename T::raw v[2][kMost];
     const char* row[2];
     __device__ __forceinline__ Shared(const ScanArgs& a, uint32_t b, int64_t t, uint32_t group) {
@@ -336,15 +335,15 @@ __device__ __forceinline__ void either(bool some, F f) {
 }
 
 // FIRST: what each chunk makes of states of zero, and its steps' sum.  Otherwise the outputs.
-template <class T, int L, int M, bool FIRST>
-__global__ __launch_bounds__(64 * L) void k_scan(const ScanArgs a) {
+template <class T, int L, int M, int W, bool FIRST>
+__global__ __launch_bounds__(64 * W) void k_scan(const ScanArgs a) {
     using raw = typename T::raw;
-    constexpr int kRow = Shared<T, L, M>::kRow, kOwn = kTile / L;
+    constexpr int kRow = Shared<T, L, M, W>::kRow, kOwn = kTile / L;
     __shared__ float shared[2][kTile][kRow];
     const uint32_t all_tiles = a.tiles * a.groups;
     // the last chunk's end is nothing that another one begins with
     const Piece w(a, blockIdx.x / all_tiles, FIRST ? a.chunks - 1 : a.chunks);
-    const Place at = place_of<L>(a, blockIdx.x % all_tiles);
+    const Place at = place_of<L, W>(a, blockIdx.x % all_tiles);
     const uint32_t b = w.b, c = at.channel;
     float h[M], rate[M];
     load_states<M>(a.A, a, at, rate, kLog2e);
@@ -358,7 +357,7 @@ __global__ __launch_bounds__(64 * L) void k_scan(const ScanArgs a) {
     Rows<raw, L> out_rows(a.out, b, w.first, at);
     float* held = FIRST || !a.held ? nullptr : a.held + ((uint64_t)b * ((a.steps + kTile - 1) / kTile) + w.first / kTile) * a.states * a.channels;
     Inputs<T, L> next_x, next_delta, next_gate;
-    Shared<T, L, M> next_shared(a, b, w.first, at.group);
+    Shared<T, L, M, W> next_shared(a, b, w.first, at.group);
     uint32_t next_starts = 0;
     auto load = [&](int64_t t) {
         const int left = (int)(w.end - t);
@@ -534,15 +533,15 @@ __global__ __launch_bounds__(256) void k_scan_join(const ScanArgs a) {
 }
 
 // What reaches the states in front of each chunk of what is behind its last step: zero there.
-template <class T, int L, int M>
-__global__ __launch_bounds__(64 * L) void k_scan_grad_first(const ScanArgs a) {
+template <class T, int L, int M, int W>
+__global__ __launch_bounds__(64 * W) void k_scan_grad_first(const ScanArgs a) {
     using raw = typename T::raw;
-    constexpr int kRow = Shared<T, L, M>::kRow, kOwn = kTile / L;
+    constexpr int kRow = Shared<T, L, M, W>::kRow, kOwn = kTile / L;
     __shared__ float shared[2][kTile][kRow];
     const uint32_t all_tiles = a.tiles * a.groups;
     // nothing reaches the steps in front of the first chunk
     const Piece w(a, blockIdx.x / all_tiles, a.chunks - 1, 1);
-    const Place at = place_of<L>(a, blockIdx.x % all_tiles);
+    const Place at = place_of<L, W>(a, blockIdx.x % all_tiles);
     const uint32_t b = w.b, c = at.channel;
     float g[M] = {}, rate[M];
     load_states<M>(a.A, a, at, rate, kLog2e);
@@ -551,7 +550,7 @@ __global__ __launch_bounds__(64 * L) void k_scan_grad_first(const ScanArgs a) {
     const int64_t top = w.top();
     Rows<const raw, L> delta_rows(a.delta, b, top, at), gate_rows(a.gate, b, top, at), grad_rows(a.grad_out, b, top, at);
     Inputs<T, L> next_delta, next_gate, next_grad;
-    Shared<T, L, M> next_shared(a, b, top, at.group);
+    Shared<T, L, M, W> next_shared(a, b, top, at.group);
     uint32_t next_starts = 0;
     auto load = [&](int64_t t) {
         const int left = (int)(w.end - t);
@@ -618,19 +617,19 @@ __global__ __launch_bounds__(64 * L) void k_scan_grad_first(const ScanArgs a) {
 // kTile steps at a time from the last to the first: forward from the states held before them, with all of their states and decays kept
 // in registers, then backward.  Sums over channels are sums over the lanes of a share, joined over the work-group's wavefronts in LDS
 // and left for each tile of channels.
-template <class T, int L, int M>
-__global__ __launch_bounds__(64 * L, 2) void k_scan_grad(const ScanArgs a) {
+template <class T, int L, int M, int W>
+__global__ __launch_bounds__(64 * W, 2) void k_scan_grad(const ScanArgs a) {
     using raw = typename T::raw;
-    constexpr int kRow = Shared<T, L, M>::kRow, kOwn = kTile / L;
+    constexpr int kRow = Shared<T, L, M, W>::kRow, kOwn = kTile / L;
     // decays of 4 states of a lane would leave no room for a second wavefront: they are computed again
     constexpr bool kKeep = M <= 2;
     __shared__ float shared[kTile][kRow];
-    __shared__ float across[L][kTile][kRow];
+    __shared__ float across[W][kTile][kRow];
     // sums over lanes by way of LDS
     constexpr bool kSpace = L == LaneSums::kSteps && M == 4;
-    __shared__ __attribute__((aligned(16))) float space[kSpace ? L * 2 * LaneSums::kWave : 1];
+    __shared__ __attribute__((aligned(16))) float space[kSpace ? W * 2 * LaneSums::kWave : 1];
     const uint32_t all_tiles = a.tiles * a.groups, tile = blockIdx.x % all_tiles, part = blockIdx.x / all_tiles;
-    const Place at = place_of<L>(a, tile);
+    const Place at = place_of<L, W>(a, tile);
     const uint32_t c = at.channel, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     float rate[M], d_rate[M] = {};
     load_states<M>(a.A, a, at, rate);
@@ -651,7 +650,7 @@ __global__ __launch_bounds__(64 * L, 2) void k_scan_grad(const ScanArgs a) {
                 }
         if (w.first >= w.end) continue;
         dx_rows = Rows<raw, L>(a.grad_x, b, top, at), dd_rows = Rows<raw, L>(a.grad_delta, b, top, at), dz_rows = Rows<raw, L>(a.grad_gate, b, top, at);
-        Shared<T, L, M> next_shared(a, b, top, at.group);
+        Shared<T, L, M, W> next_shared(a, b, top, at.group);
         const float* held = a.held + ((uint64_t)b * ((a.steps + kTile - 1) / kTile) + top / kTile) * a.states * a.channels;
         float* sums = a.shared + ((((uint64_t)(tile % a.tiles) * a.batch + b) * a.steps + top) * a.groups + at.group) * kRow;
         float g[M];                       // of the states before the step behind
@@ -793,10 +792,10 @@ __global__ __launch_bounds__(64 * L, 2) void k_scan_grad(const ScanArgs a) {
             });
             __syncthreads();
 #pragma unroll
-            for (uint32_t i = threadIdx.x; i < kTile * kRow; i += 64 * L) {
+            for (uint32_t i = threadIdx.x; i < kTile * kRow; i += 64 * W) {
                 float sum = across[0][i / kRow][i % kRow];
 #pragma unroll
-                for (int k = 1; k < L; ++k) sum += across[k][i / kRow][i % kRow];
+                for (int k = 1; k < W; ++k) sum += across[k][i / kRow][i % kRow];
                 if ((int)(i / kRow) < left) sums[(uint64_t)(i / kRow) * a.groups * kRow + i % kRow] = sum;
             }
             dx_rows.go(-1), dd_rows.go(-1), dz_rows.go(-1);
@@ -836,18 +835,24 @@ constexpr uint32_t kLeast = 64;           // steps of a chunk
 // states that the kernels have room for
 uint32_t room(uint32_t states) { return states <= 4 ? 4 : states <= 8 ? 8 : states <= 16 ? 16 : 32; }
 
-ScanArgs args_of(const bps_scan& s) {
+// Lanes of a channel, as scan_of chooses them.
+uint32_t lanes_of(uint32_t states, bool grad) { return grad && states > 16 ? 8 : 4; }
+
+ScanArgs args_of(const bps_scan& s, bool grad) {
     auto seq = [](const bps_sequence& q) { return Seq{q.at, q.batch_stride, (uint32_t)q.step_stride}; };
     ScanArgs a{seq(s.x), seq(s.delta), seq(s.gate), seq(s.B), seq(s.C), seq(s.out), seq(s.grad_out), seq(s.grad_x), seq(s.grad_delta), seq(s.grad_gate), seq(s.grad_B), seq(s.grad_C),
                s.A, s.D, s.delta_bias, s.starts, s.lengths, s.state, s.state_out, s.state_stride, s.state_out_stride, s.held, s.grad_A, s.grad_D, s.grad_delta_bias,
-               s.batch, s.steps, s.channels, s.states, s.groups, s.softplus, 0, 0, 0, 0, nullptr, nullptr, nullptr, nullptr};
-    a.tiles = (a.channels / a.groups + kWide - 1) / kWide;
-    const uint64_t groups = (uint64_t)a.batch * a.tiles * a.groups;
-    const uint64_t want = groups ? kGroups / groups : 1, most = a.steps / kLeast;
+               s.batch, s.steps, s.channels, s.states, s.groups, s.softplus, 0, 0, 0, 0, 0, nullptr, nullptr, nullptr, nullptr};
+    // work-groups of 64 channels, or of one wavefront where a quarter of their wavefronts or more would have none
+    const uint32_t lanes = lanes_of(s.states, grad), channels = a.channels / a.groups, wide = (channels + 63) / 64, narrow = (channels * lanes + 63) / 64;
+    a.waves = narrow * 4 > wide * lanes * 3 ? lanes : 1;
+    a.tiles = a.waves == 1 ? narrow : wide;
+    const uint64_t groups = (uint64_t)a.batch * a.tiles * a.groups, most_groups = a.waves == 1 ? kGroups * lanes : kGroups;
+    const uint64_t want = groups ? most_groups / groups : 1, most = a.steps / kLeast;
     const uint32_t chunks = (uint32_t)(want < most ? want : most);
     a.chunk_steps = chunks > 1 ? ((a.steps + chunks - 1) / chunks + kTile - 1) / kTile * kTile : a.steps ? a.steps : 1;
     a.chunks = a.steps ? (a.steps + a.chunk_steps - 1) / a.chunk_steps : 1;
-    const uint64_t items = (uint64_t)a.batch * a.chunks, part = kParts / (a.tiles * a.groups);
+    const uint64_t items = (uint64_t)a.batch * a.chunks, part = (a.waves == 1 ? kParts * lanes : kParts) / (a.tiles * a.groups);
     a.parts = (uint32_t)(items < part ? items : part ? part : 1);
     return a;
 }
@@ -860,7 +865,7 @@ void place_chunks(ScanArgs& a, float* space) {
     a.spans = space + (size_t)a.chunks * a.batch * a.states * a.channels;
 }
 
-template <class T, int L, int M>
+template <class T, int L, int M, int W>
 hipError_t scan(const ScanArgs& a, hipStream_t stream) {
     if (a.steps == 1 && !a.held) {
         k_scan_step<T, L * M / 4><<<a.batch * a.groups * ((a.channels / a.groups + 255) / 256), 256, 0, stream>>>(a);
@@ -868,25 +873,25 @@ hipError_t scan(const ScanArgs& a, hipStream_t stream) {
     }
     const uint32_t each = a.batch * a.tiles * a.groups;
     if (a.chunks > 1) {
-        k_scan<T, L, M, true><<<each * (a.chunks - 1), 64 * L, 0, stream>>>(a);
+        k_scan<T, L, M, W, true><<<each * (a.chunks - 1), 64 * W, 0, stream>>>(a);
         if (hipError_t e = hipGetLastError()) return e;
         k_scan_join<false><<<(uint32_t)(((uint64_t)a.batch * a.states * a.channels + 255) / 256), 256, 0, stream>>>(a);
         if (hipError_t e = hipGetLastError()) return e;
     }
-    k_scan<T, L, M, false><<<each * a.chunks, 64 * L, 0, stream>>>(a);
+    k_scan<T, L, M, W, false><<<each * a.chunks, 64 * W, 0, stream>>>(a);
     return hipGetLastError();
 }
 
-template <class T, int L, int M>
+template <class T, int L, int M, int W>
 hipError_t scan_grad(const ScanArgs& a, hipStream_t stream) {
     if (a.chunks > 1) {
-        k_scan_grad_first<T, L, M><<<a.batch * a.tiles * a.groups * (a.chunks - 1), 64 * L, 0, stream>>>(a);
+        k_scan_grad_first<T, L, M, W><<<a.batch * a.tiles * a.groups * (a.chunks - 1), 64 * W, 0, stream>>>(a);
         if (hipError_t e = hipGetLastError()) return e;
         k_scan_join<true><<<(uint32_t)(((uint64_t)a.batch * a.states * a.channels + 255) / 256), 256, 0, stream>>>(a);
         if (hipError_t e = hipGetLastError()) return e;
     }
     if (a.batch && a.steps) {
-        k_scan_grad<T, L, M><<<a.parts * a.tiles * a.groups, 64 * L, 0, stream>>>(a);
+        k_scan_grad<T, L, M, W><<<a.parts * a.tiles * a.groups, 64 * W, 0, stream>>>(a);
         if (hipError_t e = hipGetLastError()) return e;
         k_scan_grad_shared<T, L * M><<<(uint32_t)(((uint64_t)a.batch * a.steps * a.groups * 2 * L * M + 255) / 256), 256, 0, stream>>>(a);
         if (hipError_t e = hipGetLastError()) return e;
@@ -899,15 +904,23 @@ hipError_t scan_grad(const ScanArgs& a, hipStream_t stream) {
     return launch_join_parts(jobs, count, (size_t)(a.states + 2) * a.channels, stream);
 }
 
+template <class T, int L, int M>
+hipError_t one_scan(const ScanArgs& a, bool grad, hipStream_t stream) {
+    if (grad) return a.waves == 1 ? scan_grad<T, L, M, 1>(a, stream) : scan_grad<T, L, M, L>(a, stream);
+    return a.waves == 1 ? scan<T, L, M, 1>(a, stream) : scan<T, L, M, L>(a, stream);
+}
+
 template <class T>
 hipError_t scan_of(const ScanArgs& a, bool grad, hipStream_t stream) {
     switch (room(a.states)) {
-        case 4: return grad ? scan_grad<T, 4, 1>(a, stream) : scan<T, 4, 1>(a, stream);
-        case 8: return grad ? scan_grad<T, 4, 2>(a, stream) : scan<T, 4, 2>(a, stream);
-        case 16: return grad ? scan_grad<T, 4, 4>(a, stream) : scan<T, 4, 4>(a, stream);
+        case 4: return one_scan<T, 4, 1>(a, grad, stream);
+        case 8: return one_scan<T, 4, 2>(a, grad, stream);
+        case 16: return one_scan<T, 4, 4>(a, grad, stream);
         // 16 steps' states of 8 states a lane do not fit its registers in the gradient: 8 x 1024 x 1024 with 32 states takes 563 us with four lanes
         // to a channel and 305 with eight; forward, where only the present ones are held, 77 and 83
-        default: return grad ? scan_grad<T, 8, 4>(a, stream) : scan<T, 4, 8>(a, stream);
+        default:
+            if (grad) return a.waves == 1 ? scan_grad<T, 8, 4, 1>(a, stream) : scan_grad<T, 8, 4, 8>(a, stream);
+            return a.waves == 1 ? scan<T, 4, 8, 1>(a, stream) : scan<T, 4, 8, 4>(a, stream);
     }
 }
 hipError_t any_scan(const bps_scan& s, const ScanArgs& a, bool grad, hipStream_t stream) {
@@ -916,21 +929,21 @@ hipError_t any_scan(const bps_scan& s, const ScanArgs& a, bool grad, hipStream_t
 
 }  // namespace
 
-size_t scan_workspace(const bps_scan& s) { return chunk_floats(args_of(s)) * sizeof(float); }
+size_t scan_workspace(const bps_scan& s) { return chunk_floats(args_of(s, false)) * sizeof(float); }
 
 hipError_t launch_scan(const bps_scan& s, void* workspace, hipStream_t stream) {
-    ScanArgs a = args_of(s);
+    ScanArgs a = args_of(s, false);
     place_chunks(a, static_cast<float*>(workspace));
     return any_scan(s, a, false, stream);
 }
 
 size_t scan_grad_workspace(const bps_scan& s) {
-    const ScanArgs a = args_of(s);
+    const ScanArgs a = args_of(s, true);
     return (whole(chunk_floats(a)) + whole((size_t)a.parts * (a.states + 2) * a.channels) + (size_t)a.tiles * a.batch * a.steps * a.groups * 2 * room(a.states)) * sizeof(float);
 }
 
 hipError_t launch_scan_grad(const bps_scan& s, void* workspace, hipStream_t stream) {
-    ScanArgs a = args_of(s);
+    ScanArgs a = args_of(s, true);
     float* space = static_cast<float*>(workspace);
     place_chunks(a, space);
     a.sums = space + whole(chunk_floats(a));

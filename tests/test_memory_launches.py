@@ -99,21 +99,30 @@ def test_every_element_of_a_convolution_has_a_thread(fake, batch, steps, channel
 
 
 @pytest.mark.parametrize("batch,steps,channels,states,groups", [(1, 1, 1, 1, 1), (8, 4096, 2048, 16, 1), (1, 16384, 2048, 16, 1), (1024, 32, 512, 16, 1), (7, 1111, 778, 13, 2), (1, 1 << 20, 64, 32, 1),
-                                                                (1 << 20, 4, 64, 16, 1), (2, 64, 66, 5, 2), (1, 1, 4096, 4, 64), (3, 0, 12, 4, 1)])
+                                                                (1 << 20, 4, 64, 16, 1), (2, 64, 66, 5, 2), (1, 1, 4096, 4, 64), (3, 0, 12, 4, 1), (1000, 40, 20, 32, 4), (2, 4096, 40, 20, 1), (1, 300, 17, 1, 1)])
 def test_every_step_of_a_scan_is_in_a_chunk(fake, batch, steps, channels, states, groups):
     (status, space, forward), (back, back_space, backward) = _calls(fake, f"scan({batch}, {steps}, {channels}, {states}, {groups})")
     assert status == 0 and back == 0
-    tiles = batch * groups * -(-(channels // groups) // 64)
+
+    def tiles(threads, lanes):
+        """Work-groups for all sequences' channels: a wavefront has 64 / lanes of them."""
+        return batch * groups * -(-(channels // groups) // (threads // lanes))
+
+    def cut(first, last, lanes):
+        """A pass over all chunks but one, and the one over all of them."""
+        chunks = last[1] // tiles(last[2], lanes)
+        assert last[1] == chunks * tiles(last[2], lanes) and first[1] == (chunks - 1) * tiles(first[2], lanes) and first[2] == last[2]
+        assert chunks > 1 and steps // chunks >= 32 and last[1] * last[2] <= 1024 * 64 * lanes
+
     names = [n for n, _, _ in forward]
     if len(names) == 3:
         assert names == ["k_scan", "k_scan_join", "k_scan"] and space > 0
-        chunks = forward[2][1] // tiles
-        assert forward[0][1] == tiles * (chunks - 1) and chunks > 1 and chunks * tiles <= 1024 and steps // chunks >= 32
+        cut(forward[0], forward[2], 4)
     else:
-        assert names == ["k_scan"] and space == 0 and forward[0][1] == tiles
+        assert names == ["k_scan"] and space == 0 and forward[0][1] == tiles(forward[0][2], 4)
     names = [n for n, _, _ in backward]
-    expected = (["k_scan_grad_first", "k_scan_join"] if space else []) + (["k_scan_grad", "k_scan_grad_shared"] if steps else []) + ["k_join_parts"]
-    assert names == expected and back_space > 0
+    last = (["k_scan_grad", "k_scan_grad_shared"] if steps else []) + ["k_join_parts"]
+    assert names in (last, ["k_scan_grad_first", "k_scan_join", *last]) and back_space > 0
 
 
 def test_a_step_is_one_launch_without_a_workspace(fake):
