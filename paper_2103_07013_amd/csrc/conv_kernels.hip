@@ -171,12 +171,16 @@ __global__ __launch_bounds__(kGroup) void k_conv(const bps_conv a, const uint32_
 // grad_weight[k] = sum of du[t] x[t - K + 1 + k].  A run's thread goes on over K - 1 steps of the next run for its last
 // steps' sums.  The sums of weight and bias are left for each part of the runs.
 template <class T, int K, int V>
-__global__ __launch_bounds__(kGroup) void k_conv_grad(const bps_conv a, const uint32_t run, const uint32_t runs, const uint32_t parts, float* sums) {
+__global__ __launch_bounds__(kGroup) void k_conv_grad(const bps_conv a, const uint32_t run, const uint32_t runs, const uint32_t parts, const uint32_t slots, float* sums) {
     using raw = typename T::raw;
     const uint32_t vectors = (a.channels + V - 1) / V;
-    const uint64_t id = (uint64_t)blockIdx.x * kGroup + threadIdx.x, part = id / vectors;
-    if (part >= parts) return;
-    const uint32_t c = (uint32_t)(id % vectors) * V, n = min(a.channels - c, (uint32_t)V);
+    // slots > 1: a work-group has that many parts, and threads that belong to none of them
+    const uint64_t id = (uint64_t)blockIdx.x * kGroup + threadIdx.x;
+    const uint32_t slot = slots > 1 ? threadIdx.x / vectors : 0, at = slots > 1 ? threadIdx.x % vectors : (uint32_t)(id % vectors);
+    const uint64_t part = slots > 1 ? (uint64_t)blockIdx.x * slots + slot : id / vectors;
+    const bool on = slot < slots && part < parts;
+    if (slots == 1 && !on) return;
+    const uint32_t c = at * V, n = min(a.channels - c, (uint32_t)V);
     float w[K][V], bias[V], dw[K][V], db[V];
     load_taps<T, K, V>(a, c, n, w, bias);
 #pragma unroll
@@ -185,7 +189,7 @@ __global__ __launch_bounds__(kGroup) void k_conv_grad(const bps_conv a, const ui
 #pragma unroll
         for (int k = 0; k < K; ++k) dw[k][v] = 0.0f;
     }
-    for (uint64_t item = part; item < (uint64_t)a.batch * runs; item += parts) {
+    for (uint64_t item = on ? part : (uint64_t)a.batch * runs; item < (uint64_t)a.batch * runs; item += parts) {
         const uint32_t b = (uint32_t)(item / runs);
         const int64_t first = (int64_t)(item % runs) * run, last = min(first + run, (int64_t)a.steps), end = steps_of(a.lengths, b, a.steps);
         Window<T, K, V> window;
@@ -270,10 +274,29 @@ __global__ __launch_bounds__(kGroup) void k_conv_grad(const bps_conv a, const ui
                 walk(std::false_type());
         }
     }
-    float* s = sums + part * (K + 1) * (uint64_t)a.channels + c;
+    float* s = sums + (slots > 1 ? blockIdx.x : part) * (K + 1) * (uint64_t)a.channels;
+    if (slots == 1) {
 #pragma unroll
-    for (int k = 0; k < K; ++k) store_part<F32, V>(s + k * (uint64_t)a.channels, n, dw[k]);
-    store_part<F32, V>(s + K * (uint64_t)a.channels, n, db);
+        for (int k = 0; k < K; ++k) store_part<F32, V>(s + k * (uint64_t)a.channels + c, n, dw[k]);
+        store_part<F32, V>(s + K * (uint64_t)a.channels + c, n, db);
+        return;
+    }
+    // the slots' sums meet in LDS, in their order, a channel to a thread
+    __shared__ float all[V][kGroup + 1];
+    auto leave = [&](const float (&x)[V], int k) {
+        __syncthreads();
+#pragma unroll
+        for (int v = 0; v < V; ++v) all[v][threadIdx.x] = x[v];
+        __syncthreads();
+        for (uint32_t channel = threadIdx.x; channel < a.channels; channel += kGroup) {
+            float sum = 0.0f;
+            for (uint32_t other = 0; other < slots; ++other) sum += all[channel % V][other * vectors + channel / V];
+            s[k * (uint64_t)a.channels + channel] = sum;
+        }
+    };
+#pragma unroll
+    for (int k = 0; k < K; ++k) leave(dw[k], k);
+    leave(db, K);
 }
 
 constexpr uint32_t kJoinColumns = 64, kJoinSlices = 16, kJoinAhead = 8;
@@ -328,6 +351,9 @@ uint32_t parts_of(const bps_conv& a) {
     return (uint32_t)(items < most ? items : most ? most : 1);
 }
 
+// Parts that a work-group of the gradient has, whose sums it joins.
+uint32_t slots_of(uint32_t vectors) { return vectors <= kGroup / 4 ? kGroup / vectors : 1; }
+
 template <class T>
 hipError_t conv(const bps_conv& a, hipStream_t stream) {
     constexpr int V = T::kPer16;
@@ -351,23 +377,24 @@ template <class T>
 hipError_t conv_grad(const bps_conv& a, float* sums, hipStream_t stream) {
     constexpr int V = T::kPer16;
     const uint32_t vectors = vectors_of(a, true), run = run_of(a, vectors), runs = runs_of(a, run), parts = parts_of(a);
-    const dim3 grid((uint32_t)(((uint64_t)parts * vectors + kGroup - 1) / kGroup));
+    const uint32_t slots = slots_of(vectors);
+    const dim3 grid(slots > 1 ? (parts + slots - 1) / slots : (uint32_t)(((uint64_t)parts * vectors + kGroup - 1) / kGroup));
     if (parts) switch (a.taps) {
-        case 1: k_conv_grad<T, 1, V><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, sums); break;
-        case 2: k_conv_grad<T, 2, V><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, sums); break;
-        case 3: k_conv_grad<T, 3, V><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, sums); break;
-        case 4: k_conv_grad<T, 4, V><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, sums); break;
-        case 5: k_conv_grad<T, 5, V><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, sums); break;
-        case 6: k_conv_grad<T, 6, 4><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, sums); break;
-        case 7: k_conv_grad<T, 7, 4><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, sums); break;
-        default: k_conv_grad<T, 8, 4><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, sums); break;
+        case 1: k_conv_grad<T, 1, V><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, slots, sums); break;
+        case 2: k_conv_grad<T, 2, V><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, slots, sums); break;
+        case 3: k_conv_grad<T, 3, V><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, slots, sums); break;
+        case 4: k_conv_grad<T, 4, V><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, slots, sums); break;
+        case 5: k_conv_grad<T, 5, V><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, slots, sums); break;
+        case 6: k_conv_grad<T, 6, 4><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, slots, sums); break;
+        case 7: k_conv_grad<T, 7, 4><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, slots, sums); break;
+        default: k_conv_grad<T, 8, 4><<<grid, kGroup, 0, stream>>>(a, run, runs, parts, slots, sums); break;
     }
     // sums of no parts are zero
     if (hipError_t e = hipGetLastError()) return e;
     JoinJobs jobs;
     jobs.add(sums, a.channels, a.taps, a.weight_dtype, a.grad_weight);
     if (a.grad_bias) jobs.add(sums + (size_t)a.taps * a.channels, a.channels, 1, a.weight_dtype, a.grad_bias);
-    return launch_join_parts(jobs, parts, (size_t)(a.taps + 1) * a.channels, stream);
+    return launch_join_parts(jobs, (parts + slots - 1) / slots, (size_t)(a.taps + 1) * a.channels, stream);
 }
 
 }  // namespace

@@ -1,7 +1,8 @@
 // The norms around a block with its gate, its scale and the residual sum, and their gradient (include/bps_memory.h states the rule).
 //
-// W wavefronts hold a row in registers, P vectors of 16 bytes of the block's type to a lane: each input is read once and each
-// result written once.  Work-groups, of four such rows where one wavefront holds a row, go on to further rows, with the weights kept.
+// R lanes hold a row in registers, P vectors of 16 bytes of the block's type to a lane: each input is read once and each
+// result written once.  Work-groups, of 256 / R rows at a time where a wavefront holds a row or more, go on to further rows, with the weights
+// kept.
 #include <type_traits>
 
 #include "memory_device.h"
@@ -11,49 +12,49 @@ namespace bps {
 
 namespace {
 
-template <int W>
-constexpr int kSlots = W == 1 ? 4 : 1;    // rows that a work-group has at a time
+template <int R>
+constexpr int kSlots = R <= 64 ? 256 / R : 1;      // rows that a work-group has at a time
 
-// The sum over the W wavefronts of a row; `shared` is not used again before the next barrier.
-template <int W>
+// The sum over the R lanes of a row; `shared` is not used again before the next barrier.
+template <int R>
 __device__ __forceinline__ float row_sum(float x, float* shared) {
-    x = group_reduce<64>(x, [](float p, float q) { return p + q; });
-    if constexpr (W > 1) {
+    x = group_reduce<(R < 64 ? R : 64)>(x, [](float p, float q) { return p + q; });
+    if constexpr (R > 64) {
         __syncthreads();
         if (threadIdx.x % 64 == 0) shared[threadIdx.x / 64] = x;
         __syncthreads();
         x = shared[0];
 #pragma unroll
-        for (int k = 1; k < W; ++k) x += shared[k];
+        for (int k = 1; k < R / 64; ++k) x += shared[k];
     }
     return x;
 }
 
-template <class T, int W, int P>
+template <class T, int R, int P>
 __device__ __forceinline__ void load_vector(const void* p, bool wide, uint32_t width, float (&x)[P][T::kPer16], float otherwise) {
     constexpr int V = T::kPer16;
 #pragma unroll
     for (int j = 0; j < P; ++j) {
-        const uint32_t c = (j * W * 64 + threadIdx.x % (W * 64)) * V;
+        const uint32_t c = (j * R + threadIdx.x % R) * V;
 #pragma unroll
         for (int v = 0; v < V; ++v) x[j][v] = otherwise;
         if (p && c < width) load_weights<T, V>(p, c, wide, width - c, x[j]);
     }
 }
 
-template <class T, class R, int W, int P>
-__global__ __launch_bounds__(W * 64 * kSlots<W>, W == 8 ? 4 : 1) void k_norm(const bps_norm a) {
+template <class T, class S, int R, int P>
+__global__ __launch_bounds__(R * kSlots<R>, R == 512 ? 4 : 1) void k_norm(const bps_norm a) {
     constexpr int V = T::kPer16;
     using raw = typename T::raw;
-    using stream_raw = typename R::raw;
-    __shared__ float shared[W];
+    using stream_raw = typename S::raw;
+    __shared__ float shared[R < 64 ? 1 : R / 64];
     const bool wide = a.weight_dtype == BPS_F32;
     const float share = 1.0f / (float)a.width;
     float post[P][V], scale[P][V], pre[P][V];
-    load_vector<T, W, P>(a.post_weight, wide, a.width, post, 1.0f);
-    load_vector<T, W, P>(a.scale, wide, a.width, scale, 1.0f);
-    load_vector<T, W, P>(a.pre_weight, wide, a.width, pre, 1.0f);
-    for (uint64_t row = (uint64_t)blockIdx.x * kSlots<W> + threadIdx.x / (W * 64); row < a.rows; row += (uint64_t)gridDim.x * kSlots<W>) {
+    load_vector<T, R, P>(a.post_weight, wide, a.width, post, 1.0f);
+    load_vector<T, R, P>(a.scale, wide, a.width, scale, 1.0f);
+    load_vector<T, R, P>(a.pre_weight, wide, a.width, pre, 1.0f);
+    for (uint64_t row = (uint64_t)blockIdx.x * kSlots<R> + threadIdx.x / R; row < a.rows; row += (uint64_t)gridDim.x * kSlots<R>) {
         float b[P][V], r[P][V], g[P][V];
         const raw* block = static_cast<const raw*>(a.block) + (int64_t)row * a.block_stride;
         const raw* gate = static_cast<const raw*>(a.gate) + (int64_t)row * a.gate_stride;
@@ -61,23 +62,23 @@ __global__ __launch_bounds__(W * 64 * kSlots<W>, W == 8 ? 4 : 1) void k_norm(con
         float sum = 0.0f;
 #pragma unroll
         for (int j = 0; j < P; ++j) {
-            const uint32_t c = (j * W * 64 + threadIdx.x % (W * 64)) * V;
+            const uint32_t c = (j * R + threadIdx.x % R) * V;
 #pragma unroll
             for (int v = 0; v < V; ++v) b[j][v] = r[j][v] = g[j][v] = 0.0f;
             if (c < a.width) {
                 load_part<T, V>(block + c, a.width - c, b[j]);
-                load_part<R, V>(residual + c, a.width - c, r[j]);
+                load_part<S, V>(residual + c, a.width - c, r[j]);
                 if (a.gate) load_part<T, V>(gate + c, a.width - c, g[j]);
             }
 #pragma unroll
             for (int v = 0; v < V; ++v) sum = __builtin_fmaf(b[j][v], b[j][v], sum);
         }
         float root = 1.0f;
-        if (a.post_weight) root = __builtin_amdgcn_rsqf(__builtin_fmaf(row_sum<W>(sum, shared), share, a.eps));
+        if (a.post_weight) root = __builtin_amdgcn_rsqf(__builtin_fmaf(row_sum<R>(sum, shared), share, a.eps));
         float square = 0.0f;
 #pragma unroll
         for (int j = 0; j < P; ++j) {
-            const uint32_t c = (j * W * 64 + threadIdx.x % (W * 64)) * V;
+            const uint32_t c = (j * R + threadIdx.x % R) * V;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 float m = b[j][v] * root * post[j][v];
@@ -88,20 +89,20 @@ __global__ __launch_bounds__(W * 64 * kSlots<W>, W == 8 ? 4 : 1) void k_norm(con
                 r[j][v] = __builtin_fmaf(m, scale[j][v], r[j][v]);
                 square = __builtin_fmaf(r[j][v], r[j][v], square);
             }
-            if (a.residual_out && c < a.width) store_part<R, V>(static_cast<stream_raw*>(a.residual_out) + (int64_t)row * a.residual_out_stride + c, a.width - c, r[j]);
+            if (a.residual_out && c < a.width) store_part<S, V>(static_cast<stream_raw*>(a.residual_out) + (int64_t)row * a.residual_out_stride + c, a.width - c, r[j]);
         }
         float last = 1.0f;
         if (a.pre_weight) {
-            last = __builtin_amdgcn_rsqf(__builtin_fmaf(row_sum<W>(square, shared), share, a.eps));
+            last = __builtin_amdgcn_rsqf(__builtin_fmaf(row_sum<R>(square, shared), share, a.eps));
 #pragma unroll
             for (int j = 0; j < P; ++j) {
-                const uint32_t c = (j * W * 64 + threadIdx.x % (W * 64)) * V;
+                const uint32_t c = (j * R + threadIdx.x % R) * V;
 #pragma unroll
                 for (int v = 0; v < V; ++v) r[j][v] = r[j][v] * last * pre[j][v];
                 if (c < a.width) store_part<T, V>(static_cast<raw*>(a.out) + (int64_t)row * a.out_stride + c, a.width - c, r[j]);
             }
         }
-        if (a.roots && threadIdx.x % (W * 64) == 0) {
+        if (a.roots && threadIdx.x % R == 0) {
             a.roots[row] = root;
             a.roots[a.rows + row] = last;
         }
@@ -112,25 +113,25 @@ __global__ __launch_bounds__(W * 64 * kSlots<W>, W == 8 ? 4 : 1) void k_norm(con
 // sum, and so of the residual; that of m's factors follows, and through the block's norm in the same way.  What the forward pass computed is
 // computed again from its inputs.  Sums over rows are left for each work-group: those of post_weight, scale and pre_weight, as far as
 // there are such.
-template <class T, class R, int W, int P>
-__global__ __launch_bounds__(W * 64 * kSlots<W>) void k_norm_grad(const bps_norm a, float* sums) {
+template <class T, class S, int R, int P>
+__global__ __launch_bounds__(R * kSlots<R>) void k_norm_grad(const bps_norm a, float* sums) {
     constexpr int V = T::kPer16;
     using raw = typename T::raw;
-    using stream_raw = typename R::raw;
-    __shared__ float shared[W];
+    using stream_raw = typename S::raw;
+    __shared__ float shared[R < 64 ? 1 : R / 64];
     const bool wide = a.weight_dtype == BPS_F32;
     const float share = 1.0f / (float)a.width;
     float post[P][V], scale[P][V], pre[P][V], d_post[P][V] = {}, d_scale[P][V] = {}, d_pre[P][V] = {};
     auto load_weights = [&] {
-        load_vector<T, W, P>(a.post_weight, wide, a.width, post, 1.0f);
-        load_vector<T, W, P>(a.scale, wide, a.width, scale, 1.0f);
-        load_vector<T, W, P>(a.pre_weight, wide, a.width, pre, 1.0f);
+        load_vector<T, R, P>(a.post_weight, wide, a.width, post, 1.0f);
+        load_vector<T, R, P>(a.scale, wide, a.width, scale, 1.0f);
+        load_vector<T, R, P>(a.pre_weight, wide, a.width, pre, 1.0f);
     };
     // the 128 registers of a lane of 16 wavefronts have no room for them beside their gradients
-    constexpr bool kKeep = W < 16;
+    constexpr bool kKeep = R < 1024;
     if constexpr (kKeep) load_weights();
     const bool through = a.pre_weight && a.grad_out;
-    for (uint64_t row = (uint64_t)blockIdx.x * kSlots<W> + threadIdx.x / (W * 64); row < a.rows; row += (uint64_t)gridDim.x * kSlots<W>) {
+    for (uint64_t row = (uint64_t)blockIdx.x * kSlots<R> + threadIdx.x / R; row < a.rows; row += (uint64_t)gridDim.x * kSlots<R>) {
         float b[P][V], r[P][V], g[P][V], f[P][V], d[P][V], go[P][V];
         if constexpr (!kKeep) {
             __asm__ volatile("" ::: "memory");
@@ -140,7 +141,7 @@ __global__ __launch_bounds__(W * 64 * kSlots<W>) void k_norm_grad(const bps_norm
         float sum = 0.0f;
 #pragma unroll
         for (int j = 0; j < P; ++j) {
-            const uint32_t c = (j * W * 64 + threadIdx.x % (W * 64)) * V;
+            const uint32_t c = (j * R + threadIdx.x % R) * V;
 #pragma unroll
             for (int v = 0; v < V; ++v) b[j][v] = r[j][v] = g[j][v] = d[j][v] = go[j][v] = 0.0f;
             if (c < a.width) {
@@ -148,10 +149,10 @@ __global__ __launch_bounds__(W * 64 * kSlots<W>) void k_norm_grad(const bps_norm
                 load_part<T, V>(static_cast<const raw*>(a.block) + (int64_t)row * a.block_stride + c, n, b[j]);
                 if (a.gate) load_part<T, V>(static_cast<const raw*>(a.gate) + (int64_t)row * a.gate_stride + c, n, g[j]);
                 if (through) {
-                    load_part<R, V>(static_cast<const stream_raw*>(a.residual) + (int64_t)row * a.residual_stride + c, n, r[j]);
+                    load_part<S, V>(static_cast<const stream_raw*>(a.residual) + (int64_t)row * a.residual_stride + c, n, r[j]);
                     load_part<T, V>(static_cast<const raw*>(a.grad_out) + (int64_t)row * a.grad_out_stride + c, n, go[j]);
                 }
-                if (a.grad_residual_out) load_part<R, V>(static_cast<const stream_raw*>(a.grad_residual_out) + (int64_t)row * a.grad_residual_out_stride + c, n, d[j]);
+                if (a.grad_residual_out) load_part<S, V>(static_cast<const stream_raw*>(a.grad_residual_out) + (int64_t)row * a.grad_residual_out_stride + c, n, d[j]);
             }
 #pragma unroll
             for (int v = 0; v < V; ++v) {
@@ -169,16 +170,16 @@ __global__ __launch_bounds__(W * 64 * kSlots<W>) void k_norm_grad(const bps_norm
                 sum = __builtin_fmaf(go[j][v], r[j][v], sum);
             }
         }
-        if (through) sum = row_sum<W>(sum, shared) * share;
+        if (through) sum = row_sum<R>(sum, shared) * share;
         float inner = 0.0f;
 #pragma unroll
         for (int j = 0; j < P; ++j) {
-            const uint32_t c = (j * W * 64 + threadIdx.x % (W * 64)) * V;
+            const uint32_t c = (j * R + threadIdx.x % R) * V;
             if (through) {
 #pragma unroll
                 for (int v = 0; v < V; ++v) d[j][v] = __builtin_fmaf(__builtin_fmaf(-r[j][v], sum, go[j][v]), last, d[j][v]);
             }
-            if (c < a.width) store_part<R, V>(static_cast<stream_raw*>(a.grad_residual) + (int64_t)row * a.grad_residual_stride + c, a.width - c, d[j]);
+            if (c < a.width) store_part<S, V>(static_cast<stream_raw*>(a.grad_residual) + (int64_t)row * a.grad_residual_stride + c, a.width - c, d[j]);
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 const float n = b[j][v] * post[j][v];
@@ -192,10 +193,10 @@ __global__ __launch_bounds__(W * 64 * kSlots<W>) void k_norm_grad(const bps_norm
             }
             if (a.gate && c < a.width) store_part<T, V>(static_cast<raw*>(a.grad_gate) + (int64_t)row * a.grad_gate_stride + c, a.width - c, g[j]);
         }
-        if (a.post_weight) inner = row_sum<W>(inner, shared) * share;
+        if (a.post_weight) inner = row_sum<R>(inner, shared) * share;
 #pragma unroll
         for (int j = 0; j < P; ++j) {
-            const uint32_t c = (j * W * 64 + threadIdx.x % (W * 64)) * V;
+            const uint32_t c = (j * R + threadIdx.x % R) * V;
             if (a.post_weight) {
 #pragma unroll
                 for (int v = 0; v < V; ++v) d[j][v] = __builtin_fmaf(-b[j][v], inner, d[j][v]) * root;
@@ -206,27 +207,27 @@ __global__ __launch_bounds__(W * 64 * kSlots<W>) void k_norm_grad(const bps_norm
     const uint32_t vectors = (a.post_weight ? 1 : 0) + (a.scale ? 1 : 0) + (a.pre_weight ? 1 : 0);
     float* s = sums + (uint64_t)blockIdx.x * vectors * a.width;
     auto leave = [&](float (&d)[P][V]) {
-        if constexpr (kSlots<W> > 1) {
+        if constexpr (kSlots<R> > 1) {
             // the rows' sums meet in LDS, in the rows' order
-            __shared__ float other[kSlots<W>][P * V][64];
+            __shared__ float other[kSlots<R>][P * V][R];
             __syncthreads();
 #pragma unroll
             for (int j = 0; j < P; ++j)
 #pragma unroll
-                for (int v = 0; v < V; ++v) other[threadIdx.x / 64][j * V + v][threadIdx.x % 64] = d[j][v];
+                for (int v = 0; v < V; ++v) other[threadIdx.x / R][j * V + v][threadIdx.x % R] = d[j][v];
             __syncthreads();
-            if (threadIdx.x < 64)
+            if (threadIdx.x < R)
 #pragma unroll
             for (int j = 0; j < P; ++j)
 #pragma unroll
                 for (int v = 0; v < V; ++v)
 #pragma unroll
-                    for (int k = 1; k < kSlots<W>; ++k) d[j][v] += other[k][j * V + v][threadIdx.x];
+                    for (int k = 1; k < kSlots<R>; ++k) d[j][v] += other[k][j * V + v][threadIdx.x];
         }
 #pragma unroll
         for (int j = 0; j < P; ++j) {
-            const uint32_t c = (j * W * 64 + threadIdx.x % (W * 64)) * V;
-            if (c < a.width && (kSlots<W> == 1 || threadIdx.x < 64)) store_part<F32, V>(s + c, a.width - c, d[j]);
+            const uint32_t c = (j * R + threadIdx.x % R) * V;
+            if (c < a.width && (kSlots<R> == 1 || threadIdx.x < R)) store_part<F32, V>(s + c, a.width - c, d[j]);
         }
         s += a.width;
     };
@@ -236,55 +237,52 @@ __global__ __launch_bounds__(W * 64 * kSlots<W>) void k_norm_grad(const bps_norm
 }
 
 uint32_t vectors_of(const bps_norm& a) { return (a.width + (a.dtype == BPS_F32 ? 3 : 7)) / (a.dtype == BPS_F32 ? 4 : 8); }
-// Wavefronts of a row: with one vector to a lane as far as 16 of them go.
-uint32_t waves_of(const bps_norm& a) {
+// Lanes of a row, one vector to a lane as far as 16 wavefronts go.
+uint32_t lanes_of(const bps_norm& a) {
     const uint32_t vectors = vectors_of(a);
-    return vectors <= 64 ? 1 : vectors <= 128 ? 2 : vectors <= 256 ? 4 : vectors <= 512 ? 8 : 16;
+    return vectors <= 16 ? 16 : vectors <= 64 ? 64 : vectors <= 128 ? 128 : vectors <= 256 ? 256 : vectors <= 512 ? 512 : 1024;
 }
-uint32_t slots_of(const bps_norm& a) { return waves_of(a) == 1 ? kSlots<1> : 1; }
+uint32_t slots_of(uint32_t lanes) { return lanes <= 64 ? 256 / lanes : 1; }
 // Work-groups of the gradient: 2048 wavefronts at most, but one for each compute unit.
 uint32_t groups_of(const bps_norm& a) {
-    const uint32_t slots = slots_of(a), waves = waves_of(a) * slots, most = waves <= 8 ? 2048 / waves : 256;
+    const uint32_t lanes = lanes_of(a), slots = slots_of(lanes), most = lanes <= 512 ? 2048 * 64 / (lanes * slots) : 256;
     const uint64_t all = (a.rows + slots - 1) / slots;
     return all < most ? (uint32_t)all : most;
 }
 uint32_t sums_of(const bps_norm& a) { return (a.post_weight ? 1 : 0) + (a.scale ? 1 : 0) + (a.pre_weight ? 1 : 0); }
 
-template <class T, class R>
+template <class T, class S>
 hipError_t norm(const bps_norm& a, float* sums, hipStream_t stream) {
-    const uint32_t vectors = vectors_of(a), waves = waves_of(a), slots = slots_of(a);
+    const uint32_t vectors = vectors_of(a), lanes = lanes_of(a), slots = slots_of(lanes);
     const uint64_t all = (a.rows + slots - 1) / slots;
     const dim3 grid(sums ? groups_of(a) : (uint32_t)(all < 16384 ? all : 16384));
-    auto go = [&](auto w, auto p) {
-        constexpr int W = decltype(w)::value, P = decltype(p)::value;
+    auto go = [&](auto r, auto p) {
+        constexpr int R = decltype(r)::value, P = decltype(p)::value;
         if (sums)
-            k_norm_grad<T, R, W, P><<<grid, W * 64 * kSlots<W>, 0, stream>>>(a, sums);
+            k_norm_grad<T, S, R, P><<<grid, R * kSlots<R>, 0, stream>>>(a, sums);
         else
-            k_norm<T, R, W, P><<<grid, W * 64 * kSlots<W>, 0, stream>>>(a);
+            k_norm<T, S, R, P><<<grid, R * kSlots<R>, 0, stream>>>(a);
     };
     const std::integral_constant<int, 1> one;
     const std::integral_constant<int, 2> two;
-    const std::integral_constant<int, 4> four;
-    const std::integral_constant<int, 8> eight;
-    const std::integral_constant<int, 16> sixteen;
-    if (waves == 1) {
-        go(one, one);
-    } else if (waves == 2) {
-        go(two, one);
-    } else if (waves == 4) {
-        go(four, one);
-    } else if (waves == 8) {
-        go(eight, one);
-    } else if (vectors <= 1024) {
-        if (sums)
-            go(sixteen, one);
-        else
-            k_norm<T, R, 8, 2><<<grid, 512, 0, stream>>>(a);
-    } else if (T::kPer16 == 8 || vectors <= 2048) {
-        go(sixteen, two);
-    } else if constexpr (T::kPer16 == 4) {
-        go(sixteen, four);
-    }
+    if (lanes == 16)
+        go(std::integral_constant<int, 16>(), one);
+    else if (lanes == 64)
+        go(std::integral_constant<int, 64>(), one);
+    else if (lanes == 128)
+        go(std::integral_constant<int, 128>(), one);
+    else if (lanes == 256)
+        go(std::integral_constant<int, 256>(), one);
+    else if (lanes == 512)
+        go(std::integral_constant<int, 512>(), one);
+    else if (vectors <= 1024 && sums)
+        go(std::integral_constant<int, 1024>(), one);
+    else if (vectors <= 1024)             // two work-groups of 8 wavefronts on a compute unit: 8192 x 8192 bf16 218 us, with one of 16 250
+        k_norm<T, S, 512, 2><<<grid, 512, 0, stream>>>(a);
+    else if (T::kPer16 == 8 || vectors <= 2048)
+        go(std::integral_constant<int, 1024>(), two);
+    else if constexpr (T::kPer16 == 4)
+        go(std::integral_constant<int, 1024>(), std::integral_constant<int, 4>());
     return hipGetLastError();
 }
 

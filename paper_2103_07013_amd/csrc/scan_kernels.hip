@@ -397,6 +397,10 @@ __global__ __launch_bounds__(64 * W) void k_scan(const ScanArgs a) {
 #pragma unroll
             for (int j = 0; j < kOwn; ++j) {
                 apart();
+                if (L * j >= left) {      // nothing but zeros behind the end
+                    if (!FIRST && at.on && L * j + (int)at.share < rest) out_rows(j) = rounded<T>(0.0f);
+                    continue;
+                }
                 float d[L], in[L], y[L];
                 to_all<L>(d_mine[j], d);
                 to_all<L>(d_mine[j] * x_mine[j], in);
@@ -585,6 +589,7 @@ __global__ __launch_bounds__(64 * W) void k_scan_grad_first(const ScanArgs a) {
 #pragma unroll
             for (int j = kOwn - 1; j >= 0; --j) {
                 apart();
+                if (L * j >= left) continue;
                 float d[L], dy[L];
                 to_all<L>(d_mine[j], d);
                 to_all<L>(dy_mine[j], dy);
@@ -700,10 +705,18 @@ __global__ __launch_bounds__(64 * W, 2) void k_scan_grad(const ScanArgs a) {
             }
             __syncthreads();
             if (t > w.first) load(t - kTile);
-            either(starts, [&](auto some) {
+            // the first kGo of the lane's steps, behind which the sequence ends: short ones have no more than a few
+            auto walk = [&](auto some, auto go) {
                 constexpr bool kSome = decltype(some)::value;
+                constexpr int kGo = decltype(go)::value;
 #pragma unroll
-                for (int j = 0; j < kOwn; ++j) {
+                for (int j = kGo; j < kOwn; ++j)
+                    if (at.on && L * j + (int)at.share < rest) {
+                        dx_rows(j) = dd_rows(j) = rounded<T>(0.0f);
+                        if (a.gate.at) dz_rows(j) = rounded<T>(0.0f);
+                    }
+#pragma unroll
+                for (int j = 0; j < kGo; ++j) {
                     apart();
                     const int mine = L * j + (int)at.share;
                     float d[L], in[L], y[L];
@@ -737,10 +750,10 @@ __global__ __launch_bounds__(64 * W, 2) void k_scan_grad(const ScanArgs a) {
                     to[0] = sums_mine[0], to[1] = sums_mine[1];
                 };
 #pragma unroll
-                for (int j = kOwn - 1; j >= 0; --j) {
+                for (int j = kGo - 1; j >= 0; --j) {
                     apart();
                     if constexpr (kSpace)
-                        if (j + 1 < kOwn) add_up(j + 1);
+                        if (j + 1 < kGo) add_up(j + 1);
                     // handed out again rather than kept for all steps since the way forward
                     __asm__ volatile("" : "+v"(d_mine[j]), "+v"(x_mine[j]));
                     float d[L], in[L], dy[L], gb[L], dd[L];
@@ -789,6 +802,14 @@ __global__ __launch_bounds__(64 * W, 2) void k_scan_grad(const ScanArgs a) {
                     }
                 }
                 if constexpr (kSpace) add_up(0);
+            };
+            either(starts, [&](auto some) {
+                if (left <= L)
+                    walk(some, std::integral_constant<int, 1>());
+                else if (kOwn > 2 && left <= 2 * L)
+                    walk(some, std::integral_constant<int, 2>());
+                else
+                    walk(some, std::integral_constant<int, kOwn>());
             });
             __syncthreads();
 #pragma unroll
