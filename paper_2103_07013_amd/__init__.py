@@ -1,7 +1,7 @@
 """MI355X-native batch renderer for large-batch simulation (arXiv 2103.07013, Sec. 3.2), and operators of the policy
 that consumes its frames (Sec. 3.3, 3.4).
 
-Thin ctypes binding over libbps.so, the C-ABI library declared in include/bps.h.  Every
+Thin ctypes binding over libbps.so and libbps_memory.so, the C-ABI libraries declared in include/bps.h and bps_memory.h.  Every
 step of rendering, and each operator, runs in the library's HIP kernels; this package only marshals arguments.
 PyTorch is used for device memory and streams.  There is no CPU fallback: if the library
 is missing or no GPU is present, calls raise.
