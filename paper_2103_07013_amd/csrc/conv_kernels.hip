@@ -311,33 +311,36 @@ __global__ __launch_bounds__(kJoinColumns* kJoinSlices) void k_join_parts(const 
     __shared__ float all[kJoinSlices][kJoinColumns];
     const JoinJob& job = jobs.job[blockIdx.y];
     const uint32_t lane = threadIdx.x % kJoinColumns, slice = threadIdx.x / kJoinColumns;
-    const uint64_t columns = (uint64_t)job.width * job.inner, column = (uint64_t)blockIdx.x * kJoinColumns + lane;
-    if ((uint64_t)blockIdx.x * kJoinColumns >= columns) return;
-    float sum = 0.0f;
-    if (column < columns) {
-        const float* p = job.parts + column;
-        uint32_t k = slice;
-        for (; k + (kJoinAhead - 1) * kJoinSlices < count; k += kJoinAhead * kJoinSlices) {
-            float x[kJoinAhead];
+    const uint64_t columns = (uint64_t)job.width * job.inner;
+    for (uint64_t first = (uint64_t)blockIdx.x * kJoinColumns; first < columns; first += (uint64_t)gridDim.x * kJoinColumns) {
+        const uint64_t column = first + lane;
+        float sum = 0.0f;
+        if (column < columns) {
+            const float* p = job.parts + column;
+            uint32_t k = slice;
+            for (; k + (kJoinAhead - 1) * kJoinSlices < count; k += kJoinAhead * kJoinSlices) {
+                float x[kJoinAhead];
 #pragma unroll
-            for (uint32_t i = 0; i < kJoinAhead; ++i) x[i] = p[(k + i * kJoinSlices) * stride];
+                for (uint32_t i = 0; i < kJoinAhead; ++i) x[i] = p[(k + i * kJoinSlices) * stride];
 #pragma unroll
-            for (uint32_t i = 0; i < kJoinAhead; ++i) sum += x[i];
+                for (uint32_t i = 0; i < kJoinAhead; ++i) sum += x[i];
+            }
+            for (; k < count; k += kJoinSlices) sum += p[k * stride];
         }
-        for (; k < count; k += kJoinSlices) sum += p[k * stride];
-    }
-    all[slice][lane] = sum;
-    __syncthreads();
-    if (slice || column >= columns) return;
+        __syncthreads();
+        all[slice][lane] = sum;
+        __syncthreads();
+        if (slice || column >= columns) continue;
 #pragma unroll
-    for (uint32_t p = 1; p < kJoinSlices; ++p) sum += all[p][lane];
-    const uint64_t at = column % job.width * job.inner + column / job.width;
-    if (job.dtype == BPS_F32)
-        static_cast<float*>(job.out)[at] = sum;
-    else if (job.dtype == BPS_BF16)
-        static_cast<uint16_t*>(job.out)[at] = rounded<Bf16>(sum);
-    else
-        static_cast<_Float16*>(job.out)[at] = rounded<F16>(sum);
+        for (uint32_t p = 1; p < kJoinSlices; ++p) sum += all[p][lane];
+        const uint64_t at = column % job.width * job.inner + column / job.width;
+        if (job.dtype == BPS_F32)
+            static_cast<float*>(job.out)[at] = sum;
+        else if (job.dtype == BPS_BF16)
+            static_cast<uint16_t*>(job.out)[at] = rounded<Bf16>(sum);
+        else
+            static_cast<_Float16*>(job.out)[at] = rounded<F16>(sum);
+    }
 }
 
 // Steps of a run: as many as leave the launch kThreads threads, at most 64, at least 8.
@@ -412,7 +415,8 @@ hipError_t launch_join_parts(const JoinJobs& jobs, uint32_t count, size_t stride
         if (mine > columns) columns = mine;
     }
     if (!columns) return hipSuccess;
-    k_join_parts<<<dim3((uint32_t)((columns + kJoinColumns - 1) / kJoinColumns), jobs.count), kJoinColumns * kJoinSlices, 0, stream>>>(jobs, count, stride);
+    const uint64_t groups = (columns + kJoinColumns - 1) / kJoinColumns, most = 1 << 20;      // work-groups go on to further columns
+    k_join_parts<<<dim3((uint32_t)(groups < most ? groups : most), jobs.count), kJoinColumns * kJoinSlices, 0, stream>>>(jobs, count, stride);
     return hipGetLastError();
 }
 

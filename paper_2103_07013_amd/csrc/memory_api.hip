@@ -94,9 +94,9 @@ bps_status check_scan(const char* what, const bps_scan& a, bool grad) {
     if (a.channels == 0 || a.channels >= kMaxChannels) return fail_here(BPS_ERR_INVALID_ARG, "%s: channels=%u must be 1 .. 2^24 - 1", what, a.channels);
     if (a.groups == 0 || a.channels % a.groups) return fail_here(BPS_ERR_INVALID_ARG, "%s: channels=%u must be a multiple of groups=%u", what, a.channels, a.groups);
     if (a.steps >= 1u << 31) return fail_here(BPS_ERR_INVALID_ARG, "%s: steps must be below 2^31", what);
-    // a wavefront has 64 channels of a group, chunks have 32 steps at least and are 4096 at most
+    // at most 8 wavefronts for 64 channels of a group; time is cut where there are few of those only
     const uint64_t tiles = (uint64_t)a.groups * ((a.channels / a.groups + 63) / 64);
-    if (a.batch * tiles >= kMaxThreads / 64 - 4096 || (grad && (uint64_t)a.batch * a.steps * a.groups * 2 * bps::kMaxStates >= kMaxThreads - 256))
+    if (a.batch * tiles >= kMaxThreads / 512 || (grad && (uint64_t)a.batch * a.steps * a.groups * 2 * bps::kMaxStates >= kMaxThreads - 256))
         return fail_here(BPS_ERR_UNSUPPORTED, "%s: too many elements for one launch", what);
     Checks c{what, a.batch, a.steps};
     for (const bps_sequence* s : {&a.x, &a.delta, &a.gate, &a.B, &a.C, &a.out, &a.grad_out, &a.grad_x, &a.grad_delta, &a.grad_gate, &a.grad_B, &a.grad_C})

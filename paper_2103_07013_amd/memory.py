@@ -1,8 +1,8 @@
 """Operators of the memory of a policy that consumes the frames, over the C ABI of include/bps_memory.h: a causal convolution, a selective state
 space scan, and the norms around a block.  Marshalling only; tensors are torch's, on the GPU.
 
-Sequences are [batch, steps, channels] with any strides over batch and steps, so that rollouts gathered step by step are used as they
-are (x.transpose(0, 1)); `starts` [batch, steps] says where episodes begin, `lengths` [batch] where padded sequences end.  A call takes
+Sequences are [batch, steps, channels] with any strides over batch and steps (for scans below 2^26 elements from step to step), so that
+rollouts gathered step by step are used as they are (x.transpose(0, 1)); `starts` [batch, steps] says where episodes begin, `lengths` [batch] where padded sequences end.  A call takes
 a state and returns the next one; *_step does the same for one step, in place.  No gradient goes through states.
 
 Devices and streams are as for the policy's other operators: the tensors' device, torch's current stream of it unless `stream` names

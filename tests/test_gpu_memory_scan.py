@@ -73,6 +73,15 @@ def test_groups(groups, width):
     _check(a, g)
 
 
+@pytest.mark.parametrize("dtype,N", [("f32", 16), ("bf16", 16), ("f16", 14), ("bf16", 32), ("f32", 19), ("bf16", 8), ("f16", 4)])
+@pytest.mark.parametrize("width", [64, 200, 256])
+@pytest.mark.parametrize("T", [3, 6, 11, 21, 130])
+def test_channels_that_fill_work_groups(width, T, dtype, N):
+    """As many channels as the wavefronts of most work-groups take, with few steps, a few tiles of them, and chunks."""
+    a, g = _inputs(2, T, width, N, dtype, T + width, starts=0.05, ragged=T > 20, state=True)
+    _check(a, g)
+
+
 @pytest.mark.parametrize("without", [(), ("D",), ("gate",), ("delta_bias",), ("D", "gate", "delta_bias")])
 @pytest.mark.parametrize("softplus", [True, False])
 def test_what_may_be_left_out(without, softplus):

@@ -99,7 +99,8 @@ def test_every_element_of_a_convolution_has_a_thread(fake, batch, steps, channel
 
 
 @pytest.mark.parametrize("batch,steps,channels,states,groups", [(1, 1, 1, 1, 1), (8, 4096, 2048, 16, 1), (1, 16384, 2048, 16, 1), (1024, 32, 512, 16, 1), (7, 1111, 778, 13, 2), (1, 1 << 20, 64, 32, 1),
-                                                                (1 << 20, 4, 64, 16, 1), (2, 64, 66, 5, 2), (1, 1, 4096, 4, 64), (3, 0, 12, 4, 1), (1000, 40, 20, 32, 4), (2, 4096, 40, 20, 1), (1, 300, 17, 1, 1)])
+                                                                (1 << 20, 4, 64, 16, 1), (2, 64, 66, 5, 2), (1, 1, 4096, 4, 64), (3, 0, 12, 4, 1), (1000, 40, 20, 32, 4), (2, 4096, 40, 20, 1), (1, 300, 17, 1, 1), (1, 1, (1 << 24) - 1, 32, 1),
+                                                                (1, 2, (1 << 22) - 1, 1, (1 << 22) - 1), ((1 << 23) - 1, 2, 64, 1, 1)])
 def test_every_step_of_a_scan_is_in_a_chunk(fake, batch, steps, channels, states, groups):
     (status, space, forward), (back, back_space, backward) = _calls(fake, f"scan({batch}, {steps}, {channels}, {states}, {groups})")
     assert status == 0 and back == 0
@@ -133,6 +134,6 @@ def test_a_step_is_one_launch_without_a_workspace(fake):
 
 def test_calls_that_are_too_large_are_refused(fake):
     """They launch nothing; the largest that are not refused launch no more than the runtime takes."""
-    for code in ("conv(1 << 22, 1 << 14, 64)", "scan(1 << 26, 2, 64)", "scan(1 << 20, 4096, 64)"):
+    for code in ("conv(1 << 22, 1 << 14, 64)", "scan(1 << 26, 2, 64)", "scan(1 << 23, 1, 64)", "scan(1 << 20, 4096, 64, 16, 64)"):
         for status, _, launches in _calls(fake, code):
-            assert (status == 0) == bool(launches)
+            assert status != 0 and not launches
