@@ -1,9 +1,10 @@
 // Causal convolution over time, each channel by itself, and its gradient (include/bps_memory.h states the rule).
 //
-// A thread holds 16 bytes of channels and walks over a run of steps with the last inputs in registers, so that every input is
+// A thread holds 16 bytes of channels (the last one's begin earlier where the channels end inside them, and the others' are left out
+// of what it stores) and walks over a run of steps with the last inputs in registers, so that every input is
 // read once, and once more by the next run's thread for its first taps - 1 windows.  Bound by memory, as long as runs are long enough:
 // 8 x 4096 x 2048 bf16 with 4 taps 50 us, 5.4 TB/s; 1024 x 32 x 512 float32 26 us, 5.0 TB/s.  Rows of odd widths, whose
-// vectors begin anywhere: 3 x 5003 x 1111 f16 22.8 us, 2.9 TB/s.
+// vectors begin anywhere: 12 x 5003 x 1111 f16 70 us, 3.8 TB/s, 1104 channels 54 us, 4.9.  With the last channels loaded one by one the former took 82.
 #include <type_traits>
 
 #include "memory_device.h"
@@ -44,7 +45,7 @@ struct Window {
 
 // The window before step `first` of sequence b.
 template <class T, int K, int V>
-__device__ __forceinline__ void open_window(const bps_conv& a, uint32_t b, int64_t first, uint32_t c, uint32_t n, Window<T, K, V>& w) {
+__device__ __forceinline__ void open_window(const bps_conv& a, uint32_t b, int64_t first, const Place& place, Window<T, K, V>& w) {
     using raw = typename T::raw;
     w.clear();
 #pragma unroll
@@ -53,10 +54,10 @@ __device__ __forceinline__ void open_window(const bps_conv& a, uint32_t b, int64
         float x[V];
         if (t < 0) {
             if (!a.state) continue;
-            load_part<T, V>(static_cast<const raw*>(a.state) + b * a.state_stride + (K - 1 + t) * (int64_t)a.channels + c, n, x);
+            place.load<T, V>(static_cast<const raw*>(a.state) + b * a.state_stride + (K - 1 + t) * (int64_t)a.channels, x);
         } else {
             if (a.starts.at && a.starts.at[b * a.starts.batch_stride + t * a.starts.step_stride]) w.clear();
-            load_part<T, V>(static_cast<const raw*>(a.x.at) + b * a.x.batch_stride + t * a.x.step_stride + c, n, x);
+            load_part<T, V>(static_cast<const raw*>(a.x.at) + b * a.x.batch_stride + t * a.x.step_stride + place.at, place.to, x);
         }
         w.push(x);
     }
@@ -118,12 +119,14 @@ __global__ __launch_bounds__(kGroup) void k_conv(const bps_conv a, const uint32_
     const uint32_t vectors = (a.channels + V - 1) / V;
     const uint64_t id = (uint64_t)blockIdx.x * kGroup + threadIdx.x, item = id / vectors;
     if (item >= (uint64_t)a.batch * runs) return;
-    const uint32_t c = (uint32_t)(id % vectors) * V, n = min(a.channels - c, (uint32_t)V), b = (uint32_t)(item / runs);
+    const uint32_t b = (uint32_t)(item / runs);
+    const Place place = Place::inside<V>((uint32_t)(id % vectors) * V, a.channels);
+    const uint32_t c = place.at, n = place.to;
     const int64_t first = (int64_t)(item % runs) * run, last = min(first + run, (int64_t)a.steps), end = steps_of(a.lengths, b, a.steps);
     float w[K][V], bias[V];
     load_taps<T, K, V>(a, c, n, w, bias);
     Window<T, K, V> window;
-    open_window<T, K, V>(a, b, first, c, n, window);
+    open_window<T, K, V>(a, b, first, place, window);
     const raw* x_at = static_cast<const raw*>(a.x.at) + b * a.x.batch_stride + first * a.x.step_stride + c;
     raw* out_at = static_cast<raw*>(a.out.at) + b * a.out.batch_stride + first * a.out.step_stride + c;
     const int64_t stop = min(last, end);
@@ -149,7 +152,7 @@ __global__ __launch_bounds__(kGroup) void k_conv(const bps_conv a, const uint32_
                     for (int k = 0; k + 1 < K; ++k) u[v] = __builtin_fmaf(w[k][v], window.before[k][v], u[v]);
                     if (a.silu) u[v] *= sigmoid(u[v]);
                 }
-                store_part<T, V>(out_at, n, u);
+                place.store_at<T, V>(out_at, u);
                 out_at += a.out.step_stride;
                 window.push(x);
             }
@@ -161,13 +164,13 @@ __global__ __launch_bounds__(kGroup) void k_conv(const bps_conv a, const uint32_
     }
     if (a.state_out && ((first < end && end <= last) || (end == 0 && first == 0))) {
         if constexpr (K > 1) {
-            raw* s = static_cast<raw*>(a.state_out) + b * a.state_out_stride + c;
+            raw* s = static_cast<raw*>(a.state_out) + b * a.state_out_stride;
 #pragma unroll
-            for (int k = 0; k < K - 1; ++k) store_part<T, V>(s + k * (uint64_t)a.channels, n, window.before[k]);
+            for (int k = 0; k < K - 1; ++k) place.store<T, V>(s + k * (uint64_t)a.channels, window.before[k]);
         }
     }
     float zero[V] = {};
-    for (int64_t t = max(first, end); t < last; ++t, out_at += a.out.step_stride) store_part<T, V>(out_at, n, zero);
+    for (int64_t t = max(first, end); t < last; ++t, out_at += a.out.step_stride) place.store_at<T, V>(out_at, zero);
 }
 
 // With du = grad_out * slope(u):  grad_x[t] = sum over i < K of weight[K - 1 - i] du[t + i], as far as step t + i is of step t's episode;
@@ -175,8 +178,9 @@ __global__ __launch_bounds__(kGroup) void k_conv(const bps_conv a, const uint32_
 // steps' sums.  The sums of weight and bias are left for each part of the runs.  Bound by the registers that windows and sums take, 254 with
 // 4 taps of 8 channels: two wavefronts a SIMD, 8 x 4096 x 2048 bf16 110 us, 3.7 TB/s (loads ahead of their use take it to one
 // wavefront and 203 us; four channels a thread 179).
+// Four taps are held to 256 registers, which costs 8 bytes of memory a thread; five would cost 304 (8 x 4096 x 1024 150 us for 88).
 template <class T, int K, int V>
-__global__ __launch_bounds__(kGroup) void k_conv_grad(const bps_conv a, const uint32_t run, const uint32_t runs, const uint32_t parts, const uint32_t slots, float* sums) {
+__global__ __launch_bounds__(kGroup, K == 5 ? 1 : 2) void k_conv_grad(const bps_conv a, const uint32_t run, const uint32_t runs, const uint32_t parts, const uint32_t slots, float* sums) {
     using raw = typename T::raw;
     const uint32_t vectors = (a.channels + V - 1) / V;
     // slots > 1: a work-group has that many parts, and threads that belong to none of them
@@ -185,7 +189,8 @@ __global__ __launch_bounds__(kGroup) void k_conv_grad(const bps_conv a, const ui
     const uint64_t part = slots > 1 ? (uint64_t)blockIdx.x * slots + slot : id / vectors;
     const bool on = slot < slots && part < parts;
     if (slots == 1 && !on) return;
-    const uint32_t c = at * V, n = min(a.channels - c, (uint32_t)V);
+    const Place place = Place::inside<V>(at * V, a.channels);
+    const uint32_t c = place.at, n = place.to;
     float w[K][V], bias[V], dw[K][V], db[V];
     load_taps<T, K, V>(a, c, n, w, bias);
 #pragma unroll
@@ -198,7 +203,7 @@ __global__ __launch_bounds__(kGroup) void k_conv_grad(const bps_conv a, const ui
         const uint32_t b = (uint32_t)(item / runs);
         const int64_t first = (int64_t)(item % runs) * run, last = min(first + run, (int64_t)a.steps), end = steps_of(a.lengths, b, a.steps);
         Window<T, K, V> window;
-        open_window<T, K, V>(a, b, first, c, n, window);
+        open_window<T, K, V>(a, b, first, place, window);
         float sum[K][V];                  // of grad_x, of the step that is i steps back
 #pragma unroll
         for (int i = 0; i < K; ++i)
@@ -261,7 +266,7 @@ __global__ __launch_bounds__(kGroup) void k_conv_grad(const bps_conv a, const ui
 #pragma unroll
                                 for (int v = 0; v < V; ++v) sum[i][v] = __builtin_fmaf(w[K - 1 - i][v], g[v], sum[i][v]);
                     }
-                    if (plain || t + s - (K - 1) >= first) store_part<T, V>(dx_at, n, sum[K - 1]);
+                    if (plain || t + s - (K - 1) >= first) place.store_at<T, V>(dx_at, sum[K - 1]);
                     dx_at += a.grad_x.step_stride;
 #pragma unroll
                     for (int i = K - 1; i >= 1; --i)
@@ -282,8 +287,8 @@ __global__ __launch_bounds__(kGroup) void k_conv_grad(const bps_conv a, const ui
     float* s = sums + (slots > 1 ? blockIdx.x : part) * (K + 1) * (uint64_t)a.channels;
     if (slots == 1) {
 #pragma unroll
-        for (int k = 0; k < K; ++k) store_part<F32, V>(s + k * (uint64_t)a.channels + c, n, dw[k]);
-        store_part<F32, V>(s + K * (uint64_t)a.channels + c, n, db);
+        for (int k = 0; k < K; ++k) place.store<F32, V>(s + k * (uint64_t)a.channels, dw[k]);
+        place.store<F32, V>(s + K * (uint64_t)a.channels, db);
         return;
     }
     // the slots' sums meet in LDS, in their order, a channel to a thread
@@ -295,7 +300,8 @@ __global__ __launch_bounds__(kGroup) void k_conv_grad(const bps_conv a, const ui
         __syncthreads();
         for (uint32_t channel = threadIdx.x; channel < a.channels; channel += kGroup) {
             float sum = 0.0f;
-            for (uint32_t other = 0; other < slots; ++other) sum += all[channel % V][other * vectors + channel / V];
+            const uint32_t first = Place::inside<V>(channel / V * V, a.channels).at;
+            for (uint32_t other = 0; other < slots; ++other) sum += all[channel - first][other * vectors + channel / V];
             s[k * (uint64_t)a.channels + channel] = sum;
         }
     };

@@ -164,6 +164,28 @@ def test_pieces_of_a_sequence_give_the_whole():
     assert torch.equal(state, want.state)
 
 
+@pytest.mark.parametrize("dtype,D", [("f32", 3), ("f32", 67), ("bf16", 5), ("bf16", 67), ("f16", 15)])
+def test_channels_stay_apart(dtype, D):
+    """Where the last channels do not fill a vector: what one channel holds shows in no other, and steps move the same states on."""
+    import torch
+    import paper_2103_07013_amd as bps
+    a, g = _inputs(2, 19, D, 4, dtype, D, starts=0.05, state=True)
+    want, grads = bps.causal_conv(**a), bps.causal_conv_backward(g, **a)
+    for k in sorted({0, max(D - 8, 0), max(D - 4, 0), D - 2, D - 1}):
+        others = [c for c in range(D) if c != k]
+        b = dict(a, x=a["x"].clone(), state=a["state"].clone(), weight=a["weight"].clone())
+        b["x"][..., k] = float("nan")
+        b["state"][..., k] = float("inf")
+        b["weight"][k] = float("inf")
+        got, new = bps.causal_conv(**b), bps.causal_conv_backward(g, **b)
+        assert torch.equal(got.out[..., others], want.out[..., others]) and torch.equal(got.state[..., others], want.state[..., others])
+        assert torch.equal(new.x[..., others], grads.x[..., others]) and torch.equal(new.weight[others], grads.weight[others]) and torch.equal(new.bias[others], grads.bias[others])
+    state = a["state"].clone()
+    for t in range(19):
+        assert torch.equal(bps.causal_conv_step(a["x"][:, t], state, a["weight"], a["bias"], starts=a["starts"][:, t]), want.out[:, t])
+    assert torch.equal(state, want.state)
+
+
 def test_autograd():
     import torch
     import paper_2103_07013_amd as bps

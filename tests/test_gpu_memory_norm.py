@@ -139,6 +139,12 @@ def test_many_rows(rows):
     _check(a, gr, go)
 
 
+@pytest.mark.parametrize("dtype,stream,rows,width", [("f32", "f32", 8500, 17), ("f32", "f32", 8200, 3), ("bf16", "f32", 2200, 500), ("f16", "f16", 2500, 769), ("bf16", "f32", 600, 2049), ("f32", "f32", 530, 4098)])
+def test_more_rows_than_are_worked_on_at_once(dtype, stream, rows, width):
+    a, gr, go = _inputs((rows,), width, dtype, rows, stream)
+    _check(a, gr, go, activation="silu")
+
+
 def test_rows_of_zeros_and_of_large_values():
     import torch
     a, gr, go = _inputs((6,), 96, "f32", 8)
