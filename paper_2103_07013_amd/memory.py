@@ -140,9 +140,13 @@ def _state(state, shape, dtype, device):
         raise ValueError(f"state: need a {dtype} tensor of shape {tuple(shape)} on {device}")
     if not state.is_contiguous() and state.numel() and not state[0].is_contiguous():
         raise ValueError("state: each sequence's must be contiguous")
-    if state.requires_grad and torch.is_grad_enabled():
-        raise ValueError("state: no gradient goes through states (detach it)")
     return state.data_ptr(), state.stride(0)
+
+
+def _constant(state):
+    """For calls that a gradient may be recorded of, where that is known: inside an autograd function nothing is recorded."""
+    if state is not None and state.requires_grad and torch.is_grad_enabled():
+        raise ValueError("state: no gradient goes through states (detach it)")
 
 
 def _like(t):
@@ -241,6 +245,7 @@ def causal_conv(x, weight, bias=None, silu=True, starts=None, lengths=None, stat
     if stream is not None:
         with _stream(stream, x.device):
             return causal_conv(x, weight, bias, silu, starts, lengths, state)
+    _constant(state)
     if torch.is_grad_enabled() and _any_grad(x, weight, bias):
         return CausalConv(*_CausalConv.apply(x, weight, bias, silu, starts, lengths, state))
     return _causal_conv(x, weight, bias, silu, starts, lengths, state)
@@ -251,6 +256,7 @@ def causal_conv_backward(grad_out, x, weight, bias=None, silu=True, starts=None,
     if stream is not None:
         with _stream(stream, x.device):
             return causal_conv_backward(grad_out, x, weight, bias, silu, starts, lengths, state)
+    _constant(state)
     lib = _lib or _library()
     _three(x, "x")
     a, taps = _conv_args(x, weight, bias, silu, starts, lengths, state)
@@ -269,6 +275,7 @@ def causal_conv_step(x, state, weight, bias=None, silu=True, starts=None, stream
     if stream is not None:
         with _stream(stream, x.device):
             return causal_conv_step(x, state, weight, bias, silu, starts)
+    _constant(state)
     lib = _lib or _library()
     _main(x, "x")
     if x.dim() != 2:
@@ -357,6 +364,7 @@ def selective_scan(x, delta, A, B, C, D=None, gate=None, delta_bias=None, softpl
     if stream is not None:
         with _stream(stream, x.device):
             return selective_scan(x, delta, A, B, C, D, gate, delta_bias, softplus, starts, lengths, state, hold)
+    _constant(state)
     if torch.is_grad_enabled() and _any_grad(x, delta, A, B, C, D, gate, delta_bias):
         return SelectiveScan(*_SelectiveScan.apply(x, delta, A, B, C, D, gate, delta_bias, softplus, starts, lengths, state))
     return _selective_scan(x, delta, A, B, C, D, gate, delta_bias, softplus, starts, lengths, state, hold)
@@ -395,6 +403,7 @@ def selective_scan_step(x, delta, state, A, B, C, D=None, gate=None, delta_bias=
     if stream is not None:
         with _stream(stream, x.device):
             return selective_scan_step(x, delta, state, A, B, C, D, gate, delta_bias, softplus, starts)
+    _constant(state)
     lib = _lib or _library()
     _main(x, "x")
     if x.dim() != 2:
