@@ -3,7 +3,8 @@ space scan, and the norms around a block.  Marshalling only; tensors are torch's
 
 Sequences are [batch, steps, channels] with any strides over batch and steps (for scans below 2^26 elements from step to step), so that
 rollouts gathered step by step are used as they are (x.transpose(0, 1)); `starts` [batch, steps] says where episodes begin, `lengths` [batch] where padded sequences end.  A call takes
-a state and returns the next one; *_step does the same for one step, in place.  No gradient goes through states.
+a state and returns the next one; *_step does the same for one step, in place.  No gradient goes through states, and there are no
+forward-mode derivatives: states that ask for a gradient and tensors with a tangent are refused.
 
 Devices and streams are as for the policy's other operators: the tensors' device, torch's current stream of it unless `stream` names
 another, which is then current for the call.
@@ -18,7 +19,7 @@ import torch
 
 from . import build as _build
 from .binding import load_library
-from .policy import _TYPES, _checked, _on, _rows, _stream, _written
+from .policy import _TYPES, _checked, _no_tangent, _on, _rows, _stream, _written
 
 #: what causal_conv returns: the outputs, and the inputs that the next call's windows begin with
 CausalConv = collections.namedtuple("CausalConv", "out state")
@@ -245,6 +246,7 @@ def causal_conv(x, weight, bias=None, silu=True, starts=None, lengths=None, stat
     if stream is not None:
         with _stream(stream, x.device):
             return causal_conv(x, weight, bias, silu, starts, lengths, state)
+    _no_tangent(x, weight, bias, state)
     _constant(state)
     if torch.is_grad_enabled() and _any_grad(x, weight, bias):
         return CausalConv(*_CausalConv.apply(x, weight, bias, silu, starts, lengths, state))
@@ -256,6 +258,7 @@ def causal_conv_backward(grad_out, x, weight, bias=None, silu=True, starts=None,
     if stream is not None:
         with _stream(stream, x.device):
             return causal_conv_backward(grad_out, x, weight, bias, silu, starts, lengths, state)
+    _no_tangent(grad_out, x, weight, bias, state)
     _constant(state)
     lib = _lib or _library()
     _three(x, "x")
@@ -275,6 +278,7 @@ def causal_conv_step(x, state, weight, bias=None, silu=True, starts=None, stream
     if stream is not None:
         with _stream(stream, x.device):
             return causal_conv_step(x, state, weight, bias, silu, starts)
+    _no_tangent(x, state, weight, bias)
     _constant(state)
     lib = _lib or _library()
     _main(x, "x")
@@ -364,6 +368,7 @@ def selective_scan(x, delta, A, B, C, D=None, gate=None, delta_bias=None, softpl
     if stream is not None:
         with _stream(stream, x.device):
             return selective_scan(x, delta, A, B, C, D, gate, delta_bias, softplus, starts, lengths, state, hold)
+    _no_tangent(x, delta, A, B, C, D, gate, delta_bias, state)
     _constant(state)
     if torch.is_grad_enabled() and _any_grad(x, delta, A, B, C, D, gate, delta_bias):
         return SelectiveScan(*_SelectiveScan.apply(x, delta, A, B, C, D, gate, delta_bias, softplus, starts, lengths, state))
@@ -376,6 +381,7 @@ def selective_scan_backward(grad_out, x, delta, A, B, C, result, D=None, gate=No
     if stream is not None:
         with _stream(stream, x.device):
             return selective_scan_backward(grad_out, x, delta, A, B, C, result, D, gate, delta_bias, softplus, starts, lengths)
+    _no_tangent(grad_out, x, delta, A, B, C, D, gate, delta_bias)
     lib = _lib or _library()
     _three(x, "x")
     a = _scan_args(x, delta, A, B, C, D, gate, delta_bias, softplus, starts, lengths, None)
@@ -403,6 +409,7 @@ def selective_scan_step(x, delta, state, A, B, C, D=None, gate=None, delta_bias=
     if stream is not None:
         with _stream(stream, x.device):
             return selective_scan_step(x, delta, state, A, B, C, D, gate, delta_bias, softplus, starts)
+    _no_tangent(x, delta, state, A, B, C, D, gate, delta_bias)
     _constant(state)
     lib = _lib or _library()
     _main(x, "x")
@@ -500,6 +507,7 @@ def residual_norm(residual, block, post_weight=None, gate=None, scale=None, pre_
     if stream is not None:
         with _stream(stream, block.device):
             return residual_norm(residual, block, post_weight, gate, scale, pre_weight, eps, activation)
+    _no_tangent(residual, block, post_weight, gate, scale, pre_weight)
     if torch.is_grad_enabled() and _any_grad(residual, block, post_weight, gate, scale, pre_weight):
         return ResidualNorm(*_ResidualNorm.apply(residual, block, post_weight, gate, scale, pre_weight, eps, activation))
     return _residual_norm(residual, block, post_weight, gate, scale, pre_weight, eps, activation)
@@ -512,6 +520,7 @@ def residual_norm_backward(residual, block, result, grad_residual=None, grad_out
     if stream is not None:
         with _stream(stream, block.device):
             return residual_norm_backward(residual, block, result, grad_residual, grad_out, post_weight, gate, scale, pre_weight, eps, activation)
+    _no_tangent(residual, block, grad_residual, grad_out, post_weight, gate, scale, pre_weight)
     lib = _lib or _library()
     device = block.device
     held = _plain(result.held if isinstance(result, ResidualNorm) else result, "result", (2, *block.shape[:-1]), (torch.float32,), device)

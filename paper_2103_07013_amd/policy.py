@@ -4,7 +4,8 @@ embedding of tokens, and AdamW over many tensors.  Marshalling only; tensors are
 Calls take their device from the tensors and torch's current stream of it, unless `stream` names another (a
 torch.cuda.Stream or a raw hipStream_t, 0 = the default stream), which is then current for the call: what it
 allocates belongs to that stream.  A tensor that is used on another stream than its own has to be complete, and
-to be kept alive or recorded on that stream, by the caller, as for every operator of torch.
+to be kept alive or recorded on that stream, by the caller, as for every operator of torch.  Tensors with a tangent
+of forward-mode differentiation are refused.
 """
 from __future__ import annotations
 
@@ -68,6 +69,15 @@ def _checked(status):
 _current_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 # The library writes through addresses: autograd is told of tensors that were there before, so that graphs that saved them are refused.
 _written = torch.autograd.graph.increment_version
+_forward = torch.autograd.forward_ad
+
+
+def _no_tangent(*tensors):
+    """For every call that computes from tensors: forward-mode derivatives would be lost without a word."""
+    if _forward._current_level >= 0:
+        for t in tensors:
+            if torch.is_tensor(t) and _forward.unpack_dual(t).tangent is not None:
+                raise ValueError("these operators have no forward-mode derivatives: need tensors without a tangent")
 
 
 def _on(index, call, *arguments):
@@ -202,6 +212,7 @@ def log_probs(logits, tokens, mask=None, scale=1.0, top_k=0, stream=None):
     if stream is not None:
         with _stream(stream, logits.device):
             return log_probs(logits, tokens, mask, scale, top_k)
+    _no_tangent(logits)
     if logits.requires_grad and torch.is_grad_enabled():
         return LogProbs(*_LogProbs.apply(logits, tokens, mask, scale, top_k))
     return _log_probs(logits, tokens, mask, scale, top_k)
@@ -216,6 +227,7 @@ def log_probs_backward(logits, tokens, result, grad_logp=None, grad_entropy=None
     if stream is not None:
         with _stream(stream, logits.device):
             return log_probs_backward(logits, tokens, result, grad_logp, grad_entropy, mask, scale, out)
+    _no_tangent(logits, grad_logp, grad_entropy)
     lib = _lib or _library()
     shape, rows, width, step = _rows(logits, "logits")
     device = logits.device
@@ -281,6 +293,7 @@ def embedding(tokens, weight, scale=1.0, out=None, stream=None):
     if stream is not None:
         with _stream(stream, weight.device):
             return embedding(tokens, weight, scale, out)
+    _no_tangent(weight)
     if out is None and torch.is_grad_enabled() and weight.requires_grad:
         return _Embedding.apply(tokens, weight, scale)
     return _embedding(tokens, weight, scale, out)
@@ -293,6 +306,7 @@ def embedding_backward(tokens, grad_out, rows, scale=1.0, dtype=torch.float32, o
     if stream is not None:
         with _stream(stream, grad_out.device):
             return embedding_backward(tokens, grad_out, rows, scale, dtype, out, accumulate)
+    _no_tangent(grad_out)
     lib = _lib or _library()
     if accumulate and out is None:
         raise ValueError("accumulate needs out")
