@@ -229,11 +229,12 @@ class _CausalConv(torch.autograd.Function):
         if grad_out is None:
             return (None,) * 7
         x, weight, bias, starts, lengths, state = ctx.saved_tensors
-        return *causal_conv_backward(_last_contiguous(grad_out), x, weight, bias, ctx.silu, starts, lengths, state), None, None, None, None
+        return *causal_conv_backward(_as_taken(grad_out), x, weight, bias, ctx.silu, starts, lengths, state), None, None, None, None
 
 
-def _last_contiguous(t):
-    return t if t.stride(-1) == 1 else t.contiguous()
+def _as_taken(grad, steps_below=1 << 63):
+    """What autograd brings, in an order that the calls take: its strides follow from what its user did with the outputs."""
+    return grad if grad.stride(-1) == 1 and grad.stride(1) < steps_below else grad.contiguous()
 
 
 def causal_conv(x, weight, bias=None, silu=True, starts=None, lengths=None, state=None, stream=None):
@@ -350,7 +351,7 @@ class _SelectiveScan(torch.autograd.Function):
         if grad_out is None:
             return (None,) * 12
         x, delta, A, B, C, D, gate, delta_bias, starts, lengths, held = ctx.saved_tensors
-        g = selective_scan_backward(_last_contiguous(grad_out), x, delta, A, B, C, held, D, gate, delta_bias, ctx.softplus, starts, lengths)
+        g = selective_scan_backward(_as_taken(grad_out, 1 << 26), x, delta, A, B, C, held, D, gate, delta_bias, ctx.softplus, starts, lengths)
         return *g, None, None, None, None
 
 
