@@ -543,7 +543,10 @@ __global__ __launch_bounds__(256) void k_scan_join(const ScanArgs a) {
         for (uint32_t k = 0; k < kAhead; ++k) {
             if (i + k >= a.chunks) break;
             a.ends[((uint64_t)(REVERSE ? a.chunks - 1 - i - k : i + k) * a.batch + b) * per + id % per] = h;
-            h = keeps[k] != 0.0f ? __builtin_fmaf(h, __builtin_amdgcn_exp2f(span[k] * rate), end[k]) : end[k];
+            // Where states grow, a chunk's growth may be over what a float32 holds and the state behind it not: its root is applied
+            // twice, and a state of zero stays one under a growth of any size, as it does step by step.
+            const float root = __builtin_amdgcn_exp2f(span[k] * rate * 0.5f);
+            h = keeps[k] != 0.0f && h != 0.0f ? __builtin_fmaf(h * root, root, end[k]) : end[k];
         }
     }
 }
