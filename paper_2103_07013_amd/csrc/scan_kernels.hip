@@ -161,13 +161,22 @@ __device__ __forceinline__ uint32_t state_place(const ScanArgs& a, const Place& 
 
 // A lane's states of [states][channels] floats, 0 for those that there are not and where there is no s.
 template <int M>
-__device__ __forceinline__ void load_states(const float* s, const ScanArgs& a, const Place& at, float (&h)[M], float factor = 1.0f) {
+__device__ __forceinline__ void load_states(const float* s, const ScanArgs& a, const Place& at, float (&h)[M]) {
 #pragma unroll
     for (int m = 0; m < M; ++m) {
         const uint32_t n = at.share * M + m;
         h[m] = 0.0f;
-        if (s && n < a.states) h[m] = *reinterpret_cast<const float*>(reinterpret_cast<const char*>(s) + state_place(a, at, n)) * factor;
+        if (s && n < a.states) h[m] = *reinterpret_cast<const float*>(reinterpret_cast<const char*>(s) + state_place(a, at, n));
     }
+}
+// A rate of -infinity counts as -1e38, whose decays are zero as well: over a step without a size, as those behind a sequence's end
+// are, a state has to stay, and infinity times nothing is not a number.
+__device__ __forceinline__ float finite(float rate) { return rate < -1e38f ? -1e38f : rate; }
+template <int M>
+__device__ __forceinline__ void load_rates(const ScanArgs& a, const Place& at, float (&rate)[M], float factor = 1.0f) {
+    load_states<M>(a.A, a, at, rate);
+#pragma unroll
+    for (int m = 0; m < M; ++m) rate[m] = finite(rate[m]) * factor;
 }
 template <int M>
 __device__ __forceinline__ void store_states(float* s, const ScanArgs& a, const Place& at, const float (&h)[M]) {
@@ -357,7 +366,7 @@ __global__ __launch_bounds__(64 * W) void k_scan(const ScanArgs a) {
     const Place at = place_of<L, W>(a, blockIdx.x % all_tiles);
     const uint32_t b = w.b, c = at.channel;
     float h[M], rate[M];
-    load_states<M>(a.A, a, at, rate, kLog2e);
+    load_rates<M>(a, at, rate, kLog2e);
     const float bias = a.delta_bias ? a.delta_bias[c] : 0.0f, skip = !FIRST && a.D ? a.D[c] : 0.0f;
     if constexpr (FIRST)
         load_states<M>(nullptr, a, at, h);
@@ -504,7 +513,7 @@ __global__ __launch_bounds__(256) void k_scan_step(const ScanArgs a) {
         const uint32_t n = m * 4 + wave;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            h[m][e] = __builtin_fmaf(h[m][e], __builtin_amdgcn_exp2f(sizes[four + e] * (rate[m][e] * kLog2e)), inputs[four + e] * write[m]);
+            h[m][e] = __builtin_fmaf(h[m][e], __builtin_amdgcn_exp2f(sizes[four + e] * (finite(rate[m][e]) * kLog2e)), inputs[four + e] * write[m]);
             y[e] = __builtin_fmaf(h[m][e], read[m], y[e]);
         }
         if (n < a.states && a.state_out) store_part<F32, 4>(a.state_out + b * a.state_out_stride + (uint64_t)n * a.channels + c4, n4, h[m]);
@@ -527,7 +536,7 @@ __global__ __launch_bounds__(256) void k_scan_join(const ScanArgs a) {
     const uint64_t id = (uint64_t)blockIdx.x * 256 + threadIdx.x, per = (uint64_t)a.states * a.channels;
     if (id >= a.batch * per) return;
     const uint32_t b = (uint32_t)(id / per), c = (uint32_t)(id % a.channels);
-    const float rate = a.A[id % per] * kLog2e;
+    const float rate = finite(a.A[id % per]) * kLog2e;
     float h = !REVERSE && a.state ? a.state[b * a.state_stride + id % per] : 0.0f;
     constexpr uint32_t kAhead = 8;        // chunks whose inputs are on their way together
     for (uint32_t i = 0; i < a.chunks; i += kAhead) {
@@ -563,7 +572,7 @@ __global__ __launch_bounds__(64 * W) void k_scan_grad_first(const ScanArgs a) {
     const Place at = place_of<L, W>(a, blockIdx.x % all_tiles);
     const uint32_t b = w.b, c = at.channel;
     float g[M] = {}, rate[M];
-    load_states<M>(a.A, a, at, rate, kLog2e);
+    load_rates<M>(a, at, rate, kLog2e);
     const float bias = a.delta_bias ? a.delta_bias[c] : 0.0f;
     float span = 0.0f, keeps = 1.0f;
     const int64_t top = w.top();
@@ -654,7 +663,7 @@ __global__ __launch_bounds__(64 * W, 2) void k_scan_grad(const ScanArgs a) {
     const Place at = place_of<L, W>(a, tile);
     const uint32_t c = at.channel, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     float rate[M], d_rate[M] = {};
-    load_states<M>(a.A, a, at, rate);
+    load_rates<M>(a, at, rate);
     const float bias = a.delta_bias ? a.delta_bias[c] : 0.0f, skip = a.D ? a.D[c] : 0.0f;
     float d_skip = 0.0f, d_bias = 0.0f;
     for (uint32_t item = part; item < a.batch * a.chunks; item += a.parts) {
