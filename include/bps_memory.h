@@ -99,7 +99,7 @@ typedef struct {
     int32_t activation;
     uint64_t rows;
     uint32_t width;
-    float eps;                           /* > 0 */
+    float eps;                           /* >= 2^-126 */
     const void *residual, *block, *gate;
     int64_t residual_stride, block_stride, gate_stride;
     const void *post_weight, *scale, *pre_weight;   /* [width] */

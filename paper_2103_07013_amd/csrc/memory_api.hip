@@ -138,7 +138,8 @@ bps_status check_norm(const char* what, const bps_norm& a, bool grad) {
     if (a.activation != 0 && a.activation != 1) return fail_here(BPS_ERR_INVALID_ARG, "%s: unknown activation %d", what, a.activation);
     if (a.width == 0 || a.width > bps::kMaxNormWidth) return fail_here(BPS_ERR_INVALID_ARG, "%s: width=%u must be 1 .. %u", what, a.width, bps::kMaxNormWidth);
     if (a.rows >= 1ull << 40) return fail_here(BPS_ERR_INVALID_ARG, "%s: rows must be below 2^40", what);
-    if (!(a.eps > 0.0f) || !std::isfinite(a.eps)) return fail_here(BPS_ERR_INVALID_ARG, "%s: eps must be positive and finite", what);
+    // the hardware's root takes what is smaller for nothing, and a row of zeros would be zero times infinity
+    if (!(a.eps > 0.0f) || !std::isnormal(a.eps)) return fail_here(BPS_ERR_INVALID_ARG, "%s: eps must be positive, finite and no less than 2^-126", what);
     Checks c{what, 1, 1};
     const uint32_t size = size_of(a.dtype), stream_size = size_of(a.residual_dtype), weight_size = size_of(a.weight_dtype);
     const bool some = a.rows;

@@ -30,3 +30,20 @@ def test_states_that_ask_for_a_gradient_are_refused_beside_any_other_input_that_
                 call(**a)
             with pytest.raises(ValueError, match="CUDA"):
                 call(**dict(a, state=a["state"].detach()))
+
+
+@pytest.mark.parametrize("eps", [1e-45, 1e-39, 2.0 ** -127, 1.17e-38])
+def test_an_eps_that_is_no_normal_number_is_refused(eps):
+    """The root of a row of zeros would be taken of nothing, and be infinite: zero times it is not a number."""
+    import ctypes
+    import paper_2103_07013_amd as bps
+    from paper_2103_07013_amd import memory
+    lib, P = memory._library(), 4096
+    a = memory._Norm(dtype=0, residual_dtype=0, weight_dtype=0, activation=0, rows=2, width=6, eps=eps, residual=P, block=P, residual_stride=6, block_stride=6, pre_weight=P, residual_out=P, out=P + 2,
+                     residual_out_stride=6, out_stride=6, roots=P, grad_residual=P, grad_block=P, grad_residual_stride=6, grad_block_stride=6, grad_pre_weight=P)
+    assert 0.0 < a.eps < 2.0 ** -126
+    for call, rest in ((lib.bps_residual_norm, ()), (lib.bps_residual_norm_backward, (P, 1 << 30))):
+        assert call(ctypes.byref(a), *rest, None) == -1 and "eps" in bps.bps_last_error()
+    # the smallest that is taken: what is refused is an argument that is looked at later
+    a.eps = 2.0 ** -126
+    assert lib.bps_residual_norm(ctypes.byref(a), None) == -1 and "out is misaligned" in bps.bps_last_error()
