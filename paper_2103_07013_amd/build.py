@@ -37,8 +37,18 @@ def build(force: bool = True, verbose: bool = False) -> str:
     """Compile every HIP source into paper_2103_07013_amd/libbps.so and libbps_memory.so, which finds the former beside it."""
     if not force and not stale():
         return LIB
-    _make([(SOURCES, LIB, []), (MEMORY_SOURCES, MEMORY_LIB, ["-L" + HERE, "-lbps", "-Wl,-rpath,$ORIGIN"])], verbose)
+    _make([(SOURCES, LIB, []), _memory()], verbose)
     return LIB
+
+
+def build_memory(verbose: bool = False) -> str:
+    """Compile libbps_memory.so alone, beside the libbps.so that is there and may be loaded."""
+    _make([_memory()], verbose)
+    return MEMORY_LIB
+
+
+def _memory():
+    return MEMORY_SOURCES, MEMORY_LIB, ["-L" + HERE, "-lbps", "-Wl,-rpath,$ORIGIN"]
 
 
 def compile_hip(sources, lib: str, verbose: bool = False) -> str:

@@ -71,7 +71,7 @@ def _library():
     if _lib is None:
         load_library()
         if not os.path.exists(_build.MEMORY_LIB):
-            _build.build(force=True)
+            _build.build_memory()
         lib = ctypes.CDLL(_build.MEMORY_LIB)
         size = ctypes.c_size_t
         for name, args, back, forth in (("bps_causal_conv", _Conv, True, False), ("bps_selective_scan", _Scan, True, True), ("bps_residual_norm", _Norm, True, False)):
