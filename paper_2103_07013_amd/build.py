@@ -53,7 +53,7 @@ def _memory():
 
 def compile_hip(sources, lib: str, verbose: bool = False) -> str:
     """Compile HIP sources into one shared library with the flags that the numeric rule needs."""
-    _make([(sources, lib, [])], verbose)
+    _make([([os.path.abspath(s) for s in sources], lib, [])], verbose)
     return lib
 
 

@@ -25,3 +25,12 @@ def test_a_build_makes_both_libraries(monkeypatch):
     monkeypatch.setattr(build, "_make", lambda libs, verbose: made.extend(libs))
     assert build.build() == build.LIB
     assert [lib for _, lib, _ in made] == [build.LIB, build.MEMORY_LIB] and made[0][0] == build.SOURCES and made[1][0] == build.MEMORY_SOURCES
+
+
+def test_sources_are_named_as_from_the_working_folder(monkeypatch, tmp_path):
+    from paper_2103_07013_amd import build
+    monkeypatch.chdir(tmp_path)
+    (tmp_path / "k.cpp").write_text('extern "C" int answer(void) { return 42; }\n')
+    build.compile_hip(["k.cpp"], "k.so")
+    import ctypes
+    assert ctypes.CDLL(str(tmp_path / "k.so")).answer() == 42
