@@ -79,12 +79,6 @@ __device__ __forceinline__ void load_taps(const bps_conv& a, uint32_t c, uint32_
     if (a.bias) load_weights<T, V>(a.bias, c, wide, n, bias);
 }
 
-__device__ __forceinline__ int64_t steps_of(const int32_t* lengths, uint32_t b, uint32_t steps) {
-    if (!lengths) return steps;
-    const int32_t n = lengths[b];
-    return n < 0 ? 0 : (uint32_t)n < steps ? n : steps;
-}
-
 // Inputs of kAhead steps as they lie in memory, on their way together; those from `left` on are the last one before them.
 template <class T, int V>
 struct Steps {

@@ -26,6 +26,13 @@ __device__ __forceinline__ float softplus(float v) {
     return __builtin_fmaf(2.0f * s, p, fmaxf(v, 0.0f));
 }
 
+// Steps of sequence b
+__device__ __forceinline__ int64_t steps_of(const int32_t* lengths, uint32_t b, uint32_t steps) {
+    if (!lengths) return steps;
+    const int32_t n = lengths[b];
+    return n < 0 ? 0 : (uint32_t)n < steps ? n : steps;
+}
+
 // The first n of N elements (n = N: all of them, at once); the others read as zero and are not written.
 template <class T, int N>
 __device__ __forceinline__ void load_part(const typename T::raw* p, uint32_t n, float (&x)[N]) {

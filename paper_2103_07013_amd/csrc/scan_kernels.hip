@@ -54,22 +54,16 @@ struct ScanArgs {
 };
 
 // Where a lane is: its channel, whether that is one of its own, and which share of the states it holds.
-struct Place {
+struct Seat {
     uint32_t group, channel, share;
     bool on;
 };
 template <int L, int W>
-__device__ __forceinline__ Place place_of(const ScanArgs& a, uint32_t tile) {
+__device__ __forceinline__ Seat seat_of(const ScanArgs& a, uint32_t tile) {
     constexpr uint32_t kLanes = 64 / L;
     const uint32_t each = a.channels / a.groups, group = tile / a.tiles, lane = threadIdx.x % 64;
     const uint32_t c = (tile % a.tiles * W + threadIdx.x / 64) * kLanes + lane % kLanes;
     return {group, group * each + min(c, each - 1), lane / kLanes, c < each};
-}
-
-__device__ __forceinline__ int64_t steps_of(const int32_t* lengths, uint32_t b, uint32_t steps) {
-    if (!lengths) return steps;
-    const int32_t n = lengths[b];
-    return n < 0 ? 0 : (uint32_t)n < steps ? n : steps;
 }
 
 // x, which the compiler takes for a new value: what follows from it is computed where it is used and not kept in registers for a whole
@@ -85,12 +79,12 @@ template <class Raw, int L>
 struct Rows {
     char* row;
     uint32_t step, mine;                  // from row to row; the lane's channel in the row of its share
-    __device__ __forceinline__ Rows(const Seq& s, uint32_t b, int64_t t, const Place& at)
+    __device__ __forceinline__ Rows(const Seq& s, uint32_t b, int64_t t, const Seat& at)
         : row(static_cast<char*>(s.at) + (b * s.batch + t * s.step) * (int64_t)sizeof(Raw)), step(s.step * sizeof(Raw)), mine(at.channel * sizeof(Raw) + at.share * step) {}
     // of the lane's step among those from j L on
     __device__ __forceinline__ Raw& operator()(int j) const { return *reinterpret_cast<Raw*>(row + (here(mine) + j * L * step)); }
     // of a step of the tile
-    __device__ __forceinline__ Raw& of(uint32_t s, const Place& at) const { return *reinterpret_cast<Raw*>(row + (here(at.channel * sizeof(Raw)) + s * step)); }
+    __device__ __forceinline__ Raw& of(uint32_t s, const Seat& at) const { return *reinterpret_cast<Raw*>(row + (here(at.channel * sizeof(Raw)) + s * step)); }
     __device__ __forceinline__ void go(int tiles) { row += (int64_t)tiles * kTile * step; }
 };
 
@@ -98,7 +92,7 @@ struct Rows {
 template <class T, int L>
 struct Inputs {
     typename T::raw v[kTile / L];
-    __device__ __forceinline__ void load(const Rows<const typename T::raw, L>& s, int left, const Place& at) {
+    __device__ __forceinline__ void load(const Rows<const typename T::raw, L>& s, int left, const Seat& at) {
         if (left >= kTile) {
 #pragma unroll
             for (int j = 0; j < kTile / L; ++j) v[j] = s(j);
@@ -157,11 +151,11 @@ __device__ __forceinline__ uint32_t load_starts(const bps_starts& s, uint32_t b,
 }
 
 // Where state n of a lane's channel lies in [states][channels] floats, in bytes.
-__device__ __forceinline__ uint32_t state_place(const ScanArgs& a, const Place& at, uint32_t n) { return here((n * a.channels + at.channel) * 4); }
+__device__ __forceinline__ uint32_t state_place(const ScanArgs& a, const Seat& at, uint32_t n) { return here((n * a.channels + at.channel) * 4); }
 
 // A lane's states of [states][channels] floats, 0 for those that there are not and where there is no s.
 template <int M>
-__device__ __forceinline__ void load_states(const float* s, const ScanArgs& a, const Place& at, float (&h)[M]) {
+__device__ __forceinline__ void load_states(const float* s, const ScanArgs& a, const Seat& at, float (&h)[M]) {
 #pragma unroll
     for (int m = 0; m < M; ++m) {
         const uint32_t n = at.share * M + m;
@@ -173,13 +167,13 @@ __device__ __forceinline__ void load_states(const float* s, const ScanArgs& a, c
 // are, a state has to stay, and infinity times nothing is not a number.
 __device__ __forceinline__ float finite(float rate) { return rate < -1e38f ? -1e38f : rate; }
 template <int M>
-__device__ __forceinline__ void load_rates(const ScanArgs& a, const Place& at, float (&rate)[M], float factor = 1.0f) {
+__device__ __forceinline__ void load_rates(const ScanArgs& a, const Seat& at, float (&rate)[M], float factor = 1.0f) {
     load_states<M>(a.A, a, at, rate);
 #pragma unroll
     for (int m = 0; m < M; ++m) rate[m] = finite(rate[m]) * factor;
 }
 template <int M>
-__device__ __forceinline__ void store_states(float* s, const ScanArgs& a, const Place& at, const float (&h)[M]) {
+__device__ __forceinline__ void store_states(float* s, const ScanArgs& a, const Seat& at, const float (&h)[M]) {
     if (!s || !at.on) return;
 #pragma unroll
     for (int m = 0; m < M; ++m) {
@@ -330,7 +324,7 @@ struct Piece {
 
 // Step sizes of a lane's steps, 0 from `left` on.
 template <class T, int L>
-__device__ __forceinline__ void step_sizes(const Inputs<T, L>& delta, float bias, bool soft, int left, const Place& at, float (&d)[kTile / L]) {
+__device__ __forceinline__ void step_sizes(const Inputs<T, L>& delta, float bias, bool soft, int left, const Seat& at, float (&d)[kTile / L]) {
 #pragma unroll
     for (int j = 0; j < kTile / L; ++j) d[j] = delta[j] + bias;
     if (soft) {
@@ -363,7 +357,7 @@ __global__ __launch_bounds__(64 * W) void k_scan(const ScanArgs a) {
     const uint32_t all_tiles = a.tiles * a.groups;
     // the last chunk's end is nothing that another one begins with
     const Piece w(a, blockIdx.x / all_tiles, FIRST ? a.chunks - 1 : a.chunks);
-    const Place at = place_of<L, W>(a, blockIdx.x % all_tiles);
+    const Seat at = seat_of<L, W>(a, blockIdx.x % all_tiles);
     const uint32_t b = w.b, c = at.channel;
     float h[M], rate[M];
     load_rates<M>(a, at, rate, kLog2e);
@@ -569,7 +563,7 @@ __global__ __launch_bounds__(64 * W) void k_scan_grad_first(const ScanArgs a) {
     const uint32_t all_tiles = a.tiles * a.groups;
     // nothing reaches the steps in front of the first chunk
     const Piece w(a, blockIdx.x / all_tiles, a.chunks - 1, 1);
-    const Place at = place_of<L, W>(a, blockIdx.x % all_tiles);
+    const Seat at = seat_of<L, W>(a, blockIdx.x % all_tiles);
     const uint32_t b = w.b, c = at.channel;
     float g[M] = {}, rate[M];
     load_rates<M>(a, at, rate, kLog2e);
@@ -660,7 +654,7 @@ __global__ __launch_bounds__(64 * W, 2) void k_scan_grad(const ScanArgs a) {
     constexpr bool kSpace = L == LaneSums::kSteps && M == 4;
     __shared__ __attribute__((aligned(16))) float space[kSpace ? W * 2 * LaneSums::kWave : 1];
     const uint32_t all_tiles = a.tiles * a.groups, tile = blockIdx.x % all_tiles, part = blockIdx.x / all_tiles;
-    const Place at = place_of<L, W>(a, tile);
+    const Seat at = seat_of<L, W>(a, tile);
     const uint32_t c = at.channel, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     float rate[M], d_rate[M] = {};
     load_rates<M>(a, at, rate);
