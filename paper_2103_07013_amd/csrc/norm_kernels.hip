@@ -324,7 +324,7 @@ hipError_t norm(const bps_norm& a, float* sums, hipStream_t stream) {
     else if (lanes == 512)
         go(std::integral_constant<int, 512>(), one);
     else if (vectors <= 1024 && sums)     // with two vectors to a lane of 512 8192 x 8192 bf16 412 -> 460 us
-        go(std::integral_constant<int, 1024>(), one);
+        k_norm_grad<T, S, 1024, 1><<<grid, 1024, 0, stream>>>(a, sums);
     else if (vectors <= 1024)             // two work-groups of 8 wavefronts on a compute unit: 8192 x 8192 bf16 140 us
         k_norm<T, S, 512, 2><<<grid, 512, 0, stream>>>(a);
     else if (T::kPer16 == 8 || vectors <= 2048)

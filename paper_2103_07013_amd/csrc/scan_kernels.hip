@@ -255,8 +255,8 @@ __device__ __forceinline__ float lane_sums(const float* v) {
         for (int k = 0; k < K / 2; ++k) half[k] = pair_sum<S>(v[k], v[k + K / 2]);
         return lane_sums<K / 2, S / 2>(half);
     } else {
+        static_assert(S < 8, "as many values as halve 16 lanes once, or more");
         float x = v[0];
-        if constexpr (S >= 8) x += from_lane_xor<15>(x);
         if constexpr (S >= 4) x += from_lane_xor<7>(x);
         if constexpr (S >= 2) x += from_lane_xor<3>(x);
         if constexpr (S >= 1) x += from_lane_xor<1>(x);
