@@ -4,7 +4,7 @@
 // of what it stores) and walks over a run of steps with the last inputs in registers, so that every input is
 // read once, and once more by the next run's thread for its first taps - 1 windows.  Bound by memory, as long as runs are long enough:
 // 8 x 4096 x 2048 bf16 with 4 taps 50 us, 5.4 TB/s; 1024 x 32 x 512 float32 26 us, 5.0 TB/s.  Rows of odd widths, whose
-// vectors begin anywhere: 12 x 5003 x 1111 f16 70 us, 3.8 TB/s, 1104 channels 54 us, 4.9.  With the last channels loaded one by one the former took 82.
+// vectors begin anywhere: 12 x 5003 x 1111 f16 with 4 taps 70 us, 3.8 TB/s, 1104 channels 58 us, 4.6.
 #include <type_traits>
 
 #include "memory_device.h"
@@ -17,7 +17,7 @@ namespace {
 constexpr uint32_t kGroup = 256;
 constexpr uint32_t kManyTaps = 6;
 constexpr int kAhead = 4;                 // steps whose inputs are loaded together
-// 131072 / 262144 / 524288: 8 x 4096 x 2048 bf16 64 / 71 / 71 us, gradient 122 / 129 / 149
+// 131072 / 262144 / 524288: 8 x 4096 x 2048 bf16 with 4 taps 52 / 52 / 50 us, gradient 111 / 122 / 160
 constexpr uint32_t kThreads = 131072;     // that a launch has at least, where there is work for as many
 
 template <class T, int K, int V>
@@ -169,10 +169,11 @@ __global__ __launch_bounds__(kGroup) void k_conv(const bps_conv a, const uint32_
 
 // With du = grad_out * slope(u):  grad_x[t] = sum over i < K of weight[K - 1 - i] du[t + i], as far as step t + i is of step t's episode;
 // grad_weight[k] = sum of du[t] x[t - K + 1 + k].  A run's thread goes on over K - 1 steps of the next run for its last
-// steps' sums.  The sums of weight and bias are left for each part of the runs.  Bound by the registers that windows and sums take, 254 with
-// 4 taps of 8 channels: two wavefronts a SIMD, 8 x 4096 x 2048 bf16 110 us, 3.7 TB/s (loads ahead of their use take it to one
-// wavefront and 203 us; four channels a thread 179).
-// Four taps are held to 256 registers, which costs 8 bytes of memory a thread; five would cost 304 (8 x 4096 x 1024 150 us for 88).
+// steps' sums.  The sums of weight and bias are left for each part of the runs.  Bound by the registers that windows and sums take, 256 with
+// 4 taps of 8 channels: two wavefronts a SIMD, 8 x 4096 x 2048 bf16 110 us, 3.7 TB/s (four channels a thread 144; loads ahead of their use, which
+// take it to one wavefront, 203).  float32, four channels a thread: 8 x 4096 x 1024 91 us with 4 taps, 4.4 TB/s, 101 with 8.
+// Four taps are held to 256 registers, which costs 8 bytes of memory a thread; five have 302 and one wavefront (8 x 4096 x 1024 90 us, held to
+// 256 152).
 template <class T, int K, int V>
 __global__ __launch_bounds__(kGroup, K == 5 ? 1 : 2) void k_conv_grad(const bps_conv a, const uint32_t run, const uint32_t runs, const uint32_t parts, const uint32_t slots, float* sums) {
     using raw = typename T::raw;
@@ -350,7 +351,8 @@ uint32_t run_of(const bps_conv& a, uint32_t vectors) {
     return run;
 }
 // Channels of a thread: 16 bytes of them, but four of the gradient's from 6 taps on, whose sums take too many registers otherwise: 8 x 4096 x
-// 1024 bf16 with 8 taps 79 us instead of 124.
+// 1024 bf16 with four and eight 67 and 106 us with 6 taps, 73 and 127 with 8.  With 5 taps, which have eight, it is 56 and 90 as well; with 4, of 2048
+// channels, 144 and 110.
 uint32_t width_of(const bps_conv& a, bool grad) { return a.dtype == BPS_F32 || (grad && a.taps >= kManyTaps) ? 4 : 8; }
 uint32_t vectors_of(const bps_conv& a, bool grad) { return (a.channels + width_of(a, grad) - 1) / width_of(a, grad); }
 uint32_t runs_of(const bps_conv& a, uint32_t run) { return a.steps ? (a.steps - 1) / run + 1 : 1; }
@@ -360,7 +362,7 @@ uint32_t parts_of(const bps_conv& a) {
     return (uint32_t)(items < most ? items : most ? most : 1);
 }
 
-// Parts that a work-group of the gradient has, whose sums it joins: 228 x 3234 x 14 with 3 taps 110 us instead of 302.
+// Parts that a work-group of the gradient has, whose sums it joins: 228 x 3234 x 14 bf16 with 3 taps 54 us instead of 242, float32 44 instead of 134.
 uint32_t slots_of(uint32_t vectors) { return vectors <= kGroup / 4 ? kGroup / vectors : 1; }
 
 template <class T>

@@ -5,7 +5,9 @@
 // kept.  A lane's vectors are all loaded before the first is converted; waited for one by one, in the branches that load them, 8192 x 8192 bf16
 // took 208 us for 140 and 5003 x 769 f16 with its gradient 42 for 33.  Bound by memory: 32768 x 4096, bf16 blocks on a float32 stream, 400 us (4.7 TB/s) and 538
 // (5.5) for the gradient; 300000 x 256 float32 300 (5.1) and 470 (5.2); 8192 x 8192 bf16 140 (4.8) and 412 (2.6), a row to all of a compute
-// unit, whose wavefronts then wait together and whose sums leave no registers for loads ahead.  Odd widths: 20012 x 769 f16 38 us, x 768 31.
+// unit, whose wavefronts then wait together and whose sums leave no registers for loads ahead.  Odd widths: 20012 x 769 f16 39 us, x 768 33.
+// Lanes of 16 wavefronts have 128 registers, which are too few for the gradient of over 4096 columns: 100 to 136 bytes of a lane go to memory for every row,
+// 660 to 680 from 8193 columns on (4096 x 16384 bf16 1360 us, 0.8 TB/s), and 20 in the forward pass of such float32 rows (318 us, 4.2 TB/s; bf16, none, 181, 3.7).
 #include <type_traits>
 
 #include "memory_device.h"
@@ -148,7 +150,8 @@ __global__ __launch_bounds__(R * kSlots<R>) void k_norm_grad(const bps_norm a, f
         load_vector<T>(a.pre_weight, wide, place, pre[j]);
     };
     // Weights stay in registers, and the next row is on its way while this one is worked on: 32768 x 4096 538 us, 5003 x 769 f16 19 (600 and
-    // 22 without the loads ahead).  The 128 registers of a lane of 16 wavefronts have no room for either beside the sums.
+    // 22 without the loads ahead).  The 128 registers of a lane of 16 wavefronts have no room for either beside the sums, of which some go to
+    // memory even so.
     constexpr bool kKeep = R < 1024;
     if constexpr (kKeep) load_weights(0);
     const bool through = a.pre_weight && a.grad_out;
@@ -283,15 +286,16 @@ __global__ __launch_bounds__(R * kSlots<R>) void k_norm_grad(const bps_norm a, f
 }
 
 uint32_t vectors_of(const bps_norm& a) { return (a.width + (a.dtype == BPS_F32 ? 3 : 7)) / (a.dtype == BPS_F32 ? 4 : 8); }
-// Lanes of a row, one vector to a lane as far as 16 wavefronts go: with two to a lane in half the wavefronts 32768 x 4096 took 475 and 1110 us, 5003 x
-// 769 f16 16 and 46 us (before vectors were loaded together: then 403 and 700, 14 and 26).
+// Lanes of a row, one vector to a lane as far as 16 wavefronts go: 32768 x 4096 376 us forward and 534 for the gradient, 5003 x 769 f16 14 and 26.  With
+// two to a lane in half the wavefronts they took 475 and 1110, 16 and 46, as long as a lane's vectors were waited for one by one; as they are loaded
+// now, together and a row ahead, it is 360 and 440, 14 and 23, which this choice does not make use of.
 uint32_t lanes_of(const bps_norm& a) {
     const uint32_t vectors = vectors_of(a);
     return vectors <= 16 ? 16 : vectors <= 64 ? 64 : vectors <= 128 ? 128 : vectors <= 256 ? 256 : vectors <= 512 ? 512 : 1024;
 }
 uint32_t slots_of(uint32_t lanes) { return lanes <= 64 ? 256 / lanes : 1; }
-// Work-groups of the gradient: 2048 wavefronts at most, but one for each compute unit.  2048 / 4096 / 6144: 5003 x 769 f16 27 / 27 / 28 us
-// and 6 / 10 / 13 for joining the sums, 32768 x 4096 728 / 730 / 725.
+// Work-groups of the gradient: 2048 wavefronts at most, but one for each compute unit.  2048 / 4096 / 6144, with the joining of the sums: 5003 x 769
+// f16 26 / 36 / 42 us, 32768 x 4096 534 / 553 / 556.
 uint32_t groups_of(const bps_norm& a) {
     const uint32_t lanes = lanes_of(a), slots = slots_of(lanes), most = lanes <= 512 ? 2048 * 64 / (lanes * slots) : 256;
     const uint64_t all = (a.rows + slots - 1) / slots;
@@ -323,9 +327,11 @@ hipError_t norm(const bps_norm& a, float* sums, hipStream_t stream) {
         go(std::integral_constant<int, 256>(), one);
     else if (lanes == 512)
         go(std::integral_constant<int, 512>(), one);
-    else if (vectors <= 1024 && sums)     // with two vectors to a lane of 512 8192 x 8192 bf16 412 -> 460 us
+    // With two vectors to each of 512 lanes 8192 x 8192 bf16 took 460 us for 412 before rows were loaded ahead, which only those have the registers
+    // for; with that it is 166, which this choice does not make use of.
+    else if (vectors <= 1024 && sums)
         k_norm_grad<T, S, 1024, 1><<<grid, 1024, 0, stream>>>(a, sums);
-    else if (vectors <= 1024)             // two work-groups of 8 wavefronts on a compute unit: 8192 x 8192 bf16 140 us
+    else if (vectors <= 1024)             // two work-groups of 8 wavefronts on a compute unit: 8192 x 8192 bf16 142 us, one of 16 203
         k_norm<T, S, 512, 2><<<grid, 512, 0, stream>>>(a);
     else if (T::kPer16 == 8 || vectors <= 2048)
         go(std::integral_constant<int, 1024>(), two);

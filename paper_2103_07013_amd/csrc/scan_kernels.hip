@@ -11,9 +11,9 @@
 // What bounds it is the issue of vector instructions: a state's step is a product, a power of two, a product and two fused ones, five
 // instructions of which the power takes two turns, against 8 bytes of a channel's step for all of its 16 states.  With four lanes to a channel
 // 37 instructions are issued for 16 channels' step forward, 20 of them those five, and 106 for the gradient, where the least is 52;
-// the units issue in 99 % of the cycles forward and 84 % in the gradient.  One lane to a channel needs no exchange, but four times
-// the chunks, and the gradient's registers leave one wavefront on a SIMD: 8 x 4096 x 2048 bf16, 16 states, took 665 us forward and
-// 2280 for the gradient (now 530 and 1280); eight lanes 550 and 2080 where four took 490 and 1670.
+// the units issue in 99 % of the cycles forward and 84 % in the gradient.  8 x 4096 x 2048 bf16, 16 states, all launches of a call, the time
+// in four chunks: 490 us forward and 1255 for the gradient; eight lanes to a channel, as many chunks: 650 and 1715, one chunk 709 and 1474;
+// one lane, which needs no exchange, in four times the chunks for as many wavefronts: 548 and 8990, where the gradient's registers go to memory.
 #include <type_traits>
 
 #include "memory_device.h"
@@ -23,8 +23,8 @@ namespace bps {
 
 namespace {
 
-// Steps whose inputs are loaded together.  8 of them leave room for a third wavefront in the gradient, and hold twice the states in memory:
-// 8 x 4096 x 2048, 16 states, 366 and 1784 us for forward pass and gradient, 288 and 1349 with 16.
+// Steps whose inputs are loaded together.  8 of them hold twice the states in memory: 8 x 4096 x 2048 bf16, 16 states, 582 us forward with
+// held states and 1411 for the gradient, 495 and 1255 with 16.
 constexpr int kTile = (int)kHeldSteps;
 
 // A tensor of sequences as kernels have it.
@@ -266,7 +266,7 @@ __device__ __forceinline__ float lane_sums(const float* v) {
 
 // The sums of four steps over the 16 lanes of a share, of 8 values in each lane, by way of LDS: a lane adds up what 8 lanes have of four
 // of them, and the two that have the same four exchange.  8 additions and exchanges a step where permutations of lanes take 30: the
-// gradient of 8 x 4096 x 2048, 16 states, takes 1344 us with those.
+// gradient of 8 x 4096 x 2048 bf16, 16 states, takes 1360 us with those and 1255 so, all launches.
 struct LaneSums {
     static constexpr int kSteps = 4;
     static constexpr uint32_t kHalf = 64 * 4 + 16, kStep = 2 * kHalf, kWave = kSteps * kStep;      // floats; 16 of them keep halves in different banks
@@ -639,9 +639,10 @@ __global__ __launch_bounds__(64 * W) void k_scan_grad_first(const ScanArgs a) {
 //   grad_x = d sum of g B + D dy;   grad_d = x sum of g B + sum of A g a h before;   grad_A = sum over time of d g a h before
 // kTile steps at a time from the last to the first: forward from the states held before them, with all of their states and decays kept
 // in registers, then backward.  Sums over channels are sums over the lanes of a share, joined over the work-group's wavefronts in LDS
-// and left for each tile of channels.  Decays of 16 steps of 4 states do not fit beside the states (a few dozen registers that go to
-// memory make it 1870 us instead of 1090): they are computed again.  8 x 4096 x 2048 bf16, 16 states: 1031 us in its work-groups of four
-// wavefronts, two to a SIMD; 1024 x 32 x 512 float32 333 us.
+// and left for each tile of channels.  Decays of 16 steps of 4 states do not fit beside the states (registers that go to memory make all
+// launches 2160 us instead of 1255): they are computed again.  8 x 4096 x 2048 bf16, 16 states: 1020 us in its work-groups of four
+// wavefronts, two to a SIMD; 1024 x 32 x 512 float32 330 us.  In work-groups of one wavefront 9 to 16 states take 43 registers more than there are,
+// 176 bytes of memory a lane (see args_of); no other form takes any.
 template <class T, int L, int M, int W>
 __global__ __launch_bounds__(64 * W, 2) void k_scan_grad(const ScanArgs a) {
     using raw = typename T::raw;
@@ -869,8 +870,9 @@ __global__ __launch_bounds__(256) void k_scan_grad_shared(const ScanArgs a) {
     (static_cast<raw*>(s.at) + b * s.batch + t * s.step)[group * a.states + n] = rounded<T>(sum);
 }
 
-// Work-groups that a launch has, where there is time to be cut for as many: 512 / 768 / 1024 / 1536, 8 x 4096 x 2048 bf16 in both passes: 572 /
-// 542 / 531 / 534 us; 16384 x 2048 326 us with 512, 310 with 1024.
+// Work-groups that a launch has, where there is time to be cut for as many, forward and in the gradient: 256 / 512 / 768 / 1024 / 1536, 16 states
+// bf16, all launches: 8 x 4096 x 2048 585 / 554 / 500 / 490 / 485 and 1632 / 1282 / 1362 / 1255 / 1263 us, 16384 x 2048 480 / 320 / 292 / 277 / 275 and
+// 1030 / 691 / 730 / 670 / 682.
 constexpr uint32_t kGroups = 1024;
 constexpr uint32_t kParts = 1024;         // work-groups of the gradient: 512 are on the card at a time
 constexpr uint32_t kLeast = 64;           // steps of a chunk
@@ -886,8 +888,9 @@ ScanArgs args_of(const bps_scan& s, bool grad) {
     ScanArgs a{seq(s.x), seq(s.delta), seq(s.gate), seq(s.B), seq(s.C), seq(s.out), seq(s.grad_out), seq(s.grad_x), seq(s.grad_delta), seq(s.grad_gate), seq(s.grad_B), seq(s.grad_C),
                s.A, s.D, s.delta_bias, s.starts, s.lengths, s.state, s.state_out, s.state_stride, s.state_out_stride, s.held, s.grad_A, s.grad_D, s.grad_delta_bias,
                s.batch, s.steps, s.channels, s.states, s.groups, s.softplus, 0, 0, 0, 0, 0, nullptr, nullptr, nullptr, nullptr};
-    // work-groups of 64 channels, or of one wavefront where a quarter of their wavefronts or more would have none: 1623 x 3 x 20, 32 states in 4
-    // groups, scan and gradient, 89 us instead of 331; 1817 x 14 x 71, 157 instead of 217
+    // work-groups of 64 channels, or of one wavefront where a quarter of their wavefronts or more would have none: 1623 x 3 x 20 bf16, 32 states in
+    // 4 groups, scan and gradient, 72 us instead of 226; 1817 x 14 x 71 with 4 / 8 / 32 states 63 / 75 / 159 instead of 71 / 84 / 210.  With 9 to 16
+    // states, where registers of the gradient go to memory so, 145 instead of 108, and 2048 x 32 x 24 118 instead of 113
     const uint32_t lanes = lanes_of(s.states, grad), channels = a.channels / a.groups, wide = (channels + 63) / 64, narrow = (channels * lanes + 63) / 64;
     a.waves = narrow * 4 > wide * lanes * 3 ? lanes : 1;
     a.tiles = a.waves == 1 ? narrow : wide;
@@ -960,8 +963,8 @@ hipError_t scan_of(const ScanArgs& a, bool grad, hipStream_t stream) {
         case 4: return one_scan<T, 4, 1>(a, grad, stream);
         case 8: return one_scan<T, 4, 2>(a, grad, stream);
         case 16: return one_scan<T, 4, 4>(a, grad, stream);
-        // 16 steps' states of 8 states a lane do not fit its registers in the gradient: 8 x 1024 x 1024 with 32 states takes 563 us with four lanes
-        // to a channel and 305 with eight; forward, where only the present ones are held, 77 and 83
+        // 16 steps' states of 8 states a lane do not fit its registers in the gradient: 8 x 1024 x 1024 bf16 with 32 states takes 671 us with four
+        // lanes to a channel and 359 with eight; forward, where only the present ones are held, 123 and 135
         default:
             if (grad) return a.waves == 1 ? scan_grad<T, 8, 4, 1>(a, stream) : scan_grad<T, 8, 4, 8>(a, stream);
             return a.waves == 1 ? scan<T, 4, 8, 1>(a, stream) : scan<T, 4, 8, 4>(a, stream);
