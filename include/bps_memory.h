@@ -61,7 +61,7 @@ bps_status bps_causal_conv_backward(const bps_conv *args, void *workspace, size_
  *   d = delta + delta_bias, or ln(1 + e^that) with softplus
  *   h[n] = e^(d A[n]) h[n] + d x B[n];   y = sum over n of C[n] h[n] + D x;   out = y gate / (1 + e^-gate), or y without a gate
  * B and C are shared by the channels / groups channels of a group.  h is float32, 0 before an episode, the state's before step 0.
- * A rate A of -infinity counts as -1e38, whose decays are 0 as well.
+ * Rates A below -1e38, -infinity among them, count as that: their decays are 0 as well.
  * 1 <= states <= 32, channels < 2^24 and a multiple of groups, steps < 2^31, 0 <= step_stride < 2^26. */
 typedef struct {
     int32_t dtype;                       /* of x, delta, gate, B, C, out and their gradients */

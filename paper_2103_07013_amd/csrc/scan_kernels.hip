@@ -163,8 +163,8 @@ __device__ __forceinline__ void load_states(const float* s, const ScanArgs& a, c
         if (s && n < a.states) h[m] = *reinterpret_cast<const float*>(reinterpret_cast<const char*>(s) + state_place(a, at, n));
     }
 }
-// A rate of -infinity counts as -1e38, whose decays are zero as well: over a step without a size, as those behind a sequence's end
-// are, a state has to stay, and infinity times nothing is not a number.
+// Rates below -1e38, -infinity among them, count as that, whose decays are zero as well: over a step without a size, as those behind a
+// sequence's end are, a state has to stay, and infinity times nothing is not a number.
 __device__ __forceinline__ float finite(float rate) { return rate < -1e38f ? -1e38f : rate; }
 template <int M>
 __device__ __forceinline__ void load_rates(const ScanArgs& a, const Seat& at, float (&rate)[M], float factor = 1.0f) {

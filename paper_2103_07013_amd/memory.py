@@ -361,7 +361,7 @@ def selective_scan(x, delta, A, B, C, D=None, gate=None, delta_bias=None, softpl
 
     x, delta, gate float32, bfloat16 or float16 [batch, steps, channels]; B, C of x's type [batch, steps, states], or [batch, steps, groups,
     states] where each group's are for channels / groups channels; A float32 [states, channels], 1 to 32 states, negative where states are to
-    decay; D, delta_bias float32 [channels]; starts bool [batch, steps], where an episode begins (with a state of zero); lengths int32
+    decay (what is below -1e38 counts as that); D, delta_bias float32 [channels]; starts bool [batch, steps], where an episode begins (with a state of zero); lengths int32
     [batch], where padded sequences end; state float32 [batch, states, channels] (None: zeros).
     -> SelectiveScan(out, state, held): out is zero behind a sequence's end and carries a gradient to all inputs but the state; state is the next
     call's; held float32 [batch, ceil(steps / 16), states, channels], with hold or where a gradient is recorded, is for
