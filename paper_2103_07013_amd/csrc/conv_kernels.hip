@@ -323,8 +323,12 @@ __global__ __launch_bounds__(kJoinColumns* kJoinSlices) void k_join_parts(const 
                 float x[kJoinAhead];
 #pragma unroll
                 for (uint32_t i = 0; i < kJoinAhead; ++i) x[i] = p[(k + i * kJoinSlices) * stride];
+                // in pairs, whose roundings are those of three additions and not of eight
 #pragma unroll
-                for (uint32_t i = 0; i < kJoinAhead; ++i) sum += x[i];
+                for (uint32_t n = kJoinAhead / 2; n; n /= 2)
+#pragma unroll
+                    for (uint32_t i = 0; i < n; ++i) x[i] += x[i + n];
+                sum += x[0];
             }
             for (; k < count; k += kJoinSlices) sum += p[k * stride];
         }

@@ -26,6 +26,9 @@ namespace {
 // Steps whose inputs are loaded together.  8 of them hold twice the states in memory: 8 x 4096 x 2048 bf16, 16 states, 582 us forward with
 // held states and 1411 for the gradient, 495 and 1255 with 16.
 constexpr int kTile = (int)kHeldSteps;
+// Tiles whose sums over time the gradient adds up in registers; joining those in memory costs 1 or 2 %: 8 x 4096 x 2048 bf16 1268 us, 1024 x 32 x 512 float32
+// 316, without it 1255, as in the comparisons of other choices here, and 309.
+constexpr uint32_t kSumTiles = 16;
 
 // A tensor of sequences as kernels have it.
 struct Seq {
@@ -641,8 +644,8 @@ __global__ __launch_bounds__(64 * W) void k_scan_grad_first(const ScanArgs a) {
 // in registers, then backward.  Sums over channels are sums over the lanes of a share, joined over the work-group's wavefronts in LDS
 // and left for each tile of channels.  Decays of 16 steps of 4 states do not fit beside the states (registers that go to memory make all
 // launches 2160 us instead of 1255): they are computed again.  8 x 4096 x 2048 bf16, 16 states: 1020 us in its work-groups of four
-// wavefronts, two to a SIMD; 1024 x 32 x 512 float32 330 us.  In work-groups of one wavefront 9 to 16 states take 43 registers more than there are,
-// 176 bytes of memory a lane (see args_of); no other form takes any.
+// wavefronts, two to a SIMD; 1024 x 32 x 512 float32 330 us.  In work-groups of one wavefront 9 to 16 states take 48 registers more than there are,
+// 196 bytes of memory a lane (see args_of); no other form takes any.
 template <class T, int L, int M, int W>
 __global__ __launch_bounds__(64 * W, 2) void k_scan_grad(const ScanArgs a) {
     using raw = typename T::raw;
@@ -661,6 +664,27 @@ __global__ __launch_bounds__(64 * W, 2) void k_scan_grad(const ScanArgs a) {
     load_rates<M>(a, at, rate);
     const float bias = a.delta_bias ? a.delta_bias[c] : 0.0f, skip = a.D ? a.D[c] : 0.0f;
     float d_skip = 0.0f, d_bias = 0.0f;
+    // The sums of kSumTiles tiles join those of the tiles before, in memory: one after another over all steps of a work-group their roundings would be
+    // those of thousands of additions (64 x 512 x 512 float32, 4096 for each: grad_A 20 x 2^-24 off instead of 7).
+    float* all_sums = a.sums + (uint64_t)part * (a.states + 2) * a.channels;
+    uint32_t summed = 0;
+    bool begun = false;
+    auto leave = [&]() {
+        float before[M];
+        load_states<M>(begun && at.on ? all_sums : nullptr, a, at, before);
+#pragma unroll
+        for (int m = 0; m < M; ++m) d_rate[m] += before[m];
+        store_states<M>(all_sums, a, at, d_rate);
+        d_skip = share_sum<L>(d_skip), d_bias = share_sum<L>(d_bias);
+        if (at.on && at.share == 0) {
+            float* s = all_sums + a.states * (uint64_t)a.channels + c;
+            s[0] = begun ? s[0] + d_skip : d_skip;
+            s[a.channels] = begun ? s[a.channels] + d_bias : d_bias;
+        }
+#pragma unroll
+        for (int m = 0; m < M; ++m) d_rate[m] = 0.0f;
+        d_skip = d_bias = 0.0f, summed = 0, begun = true;
+    };
     for (uint32_t item = part; item < a.batch * a.chunks; item += a.parts) {
         const Piece w(a, item, a.chunks);
         const uint32_t b = w.b;
@@ -699,6 +723,8 @@ __global__ __launch_bounds__(64 * W, 2) void k_scan_grad(const ScanArgs a) {
         };
         load(top);
         for (int64_t t = top; t >= w.first; t -= kTile) {
+            if (summed == kSumTiles) leave();
+            ++summed;
             const int left = (int)(w.end - t), rest = (int)(w.last - t);
             const uint32_t starts = next_starts;
             float h[kTile + 1][M], decay[kKeep ? kTile : 1][M];
@@ -844,13 +870,7 @@ __global__ __launch_bounds__(64 * W, 2) void k_scan_grad(const ScanArgs a) {
             sums -= (uint64_t)kTile * a.groups * kRow;
         }
     }
-    float* s = a.sums + (uint64_t)part * (a.states + 2) * a.channels;
-    store_states<M>(s, a, at, d_rate);
-    d_skip = share_sum<L>(d_skip), d_bias = share_sum<L>(d_bias);
-    if (at.on && at.share == 0) {
-        s[a.states * (uint64_t)a.channels + c] = d_skip;
-        s[(a.states + 1) * (uint64_t)a.channels + c] = d_bias;
-    }
+    leave();
 }
 
 // grad_B and grad_C: the sums of all tiles of a group, zero behind a sequence's end.
