@@ -37,3 +37,22 @@ def test_sums_over_the_steps_of_a_scan():
     want = torch.autograd.grad(out, leaves, grad)
     for name, p, q in zip(("A", "D", "delta_bias"), (got.A, got.D, got.delta_bias), want):
         assert _off(p, q) < LIMIT, (name, _off(p, q) * 2 ** 24)
+
+
+def test_sums_over_the_rows_of_norms():
+    """Rows of 16 lanes, of which 8192 are worked on at a time: 2048 terms of each sum."""
+    import torch
+    import paper_2103_07013_amd as bps
+    g = torch.Generator(device="cuda").manual_seed(2)
+    n = lambda *s: torch.randn(s, generator=g, device="cuda")  # noqa: E731
+    rows, width = 1 << 24, 32
+    residual, block, grad = n(rows, width), n(rows, width), n(rows, width)
+    scale, post = torch.rand(width, generator=g, device="cuda") + 0.5, torch.rand(width, generator=g, device="cuda") + 0.5
+    r = bps.residual_norm(residual, block, post_weight=post, scale=scale)
+    got = bps.residual_norm_backward(residual, block, r, grad_residual=grad, post_weight=post, scale=scale)
+    want = torch.zeros(width, dtype=torch.float64, device="cuda")
+    for k in range(0, rows, 1 << 22):
+        b = block[k:k + (1 << 22)].double()
+        want += (grad[k:k + (1 << 22)].double() * b * (b.square().mean(1, keepdim=True) + 1e-6).rsqrt()).sum(0)
+    for name, p, factor in (("scale", got.scale, post), ("post_weight", got.post_weight, scale)):
+        assert _off(p, want * factor.double()) < LIMIT, (name, _off(p, want * factor.double()) * 2 ** 24)
