@@ -296,12 +296,13 @@ uint32_t lanes_of(const bps_norm& a) {
 uint32_t slots_of(uint32_t lanes) { return lanes <= 64 ? 256 / lanes : 1; }
 // Work-groups of the gradient: 2048 wavefronts at most, but one for each compute unit.  2048 / 4096 / 6144, with the joining of the sums: 5003 x 769
 // f16 26 / 36 / 42 us, 32768 x 4096 534 / 553 / 556.
-// But as many as leave 256 rows to a lane, up to 2^20: sums of thousands of rows one after another are further from 64 bits than what they are made of
-// (2^24 x 32 float32, 2048 rows each, 11 x 2^-24 off instead of 6; 6250000 x 16 907 us with its join, 1065 by 8192 rows at a time).
+// Of rows to 64 lanes or fewer as many times that as leave a lane about 256: sums of thousands of rows one after another are further from 64 bits than what they
+// are made of (2^24 x 32 float32, 2048 rows each, 11 x 2^-24 off instead of 6), and more work-groups than are on the card at a time are no slower there:
+// 6250000 x 16 float32 853 us for 1050, 1470000 x 68 933 for 1030; 300000 x 2048 bf16, which is left as it is, would take 2010 for 1800.
 uint32_t groups_of(const bps_norm& a) {
-    const uint32_t lanes = lanes_of(a), slots = slots_of(lanes), least = lanes <= 512 ? 2048 * 64 / (lanes * slots) : 256;
-    const uint64_t all = (a.rows + slots - 1) / slots, exact = (all + 255) / 256, most = exact > least ? exact < 1 << 20 ? exact : 1 << 20 : least;
-    return (uint32_t)(all < most ? all : most);
+    const uint32_t lanes = lanes_of(a), slots = slots_of(lanes), least = lanes <= 512 ? 2048 * 64 / (lanes * slots) : 256, limit = lanes <= 64 ? (1 << 20) / least : 1;
+    const uint64_t all = (a.rows + slots - 1) / slots, times = (all / 256 + least - 1) / least;
+    return (uint32_t)(all < least ? all : least * (times < 1 ? 1 : times < limit ? times : limit));
 }
 uint32_t sums_of(const bps_norm& a) { return (a.post_weight ? 1 : 0) + (a.scale ? 1 : 0) + (a.pre_weight ? 1 : 0); }
 
