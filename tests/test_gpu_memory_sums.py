@@ -40,7 +40,7 @@ def test_sums_over_the_steps_of_a_scan():
 
 
 def test_sums_over_the_rows_of_norms():
-    """Rows of 16 lanes, of which 8192 are worked on at a time: 2048 terms of each sum."""
+    """Rows of 16 lanes, 2048 of them for each of the 8192 that are worked on at a time."""
     import torch
     import paper_2103_07013_amd as bps
     g = torch.Generator(device="cuda").manual_seed(2)
